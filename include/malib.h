@@ -64,7 +64,8 @@ typedef enum malib_policy_kind {
 
 typedef enum malib_dtype {
     MALIB_F32 = 0,            /* fp32 weights, fp32 forward */
-    MALIB_BF16 = 1            /* bf16 weights and layer inputs, fp32 accumulation */
+    MALIB_BF16 = 1,           /* bf16 weights and layer inputs, fp32 accumulation */
+    MALIB_F16 = 2             /* fp16 logits of the token losses (no policies of it) */
 } malib_dtype;
 
 /* Flags of malib_env_spec.flags and malib_eval_payoff_ex(). */
@@ -476,6 +477,128 @@ int malib_adam_step(malib_ctx* ctx, float* params, const float* grad, float* m, 
  * may be reused. Errors: EINVAL, ESTATE.
  */
 int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int64_t nbytes);
+
+/* ---- losses of token policies: log-probabilities, losses and their gradients ----
+ *
+ * A token policy acts by choosing one of V entries (a vocabulary, or any action
+ * set too large for the policies above); its network lies outside this library
+ * and gives one row of V logits for every position. These calls are the learner's
+ * side of it (Sec. 3.3, App. C.2): from the logits of n_rows positions they compute
+ * a loss and the gradient at the logits, which the caller's network carries back.
+ * With the row's logits z and temperature T > 0, y = z / T, the policy is
+ *   ln p_j = y_j - ln sum_i exp(y_i),   H = -sum_j p_j ln p_j.
+ * Logits of -infinity are masked entries: p_j = 0, no entropy, gradient 0. A NaN
+ * or +infinity among the logits makes the row's results NaN.
+ * Rows that are LEFT OUT: those with a negative token (a prompt, padding), weight
+ * 0, no teacher entry, or logits that are all -infinity. They add nothing to
+ * losses, sequence sums and statistics, their outputs per row are 0 and their
+ * gradient rows are written as 0.
+ * All arithmetic is fp32 with statistics summed in fp64 in a fixed order (the same
+ * call gives the same bits); the gradient is rounded once to the logits' type.
+ * All buffers are DEVICE memory of the context's device, aligned to their element;
+ * the context needs no population. Calls are asynchronous on the context's
+ * stream and allocate at most their first time at a size (context-owned work
+ * space: a context's calls must be ordered, also across malib_set_stream). A token
+ * or teacher entry >= V leaves its row, or the entry, out and gives MALIB_EINVAL
+ * at the next malib_sync. n_rows == 0 is valid. Errors: EINVAL, ENOMEM, ECUDA.
+ */
+typedef struct malib_token_batch {
+    const void* logits;       /* [n_rows][ld], the first vocab of each row are used */
+    const int32_t* tokens;    /* [n_rows] the token that was chosen; < 0: row left out */
+    int64_t n_rows;
+    int64_t ld;               /* row stride in elements; >= vocab, or 0 for one row that all share */
+    int32_t vocab;            /* 1 <= V <= 2^24 */
+    int32_t dtype;            /* malib_dtype of logits and gradient */
+    float temperature;
+} malib_token_batch;
+
+/* The gradient at the logits: grad [n_rows][ld] of the logits' type, ld >= vocab
+ * (columns from vocab on are not written); NULL for the loss alone. grad may be the
+ * logits' buffer with the same ld (written in place) but must not overlap it
+ * otherwise. scale multiplies the gradient (an upstream factor, or a loss scale
+ * for fp16), not the loss. */
+typedef struct malib_token_grad {
+    void* grad;
+    int64_t ld;
+    float scale;
+} malib_token_grad;
+
+/*
+ * malib_token_logprob - ln p of each row's token into logp_out [n_rows] and H into
+ * entropy_out [n_rows] (either may be NULL). What a rollout records about the
+ * behavior policy, one row per live sequence and step, and what the reference
+ * policy's pass gives to the losses below.
+ */
+int malib_token_logprob(malib_ctx* ctx, const malib_token_batch* batch, float* logp_out, float* entropy_out);
+
+/*
+ * malib_learn_token_ppo - PPO's clipped surrogate (malib_learn_ppo_batch's, per
+ * token) with a KL term to a reference policy and an entropy term. For row i with
+ * token a, ln p its log-probability, rho = exp(ln p - old_logp_i), A = advantage_i,
+ * r = ref_logp_i - ln p:
+ *   l_i = -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *         + kl_coef (e^r - r - 1) - entropy_coef H_i
+ *   L = sum_i w_i l_i
+ * (e^r - r - 1 >= 0 is an unbiased estimate of KL(p || ref) from p's samples.) The
+ * unclipped term carries the gradient where it is the minimum, ties included.
+ * weight [n_rows] is w, e.g. 1 / (number of tokens), or 1 / (length of the row's
+ * sequence) for a mean over sequences; NULL: 1 / n_rows for every row. ref_logp may
+ * be NULL (no KL term). clip_low in (0, 1), clip_high > 0, kl_coef, entropy_coef >= 0.
+ * logp_out [n_rows] (optional): ln p. stats_out (optional) float [5]: rows counted,
+ * L, share of counted rows on the clipped side, their mean e^r - r - 1 (0 without
+ * ref_logp), their mean H.
+ */
+typedef struct malib_token_ppo {
+    const float* old_logp;
+    const float* advantage;
+    const float* weight;
+    const float* ref_logp;
+    float clip_low, clip_high, kl_coef, entropy_coef;
+} malib_token_ppo;
+int malib_learn_token_ppo(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_ppo* loss,
+                          const malib_token_grad* grad, float* logp_out, float* stats_out);
+
+/*
+ * malib_learn_token_pref - the preference loss on pairs of answers. offsets int64
+ * [2 n_pairs + 1] rises from 0 to n_rows; rows offsets[2k] .. offsets[2k+1] - 1 are
+ * pair k's chosen answer, those up to offsets[2k+2] - 1 the rejected one (either
+ * may be empty). With the answers' rewards
+ *   R = beta sum over the answer's rows (ln p - ref_logp),   D_k = R_chosen - R_rejected:
+ *   L = (1 / n_pairs) sum_k -(1 - smooth) ln s(D_k) - smooth ln s(-D_k),  s(x) = 1 / (1 + e^-x).
+ * ref_logp [n_rows] may be NULL (0). beta > 0, smooth = label_smoothing in [0, 1).
+ * reward_out [2 n_pairs] (optional): the rewards in the offsets' order. stats_out
+ * (optional) float [5]: n_pairs, L, share of pairs with D > 0, mean reward of the chosen,
+ * of the rejected. Offsets that do not rise from 0 to n_rows give MALIB_EINVAL at the
+ * next malib_sync (outputs undefined). n_pairs >= 1.
+ */
+typedef struct malib_token_pref {
+    const int64_t* offsets;
+    const float* ref_logp;
+    int32_t n_pairs;
+    float beta, label_smoothing;
+} malib_token_pref;
+int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_pref* loss,
+                           const malib_token_grad* grad, float* reward_out, float* stats_out);
+
+/*
+ * malib_learn_token_distill - distillation from a teacher's top entries, e.g. of the
+ * best member of a population into one policy. Row i has `top` teacher entries: ids
+ * int32 [n_rows][top] (< 0: absent) with logits teacher [n_rows][top] of type
+ * teacher_dtype (-infinity: absent too). The teacher's distribution is their softmax
+ * at the batch's temperature, q; an id listed twice has the sum of its q:
+ *   l_i = T^2 sum_k q_k (ln q_k - ln p_{id_k}),   L = sum_i w_i l_i.
+ * batch->tokens must be NULL. 1 <= top <= 1024. weight as above. loss_out [n_rows]
+ * (optional): l. stats_out (optional) float [3]: rows counted, L, mean l of those.
+ */
+typedef struct malib_token_distill {
+    const int32_t* ids;
+    const void* teacher;
+    const float* weight;
+    int32_t top;
+    int32_t teacher_dtype;
+} malib_token_distill;
+int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_distill* loss,
+                              const malib_token_grad* grad, float* loss_out, float* stats_out);
 
 /* ---- measurement and self-test entry points (used by tests and the benchmark) ---- */
 

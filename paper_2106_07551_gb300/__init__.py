@@ -17,13 +17,14 @@ from . import _abi
 from ._abi import (MALIB_BF16, MALIB_DUMP_LOGITS, MALIB_ENOTCONVERGED, MALIB_ENV_KUHN,
                    MALIB_ENV_LEDUC, MALIB_ENV_SPREAD, MALIB_ENV_ADVERSARY, MALIB_ENV_SPEAKER_LISTENER,
                    MALIB_ENV_PUSH, MALIB_ENV_TAG, MALIB_ENV_REFERENCE, MALIB_EXACT_EXPECTATION, MALIB_F32, MALIB_POL_MLP,
-                   MALIB_POL_TABULAR, MALIB_SPREAD_CONTACT, EnvSpec, PolicyDesc, Traj)
+                   MALIB_F16, MALIB_POL_TABULAR, MALIB_SPREAD_CONTACT, EnvSpec, PolicyDesc, TokenBatch, TokenDistill,
+                   TokenGrad, TokenPpo, TokenPref, Traj)
 
 __all__ = ["MalibError", "Context", "EnvSpec", "make_spec", "policy_desc", "alloc_traj",
            "alloc_eval_dump", "malib_create", "malib_pop_load", "malib_rollout",
            "malib_eval_payoff", "malib_eval_payoff_ex", "malib_eval_payoff_noalloc", "MALIB_ENV_KUHN", "MALIB_ENV_LEDUC",
            "MALIB_ENV_SPREAD", "MALIB_ENV_ADVERSARY", "MALIB_ENV_SPEAKER_LISTENER", "MALIB_ENV_PUSH",
-           "MALIB_ENV_TAG", "MALIB_ENV_REFERENCE", "MALIB_POL_TABULAR", "MALIB_POL_MLP", "MALIB_F32", "MALIB_BF16",
+           "MALIB_ENV_TAG", "MALIB_ENV_REFERENCE", "MALIB_POL_TABULAR", "MALIB_POL_MLP", "MALIB_F32", "MALIB_BF16", "MALIB_F16",
            "MALIB_DUMP_LOGITS", "MALIB_EXACT_EXPECTATION", "MALIB_SPREAD_CONTACT", "MALIB_ENOTCONVERGED"]
 
 
@@ -151,6 +152,50 @@ def alloc_eval_dump(env_kind: int, n_pairs: int, n_dump: int, device="cuda"):
     if P4:
         out["obs"] = torch.empty((n_pairs, n_dump, S, P4), dtype=torch.float32, device=device)
     return out
+
+
+def _vector(x, n, dtype, what):
+    """Address of a contiguous tensor of n values of a type (None -> NULL)."""
+    if x is None:
+        return None
+    if str(x.dtype) != dtype or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} values")
+    return x.data_ptr()
+
+
+_TOKEN_DTYPES = {"torch.float32": MALIB_F32, "torch.bfloat16": MALIB_BF16, "torch.float16": MALIB_F16}
+
+
+def _token_dtype(x, what):
+    code = _TOKEN_DTYPES.get(str(x.dtype))
+    if code is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16")
+    return code
+
+
+def _token_rows(x, what):
+    """(rows, vocabulary, row stride) of a matrix whose rows are contiguous."""
+    if x.dim() != 2:
+        raise ValueError(f"{what} must have two dimensions (rows, vocabulary)")
+    n, V = x.shape
+    if V < 1 or (V > 1 and x.stride(1) != 1):
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return n, V, x.stride(0) if n > 1 else V
+
+
+def _token_batch(logits, tokens, temperature):
+    n, V, ld = _token_rows(logits, "logits")
+    return TokenBatch(logits.data_ptr(), _vector(tokens, n, "torch.int32", "tokens"), n, ld, V,
+                      _token_dtype(logits, "logits"), temperature)
+
+
+def _token_grad(logits, grad, scale):
+    if grad is None:
+        return None
+    n, V, ld = _token_rows(grad, "grad_out")
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad_out must have the shape and type of logits")
+    return C.byref(TokenGrad(grad.data_ptr(), ld, scale))
 
 
 class Context:
@@ -315,6 +360,72 @@ class Context:
         """Replaces a loaded policy's parameters (same shape), host or device."""
         nbytes = int(params.numel()) * 4 if hasattr(params, "numel") else int(params.size) * 4
         _check(self.lib, self.handle, self.lib.malib_pop_update(self.handle, policy_id, _ptr(params), nbytes))
+
+    # ---- losses of token policies (device tensors; logits [rows][vocabulary], rows contiguous) ----
+    def token_logprob(self, logits, tokens, logp_out=None, entropy_out=None, temperature=1.0):
+        """ln p of each row's token into logp_out [rows] and the row's entropy into
+        entropy_out [rows]; rows with a negative token are left out (0)."""
+        b = _token_batch(logits, tokens, temperature)
+        n = b.n_rows
+        _check(self.lib, self.handle,
+               self.lib.malib_token_logprob(self.handle, C.byref(b), _vector(logp_out, n, "torch.float32", "logp_out"),
+                                            _vector(entropy_out, n, "torch.float32", "entropy_out")))
+
+    def learn_token_ppo(self, logits, tokens, old_logp, advantage, grad_out=None, stats_out=None, weight=None,
+                        ref_logp=None, logp_out=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0,
+                        temperature=1.0, grad_scale=1.0):
+        """The clipped surrogate per token, with a KL term to a reference and an
+        entropy term: the gradient at the logits into grad_out (may be logits
+        itself) and (rows counted, loss, clipped share, mean KL, mean entropy) into
+        stats_out (fp32 [5])."""
+        b = _token_batch(logits, tokens, temperature)
+        n, f32 = b.n_rows, "torch.float32"
+        p = TokenPpo(_vector(old_logp, n, f32, "old_logp"), _vector(advantage, n, f32, "advantage"),
+                     _vector(weight, n, f32, "weight"), _vector(ref_logp, n, f32, "ref_logp"), clip_low, clip_high,
+                     kl_coef, entropy_coef)
+        _check(self.lib, self.handle,
+               self.lib.malib_learn_token_ppo(self.handle, C.byref(b), C.byref(p),
+                                              _token_grad(logits, grad_out, grad_scale),
+                                              _vector(logp_out, n, f32, "logp_out"),
+                                              _vector(stats_out, 5, f32, "stats_out")))
+
+    def learn_token_pref(self, logits, tokens, offsets, grad_out=None, stats_out=None, ref_logp=None, reward_out=None,
+                         beta=0.1, label_smoothing=0.0, temperature=1.0, grad_scale=1.0):
+        """The preference loss of (chosen, rejected) answers, whose rows follow one
+        another as offsets (int64 [2 pairs + 1]) says: the gradient at the logits
+        into grad_out, the rewards [2 pairs] into reward_out and (pairs, loss, share
+        of pairs in order, mean reward chosen, rejected) into stats_out (fp32 [5])."""
+        b = _token_batch(logits, tokens, temperature)
+        n, f32, S = b.n_rows, "torch.float32", int(offsets.numel()) - 1
+        if S < 2 or S % 2:
+            raise ValueError("offsets must hold 2 pairs + 1 values")
+        p = TokenPref(_vector(offsets, S + 1, "torch.int64", "offsets"), _vector(ref_logp, n, f32, "ref_logp"), S // 2,
+                      beta, label_smoothing)
+        _check(self.lib, self.handle,
+               self.lib.malib_learn_token_pref(self.handle, C.byref(b), C.byref(p),
+                                               _token_grad(logits, grad_out, grad_scale),
+                                               _vector(reward_out, S, f32, "reward_out"),
+                                               _vector(stats_out, 5, f32, "stats_out")))
+
+    def learn_token_distill(self, logits, teacher_ids, teacher_logits, grad_out=None, stats_out=None, weight=None,
+                            loss_out=None, temperature=1.0, grad_scale=1.0):
+        """Distillation from a teacher's top entries, ids int32 [rows][top] (< 0:
+        absent) with their logits [rows][top]: the gradient at the logits into
+        grad_out, the rows' losses into loss_out [rows] and (rows counted, loss,
+        mean row loss) into stats_out (fp32 [3])."""
+        b = _token_batch(logits, None, temperature)
+        n, f32 = b.n_rows, "torch.float32"
+        if teacher_ids.dim() != 2 or teacher_ids.shape[0] != n or teacher_logits.shape != teacher_ids.shape:
+            raise ValueError("teacher_ids and teacher_logits must be [rows][top]")
+        top = teacher_ids.shape[1]
+        p = TokenDistill(_vector(teacher_ids, n * top, "torch.int32", "teacher_ids"),
+                         _vector(teacher_logits, n * top, str(teacher_logits.dtype), "teacher_logits"),
+                         _vector(weight, n, f32, "weight"), top, _token_dtype(teacher_logits, "teacher_logits"))
+        _check(self.lib, self.handle,
+               self.lib.malib_learn_token_distill(self.handle, C.byref(b), C.byref(p),
+                                                  _token_grad(logits, grad_out, grad_scale),
+                                                  _vector(loss_out, n, f32, "loss_out"),
+                                                  _vector(stats_out, 3, f32, "stats_out")))
 
     def exploitability(self, ids0, x, ids1, y):
         """(b0, b1, exploitability) of the seat mixtures (ids with fp64 weights)."""

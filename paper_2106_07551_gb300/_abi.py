@@ -20,7 +20,7 @@ STATUS_NAMES = {0: "OK", -1: "EINVAL", -2: "ENOMEM", -3: "ECUDA", -4: "ESTATE", 
 MALIB_ENV_KUHN, MALIB_ENV_LEDUC, MALIB_ENV_SPREAD, MALIB_ENV_ADVERSARY = 1, 2, 3, 4
 MALIB_ENV_SPEAKER_LISTENER, MALIB_ENV_PUSH, MALIB_ENV_TAG, MALIB_ENV_REFERENCE = 5, 6, 7, 8
 MALIB_POL_TABULAR, MALIB_POL_MLP = 1, 2
-MALIB_F32, MALIB_BF16 = 0, 1
+MALIB_F32, MALIB_BF16, MALIB_F16 = 0, 1, 2
 MALIB_DUMP_LOGITS, MALIB_EXACT_EXPECTATION, MALIB_SPREAD_LOCAL_RATIO = 1, 2, 4
 MALIB_SPREAD_CONTACT = 8
 
@@ -36,7 +36,8 @@ EXPORTS = (
     "malib_meta_lp_nash_ex",
     "malib_meta_aggregate", "malib_exploitability", "malib_learn_pg", "malib_learn_pg_batch",
     "malib_learn_ppo_batch", "malib_adam_step",
-    "malib_pop_update",
+    "malib_pop_update", "malib_token_logprob", "malib_learn_token_ppo", "malib_learn_token_pref",
+    "malib_learn_token_distill",
 )
 
 
@@ -55,6 +56,31 @@ class PolicyDesc(C.Structure):
 class Traj(C.Structure):
     _fields_ = [("obs", C.c_void_p), ("action", C.c_void_p), ("reward", C.c_void_p),
                 ("done", C.c_void_p), ("logits", C.c_void_p)]
+
+
+class TokenBatch(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("tokens", C.c_void_p), ("n_rows", C.c_int64), ("ld", C.c_int64),
+                ("vocab", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class TokenGrad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_float)]
+
+
+class TokenPpo(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("advantage", C.c_void_p), ("weight", C.c_void_p),
+                ("ref_logp", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_coef", C.c_float), ("entropy_coef", C.c_float)]
+
+
+class TokenPref(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("ref_logp", C.c_void_p), ("n_pairs", C.c_int32), ("beta", C.c_float),
+                ("label_smoothing", C.c_float)]
+
+
+class TokenDistill(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("teacher", C.c_void_p), ("weight", C.c_void_p), ("top", C.c_int32),
+                ("teacher_dtype", C.c_int32)]
 
 
 _lock = threading.Lock()
@@ -114,6 +140,13 @@ def load(path: str | None = None):
                                                 C.c_float, C.c_float, C.c_float, P, P]),
             "malib_adam_step": (C.c_int, [P, P, P, P, P, i64, i64, C.c_float, C.c_float, C.c_float, C.c_float]),
             "malib_pop_update": (C.c_int, [P, i32, P, i64]),
+            "malib_token_logprob": (C.c_int, [P, C.POINTER(TokenBatch), P, P]),
+            "malib_learn_token_ppo": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenPpo), C.POINTER(TokenGrad),
+                                                P, P]),
+            "malib_learn_token_pref": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenPref),
+                                                 C.POINTER(TokenGrad), P, P]),
+            "malib_learn_token_distill": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenDistill),
+                                                    C.POINTER(TokenGrad), P, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -15,6 +15,8 @@ enum : int {
     ERRBIT_BAD_PAIR = 1,      // an id in a device pair table is out of range / wrong seat
     ERRBIT_TIMEOUT = 2,       // a bounded mbarrier wait expired
     ERRBIT_NOT_CONVERGED = 4, // an iterative solver reached its iteration limit
+    ERRBIT_BAD_TOKEN = 8,     // a token or a teacher entry is past the vocabulary
+    ERRBIT_BAD_OFFSETS = 16,  // sequence offsets that do not rise from 0 to the row count
 };
 
 // fp32 MLP policy, kernel layout of one population member (floats, every
@@ -249,6 +251,10 @@ void ctx_count_launches(void* ctx, int n);
 int ctx_policy_seat(const void* ctx, int32_t id);
 // Device work space owned by the context, grown on its stream (cudaMallocAsync).
 int ctx_scratch(void* ctx, int64_t bytes, void** out);
+// Work space of the token losses: a fixed part of kTokenFixedBytes, zero when first
+// handed out, then `bytes` more.
+constexpr int64_t kTokenFixedBytes = 512 << 10;
+int ctx_token_work(void* ctx, int64_t bytes, void** fixed, void** more);
 
 // Meta-game solvers (meta_solver.cu).
 cudaError_t launch_fictitious_play(const double* P, int32_t G, int32_t m, int32_t n, int32_t stride,

@@ -69,6 +69,10 @@ struct malib_ctx {
     int64_t learn_work_cap = 0;
     float* learn_grad = nullptr;       // the gradient when the caller's buffer is host memory
     int64_t learn_grad_cap = 0;
+    uint8_t* token_fixed = nullptr;    // token losses: partial sums of the statistics, counters
+    int64_t token_fixed_cap = 0;
+    uint8_t* token_rows = nullptr;     // rows' statistics of preference pairs
+    int64_t token_rows_cap = 0;
 
     int64_t launches = 0;
     bool timing = false;
@@ -288,6 +292,10 @@ int read_device_errors(malib_ctx* c) {
             return fail(c, MALIB_ETIMEOUT, "a bounded device wait expired");
         if (h & ERRBIT_BAD_PAIR)
             return fail(c, MALIB_EINVAL, "a device pair table held an invalid policy id or seat");
+        if (h & ERRBIT_BAD_TOKEN)
+            return fail(c, MALIB_EINVAL, "a token or a teacher entry lies past the vocabulary");
+        if (h & ERRBIT_BAD_OFFSETS)
+            return fail(c, MALIB_EINVAL, "sequence offsets do not rise from 0 to the number of rows");
         if (h & ERRBIT_NOT_CONVERGED)
             return fail(c, MALIB_ENOTCONVERGED, "the LP solver reached its pivot limit");
     }
@@ -371,6 +379,21 @@ int ctx_scratch(void* ctx, int64_t bytes, void** out) {
     return MALIB_OK;
 }
 
+int ctx_token_work(void* ctx, int64_t bytes, void** fixed, void** more) {
+    malib_ctx* c = static_cast<malib_ctx*>(ctx);
+    if (!c || !fixed || bytes < 0) return MALIB_EINVAL;
+    if (!c->token_fixed) {
+        const int r = ensure(c, c->token_fixed, c->token_fixed_cap, kTokenFixedBytes, "token work space");
+        if (r != MALIB_OK) return r;
+        CK(cudaMemsetAsync(c->token_fixed, 0, kTokenFixedBytes, c->stream), "token work space");
+    }
+    const int r = ensure(c, c->token_rows, c->token_rows_cap, bytes, "token work space");
+    if (r != MALIB_OK) return r;
+    *fixed = c->token_fixed;
+    if (more) *more = c->token_rows;
+    return MALIB_OK;
+}
+
 int ctx_policy_seat(const void* ctx, int32_t id) { return static_cast<const malib_ctx*>(ctx)->pols[id].seat; }
 
 void ctx_count_launches(void* ctx, int n) {
@@ -425,6 +448,8 @@ void malib_destroy(malib_ctx* c) {
     cudaFree(c->lwork);
     cudaFree(c->learn_work);
     cudaFree(c->learn_grad);
+    cudaFree(c->token_fixed);
+    cudaFree(c->token_rows);
     cudaFree(c->d_stage);
     cudaFree(c->d_jobs);
     delete c;

@@ -1,0 +1,362 @@
+// Losses of token policies (token_common.cuh has the mathematics): one CTA takes a row
+// at a time, gathers its statistics in a first pass over the row and writes the
+// gradient in a second one.
+#include "token_common.cuh"
+
+namespace malib {
+
+namespace {
+
+constexpr int kT = 512, kW = kT / 32;
+
+// A row's elements in 16-byte vectors of its address: the first and last may be partial.
+template <class T>
+struct RowFrame {
+    static constexpr int W = Elt<T>::W;
+    const T* p;
+    int h, nv, V;                                    // elements before the row in its first vector; vectors
+    __device__ RowFrame(const T* row, int V_) : p(row), V(V_) {
+        h = (int)(((uintptr_t)row & 15u) / sizeof(T));
+        nv = (h + V + W - 1) / W;
+    }
+    // Entries outside the row read as -infinity.
+    __device__ __forceinline__ void load(int i, float (&v)[W]) const {
+        const int j = i * W - h;
+        if (j >= 0 && j + W <= V) {
+            Elt<T>::unpack(*reinterpret_cast<const uint4*>(p + j), v);
+        } else {
+#pragma unroll
+            for (int q = 0; q < W; ++q) v[q] = j + q >= 0 && j + q < V ? Elt<T>::get(p[j + q]) : -INFINITY;
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void store_vec(T* g, int j, int V, bool aligned, const float (&v)[Elt<T>::W]) {
+    constexpr int W = Elt<T>::W;
+    if (aligned && j >= 0 && j + W <= V) {
+        *reinterpret_cast<uint4*>(g + j) = Elt<T>::pack(v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < W; ++q)
+            if (j + q >= 0 && j + q < V) g[j + q] = Elt<T>::put(v[q]);
+    }
+}
+
+template <class T>
+__device__ void zero_row(T* g, int V) {
+    const RowFrame<T> f(g, V);
+    const float z[Elt<T>::W] = {};
+    for (int i = threadIdx.x; i < f.nv; i += kT) store_vec(g, i * Elt<T>::W - f.h, V, true, z);
+}
+
+// The gradient of a whole row (every thread of the block).
+template <class T>
+__device__ void write_row(const T* z, T* g, int V, float k, const RowGrad& c, int token) {
+    constexpr int W = Elt<T>::W;
+    const RowFrame<T> f(z, V);
+    const bool aligned = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+    for (int i = threadIdx.x; i < f.nv; i += kT) {
+        float v[W];
+        f.load(i, v);
+        const int j = i * W - f.h;
+#pragma unroll
+        for (int q = 0; q < W; ++q) {
+            const float x = (v[q] - c.m) * k, e = exp2_fast(x);
+            v[q] = e * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
+            if (j + q == token) v[q] += c.at;
+        }
+        store_vec(g, j, V, aligned, v);
+    }
+}
+
+__device__ __forceinline__ float teacher_at(const TokenArgs& a, int64_t i) {
+    if (a.tdtype == MALIB_F32) return static_cast<const float*>(a.teacher)[i];
+    if (a.tdtype == MALIB_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.teacher)[i]);
+    return __half2float(static_cast<const __half*>(a.teacher)[i]);
+}
+
+struct TopEntry {
+    int id;                                          // -1: absent
+    float q;                                         // the teacher's probability of the entry
+};
+
+// The teacher's distribution over a row's entries by one warp: q in list, and sum q ln q
+// as the return value; *live: the list has an entry. Teacher logits of -infinity are
+// absent.
+__device__ float teacher_row(const TokenArgs& a, int64_t row, TopEntry* list, bool* live) {
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY;
+    for (int j = lane; j < a.top; j += 32) {
+        int id = a.ids[row * a.top + j];
+        const float t = teacher_at(a, row * a.top + j);
+        if (id >= a.V) {
+            atomicOr(a.err, ERRBIT_BAD_TOKEN);
+            id = -1;
+        }
+        if (id < 0 || t == -INFINITY) id = -1;
+        else m = max_nan(m, t);
+        list[j] = TopEntry{id, t};
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    *live = m != -INFINITY;
+    float s = 0.f;
+    for (int j = lane; j < a.top; j += 32) {
+        const float d = (list[j].q - m) * a.inv_t;
+        if (list[j].id >= 0) s += expf(d);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const float ls = logf(s);
+    float h = 0.f;
+    for (int j = lane; j < a.top; j += 32) {
+        const float lq = (list[j].q - m) * a.inv_t - ls, q = expf(lq);
+        list[j].q = list[j].id >= 0 ? q : 0.f;
+        if (list[j].id >= 0 && q != 0.f) h += q * lq;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) h += __shfl_xor_sync(0xffffffffu, h, o);
+    __syncwarp();
+    return h;
+}
+
+template <class T, int kOp>
+__global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
+    constexpr int W = Elt<T>::W;
+    __shared__ RowStat red[2][kW];
+    __shared__ RowGrad grad;
+    __shared__ TopEntry list[kOp == kTokDistill ? kTokenMaxTop : 1];
+    __shared__ bool list_live;
+    __shared__ float list_h;
+    double acc[kTokenStats] = {};                    // thread 0
+    int buf = 0;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        T* g = a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
+        int token = -1;
+        bool live = true;
+        float w = 1.f;
+        if (kOp == kTokDistill) {
+            if (threadIdx.x < 32) {
+                bool l;
+                const float h = teacher_row(a, row, list, &l);
+                if (threadIdx.x == 0) {
+                    list_live = l;
+                    list_h = h;
+                }
+            }
+            __syncthreads();
+            live = list_live;
+        } else {
+            token = a.tokens[row];
+            live = token >= 0 && token < a.V;
+            if (token >= a.V && threadIdx.x == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        }
+        if (kOp != kTokLogp) {
+            w = a.weight ? a.weight[row] : a.w0;
+            live = live && w != 0.f;
+        }
+        RowStat r{-INFINITY, 0.f, 0.f};
+        if (live) {
+            const RowFrame<T> f(z, a.V);
+            for (int i = threadIdx.x; i < f.nv; i += kT) {
+                float v[W];
+                f.load(i, v);
+                add_entries(r, v, a.k);
+            }
+            r = block_stat<kW>(r, a.k, red[buf]);
+            buf ^= 1;                                // one barrier a row: the other slots next
+            live = r.m != -INFINITY;                 // a row without an entry has no distribution
+        }
+        float loss = 0.f, logp = 0.f, H = 0.f;
+        if (kOp == kTokDistill && live && threadIdx.x < 32) {
+            // T^2 sum_k q_k (ln q_k - ln p_k)
+            float c = 0.f;
+            for (int j = threadIdx.x; j < a.top; j += 32)
+                if (list[j].q != 0.f) c += list[j].q * log_prob(r, Elt<T>::get(z[list[j].id]), a.inv_t);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+            loss = a.tt * (list_h - c);
+        }
+        if (threadIdx.x == 0) {
+            if (live) {
+                acc[0] += 1.0;
+                RowGrad c{r.m, 0.f, 0.f, 0.f};
+                if (kOp == kTokDistill) {
+                    c.c0 = w * a.gscale * a.tt * a.inv_t / r.s;
+                    acc[1] += (double)w * loss;
+                    acc[2] += loss;
+                } else {
+                    logp = log_prob(r, Elt<T>::get(z[token]), a.inv_t);
+                    if (kOp == kTokPpo) {
+                        float clipped, kl;
+                        c = ppo_row(a, row, r, logp, w, &loss, &clipped, &kl, &H);
+                        acc[1] += (double)w * loss;
+                        acc[2] += clipped;
+                        acc[3] += kl;
+                        acc[4] += H;
+                    }
+                }
+                grad = c;
+            }
+            if (kOp == kTokLogp) {
+                if (a.logp) a.logp[row] = logp;
+                if (a.entropy) a.entropy[row] = live ? row_entropy(r) : 0.f;
+                if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, live ? 1 : 0};
+            }
+            if (kOp == kTokPpo && a.logp) a.logp[row] = logp;
+            if (kOp == kTokDistill && a.loss) a.loss[row] = loss;
+        }
+        if (kOp == kTokLogp) continue;
+        __syncthreads();
+        if (g) {
+            if (!live) {
+                zero_row(g, a.V);
+            } else if (kOp == kTokPpo) {
+                write_row(z, g, a.V, a.k, grad, token);
+            } else {
+                // the student's probabilities at the teacher's entries, before the row is
+                // written (it may be written in place)
+                const RowGrad c = grad;
+                float v[kTokenMaxTop / kT];
+#pragma unroll
+                for (int u = 0; u < kTokenMaxTop / kT; ++u) {
+                    const int j = threadIdx.x + u * kT;
+                    if (j >= a.top || list[j].id < 0) continue;
+                    // an entry listed more than once has the sum of its probabilities
+                    float q = 0.f;
+                    for (int o = 0; o < a.top; ++o)
+                        if (list[o].id == list[j].id) q += list[o].q;
+                    v[u] = c.c0 * exp2_fast((Elt<T>::get(z[list[j].id]) - c.m) * a.k) - w * a.gscale * a.tt * a.inv_t * q;
+                }
+                __syncthreads();
+                write_row(z, g, a.V, a.k, c, -1);
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < kTokenMaxTop / kT; ++u) {
+                    const int j = threadIdx.x + u * kT;
+                    if (j < a.top && list[j].id >= 0) g[list[j].id] = Elt<T>::put(v[u]);
+                }
+            }
+        }
+        __syncthreads();                             // grad and list are free
+    }
+    if (kOp == kTokLogp || !a.stats) return;
+    double v[kTokenStats];
+    if (!sum_partials<kT>(a.part, a.ticket, acc, v)) return;
+    const double M = v[0] > 0.0 ? v[0] : 1.0;
+    a.stats[0] = (float)v[0];
+    a.stats[1] = (float)v[1];
+    a.stats[2] = (float)(v[2] / M);
+    if (kOp == kTokPpo) {
+        a.stats[3] = (float)(v[3] / M);
+        a.stats[4] = (float)(v[4] / M);
+    }
+}
+
+constexpr int kPairT = 128;
+
+// One CTA a pair: the rewards of its two sequences, the loss, and the factor of its
+// rows' gradients. Sums in fp64, in a fixed order.
+__global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
+    __shared__ double red[kPairT / 32];
+    double acc[kTokenStats] = {};
+    for (int p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
+        const int64_t o0 = a.offsets[2 * p], o1 = a.offsets[2 * p + 1], o2 = a.offsets[2 * p + 2];
+        const bool ok = o0 >= 0 && o0 <= o1 && o1 <= o2 && o2 <= a.n && (p > 0 || o0 == 0) &&
+                        (p + 1 < a.n_pairs || o2 == a.n);
+        if (!ok && threadIdx.x == 0) atomicOr(a.err, ERRBIT_BAD_OFFSETS);
+        float rew[2];
+        for (int side = 0; side < 2; ++side) {
+            const int64_t lo = !ok ? 0 : side ? o1 : o0, hi = !ok ? 0 : side ? o2 : o1;
+            double s = 0.0;
+            for (int64_t i = lo + threadIdx.x; i < hi; i += kPairT)
+                if (a.rows[i].live) s += (double)a.rows[i].logp - (a.ref ? (double)a.ref[i] : 0.0);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+            __syncthreads();
+            s = 0.0;
+            for (int w = 0; w < kPairT / 32; ++w) s += red[w];
+            rew[side] = (float)(a.beta * s);
+            if (threadIdx.x == 0) {
+                if (a.reward) a.reward[2 * p + side] = rew[side];
+                acc[3 + side] += a.beta * s;
+            }
+        }
+        if (threadIdx.x == 0) {
+            const float d = rew[0] - rew[1];
+            // -ln s(x) = max(-x, 0) + ln(1 + e^-|x|)
+            const float tail = log1pf(expf(-fabsf(d)));
+            const float lp = fmaxf(-d, 0.f) + tail, ln = fmaxf(d, 0.f) + tail;
+            acc[0] += 1.0;
+            acc[1] += (double)((1.f - a.smooth) * lp + a.smooth * ln);
+            acc[2] += d > 0.f ? 1.0 : 0.0;
+            // smooth s(d) - (1 - smooth) s(-d)
+            const float slope = a.smooth / (1.f + expf(-d)) - (1.f - a.smooth) / (1.f + expf(d));
+            a.pair_coef[p] = ok ? slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs : 0.f;
+        }
+    }
+    if (!a.stats) return;
+    double v[kTokenStats];
+    if (!sum_partials<kPairT>(a.part, a.ticket, acc, v)) return;
+    a.stats[0] = (float)v[0];
+    for (int i = 1; i < 5; ++i) a.stats[i] = (float)(v[i] / v[0]);
+}
+
+// The gradient of preference pairs from the rows' statistics and the pairs' factors.
+template <class T>
+__global__ void __launch_bounds__(kT) token_pair_grad_kernel(TokenArgs a) {
+    __shared__ RowGrad grad;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        if (threadIdx.x == 0) {
+            int lo = 0, hi = 2 * a.n_pairs;          // offsets[lo] <= row < offsets[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.offsets[mid] <= row) lo = mid;
+                else hi = mid;
+            }
+            const TokenRow r = a.rows[row];
+            const float c = (lo & 1) ? -a.pair_coef[lo >> 1] : a.pair_coef[lo >> 1];
+            grad = RowGrad{r.m, -c * r.inv_s, 0.f, c};
+        }
+        __syncthreads();
+        T* g = static_cast<T*>(a.g) + row * a.gld;
+        if (a.rows[row].live) write_row(static_cast<const T*>(a.z) + row * a.ld, g, a.V, a.k, grad, a.tokens[row]);
+        else zero_row(g, a.V);
+        __syncthreads();
+    }
+}
+
+template <class T>
+cudaError_t launch_rows_t(const TokenArgs& a, int op, int grid, cudaStream_t s) {
+    if (op == kTokLogp) token_rows_kernel<T, kTokLogp><<<grid, kT, 0, s>>>(a);
+    else if (op == kTokPpo) token_rows_kernel<T, kTokPpo><<<grid, kT, 0, s>>>(a);
+    else token_rows_kernel<T, kTokDistill><<<grid, kT, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    const int grid = (int)(a.n < 4 * (int64_t)n_sm ? (a.n > 0 ? a.n : 1) : 4 * (int64_t)n_sm);
+    if (a.dtype == MALIB_F32) return launch_rows_t<float>(a, op, grid, s);
+    if (a.dtype == MALIB_BF16) return launch_rows_t<__nv_bfloat16>(a, op, grid, s);
+    return launch_rows_t<__half>(a, op, grid, s);
+}
+
+cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    cudaError_t e = a.n > 0 ? launch_token_rows(a, kTokLogp, n_sm, s) : cudaSuccess;
+    if (e != cudaSuccess) return e;
+    token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
+    if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
+    const int grid = (int)(a.n < 4 * (int64_t)n_sm ? a.n : 4 * (int64_t)n_sm);
+    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kT, 0, s>>>(a);
+    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kT, 0, s>>>(a);
+    else token_pair_grad_kernel<__half><<<grid, kT, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace malib

@@ -485,7 +485,7 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
  * and gives one row of V logits for every position. These calls are the learner's
  * side of it (Sec. 3.3, App. C.2): from the logits of n_rows positions they compute
  * a loss and the gradient at the logits, which the caller's network carries back.
- * With the row's logits z and temperature T > 0, y = z / T, the policy is
+ * With the row's logits z and temperature T in [1e-6, 1e6], y = z / T, the policy is
  *   ln p_j = y_j - ln sum_i exp(y_i),   H = -sum_j p_j ln p_j.
  * Logits of -infinity are masked entries: p_j = 0, no entropy, gradient 0. A NaN
  * or +infinity among the logits makes the row's results NaN.

@@ -41,9 +41,9 @@ struct Call {
         if (b->ld != 0 && b->ld < b->vocab) return bad("logits row stride below vocab");
         const int64_t es = elt_size(b->dtype);
         if (b->n_rows > 0 && b->ld > INT64_MAX / es / b->n_rows) return bad("logits do not fit the address space");
-        const float k = (float)(1.4426950408889634074 / (double)b->temperature);
-        if (!(b->temperature > 0.0f) || !std::isfinite(b->temperature) || !std::isfinite(k) || !(k >= 1e-30f))
-            return bad("temperature must be positive and finite");
+        if (!(b->temperature >= 1e-6f && b->temperature <= 1e6f)) return bad("temperature must lie in [1e-6, 1e6]");
+        const double exact_k = 1.4426950408889634074 / (double)b->temperature;
+        const float k = (float)exact_k;
         if (b->n_rows > 0) {
             if (!dev(b->logits, (int)es)) return bad("logits must be aligned device memory of the context's device");
             if (tokens && !dev(b->tokens, 4)) return bad("tokens must be aligned device memory of the context's device");
@@ -55,6 +55,7 @@ struct Call {
         a.V = b->vocab;
         a.dtype = b->dtype;
         a.k = k;
+        a.dk = (float)(0.69314718055994530942 * (exact_k / (double)k - 1.0));
         a.inv_t = (float)(1.0 / (double)b->temperature);
         a.tt = b->temperature * b->temperature;
         a.tokens = b->tokens;
@@ -169,10 +170,8 @@ int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const
     if ((c.a.n > 0 && !c.opt(loss->ref_logp, 4)) || !c.opt(reward_out, 4) || !c.opt(stats_out, 4))
         return c.bad("ref_logp, reward_out and stats must be device memory of the context's device");
     void* rows = nullptr;
-    const int64_t row_bytes = (c.a.n * (int64_t)sizeof(TokenRow) + 255) / 256 * 256;
-    if ((r = c.work(row_bytes + (int64_t)loss->n_pairs * 4, &rows)) != MALIB_OK) return r;
+    if ((r = c.work(c.a.n * (int64_t)sizeof(TokenRow), &rows)) != MALIB_OK) return r;
     c.a.rows = static_cast<TokenRow*>(rows);
-    c.a.pair_coef = reinterpret_cast<float*>(static_cast<uint8_t*>(rows) + row_bytes);
     c.a.offsets = loss->offsets;
     c.a.n_pairs = loss->n_pairs;
     c.a.ref = loss->ref_logp;

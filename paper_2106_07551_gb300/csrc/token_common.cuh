@@ -4,8 +4,10 @@
 //   ln p_j = y_j - max y - ln S,  H = ln S - (1 / S) sum_j exp(y_j - max y) (y_j - max y).
 // Everything is computed in base 2 on x_j = (z_j - m) k, m = max z, k = log2(e) / T:
 // p_j = 2^x_j / S. The difference is taken before the product, so that neither the
-// lowest finite values of a type nor large logits overflow on the way, and a row of
-// equal values of any size is uniform.
+// lowest finite values of a type nor large logits overflow on the way, a row of equal
+// values of any size is uniform, and S >= 1: no ln p is above 0. (One fused
+// multiply-add z k - m k would save an operation for fp32 logits; 16-bit ones are
+// widened by the subtraction itself.)
 // A row's statistics are (m, S, t), t = sum_j 2^x_j x_j, gathered in one pass over the
 // row with a running maximum; two partial statistics combine by scaling with
 // 2^((m_a - m) k). They are held in fp32: a row's sum has at most a few hundred
@@ -21,6 +23,7 @@
 #include <cuda_runtime.h>
 
 #include "device_common.cuh"
+#include "f32x2.cuh"
 
 namespace malib {
 
@@ -28,11 +31,13 @@ constexpr int kTokenMaxTop = 1024;                   // teacher entries of a row
 constexpr int kTokenStats = 5;                       // sums of a call's statistics
 constexpr int kTokenMaxCtas = 8192;                  // CTAs whose partial sums the work space holds
 
-enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2 };
+enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3 };
 
-// What a row's statistics leave for a preference pair's sums and its gradient.
-struct TokenRow {
-    float m, inv_s, logp;
+// What a row's statistics leave for a preference pair's sums and its gradient: first
+// value is ln p of the token; the pair's sums put d L / d logit of the token before
+// -p in its place.
+struct __align__(16) TokenRow {
+    float m, inv_s, value;
     int32_t live;
 };
 
@@ -45,6 +50,7 @@ struct TokenArgs {
     int32_t V;
     int32_t dtype;
     float k, inv_t;              // log2(e) / T, 1 / T
+    float dk;                    // ln 2 times the relative error of k's rounding
     const int32_t* tokens;       // [n], < 0: the row is left out
     int* err;
     // policy loss, distillation
@@ -65,7 +71,6 @@ struct TokenArgs {
     const int64_t* offsets;      // [2 pairs + 1]
     int32_t n_pairs;
     float beta, smooth;
-    float* pair_coef;            // [n_pairs] d loss / d (reward difference), scaled for the gradient
     TokenRow* rows;              // [n]
     // results
     float* logp;
@@ -77,65 +82,108 @@ struct TokenArgs {
     unsigned* ticket;            // CTAs that have written their partial sums
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+using F2 = unsigned long long;                       // two floats
+__device__ __forceinline__ F2 f2_make(float lo, float hi) {
+    return f2_pack(__float_as_uint(lo), __float_as_uint(hi));
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 template <class T>
 struct Elt;                      // W elements in 16 bytes
 template <>
 struct Elt<float> {
     static constexpr int W = 4;
+    __device__ static float word(const uint32_t (&w)[4], int i) { return __uint_as_float(w[i]); }   // entry i
     __device__ static float get(float v) { return v; }
     __device__ static float put(float v) { return v; }
-    __device__ static void unpack(const uint4& q, float (&v)[4]) {
-        v[0] = __uint_as_float(q.x);
-        v[1] = __uint_as_float(q.y);
-        v[2] = __uint_as_float(q.z);
-        v[3] = __uint_as_float(q.w);
+    // the entries, two by two
+    __device__ static void pairs(const uint4& q, F2 (&v)[2]) {
+        v[0] = f2_pack(q.x, q.y);
+        v[1] = f2_pack(q.z, q.w);
     }
-    __device__ static uint4 pack(const float (&v)[4]) {
-        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    // their maximum (NaN if one is NaN)
+    __device__ static float max(const uint4& q) {
+        return max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)),
+                       max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+    __device__ static uint4 pack(const F2 (&v)[2]) {
+        const float2 a = f2_split(v[0]), b = f2_split(v[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
 };
 template <>
 struct Elt<__nv_bfloat16> {
     static constexpr int W = 8;
+    __device__ static __nv_bfloat16 word(const uint32_t (&w)[4], int i) {
+        return __ushort_as_bfloat16((unsigned short)(w[i >> 1] >> 16 * (i & 1)));
+    }
     __device__ static float get(__nv_bfloat16 v) { return __bfloat162float(v); }
     __device__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
-    __device__ static void unpack(const uint4& q, float (&v)[8]) {
+    __device__ static void pairs(const uint4& q, F2 (&v)[4]) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) v[i] = f2_pack(w[i] << 16, w[i] & 0xffff0000u);
     }
-    __device__ static uint4 pack(const float (&v)[8]) {
+    __device__ static float max(const uint4& q) {
+        uint32_t m;
+        asm("{\n .reg .b32 a, b;\n max.NaN.bf16x2 a, %1, %2;\n max.NaN.bf16x2 b, %3, %4;\n max.NaN.bf16x2 %0, a, b;\n}"
+            : "=r"(m) : "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w));
+        return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+    __device__ static uint4 pack(const F2 (&v)[4]) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = f2_split(v[i]);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f.y), "f"(f.x));
+        }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 template <>
 struct Elt<__half> {
     static constexpr int W = 8;
+    __device__ static __half word(const uint32_t (&w)[4], int i) {
+        return __ushort_as_half((unsigned short)(w[i >> 1] >> 16 * (i & 1)));
+    }
     __device__ static float get(__half v) { return __half2float(v); }
     __device__ static __half put(float v) { return __float2half_rn(v); }
-    __device__ static void unpack(const uint4& q, float (&v)[8]) {
+    __device__ static void pairs(const uint4& q, F2 (&v)[4]) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             __half2 h;
             *reinterpret_cast<uint32_t*>(&h) = w[i];
             const float2 f = __half22float2(h);
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
+            v[i] = f2_make(f.x, f.y);
         }
     }
-    __device__ static uint4 pack(const float (&v)[8]) {
+    __device__ static float max(const uint4& q) {
+        uint32_t m;
+        asm("{\n .reg .b32 a, b;\n max.NaN.f16x2 a, %1, %2;\n max.NaN.f16x2 b, %3, %4;\n max.NaN.f16x2 %0, a, b;\n}"
+            : "=r"(m) : "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w));
+        __half2 h;
+        *reinterpret_cast<uint32_t*>(&h) = m;
+        const float2 f = __half22float2(h);
+        return max_nan(f.x, f.y);
+    }
+    __device__ static uint4 pack(const F2 (&v)[4]) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = f2_split(v[i]);
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f.y), "f"(f.x));
+        }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
@@ -143,15 +191,19 @@ struct Elt<__half> {
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kXMin = -200.f;
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+__device__ __forceinline__ F2 f2_exp2(F2 x) {
+    const float2 v = f2_split(x);
+    return f2_make(exp2_fast(v.x), exp2_fast(v.y));
+}
+__device__ __forceinline__ F2 f2_floor_x(F2 x) {
+    const float2 v = f2_split(x);
+    return f2_make(fmaxf(v.x, kXMin), fmaxf(v.y, kXMin));
 }
 
 struct RowStat {
@@ -170,47 +222,58 @@ __device__ __forceinline__ RowStat combine(const RowStat& a, const RowStat& b, f
     return r;
 }
 
-// W further entries of a row join r.
-template <int W>
-__device__ __forceinline__ void add_entries(RowStat& r, const float (&v)[W], float k) {
-    float mx = v[0];
+// A running maximum takes in mx: sums so far are scaled to the new one.
+__device__ __forceinline__ void raise(RowStat& r, float mx, float k) {
+    if (mx <= r.m) return;                           // neither a new maximum nor a NaN
+    const float m = max_nan(r.m, mx);
+    const float d = fmaxf((r.m - m) * k, kXMin), f = exp2_fast(d);
+    r.t = f * fmaf(r.s, d, r.t);
+    r.s *= f;
+    r.m = m;
+}
+
+// 16 bytes of logits join r, whose maximum covers them already and is not -infinity.
+template <class T>
+__device__ __forceinline__ void gather(RowStat& r, const uint4& q, float k) {
+    constexpr int P = Elt<T>::W / 2;
+    F2 y[P], s = 0ull, t = 0ull;
+    Elt<T>::pairs(q, y);
+    const F2 k2 = f2_dup(k), neg = f2_dup(-r.m);
 #pragma unroll
-    for (int i = 1; i < W; ++i) mx = max_nan(mx, v[i]);
-    if (!(mx <= r.m)) {                              // a new maximum, or a NaN
-        const float m = max_nan(r.m, mx);
-        const float d = fmaxf((r.m - m) * k, kXMin), f = exp2_fast(d);
-        r.t = f * fmaf(r.s, d, r.t);
-        r.s *= f;
-        r.m = m;
+    for (int i = 0; i < P; ++i) {
+        const F2 x = f2_mul(f2_add(y[i], neg), k2), e = f2_exp2(x);
+        s = f2_add(s, e);
+        f2_fma(t, e, f2_floor_x(x));
     }
-    if (r.m == -INFINITY) return;
+    const float2 s2 = f2_split(s), t2 = f2_split(t);
+    r.s += s2.x + s2.y;
+    r.t += t2.x + t2.y;
+}
+
+// Statistics of N lanes that follow one another, the same in each: their maximum, then
+// their sums to its base.
+template <int N>
+__device__ __forceinline__ RowStat reduce_stat(RowStat r, float k) {
+    float m = r.m;
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const float x = (v[i] - r.m) * k;
-        const float e = exp2_fast(x);
-        r.s += e;
-        r.t = fmaf(e, fmaxf(x, kXMin), r.t);
+    for (int o = N / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    r = combine(r, RowStat{m, 0.f, 0.f}, k);
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) {
+        r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+        r.t += __shfl_xor_sync(0xffffffffu, r.t, o);
     }
+    return r;
 }
 
 // Statistics of the whole block, the same in every thread. red: a slot a warp.
 template <int kWarps>
 __device__ __forceinline__ RowStat block_stat(RowStat r, float k, RowStat* red) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        RowStat b;
-        b.m = __shfl_xor_sync(0xffffffffu, r.m, o);
-        b.s = __shfl_xor_sync(0xffffffffu, r.s, o);
-        b.t = __shfl_xor_sync(0xffffffffu, r.t, o);
-        r = combine(r, b, k);
-    }
+    r = reduce_stat<32>(r, k);
     if (lane == 0) red[warp] = r;
     __syncthreads();
-    r = red[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) r = combine(r, red[w], k);
-    return r;
+    return reduce_stat<kWarps>(red[lane % kWarps], k);
 }
 
 // The gradient at entry j is 2^x_j (c0 + c1 x_j), and `at` more at the row's token.
@@ -218,19 +281,64 @@ struct RowGrad {
     float m, c0, c1, at;
 };
 
+// ln S. k's rounding to fp32 shifts every row's ln S the same way, by ln 2 (dk / k) t / S,
+// which a sequence's sum would add up; taken out here.
+__device__ __forceinline__ float log_sum(const TokenArgs& a, const RowStat& r) {
+    return logf(r.s) + a.dk * (r.t / r.s);
+}
+// 16 bytes of the gradient. kEntropy: with the term in x.
+template <class T, bool kEntropy>
+__device__ __forceinline__ void emit(const uint4& q, const RowGrad& c, float k, F2 (&v)[Elt<T>::W / 2]) {
+    Elt<T>::pairs(q, v);
+    const F2 k2 = f2_dup(k), neg = f2_dup(-c.m), c0 = f2_dup(c.c0), c1 = f2_dup(c.c1);
+#pragma unroll
+    for (int i = 0; i < Elt<T>::W / 2; ++i) {
+        const F2 x = f2_mul(f2_add(v[i], neg), k2), e = f2_exp2(x);
+        F2 f = c0;
+        if (kEntropy) f2_fma(f, f2_floor_x(x), c1);
+        v[i] = f2_mul(e, f);
+    }
+}
+// `by` joins entry i.
+template <int P>
+__device__ __forceinline__ void add_at(F2 (&v)[P], int i, float by) {
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        const float2 f = f2_split(v[q]);
+        v[q] = f2_make(i == 2 * q ? f.x + by : f.x, i == 2 * q + 1 ? f.y + by : f.y);
+    }
+}
+// 16 bytes to a row's entries j .. of which only those in [0, V) are the row's.
+template <class T>
+__device__ __forceinline__ void store_part(T* g, int j, int V, const uint4& q) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < Elt<T>::W; ++i)
+        if (j + i >= 0 && j + i < V) g[i] = Elt<T>::word(w, i);
+}
+
 // ln p of the entry with logit z.
-__device__ __forceinline__ float log_prob(const RowStat& r, float z, float inv_t) {
-    return (z - r.m) * inv_t - logf(r.s);
+__device__ __forceinline__ float log_prob(const TokenArgs& a, const RowStat& r, float z) {
+    // ln 2 x (1 + d) for k's relative rounding d: (z - m) / T
+    const float x = (z - r.m) * a.k;
+    return fmaf(kLn2, x, a.dk * x) - log_sum(a, r);
 }
 __device__ __forceinline__ float row_entropy(const RowStat& r) {
     return logf(r.s) - kLn2 * (r.t / r.s);
 }
 
+struct PpoRow {
+    float old, adv, ref;
+};
+__device__ __forceinline__ PpoRow ppo_load(const TokenArgs& a, int64_t row) {
+    return PpoRow{a.old_logp[row], a.adv[row], a.ref ? a.ref[row] : 0.f};
+}
+
 // The clipped policy loss of one row (l, before its weight) and its gradient.
-__device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, int64_t row, const RowStat& r, float logp, float w,
+__device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in, const RowStat& r, float logp, float w,
                                            float* loss, float* clipped, float* kl, float* H) {
-    const float A = a.adv[row];
-    const float rho = expf(logp - a.old_logp[row]);
+    const float A = in.adv;
+    const float rho = expf(logp - in.old);
     const float free_ = rho * A;
     // a NaN ratio stays one (fminf and fmaxf would drop it)
     const float cut = (rho < a.ratio_lo ? a.ratio_lo : rho > a.ratio_hi ? a.ratio_hi : rho) * A;
@@ -240,7 +348,7 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, int64_t row, cons
     float slope = clip ? 0.f : -free_;               // d l / d ln p of the token
     *kl = 0.f;
     if (a.ref) {
-        const float d = a.ref[row] - logp, e = expm1f(d);
+        const float d = in.ref - logp, e = expm1f(d);
         *kl = e - d;
         l = fmaf(a.kl, *kl, l);
         slope = fmaf(-a.kl, e, slope);
@@ -251,6 +359,21 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, int64_t row, cons
     const float gt = f * slope, h = f * a.ent, inv_s = 1.f / r.s;
     // p (-gt + h (ln p + H)),  ln p = x ln 2 - ln S
     return RowGrad{r.m, inv_s * (a.ent != 0.f ? fmaf(h, *H - logf(r.s), -gt) : -gt), inv_s * h * kLn2, gt};
+}
+
+// The outputs of a row whose log-probability is all that is asked for.
+__device__ __forceinline__ void logp_row(const TokenArgs& a, int64_t row, bool live, const RowStat& r, float z) {
+    const float logp = live ? log_prob(a, r, z) : 0.f;
+    if (a.logp) a.logp[row] = logp;
+    if (a.entropy) a.entropy[row] = live ? row_entropy(r) : 0.f;
+    if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, live ? 1 : 0};
+}
+
+__device__ __forceinline__ void ppo_stats(const TokenArgs& a, const double (&v)[kTokenStats]) {
+    const double M = v[0] > 0.0 ? v[0] : 1.0;
+    a.stats[0] = (float)v[0];
+    a.stats[1] = (float)v[1];
+    for (int i = 2; i < 5; ++i) a.stats[i] = (float)(v[i] / M);
 }
 
 // Partial sums of a call's statistics: the CTA's, then, in the CTA that comes last,
@@ -291,6 +414,8 @@ __device__ __forceinline__ bool sum_partials(double* part, unsigned* ticket, con
 }
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+// Rows of at least a few KB (token_ring.cu); false: the shape is not taken.
+bool launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s, cudaError_t* e);
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s);
 
 }  // namespace malib

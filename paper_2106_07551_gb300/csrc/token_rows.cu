@@ -20,33 +20,29 @@ struct RowFrame {
         nv = (h + V + W - 1) / W;
     }
     // Entries outside the row read as -infinity.
-    __device__ __forceinline__ void load(int i, float (&v)[W]) const {
+    __device__ __forceinline__ uint4 load(int i) const {
         const int j = i * W - h;
-        if (j >= 0 && j + W <= V) {
-            Elt<T>::unpack(*reinterpret_cast<const uint4*>(p + j), v);
-        } else {
+        if (j >= 0 && j + W <= V) return *reinterpret_cast<const uint4*>(p + j);
+        F2 v[W / 2];
 #pragma unroll
-            for (int q = 0; q < W; ++q) v[q] = j + q >= 0 && j + q < V ? Elt<T>::get(p[j + q]) : -INFINITY;
-        }
+        for (int q = 0; q < W; q += 2)
+            v[q / 2] = f2_make(j + q >= 0 && j + q < V ? Elt<T>::get(p[j + q]) : -INFINITY,
+                               j + q + 1 >= 0 && j + q + 1 < V ? Elt<T>::get(p[j + q + 1]) : -INFINITY);
+        return Elt<T>::pack(v);
     }
 };
 
 template <class T>
-__device__ __forceinline__ void store_vec(T* g, int j, int V, bool aligned, const float (&v)[Elt<T>::W]) {
+__device__ __forceinline__ void store_vec(T* g, int j, int V, bool aligned, const uint4& v) {
     constexpr int W = Elt<T>::W;
-    if (aligned && j >= 0 && j + W <= V) {
-        *reinterpret_cast<uint4*>(g + j) = Elt<T>::pack(v);
-    } else {
-#pragma unroll
-        for (int q = 0; q < W; ++q)
-            if (j + q >= 0 && j + q < V) g[j + q] = Elt<T>::put(v[q]);
-    }
+    if (aligned && j >= 0 && j + W <= V) *reinterpret_cast<uint4*>(g + j) = v;
+    else store_part(g + j, j, V, v);
 }
 
 template <class T>
 __device__ void zero_row(T* g, int V) {
     const RowFrame<T> f(g, V);
-    const float z[Elt<T>::W] = {};
+    const uint4 z = make_uint4(0, 0, 0, 0);
     for (int i = threadIdx.x; i < f.nv; i += kT) store_vec(g, i * Elt<T>::W - f.h, V, true, z);
 }
 
@@ -57,16 +53,11 @@ __device__ void write_row(const T* z, T* g, int V, float k, const RowGrad& c, in
     const RowFrame<T> f(z, V);
     const bool aligned = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
     for (int i = threadIdx.x; i < f.nv; i += kT) {
-        float v[W];
-        f.load(i, v);
+        F2 v[W / 2];
+        emit<T, true>(f.load(i), c, k, v);
         const int j = i * W - f.h;
-#pragma unroll
-        for (int q = 0; q < W; ++q) {
-            const float x = (v[q] - c.m) * k, e = exp2_fast(x);
-            v[q] = e * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
-            if (j + q == token) v[q] += c.at;
-        }
-        store_vec(g, j, V, aligned, v);
+        if ((unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
+        store_vec(g, j, V, aligned, Elt<T>::pack(v));
     }
 }
 
@@ -123,7 +114,6 @@ __device__ float teacher_row(const TokenArgs& a, int64_t row, TopEntry* list, bo
 
 template <class T, int kOp>
 __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
-    constexpr int W = Elt<T>::W;
     __shared__ RowStat red[2][kW];
     __shared__ RowGrad grad;
     __shared__ TopEntry list[kOp == kTokDistill ? kTokenMaxTop : 1];
@@ -161,9 +151,9 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
         if (live) {
             const RowFrame<T> f(z, a.V);
             for (int i = threadIdx.x; i < f.nv; i += kT) {
-                float v[W];
-                f.load(i, v);
-                add_entries(r, v, a.k);
+                const uint4 q = f.load(i);
+                raise(r, Elt<T>::max(q), a.k);
+                if (r.m != -INFINITY) gather<T>(r, q, a.k);
             }
             r = block_stat<kW>(r, a.k, red[buf]);
             buf ^= 1;                                // one barrier a row: the other slots next
@@ -174,7 +164,7 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
             // T^2 sum_k q_k (ln q_k - ln p_k)
             float c = 0.f;
             for (int j = threadIdx.x; j < a.top; j += 32)
-                if (list[j].q != 0.f) c += list[j].q * log_prob(r, Elt<T>::get(z[list[j].id]), a.inv_t);
+                if (list[j].q != 0.f) c += list[j].q * log_prob(a, r, Elt<T>::get(z[list[j].id]));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
             loss = a.tt * (list_h - c);
@@ -187,24 +177,18 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
                     c.c0 = w * a.gscale * a.tt * a.inv_t / r.s;
                     acc[1] += (double)w * loss;
                     acc[2] += loss;
-                } else {
-                    logp = log_prob(r, Elt<T>::get(z[token]), a.inv_t);
-                    if (kOp == kTokPpo) {
-                        float clipped, kl;
-                        c = ppo_row(a, row, r, logp, w, &loss, &clipped, &kl, &H);
-                        acc[1] += (double)w * loss;
-                        acc[2] += clipped;
-                        acc[3] += kl;
-                        acc[4] += H;
-                    }
+                } else if (kOp == kTokPpo) {
+                    logp = log_prob(a, r, Elt<T>::get(z[token]));
+                    float clipped, kl;
+                    c = ppo_row(a, ppo_load(a, row), r, logp, w, &loss, &clipped, &kl, &H);
+                    acc[1] += (double)w * loss;
+                    acc[2] += clipped;
+                    acc[3] += kl;
+                    acc[4] += H;
                 }
                 grad = c;
             }
-            if (kOp == kTokLogp) {
-                if (a.logp) a.logp[row] = logp;
-                if (a.entropy) a.entropy[row] = live ? row_entropy(r) : 0.f;
-                if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, live ? 1 : 0};
-            }
+            if (kOp == kTokLogp) logp_row(a, row, live, r, live ? Elt<T>::get(z[token]) : 0.f);
             if (kOp == kTokPpo && a.logp) a.logp[row] = logp;
             if (kOp == kTokDistill && a.loss) a.loss[row] = loss;
         }
@@ -245,13 +229,12 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
     if (kOp == kTokLogp || !a.stats) return;
     double v[kTokenStats];
     if (!sum_partials<kT>(a.part, a.ticket, acc, v)) return;
-    const double M = v[0] > 0.0 ? v[0] : 1.0;
-    a.stats[0] = (float)v[0];
-    a.stats[1] = (float)v[1];
-    a.stats[2] = (float)(v[2] / M);
     if (kOp == kTokPpo) {
-        a.stats[3] = (float)(v[3] / M);
-        a.stats[4] = (float)(v[4] / M);
+        ppo_stats(a, v);
+    } else {
+        a.stats[0] = (float)v[0];
+        a.stats[1] = (float)v[1];
+        a.stats[2] = (float)(v[2] / (v[0] > 0.0 ? v[0] : 1.0));
     }
 }
 
@@ -268,11 +251,12 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
                         (p + 1 < a.n_pairs || o2 == a.n);
         if (!ok && threadIdx.x == 0) atomicOr(a.err, ERRBIT_BAD_OFFSETS);
         float rew[2];
+        __shared__ float factor;
         for (int side = 0; side < 2; ++side) {
             const int64_t lo = !ok ? 0 : side ? o1 : o0, hi = !ok ? 0 : side ? o2 : o1;
             double s = 0.0;
             for (int64_t i = lo + threadIdx.x; i < hi; i += kPairT)
-                if (a.rows[i].live) s += (double)a.rows[i].logp - (a.ref ? (double)a.ref[i] : 0.0);
+                if (a.rows[i].live) s += (double)a.rows[i].value - (a.ref ? (double)a.ref[i] : 0.0);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
             __syncthreads();
@@ -296,7 +280,12 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
             acc[2] += d > 0.f ? 1.0 : 0.0;
             // smooth s(d) - (1 - smooth) s(-d)
             const float slope = a.smooth / (1.f + expf(-d)) - (1.f - a.smooth) / (1.f + expf(d));
-            a.pair_coef[p] = ok ? slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs : 0.f;
+            factor = slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs;
+        }
+        __syncthreads();
+        const float f = factor;
+        if (a.g && ok) {
+            for (int64_t i = o0 + threadIdx.x; i < o2; i += kPairT) a.rows[i].value = i < o1 ? f : -f;
         }
     }
     if (!a.stats) return;
@@ -312,15 +301,8 @@ __global__ void __launch_bounds__(kT) token_pair_grad_kernel(TokenArgs a) {
     __shared__ RowGrad grad;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         if (threadIdx.x == 0) {
-            int lo = 0, hi = 2 * a.n_pairs;          // offsets[lo] <= row < offsets[hi]
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (a.offsets[mid] <= row) lo = mid;
-                else hi = mid;
-            }
             const TokenRow r = a.rows[row];
-            const float c = (lo & 1) ? -a.pair_coef[lo >> 1] : a.pair_coef[lo >> 1];
-            grad = RowGrad{r.m, -c * r.inv_s, 0.f, c};
+            grad = RowGrad{r.m, -r.value * r.inv_s, 0.f, r.value};
         }
         __syncthreads();
         T* g = static_cast<T*>(a.g) + row * a.gld;
@@ -340,7 +322,14 @@ cudaError_t launch_rows_t(const TokenArgs& a, int op, int grid, cudaStream_t s) 
 
 }  // namespace
 
+// From this many bytes on a row is long: it goes through shared memory.
+constexpr int kRingBytes = 2048;
+
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    cudaError_t e;
+    if (op != kTokDistill && a.n > 0 && (int64_t)a.V * (a.dtype == MALIB_F32 ? 4 : 2) >= kRingBytes &&
+        launch_token_ring(a, op, n_sm, s, &e))
+        return e;
     const int grid = (int)(a.n < 4 * (int64_t)n_sm ? (a.n > 0 ? a.n : 1) : 4 * (int64_t)n_sm);
     if (a.dtype == MALIB_F32) return launch_rows_t<float>(a, op, grid, s);
     if (a.dtype == MALIB_BF16) return launch_rows_t<__nv_bfloat16>(a, op, grid, s);
@@ -352,6 +341,8 @@ cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
+    if ((int64_t)a.V * (a.dtype == MALIB_F32 ? 4 : 2) >= kRingBytes && launch_token_ring(a, kTokPairGrad, n_sm, s, &e))
+        return e;
     const int grid = (int)(a.n < 4 * (int64_t)n_sm ? a.n : 4 * (int64_t)n_sm);
     if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kT, 0, s>>>(a);
     else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kT, 0, s>>>(a);

@@ -251,10 +251,10 @@ void ctx_count_launches(void* ctx, int n);
 int ctx_policy_seat(const void* ctx, int32_t id);
 // Device work space owned by the context, grown on its stream (cudaMallocAsync).
 int ctx_scratch(void* ctx, int64_t bytes, void** out);
-// Work space of the token losses: a fixed part of kTokenFixedBytes, zero when first
-// handed out, then `bytes` more.
+// Work space of the token losses: kTokenFixedBytes that are 0 when first handed out (the
+// kernels leave their counters so), and `bytes` of any content.
 constexpr int64_t kTokenFixedBytes = 512 << 10;
-int ctx_token_work(void* ctx, int64_t bytes, void** fixed, void** more);
+int ctx_token_work(void* ctx, int64_t bytes, void** fixed_out, void** out);
 
 // Meta-game solvers (meta_solver.cu).
 cudaError_t launch_fictitious_play(const double* P, int32_t G, int32_t m, int32_t n, int32_t stride,

@@ -69,9 +69,9 @@ struct malib_ctx {
     int64_t learn_work_cap = 0;
     float* learn_grad = nullptr;       // the gradient when the caller's buffer is host memory
     int64_t learn_grad_cap = 0;
-    uint8_t* token_fixed = nullptr;    // token losses: partial sums of the statistics, counters
+    uint8_t* token_fixed = nullptr;    // token losses: counters, partial sums
     int64_t token_fixed_cap = 0;
-    uint8_t* token_rows = nullptr;     // rows' statistics of preference pairs
+    uint8_t* token_rows = nullptr;     // a row's statistics or share of a call's
     int64_t token_rows_cap = 0;
 
     int64_t launches = 0;
@@ -379,18 +379,17 @@ int ctx_scratch(void* ctx, int64_t bytes, void** out) {
     return MALIB_OK;
 }
 
-int ctx_token_work(void* ctx, int64_t bytes, void** fixed, void** more) {
+int ctx_token_work(void* ctx, int64_t bytes, void** fixed_out, void** out) {
     malib_ctx* c = static_cast<malib_ctx*>(ctx);
-    if (!c || !fixed || bytes < 0) return MALIB_EINVAL;
+    if (!c || bytes < 0) return MALIB_EINVAL;
+    int r;
     if (!c->token_fixed) {
-        const int r = ensure(c, c->token_fixed, c->token_fixed_cap, kTokenFixedBytes, "token work space");
-        if (r != MALIB_OK) return r;
+        if ((r = ensure(c, c->token_fixed, c->token_fixed_cap, kTokenFixedBytes, "token work space")) != MALIB_OK) return r;
         CK(cudaMemsetAsync(c->token_fixed, 0, kTokenFixedBytes, c->stream), "token work space");
     }
-    const int r = ensure(c, c->token_rows, c->token_rows_cap, bytes, "token work space");
-    if (r != MALIB_OK) return r;
-    *fixed = c->token_fixed;
-    if (more) *more = c->token_rows;
+    if ((r = ensure(c, c->token_rows, c->token_rows_cap, bytes, "token work space")) != MALIB_OK) return r;
+    *fixed_out = c->token_fixed;
+    *out = c->token_rows;
     return MALIB_OK;
 }
 

@@ -58,6 +58,7 @@ struct Call {
         a.dk = (float)(0.69314718055994530942 * (exact_k / (double)k - 1.0));
         a.inv_t = (float)(1.0 / (double)b->temperature);
         a.tt = b->temperature * b->temperature;
+        a.top_scale = b->temperature;
         a.tokens = b->tokens;
         a.err = v.err;
         return MALIB_OK;
@@ -89,12 +90,16 @@ struct Call {
         return MALIB_OK;
     }
 
-    int work(int64_t more, void** rows) {
-        void* fixed = nullptr;
-        const int r = ctx_token_work(ctx, more, &fixed, rows);
+    // Work space: counters, partial sums, and a row's statistics or share of them.
+    int work() {
+        static_assert(sizeof(TokenRow) == sizeof(RowSum), "one work space for either");
+        void *fixed = nullptr, *rows = nullptr;
+        const int r = ctx_token_work(ctx, a.n * (int64_t)sizeof(RowSum), &fixed, &rows);
         if (r != MALIB_OK) return r;
         a.ticket = static_cast<unsigned*>(fixed);
+        a.claims = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(fixed) + 128);
         a.part = reinterpret_cast<double*>(static_cast<uint8_t*>(fixed) + kPartOffset);
+        a.row_sums = static_cast<RowSum*>(rows);
         return MALIB_OK;
     }
 
@@ -113,11 +118,12 @@ int malib_token_logprob(malib_ctx* ctx, const malib_token_batch* batch, float* l
     Call c{ctx};
     if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
     DevSel d(c.v.device);
-    const int r = c.begin(batch, true);
+    int r = c.begin(batch, true);
     if (r != MALIB_OK) return r;
     if (c.a.n == 0) return MALIB_OK;
     if (!c.opt(logp_out, 4) || !c.opt(entropy_out, 4))
         return c.bad("outputs must be device memory of the context's device");
+    if ((r = c.work()) != MALIB_OK) return r;
     c.a.logp = logp_out;
     c.a.entropy = entropy_out;
     return c.done(launch_token_rows(c.a, kTokLogp, c.v.n_sm, c.v.stream), 1);
@@ -141,7 +147,7 @@ int malib_learn_token_ppo(malib_ctx* ctx, const malib_token_batch* batch, const 
                       !c.opt(logp_out, 4)))
         return c.bad("old_logp, advantage, ref_logp and logp_out must be device memory of the context's device");
     if (!c.opt(stats_out, 4)) return c.bad("stats must be device memory of the context's device");
-    if ((r = c.work(0, nullptr)) != MALIB_OK) return r;
+    if ((r = c.work()) != MALIB_OK) return r;
     c.a.old_logp = loss->old_logp;
     c.a.adv = loss->advantage;
     c.a.ref = loss->ref_logp;
@@ -169,9 +175,8 @@ int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const
     if (!c.dev(loss->offsets, 8)) return c.bad("offsets must be aligned device memory of the context's device");
     if ((c.a.n > 0 && !c.opt(loss->ref_logp, 4)) || !c.opt(reward_out, 4) || !c.opt(stats_out, 4))
         return c.bad("ref_logp, reward_out and stats must be device memory of the context's device");
-    void* rows = nullptr;
-    if ((r = c.work(c.a.n * (int64_t)sizeof(TokenRow), &rows)) != MALIB_OK) return r;
-    c.a.rows = static_cast<TokenRow*>(rows);
+    if ((r = c.work()) != MALIB_OK) return r;
+    c.a.rows = reinterpret_cast<TokenRow*>(c.a.row_sums);
     c.a.offsets = loss->offsets;
     c.a.n_pairs = loss->n_pairs;
     c.a.ref = loss->ref_logp;
@@ -196,7 +201,7 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
     if (c.a.n > 0 && (!c.dev(loss->ids, 4) || !c.dev(loss->teacher, elt_size(loss->teacher_dtype)) || !c.opt(loss_out, 4)))
         return c.bad("ids, teacher and loss_out must be aligned device memory of the context's device");
     if (!c.opt(stats_out, 4)) return c.bad("stats must be device memory of the context's device");
-    if ((r = c.work(0, nullptr)) != MALIB_OK) return r;
+    if ((r = c.work()) != MALIB_OK) return r;
     c.a.ids = loss->ids;
     c.a.teacher = loss->teacher;
     c.a.tdtype = loss->teacher_dtype;

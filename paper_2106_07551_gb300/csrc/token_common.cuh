@@ -31,7 +31,7 @@ constexpr int kTokenMaxTop = 1024;                   // teacher entries of a row
 constexpr int kTokenStats = 5;                       // sums of a call's statistics
 constexpr int kTokenMaxCtas = 8192;                  // CTAs whose partial sums the work space holds
 
-enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3 };
+enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2 };
 
 // What a row's statistics leave for a preference pair's sums and its gradient: first
 // value is ln p of the token; the pair's sums put d L / d logit of the token before
@@ -39,6 +39,12 @@ enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3 };
 struct __align__(16) TokenRow {
     float m, inv_s, value;
     int32_t live;
+};
+
+// A row's share of a call's statistics.
+struct __align__(16) RowSum {
+    float loss, x, y;                                // w l; policy loss: KL, H; distillation: l
+    int32_t flags;                                   // bit 0: counted; bit 1: clipped
 };
 
 struct TokenArgs {
@@ -66,7 +72,7 @@ struct TokenArgs {
     const int32_t* ids;          // [n][top], < 0: absent
     const void* teacher;         // [n][top]
     int32_t tdtype, top;
-    float tt;                    // T^2
+    float tt, top_scale;         // T^2, T
     // preference pairs
     const int64_t* offsets;      // [2 pairs + 1]
     int32_t n_pairs;
@@ -79,7 +85,9 @@ struct TokenArgs {
     float* reward;               // [2 n_pairs]
     float* stats;
     double* part;                // [kTokenMaxCtas][kTokenStats]
-    unsigned* ticket;            // CTAs that have written their partial sums
+    unsigned* ticket;            // CTAs that have written their sums
+    RowSum* row_sums;            // [n]
+    unsigned long long* claims;  // rows claimed
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -103,6 +111,7 @@ struct Elt;                      // W elements in 16 bytes
 template <>
 struct Elt<float> {
     static constexpr int W = 4;
+    __device__ static uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }   // -infinity
     __device__ static float word(const uint32_t (&w)[4], int i) { return __uint_as_float(w[i]); }   // entry i
     __device__ static float get(float v) { return v; }
     __device__ static float put(float v) { return v; }
@@ -124,6 +133,7 @@ struct Elt<float> {
 template <>
 struct Elt<__nv_bfloat16> {
     static constexpr int W = 8;
+    __device__ static uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }   // -infinity
     __device__ static __nv_bfloat16 word(const uint32_t (&w)[4], int i) {
         return __ushort_as_bfloat16((unsigned short)(w[i >> 1] >> 16 * (i & 1)));
     }
@@ -153,6 +163,7 @@ struct Elt<__nv_bfloat16> {
 template <>
 struct Elt<__half> {
     static constexpr int W = 8;
+    __device__ static uint4 none() { return make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u); }   // -infinity
     __device__ static __half word(const uint32_t (&w)[4], int i) {
         return __ushort_as_half((unsigned short)(w[i >> 1] >> 16 * (i & 1)));
     }
@@ -317,6 +328,18 @@ __device__ __forceinline__ void store_part(T* g, int j, int V, const uint4& q) {
         if (j + i >= 0 && j + i < V) g[i] = Elt<T>::word(w, i);
 }
 
+// Entries j .. of a row as 16 bytes, -infinity outside [0, V).
+template <class T>
+__device__ __forceinline__ uint4 load_part(const T* p, int j, int V) {
+    constexpr int W = Elt<T>::W;
+    F2 v[W / 2];
+#pragma unroll
+    for (int q = 0; q < W; q += 2)
+        v[q / 2] = f2_make(j + q >= 0 && j + q < V ? Elt<T>::get(p[j + q]) : -INFINITY,
+                           j + q + 1 >= 0 && j + q + 1 < V ? Elt<T>::get(p[j + q + 1]) : -INFINITY);
+    return Elt<T>::pack(v);
+}
+
 // ln p of the entry with logit z.
 __device__ __forceinline__ float log_prob(const TokenArgs& a, const RowStat& r, float z) {
     // ln 2 x (1 + d) for k's relative rounding d: (z - m) / T
@@ -414,8 +437,9 @@ __device__ __forceinline__ bool sum_partials(double* part, unsigned* ticket, con
 }
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
-// Rows of at least a few KB (token_ring.cu); false: the shape is not taken.
-bool launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s, cudaError_t* e);
+// Rows of at least a few KB (token_ring.cu).
+cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s);
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s);
 
 }  // namespace malib

@@ -5,26 +5,35 @@
 // A cluster of C CTAs takes a row, each a slice of it. One warp of a CTA (the producer)
 // runs ahead and copies slices into a ring of 16 KB stages with bulk copies, completing
 // on an mbarrier per stage; eight warps (the consumers) gather the slice's statistics
-// stage by stage, exchange them with the row's other CTAs through distributed shared
-// memory (asynchronous stores that complete on an mbarrier), and go through the same
-// stages again, writing the gradient to global memory and freeing each stage as they
-// leave it. The next row's copies fill the freed stages meanwhile.
+// stage by stage; warp 0 exchanges them with the row's other CTAs through distributed
+// shared memory (asynchronous stores that complete on an mbarrier) and computes the
+// row's loss; and the consumers go through the same stages again, writing the gradient
+// to global memory and freeing each stage as they leave it. The next row's copies fill
+// the freed stages meanwhile. For distillation a further warp (the teacher) prepares the
+// row's list of entries ahead.
 //
-// Bound by memory: the ring of two CTAs an SM holds 2 x 96 KB in flight or in work, and
-// a CTA that waits for its row's sums leaves the SM's other CTA to compute. Per entry
-// the first sweep takes about 6 issue slots and one exponential, the second 5 and
-// another one, where the memory's rate leaves about 21 a 16-bit entry (read and written)
-// and twice that a 32-bit one.
+// Rows are claimed, not dealt: SMs do not all get the same share of the memory's rate, and
+// rows that are left out cost a write and no read; with a fixed share each, SMs stood
+// idle for 10 to 20% of a call. The producer of the cluster's first CTA claims a row ahead
+// (an atomic counter), reads its token and weight, and puts it into every CTA's queue of
+// kQueue rows. What a row adds to the statistics is stored by itself and summed in the
+// rows' order at the end, so that a call's results do not depend on who took what.
+//
+// Bound by memory: the rings of two CTAs an SM hold 2 x 96 KB in flight or in work, and
+// while a CTA waits for its row's sums the SM's other one computes.
 //
 // Rows start at any element: a row's vectors are the 16-byte blocks of its address, the
 // full ones copied in bulk, a partial first or last one filled in by the producer's
-// lanes with -infinity outside the row. Where logits and gradient rows are aligned alike
-// (mod 16 bytes) the gradient is written in vectors, otherwise entry by entry with
-// consecutive lanes on consecutive entries.
+// lanes with -infinity outside the row. Where logits and gradient rows are not aligned
+// alike (mod 16 bytes) a gradient's vector is put together from two of the ring's.
+//
+// Every wait is bounded, between the warps too: one that expires ends the CTA's work and
+// is reported as MALIB_ETIMEOUT.
 #include <mutex>
 
 #include "token_common.cuh"
 #include "token_peer.cuh"
+#include "token_top.cuh"
 
 namespace malib {
 
@@ -33,24 +42,24 @@ namespace {
 constexpr int kConsumers = 256, kConsumerWarps = kConsumers / 32;
 constexpr int kPer = 4;                              // vectors a thread and stage
 constexpr int kStageVecs = kPer * kConsumers, kStageBytes = kStageVecs * 16;
-constexpr int kMaxStages = 13, kMaxCluster = 8;
-
-// A stage of nothing but full vectors, the row's token not among them.
-template <class T, bool kEntropy>
-__device__ __forceinline__ void emit_stage(const uint4* q, T* out, const RowGrad& c, float k) {
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-        F2 v[Elt<T>::W / 2];
-        emit<T, kEntropy>(q[u * kConsumers], c, k, v);
-        __stcs(reinterpret_cast<uint4*>(out + u * kConsumers * Elt<T>::W), Elt<T>::pack(v));
-    }
-}
-
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory"); }
+constexpr int kMaxStages = 8, kMaxCluster = 8;
+constexpr int kQueue = 4;                            // most rows known ahead
+constexpr int kRingTwo = 104 * 1024;                 // dynamic shared memory with two CTAs an SM
 
 // What the row's CTAs exchange, and what a warp leaves for its CTA.
 struct __align__(16) Partial {
-    float m, s, t, z;                                // z: the logit of the row's token
+    float m, s, t, unused;
+};
+// A queued row: token < 0 if it is left out; row < 0 after the last one.
+struct __align__(16) Queued {
+    int64_t row;
+    int32_t token;
+    float w;
+};
+// What warp 0 leaves for the second sweep.
+struct RowOut {
+    RowGrad c;
+    int32_t live;
 };
 
 // A place in the ring: the stage and the parity of its present use.
@@ -68,37 +77,183 @@ struct Cursor {
 struct Shape {
     int cluster, stages;                             // CTAs a row, stages a CTA
     int slice;                                       // vectors of a CTA's slice
+    int keep;                                        // stages that hold parts of a row for its second sweep
+    int queue_log, batch;                            // rows known ahead (log 2), rows a claim takes
 };
 
-// A row's scalars.
-struct RowIn {
-    int token;
-    float w;
-    PpoRow ppo;
-    TokenRow row;
-};
-template <int kOp>
-__device__ __forceinline__ RowIn load_row(const TokenArgs& a, int64_t row) {
-    RowIn in{};
-    in.token = a.tokens[row];
-    in.w = kOp == kTokPpo ? (a.weight ? a.weight[row] : a.w0) : 1.f;
-    if (kOp == kTokPpo) in.ppo = ppo_load(a, row);
-    if (kOp == kTokPairGrad) in.row = a.rows[row];
-    return in;
+// Sixteen bytes of shared memory from a byte offset that need not be a multiple of 16.
+template <int kWord>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t bits) {
+    const uint32_t w[9] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, 0};
+    return make_uint4(__funnelshift_r(w[kWord], w[kWord + 1], bits), __funnelshift_r(w[kWord + 1], w[kWord + 2], bits),
+                      __funnelshift_r(w[kWord + 2], w[kWord + 3], bits),
+                      __funnelshift_r(w[kWord + 3], w[kWord + 4], bits));
+}
+__device__ __forceinline__ uint4 load_shifted(const uint8_t* p, int by) {   // p: 16-byte aligned, 0 < by < 16
+    const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 16);
+    const uint32_t bits = 8u * (by & 3);
+    switch (by >> 2) {
+        case 0: return shifted<0>(a, b, bits);
+        case 1: return shifted<1>(a, b, bits);
+        case 2: return shifted<2>(a, b, bits);
+        default: return shifted<3>(a, b, bits);
+    }
+}
+
+// One entry of the gradient.
+template <class T>
+__device__ __forceinline__ float emit_one(T z, const RowGrad& c, float k) {
+    const float x = (Elt<T>::get(z) - c.m) * k;
+    return exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
+}
+
+// The gradient of a stage: entries [j0, j1) of the row, those of the n vectors at src,
+// the first of which is entry `first` (before the row where the row starts inside it).
+template <class T, bool kEntropy>
+__device__ __forceinline__ void emit_stage(const uint8_t* src, int first, int j0, int j1, int n, T* g, bool alike,
+                                           const RowGrad& c, float k, int token) {
+    constexpr int W = Elt<T>::W;
+    const int tid = threadIdx.x;
+    const T* e = reinterpret_cast<const T*>(src) - first;            // entry j at e[j]
+    F2 v[W / 2];
+    if (alike) {
+        const uint4* q = reinterpret_cast<const uint4*>(src) + tid;
+        T* out = g + (first + tid * W);
+        if (j0 == first && j1 - j0 == kStageVecs * W) {
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                emit<T, kEntropy>(q[u * kConsumers], c, k, v);
+                __stcs(reinterpret_cast<uint4*>(out + u * kConsumers * W), Elt<T>::pack(v));
+            }
+        } else {
+            for (int i = tid; i < n; i += kConsumers, q += kConsumers, out += kConsumers * W) {
+                emit<T, kEntropy>(*q, c, k, v);
+                const int j = first + i * W;
+                if (j >= j0 && j + W <= j1) __stcs(reinterpret_cast<uint4*>(out), Elt<T>::pack(v));
+                else store_part(out, j - j0, j1 - j0, Elt<T>::pack(v));
+            }
+        }
+        // the token's entry, by the thread that has just written it
+        if (token >= j0 && token < j1 && (token - first) / W % kConsumers == tid)
+            g[token] = Elt<T>::put(emit_one(e[token], c, k) + c.at);
+    } else {
+        // vectors of the gradient's own alignment, entry by entry what is left at the ends
+        const int to = (int)((16u - ((uintptr_t)(g + j0) & 15u) & 15u) / sizeof(T));
+        const int a0 = min(j0 + to, j1), nv = (j1 - a0) / W, a1 = a0 + nv * W;
+        const uint8_t* p = reinterpret_cast<const uint8_t*>(e + a0);
+        const int by = (int)((uintptr_t)p & 15u);
+        p -= by;
+        for (int i = tid; i < nv; i += kConsumers) {
+            emit<T, kEntropy>(load_shifted(p + i * 16, by), c, k, v);
+            __stcs(reinterpret_cast<uint4*>(g + (a0 + i * W)), Elt<T>::pack(v));
+        }
+        const int j = tid < W ? j0 + tid : a1 + tid - W;
+        if (tid < 2 * W && j < (tid < W ? a0 : j1)) g[j] = Elt<T>::put(emit_one(e[j], c, k));
+        if (token >= j0 && token < j1) {
+            const int owner = token < a0 ? token - j0 : token >= a1 ? token - a1 + W : (token - a0) / W % kConsumers;
+            if (owner == tid) g[token] = Elt<T>::put(emit_one(e[token], c, k) + c.at);
+        }
+    }
+}
+
+// Zeros to entries [j0, j1) of a row.
+template <class T>
+__device__ __forceinline__ void zero_entries(T* g, int j0, int j1) {
+    constexpr int W = Elt<T>::W;
+    const int tid = threadIdx.x;
+    const int to = (int)((16u - ((uintptr_t)(g + j0) & 15u) & 15u) / sizeof(T));
+    const int a0 = min(j0 + to, j1), nv = (j1 - a0) / W, a1 = a0 + nv * W;
+    for (int i = tid; i < nv; i += kConsumers)
+        __stcs(reinterpret_cast<uint4*>(g + (a0 + i * W)), make_uint4(0, 0, 0, 0));
+    const int j = tid < W ? j0 + tid : a1 + tid - W;
+    if (tid < 2 * W && j < (tid < W ? a0 : j1)) g[j] = Elt<T>::put(0.f);
+}
+
+// The statistics of a call from its rows' shares, in the rows' order (every thread of one
+// block).
+template <int kOp, int kThreads>
+__device__ __forceinline__ void sum_rows(const TokenArgs& a) {
+    __shared__ double part[kThreads / 32][kTokenStats];
+    __threadfence();
+    // counts are whole numbers; a thread's other sums are fp32 with their rounding errors
+    // (two-sum), fp64 from the warps on: its rate is a sixtieth of fp32's here
+    int rows = 0, clipped = 0;
+    float sum[3] = {}, err[3] = {};
+    constexpr int kAt = 8;                           // loads in flight
+    for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kAt * kThreads) {
+        float4 q[kAt];
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+            const int64_t i = i0 + u * kThreads;
+            q[u] = i < a.n ? __ldcg(reinterpret_cast<const float4*>(a.row_sums + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+            const int flags = __float_as_int(q[u].w);
+            rows += flags & 1;
+            clipped += flags >> 1;
+            const float x[3] = {q[u].x, q[u].y, q[u].z};
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const float s = __fadd_rn(sum[i], x[i]), y = __fsub_rn(s, sum[i]);
+                err[i] += __fadd_rn(__fsub_rn(sum[i], __fsub_rn(s, y)), __fsub_rn(x[i], y));
+                sum[i] = s;
+            }
+        }
+    }
+    double v[kTokenStats];
+    v[0] = __reduce_add_sync(0xffffffffu, rows);
+    if (kOp == kTokPpo) v[2] = __reduce_add_sync(0xffffffffu, clipped);
+    // an infinite sum has an error that is NaN, and none to speak of
+    auto whole = [&](int i) { return (double)sum[i] + (fabsf(sum[i]) < INFINITY ? (double)err[i] : 0.0); };
+    v[1] = whole(0);
+    v[kOp == kTokPpo ? 3 : 2] = whole(1);
+    if (kOp == kTokPpo) v[4] = whole(2);
+    constexpr int kSums = kOp == kTokPpo ? 5 : 3;
+#pragma unroll
+    for (int i = 1; i < kSums; ++i) {
+        if (kOp == kTokPpo && i == 2) continue;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) part[threadIdx.x >> 5][i] = v[i];
+    __syncthreads();
+    if (threadIdx.x >= kSums) return;
+    double all = 0.0;
+    for (int w = 0; w < kThreads / 32; ++w) all += part[w][threadIdx.x];
+    part[0][threadIdx.x] = all;                      // (its own column)
+    __syncwarp((1u << kSums) - 1u);
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) v[i] = part[0][i];
+    if (kOp == kTokPpo) ppo_stats(a, v);
+    else distill_stats(a, v);
 }
 
 template <class T, int kOp>
-__global__ void __launch_bounds__(kConsumers + 32, kOp == kTokLogp ? 3 : 2) token_ring_kernel(TokenArgs a, Shape sh) {
+__global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), kOp == kTokLogp ? 3 : 2)
+    token_ring_kernel(TokenArgs a, Shape sh) {
     constexpr int W = Elt<T>::W;
-    constexpr int kThreads = kConsumers + 32;
+    constexpr int kThreads = kConsumers + (kOp == kTokDistill ? 64 : 32);
+    constexpr bool kTop = kOp == kTokDistill;
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], xbar[2];
-    __shared__ Partial red[2][kConsumerWarps], xslot[2][kMaxCluster];
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages];
+    // per queued row: known, no longer needed; per row that is read: the warps' statistics
+    // are there, the CTAs', the result, the written slice
+    __shared__ __align__(8) uint64_t qfull[kQueue], qempty[kQueue], sfull[kQueue], xfull[kQueue], rfull[kQueue],
+        pfull[kQueue];
+    __shared__ __align__(8) uint64_t tfull[2], tempty[2];
+    __shared__ Queued queue[kQueue];
+    __shared__ Partial red[kQueue][kConsumerWarps], xslot[kQueue][kMaxCluster];
+    __shared__ RowOut rout[kQueue];
+    __shared__ TopRow top[2];
     __shared__ int dead;                             // a bounded wait has expired: nothing waits any more
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = sh.cluster, rank = C > 1 ? (int)cluster_rank() : 0;
-    const int64_t first = blockIdx.x / C, step = gridDim.x / C;
     const int v_lo = rank * sh.slice;
+    TopEntry* entries = reinterpret_cast<TopEntry*>(ring + sh.stages * kStageBytes);   // [2][a.top]
 
     if (tid == 0) {
         dead = 0;
@@ -106,8 +261,18 @@ __global__ void __launch_bounds__(kConsumers + 32, kOp == kTokLogp ? 3 : 2) toke
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], kConsumerWarps);
         }
-        mbar_init(&xbar[0], 1);
-        mbar_init(&xbar[1], 1);
+        for (int i = 0; i < kQueue; ++i) {
+            mbar_init(&qfull[i], 1);
+            mbar_init(&qempty[i], C * (kThreads / 32));
+            mbar_init(&sfull[i], kConsumerWarps);
+            mbar_init(&xfull[i], 1);
+            mbar_init(&rfull[i], 1);
+            mbar_init(&pfull[i], kConsumerWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&tfull[i], 1);
+            mbar_init(&tempty[i], kConsumerWarps);
+        }
         fence_proxy_async_smem();
     }
     __syncthreads();
@@ -125,42 +290,115 @@ __global__ void __launch_bounds__(kConsumers + 32, kOp == kTokLogp ? 3 : 2) toke
         if (mbar_try_wait(bar, parity) || *gone) return;
         if (!mbar_wait_bounded(bar, parity, kWaitLimitNs)) expired();
     };
-    // Whether a row's logits are read: known from its token and weight alone.
-    auto wanted = [&](int token, float w) { return token >= 0 && token < a.V && w != 0.f; };
-    double acc[kTokenStats] = {};
+    auto wait_peers = [&](uint64_t* bar, uint32_t parity) {
+        if (!*gone && !peer_wait_bounded(bar, parity, kWaitLimitNs)) expired();
+    };
+    auto slot_of = [&](uint32_t t) { return t & ((1u << sh.queue_log) - 1u); };
+    auto parity_of = [&](uint32_t t) { return t >> sh.queue_log & 1u; };
+    // Turn t's row, as every warp of the cluster sees it; row < 0: there is none.
+    auto take = [&](uint32_t t) {
+        if (C > 1) wait_peers(&qfull[slot_of(t)], parity_of(t));
+        else wait(&qfull[slot_of(t)], parity_of(t));
+        Queued q = queue[slot_of(t)];
+        if (*gone) q.row = -1;
+        return q;
+    };
+    // The warp needs nothing of turn t any more.
+    auto leave = [&](uint32_t t) {
+        __syncwarp();
+        if (lane != 0) return;
+        if (C > 1) peer_arrive(&qempty[slot_of(t)], 0);
+        else mbar_arrive_release(&qempty[slot_of(t)]);
+    };
 
     if (warp == kConsumerWarps) {
         // ---- producer
-        const T* z0 = static_cast<const T*>(a.z);
+        // rank 0: claimed rows in batches, lane i with the i-th row's token and weight; the
+        // next batch, whose tokens are on their way, and the start of the one after that,
+        // whose claim is (lane 0): none is waited for where it is asked for
+        struct Batch {
+            int64_t row;
+            int32_t token;
+            float w;
+        };
+        auto look = [&](int64_t row) {
+            Batch b{row, -1, 1.f};
+            if (lane < sh.batch && row + lane < a.n) {
+                b.token = kTop ? 0 : a.tokens[row + lane];
+                if (kOp != kTokLogp) b.w = a.weight ? a.weight[row + lane] : a.w0;
+            }
+            return b;
+        };
+        const int64_t clusters = gridDim.x / C;
+        Batch now{}, next{};
+        unsigned long long claim = 0;
+        int used = 0;
+        // with a batch for every row there is nothing to claim
+        const bool claims = a.n > clusters * sh.batch;
+        auto more = [&] {
+            if (claims && lane == 0) claim = atomicAdd(a.claims, (unsigned long long)sh.batch);
+        };
+        auto look_next = [&] {
+            if (claims) next = look((int64_t)(clusters * sh.batch + __shfl_sync(0xffffffffu, claim, 0)));
+            else next.row = a.n;
+            more();
+        };
+        if (rank == 0) {
+            more();
+            now = look((int64_t)(blockIdx.x / C) * sh.batch);
+        }
         Cursor at, issued;
         bool wrapped = false;
-        for (int64_t base = first; base < a.n; base += 32 * step) {
-            const int64_t mine = base + lane * step;
-            bool want = false;
-            if (mine < a.n) {
-                if (kOp == kTokPairGrad) want = a.rows[mine].live != 0;
-                else want = wanted(a.tokens[mine], kOp == kTokLogp ? 1.f : a.weight ? a.weight[mine] : a.w0);
+        for (uint32_t t = 0;; ++t) {
+            const int slot = slot_of(t);
+            // the cluster's instructions only in launches with clusters
+            if (C > 1 && lane == 0) mbar_arrive_expect_tx(&qfull[slot], sizeof(Queued));
+            if (rank == 0) {
+                Queued q{now.row + used < a.n ? now.row + used : -1, __shfl_sync(0xffffffffu, now.token, used),
+                         __shfl_sync(0xffffffffu, now.w, used)};
+                if (q.token >= a.V && lane == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+                if (q.token >= a.V || q.w == 0.f) q.token = -1;
+                if (C > 1) {
+                    wait_peers(&qempty[slot], parity_of(t) ^ 1u);
+                    if (lane < C)
+                        peer_store(&queue[slot], &qfull[slot], lane,
+                                   make_float4(__int_as_float((int)(uint32_t)q.row), __int_as_float((int)(q.row >> 32)),
+                                               __int_as_float(q.token), q.w));
+                } else {
+                    wait(&qempty[slot], parity_of(t) ^ 1u);
+                    if (lane == 0) {
+                        queue[slot] = q;
+                        mbar_arrive_release(&qfull[slot]);
+                    }
+                }
+                if (t == 0) look_next();
+                if (++used == sh.batch) {
+                    used = 0;
+                    now = next;
+                    look_next();
+                }
             }
-            unsigned todo = __ballot_sync(0xffffffffu, want);
-            while (todo) {
-                const int64_t row = base + (__ffs(todo) - 1) * step;
-                todo &= todo - 1;
-                const T* z = z0 + row * a.ld;
+            const Queued q = take(t);
+            if (q.row < 0) break;
+            if (q.token >= 0) {
+                const T* z = static_cast<const T*>(a.z) + q.row * a.ld;
                 const int h = (int)(((uintptr_t)z & 15u) / sizeof(T)), nv = (h + a.V + W - 1) / W;
-                const int hi = min(nv, v_lo + sh.slice);
-                for (int v = v_lo; v < hi; v += kStageVecs, at.next(sh.stages)) {
+                const int hi = max(v_lo, min(nv, v_lo + sh.slice)), parts = (hi - v_lo + kStageVecs - 1) / kStageVecs;
+                const int again = kOp != kTokLogp && a.g ? max(0, parts - sh.keep) : 0;
+                for (int part = 0; part < parts + again; ++part, at.next(sh.stages)) {
+                    const int v = v_lo + (part < parts ? part : part - parts) * kStageVecs;
                     const int n = min(kStageVecs, hi - v), stage = at.stage;
                     uint8_t* dst = ring + stage * kStageBytes;
                     // a partial first (lanes 0..7) or last (lanes 16..23) vector of the row
                     const bool head = v == 0 && h > 0, tail = v + n == nv && (h + a.V) % W != 0;
                     const int pv = lane < 16 ? 0 : nv - 1, pj = pv * W - h + (lane & 15);
                     const bool fill = (lane & 15) < W && (lane < 16 ? head : tail);
-                    T part = Elt<T>::put(-INFINITY);
-                    if (fill && pj >= 0 && pj < a.V) part = z[pj];
+                    T entry = Elt<T>::put(-INFINITY);
+                    if (fill && pj >= 0 && pj < a.V) entry = z[pj];
                     wait(&empty[stage], at.parity ^ 1u);
-                    if (fill) reinterpret_cast<T*>(dst)[(pv - v) * W + (lane & 15)] = part;
+                    if (fill) reinterpret_cast<T*>(dst)[(pv - v) * W + (lane & 15)] = entry;
                     __syncwarp();
-                    if (*gone) continue;
+                    if (*gone) break;
                     wrapped |= stage + 1 == sh.stages;
                     issued = at;
                     if (lane == 0) {
@@ -172,165 +410,180 @@ __global__ void __launch_bounds__(kConsumers + 32, kOp == kTokLogp ? 3 : 2) toke
                     __syncwarp();
                 }
             }
+            leave(t);
         }
         if (*gone)                                   // copies in flight end before the block does
             for (int i = 0; i < sh.stages; ++i)
-                if (i <= issued.stage || wrapped)
+                if (wrapped || i <= issued.stage)
                     mbar_wait_bounded(&full[i], i <= issued.stage ? issued.parity : issued.parity ^ 1u, 1000000);
+    } else if (warp > kConsumerWarps) {
+        // ---- teacher
+        if (kTop) {
+            uint32_t turn = 0;                       // rows that are read
+            for (uint32_t t = 0;; ++t) {
+                const Queued q = take(t);
+                if (q.row < 0) break;
+                if (q.token >= 0) {
+                    const int b = turn & 1u;
+                    wait(&tempty[b], (turn >> 1 & 1u) ^ 1u);
+                    const TopRow r = top_row<T>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld, entries + b * a.top);
+                    if (lane == 0) top[b] = r;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release(&tfull[b]);
+                    ++turn;
+                }
+                leave(t);
+            }
+        }
     } else {
         // ---- consumers
         Cursor at;
-        uint32_t exch = 0;
-        // a row's scalars are read while the row before is worked on
-        RowIn next = load_row<kOp>(a, first);
-        for (int64_t row = first; row < a.n; row += step) {
-            const RowIn in = next;
-            if (row + step < a.n) next = load_row<kOp>(a, row + step);
+        uint32_t turn = 0;                           // rows that are read
+        for (uint32_t t = 0;; ++t) {
+            const Queued q = take(t);
+            if (q.row < 0) break;
+            const int slot = slot_of(turn), b = turn & 1u;
+            const uint32_t parity = parity_of(turn);
+            const int64_t row = q.row;
             const T* z = static_cast<const T*>(a.z) + row * a.ld;
             T* g = kOp != kTokLogp && a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
             const int h = (int)(((uintptr_t)z & 15u) / sizeof(T)), nv = (h + a.V + W - 1) / W;
             const int v_hi = max(v_lo, min(nv, v_lo + sh.slice));
-            const int token = in.token;
-            const float w = in.w;
-            // whether the row's logits are read, and then whether it has a distribution
-            const bool read = kOp == kTokPairGrad ? in.row.live != 0 : wanted(token, w);
-            bool live = read;
-            RowGrad c{0.f, 0.f, 0.f, 0.f};
-            const Cursor begin = at;
-            if (kOp == kTokPairGrad) {
-                c = RowGrad{in.row.m, -in.row.value * in.row.inv_s, 0.f, in.row.value};
-            } else {
-                if (token >= a.V && rank == 0 && tid == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
-                RowStat r{-INFINITY, 0.f, 0.f};
-                float zt = 0.f;
-                if (read) {
-                    if (tid == 0) zt = Elt<T>::get(z[token]);
-                    for (int v = v_lo; v < v_hi; v += kStageVecs, at.next(sh.stages)) {
-                        const int n = min(kStageVecs, v_hi - v), stage = at.stage;
-                        const uint4* src = reinterpret_cast<const uint4*>(ring + stage * kStageBytes);
-                        wait(&full[stage], at.parity);
-                        if (n == kStageVecs) {
-                            uint4 q[kPer];
-#pragma unroll
-                            for (int u = 0; u < kPer; ++u) q[u] = src[tid + u * kConsumers];
-                            float mx = Elt<T>::max(q[0]);
-#pragma unroll
-                            for (int u = 1; u < kPer; ++u) mx = max_nan(mx, Elt<T>::max(q[u]));
-                            raise(r, mx, a.k);
-                            if (r.m != -INFINITY) {
-#pragma unroll
-                                for (int u = 0; u < kPer; ++u) gather<T>(r, q[u], a.k);
-                            }
-                        } else {
-                            for (int i = tid; i < n; i += kConsumers) {
-                                const uint4 q = src[i];
-                                raise(r, Elt<T>::max(q), a.k);
-                                if (r.m != -INFINITY) gather<T>(r, q, a.k);
-                            }
-                        }
-                        if (!g) {                    // the slice is not read again
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_release(&empty[stage]);
-                        }
-                    }
-                    r = reduce_stat<32>(r, a.k);
-                    // the token's logit goes through warp 0's entry: it has been read before
-                    // any of the row is written
-                    const int slot = exch & 1u;
-                    if (lane == 0) red[slot][warp] = Partial{r.m, r.s, r.t, zt};
-                    consumer_sync();
-                    if (C > 1) {
-                        // Two slots are enough: a peer fills this one again only after this
-                        // CTA's sums of the next row, which every thread here joins first.
-                        if (warp == 0) {
-                            const Partial& pw = red[slot][lane & (kConsumerWarps - 1)];
-                            r = reduce_stat<kConsumerWarps>(RowStat{pw.m, pw.s, pw.t}, a.k);
-                            if (lane == 0) mbar_arrive_expect_tx(&xbar[slot], (uint32_t)(C * sizeof(Partial)));
-                            if (lane < C) peer_store(&xslot[slot][rank], &xbar[slot], lane, make_float4(r.m, r.s, r.t, zt));
-                        }
-                        if (!*gone && !peer_wait_bounded(&xbar[slot], exch >> 1 & 1u, kWaitLimitNs)) expired();
-                    }
-                    if (C > 1) {
-                        const Partial& px = xslot[slot][lane & (kMaxCluster - 1)];
-                        r = reduce_stat<kMaxCluster>(
-                            lane % kMaxCluster < C ? RowStat{px.m, px.s, px.t} : RowStat{-INFINITY, 0.f, 0.f}, a.k);
-                    } else {
-                        const Partial& pw = red[slot][lane & (kConsumerWarps - 1)];
-                        r = reduce_stat<kConsumerWarps>(RowStat{pw.m, pw.s, pw.t}, a.k);
-                    }
-                    zt = red[slot][0].z;
-                    ++exch;
-                    live = r.m != -INFINITY;
+            const bool first = tid == 0 && rank == 0;
+            if (q.token < 0) {
+                if (first) {
+                    if (kOp == kTokLogp) logp_row(a, row, false, RowStat{0.f, 1.f, 0.f}, 0.f);
+                    if (kOp == kTokPpo && a.logp) a.logp[row] = 0.f;
+                    if (kTop && a.loss) a.loss[row] = 0.f;
+                    if (kOp != kTokLogp) a.row_sums[row] = RowSum{0.f, 0.f, 0.f, 0};
                 }
-                if (kOp == kTokLogp) {
-                    if (tid == 0 && rank == 0) logp_row(a, row, live, r, zt);
-                    continue;
-                }
-                float logp = 0.f;
-                if (live) {
-                    float loss, clipped, kl, H;
-                    logp = log_prob(a, r, zt);
-                    c = ppo_row(a, in.ppo, r, logp, w, &loss, &clipped, &kl, &H);
-                    if (tid == 0 && rank == 0) {
-                        acc[0] += 1.0;
-                        acc[1] += (double)w * loss;
-                        acc[2] += clipped;
-                        acc[3] += kl;
-                        acc[4] += H;
-                    }
-                }
-                if (a.logp && tid == 0 && rank == 0) a.logp[row] = logp;
+                if (g) zero_entries(g, max(0, v_lo * W - h), max(0, min(a.V, v_hi * W - h)));
+                leave(t);
+                continue;
             }
-            if (!g) continue;
-            // the slice again: the gradient
-            const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
-            at = begin;
-            for (int v = v_lo; v < v_hi; v += kStageVecs) {
-                const int n = min(kStageVecs, v_hi - v);
-                const uint8_t* src = ring + at.stage * kStageBytes;
-                if (kOp == kTokPairGrad && read) wait(&full[at.stage], at.parity);
-                if (alike) {
-                    // whether the stage has nothing but full vectors of the row, and not its token
-                    const int j_lo = v * W - h;
-                    const bool inner = n == kStageVecs && j_lo >= 0 && j_lo + kStageVecs * W <= a.V &&
-                                       (unsigned)(token - j_lo) >= (unsigned)(kStageVecs * W);
-                    const uint4* q = reinterpret_cast<const uint4*>(src) + tid;
-                    T* out = g + (j_lo + tid * W);
-                    if (inner && live) {
-                        if (kOp == kTokPpo && c.c1 != 0.f) emit_stage<T, true>(q, out, c, a.k);
-                        else emit_stage<T, false>(q, out, c, a.k);
-                    } else {
-                        for (int i = tid; i < n; i += kConsumers, q += kConsumers, out += kConsumers * W) {
-                            const int j = j_lo + i * W;
-                            F2 x[W / 2] = {};
-                            if (live) {
-                                emit<T, true>(*q, c, a.k, x);
-                                if ((unsigned)(token - j) < (unsigned)W) add_at(x, token - j, c.at);
-                            }
-                            if (j >= 0 && j + W <= a.V) __stcs(reinterpret_cast<uint4*>(out), Elt<T>::pack(x));
-                            else store_part(out, j, a.V, Elt<T>::pack(x));
-                        }
-                    }
-                } else {
-                    const int j0 = max(0, v * W - h), j1 = min(a.V, (v + n) * W - h);
-                    const T* e0 = reinterpret_cast<const T*>(src) - (v * W - h);
-#pragma unroll 4
-                    for (int j = j0 + tid; j < j1; j += kConsumers) {
-                        float f = 0.f;
-                        if (live) {
-                            const float x = (Elt<T>::get(e0[j]) - c.m) * a.k;
-                            f = exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
-                            if (j == token) f += c.at;
-                        }
-                        g[j] = Elt<T>::put(f);
-                    }
+            T z_token = Elt<T>::put(0.f);            // widened where it is used: nothing waits for it here
+            PpoRow in{};
+            if (warp == 0) {
+                if (!kTop) z_token = z[q.token];
+                if (kOp == kTokPpo) in = ppo_load(a, row);
+            }
+            // the row's last parts stay in the ring, the others come again for the second sweep
+            const int parts = (v_hi - v_lo + kStageVecs - 1) / kStageVecs, kept = g ? max(0, parts - sh.keep) : parts;
+            Cursor begin;
+            RowStat r{-INFINITY, 0.f, 0.f};
+            for (int part = 0; part < parts; ++part, at.next(sh.stages)) {
+                const int n = min(kStageVecs, v_hi - v_lo - part * kStageVecs);
+                if (part == kept) begin = at;
+                const uint4* src = reinterpret_cast<const uint4*>(ring + at.stage * kStageBytes);
+                wait(&full[at.stage], at.parity);
+                uint4 x[kPer];
+#pragma unroll
+                for (int u = 0; u < kPer; ++u)
+                    x[u] = tid + u * kConsumers < n ? src[tid + u * kConsumers] : Elt<T>::none();
+                float mx = Elt<T>::max(x[0]);
+#pragma unroll
+                for (int u = 1; u < kPer; ++u) mx = max_nan(mx, Elt<T>::max(x[u]));
+                raise(r, mx, a.k);
+                if (r.m != -INFINITY) {
+#pragma unroll
+                    for (int u = 0; u < kPer; ++u) gather<T>(r, x[u], a.k);
                 }
-                if (read) {
+                if (part < kept) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&empty[at.stage]);
-                    at.next(sh.stages);
                 }
             }
+            r = reduce_stat<32>(r, a.k);
+            if (lane == 0) {
+                red[slot][warp] = Partial{r.m, r.s, r.t, 0.f};
+                mbar_arrive_release(&sfull[slot]);
+            }
+            if (warp == 0) {
+                wait(&sfull[slot], parity);
+                const Partial& pw = red[slot][lane & (kConsumerWarps - 1)];
+                r = reduce_stat<kConsumerWarps>(RowStat{pw.m, pw.s, pw.t}, a.k);
+                if (kTop) wait(&tfull[b], turn >> 1 & 1u);
+                const float zt = Elt<T>::get(z_token);
+                if (C > 1) {
+                    // The logits that the loss takes (zt, the teacher's entries) have been read
+                    // before any CTA of the row writes its part: they go before these sums.
+                    if (lane == 0) mbar_arrive_expect_tx(&xfull[slot], (uint32_t)(C * sizeof(Partial)));
+                    if (lane < C) peer_store(&xslot[slot][rank], &xfull[slot], lane, make_float4(r.m, r.s, r.t, zt));
+                    wait_peers(&xfull[slot], parity);
+                    const Partial& px = xslot[slot][lane & (kMaxCluster - 1)];
+                    r = reduce_stat<kMaxCluster>(
+                        lane % kMaxCluster < C ? RowStat{px.m, px.s, px.t} : RowStat{-INFINITY, 0.f, 0.f}, a.k);
+                }
+                bool live = r.m != -INFINITY;
+                if (kOp == kTokLogp) {
+                    if (first) logp_row(a, row, live, r, zt);
+                } else {
+                    float loss = 0.f;
+                    RowGrad c{0.f, 0.f, 0.f, 0.f};
+                    RowSum sum{0.f, 0.f, 0.f, 0};
+                    if (kOp == kTokPpo) {
+                        float logp = 0.f;
+                        if (live) {
+                            float clipped, kl, H;
+                            logp = log_prob(a, r, zt);
+                            c = ppo_row(a, in, r, logp, q.w, &loss, &clipped, &kl, &H);
+                            sum = RowSum{q.w * loss, kl, H, clipped != 0.f ? 3 : 1};
+                        }
+                        if (a.logp && first) a.logp[row] = logp;
+                    } else {
+                        live = live && top[b].live;
+                        if (live) {
+                            const float f = q.w * a.gscale * a.top_scale;
+                            loss = top_loss(a, r, top[b]);
+                            c = RowGrad{r.m, f / r.s, 0.f, f};               // at: the factor of the teacher's q
+                            sum = RowSum{q.w * loss, loss, 0.f, 1};
+                        }
+                        if (a.loss && first) a.loss[row] = loss;
+                    }
+                    if (first) a.row_sums[row] = sum;
+                    if (lane == 0) {
+                        rout[slot] = RowOut{c, live};
+                        mbar_arrive_release(&rfull[slot]);
+                    }
+                }
+            }
+            if (g) {
+                wait(&rfull[slot], parity);
+                const RowGrad c = rout[slot].c;
+                const bool live = rout[slot].live != 0, alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+                if (kept < parts) at = begin;
+                for (int i = 0; i < parts; ++i, at.next(sh.stages)) {
+                    const int part = kept + i < parts ? kept + i : kept + i - parts, v = v_lo + part * kStageVecs;
+                    const int n = min(kStageVecs, v_hi - v), j = v * W - h;
+                    if (part < kept) wait(&full[at.stage], at.parity);
+                    const int j0 = max(0, j), j1 = min(a.V, j + n * W);
+                    const uint8_t* src = ring + at.stage * kStageBytes;
+                    const int token = kTop ? -1 : q.token;
+                    if (!live) zero_entries(g, j0, j1);
+                    else if (kOp == kTokPpo && c.c1 != 0.f) emit_stage<T, true>(src, j, j0, j1, n, g, alike, c, a.k, token);
+                    else emit_stage<T, false>(src, j, j0, j1, n, g, alike, c, a.k, token);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release(&empty[at.stage]);
+                }
+                if (kTop) {
+                    // the teacher's entries of this slice, over what the CTA's warps have written
+                    if (lane == 0) mbar_arrive_release(&pfull[slot]);
+                    wait(&pfull[slot], parity);
+                    const int j0 = max(0, v_lo * W - h), j1 = min(a.V, v_hi * W - h);
+                    if (live)
+                        for (int i = tid; i < a.top; i += kConsumers) {
+                            const TopEntry e = entries[b * a.top + i];
+                            if (e.id >= j0 && e.id < j1)
+                                g[e.id] = Elt<T>::put(c.c0 * exp2_fast((e.z - c.m) * a.k) - c.at * e.q);
+                        }
+                }
+            }
+            if (kTop) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive_release(&tempty[b]);
+            }
+            ++turn;
+            leave(t);
         }
     }
     if (C > 1) {
@@ -338,22 +591,78 @@ __global__ void __launch_bounds__(kConsumers + 32, kOp == kTokLogp ? 3 : 2) toke
         cluster_arrive();
         cluster_wait();
     }
-    if (kOp != kTokPpo || !a.stats) return;
-    double v[kTokenStats];
-    if (!sum_partials<kThreads>(a.part, a.ticket, acc, v)) return;
-    ppo_stats(a, v);
+    __syncthreads();
+    // the CTA that ends last clears the claims for the next call and sums the statistics
+    const bool stats = kOp != kTokLogp && a.stats;
+    if (!stats && a.n <= (int64_t)(gridDim.x / C) * sh.batch) return;
+    __shared__ bool last;
+    if (tid == 0) {
+        __threadfence();
+        last = atomicInc(a.ticket, gridDim.x - 1) == gridDim.x - 1;   // back at 0 for the next call
+    }
+    __syncthreads();
+    if (!last) return;
+    if (tid == 0) *a.claims = 0ull;
+    if (stats) sum_rows<kOp, kThreads>(a);
 }
 
-// CTAs of a kernel that the device holds at once, by cluster size and stages.
+// The gradient of preference pairs from the rows' statistics and factors: a CTA per part
+// of a row, entries straight from and to global memory, as a copy would go.
+template <class T>
+__global__ void __launch_bounds__(kConsumers) token_pair_grad_kernel(TokenArgs a, int parts) {
+    constexpr int W = Elt<T>::W;
+    const int tid = threadIdx.x;
+    const int64_t total = a.n * parts;
+    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+        const int64_t row = at / parts;
+        const int v0 = (int)(at - row * parts) * kStageVecs;
+        const TokenRow r = a.rows[row];
+        const int token = a.tokens[row];
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        T* g = static_cast<T*>(a.g) + row * a.gld;
+        const int h = (int)(((uintptr_t)g & 15u) / sizeof(T));       // vectors of the gradient's own alignment
+        const int zo = (int)((uintptr_t)z & 15u) - (int)((uintptr_t)g & 15u);
+        const RowGrad c{r.m, -r.value * r.inv_s, 0.f, r.value};
+        uint4 q[kPer];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int j = (v0 + tid + u * kConsumers) * W - h;
+            q[u] = Elt<T>::none();
+            if (r.live == 0 || j >= a.V) continue;
+            if (zo == 0 && j >= 0 && j + W <= a.V) {
+                q[u] = __ldcs(reinterpret_cast<const uint4*>(z + j));
+            } else {
+                // a vector that starts inside one of the logits' blocks, or a partial one
+                const uint8_t* p = reinterpret_cast<const uint8_t*>(z + j);
+                const int by = (int)((uintptr_t)p & 15u);
+                if (j - W >= 0 && j + 2 * W <= a.V) q[u] = by ? load_shifted(p - by, by) : *reinterpret_cast<const uint4*>(p);
+                else q[u] = load_part(z, j, a.V);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int j = (v0 + tid + u * kConsumers) * W - h;
+            if (j >= a.V) continue;
+            F2 v[W / 2];
+            emit<T, false>(q[u], c, a.k, v);
+            if ((unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
+            uint4 out = Elt<T>::pack(v);
+            if (r.live == 0) out = make_uint4(0, 0, 0, 0);
+            if (j >= 0 && j + W <= a.V) __stcs(reinterpret_cast<uint4*>(g + j), out);
+            else store_part(g + j, j, a.V, out);
+        }
+    }
+}
+
 template <class T, int kOp>
-cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int per_sm, int n_sm, cudaStream_t s) {
+cudaError_t launch_ring(const TokenArgs& a, Shape sh, int per_sm, int n_sm, cudaStream_t s) {
     const void* f = (const void*)token_ring_kernel<T, kOp>;
-    const int bytes = sh.stages * kStageBytes;
-    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStages * kStageBytes);
+    const int bytes = sh.stages * kStageBytes + (kOp == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0);
+    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingTwo);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
-    cfg.blockDim = dim3(kConsumers + 32);
+    cfg.blockDim = dim3(kConsumers + (kOp == kTokDistill ? 64 : 32));
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     int64_t clusters = (int64_t)per_sm * n_sm;
@@ -363,7 +672,9 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int per_sm, int n_s
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        // clusters lie within a part of the device: fewer fit than the SMs' number says
+        // Clusters lie within a part of the device: fewer fit than the SMs' number says.
+        // How many, asked once per device, cluster and stages (lists that take less than a
+        // stage more do not change what fits).
         static std::mutex mu;
         static int held[3][kMaxCluster + 1][kMaxStages + 1];
         static int held_dev = -1;
@@ -385,6 +696,9 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int per_sm, int n_s
         clusters = n;
     }
     if (clusters > a.n) clusters = a.n;
+    // a claim leaves every cluster several more
+    if (sh.batch > a.n / (4 * clusters)) sh.batch = (int)(a.n / (4 * clusters));
+    if (sh.batch < 1) sh.batch = 1;
     cfg.gridDim = dim3((unsigned)(clusters * sh.cluster));
     e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp>, a, sh);
     return e != cudaSuccess ? e : cudaGetLastError();
@@ -394,37 +708,43 @@ template <class T>
 cudaError_t launch_ring_t(const TokenArgs& a, int op, const Shape& sh, int per_sm, int n_sm, cudaStream_t s) {
     if (op == kTokLogp) return launch_ring<T, kTokLogp>(a, sh, per_sm, n_sm, s);
     if (op == kTokPpo) return launch_ring<T, kTokPpo>(a, sh, per_sm, n_sm, s);
-    return launch_ring<T, kTokPairGrad>(a, sh, per_sm, n_sm, s);
+    return launch_ring<T, kTokDistill>(a, sh, per_sm, n_sm, s);
 }
 
 }  // namespace
 
-bool launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s, cudaError_t* e) {
+cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
     const int64_t nv = (a.V + 2 * (int64_t)W - 2) / W;               // most vectors of a row
-    // The smallest cluster that leaves the ring a stage more than a slice; where only
-    // the statistics are needed no slice has to stay, and one CTA takes any row.
-    const bool whole = op == kTokPpo && a.g;
-    Shape sh{1, op == kTokLogp ? 4 : 6, 0};
-    int per_sm = op == kTokLogp ? 3 : 2;
+    const int lists = op == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0;
+    const int per_sm = op == kTokLogp ? 3 : 2;
+    Shape sh{1, op == kTokLogp ? 4 : (kRingTwo - lists) / kStageBytes, 0, 0, 0, 1};
     auto slice = [&](int c) { return (nv + c - 1) / c; };
-    if (whole) {
-        while (sh.cluster < kMaxCluster && slice(sh.cluster) > (sh.stages - 1) * kStageVecs) sh.cluster *= 2;
-        if (slice(sh.cluster) > (sh.stages - 1) * kStageVecs) {
-            sh.stages = kMaxStages;
-            per_sm = 1;
-            if (slice(sh.cluster) > kMaxStages * kStageVecs) return false;
-        }
-    }
-    // Few rows: more CTAs a row, down to half a stage.
+    // Few rows: more CTAs a row, down to half a stage a slice.
     while (sh.cluster < kMaxCluster && a.n * sh.cluster * 2 <= (int64_t)per_sm * n_sm &&
            slice(sh.cluster * 2) >= kStageVecs / 2)
         sh.cluster *= 2;
     sh.slice = (int)slice(sh.cluster);
-    if (a.dtype == MALIB_F32) *e = launch_ring_t<float>(a, op, sh, per_sm, n_sm, s);
-    else if (a.dtype == MALIB_BF16) *e = launch_ring_t<__nv_bfloat16>(a, op, sh, per_sm, n_sm, s);
-    else *e = launch_ring_t<__half>(a, op, sh, per_sm, n_sm, s);
-    return true;
+    sh.keep = sh.slice <= (sh.stages - 1) * kStageVecs ? sh.stages - 1 : sh.stages - 2;
+    // Rows of a stage or more are claimed one by one and known one ahead, so that no CTA holds
+    // several while others run out; short ones in batches of about two stages.
+    sh.queue_log = sh.slice >= kStageVecs ? 1 : 2;
+    sh.batch = sh.slice >= kStageVecs ? 1 : 2 * kStageVecs / sh.slice;
+    if (sh.batch > 16) sh.batch = 16;
+    if (a.dtype == MALIB_F32) return launch_ring_t<float>(a, op, sh, per_sm, n_sm, s);
+    if (a.dtype == MALIB_BF16) return launch_ring_t<__nv_bfloat16>(a, op, sh, per_sm, n_sm, s);
+    return launch_ring_t<__half>(a, op, sh, per_sm, n_sm, s);
+}
+
+cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s) {
+    const int W = a.dtype == MALIB_F32 ? 4 : 8;
+    const int parts = (int)(((a.V + 2 * (int64_t)W - 2) / W + kStageVecs - 1) / kStageVecs);
+    const int64_t total = a.n * parts;
+    const unsigned grid = (unsigned)(total < (1 << 30) ? total : (1 << 30));
+    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kConsumers, 0, s>>>(a, parts);
+    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kConsumers, 0, s>>>(a, parts);
+    else token_pair_grad_kernel<__half><<<grid, kConsumers, 0, s>>>(a, parts);
+    return cudaGetLastError();
 }
 
 }  // namespace malib

@@ -2,6 +2,7 @@
 // at a time, gathers its statistics in a first pass over the row and writes the
 // gradient in a second one.
 #include "token_common.cuh"
+#include "token_top.cuh"
 
 namespace malib {
 
@@ -23,12 +24,7 @@ struct RowFrame {
     __device__ __forceinline__ uint4 load(int i) const {
         const int j = i * W - h;
         if (j >= 0 && j + W <= V) return *reinterpret_cast<const uint4*>(p + j);
-        F2 v[W / 2];
-#pragma unroll
-        for (int q = 0; q < W; q += 2)
-            v[q / 2] = f2_make(j + q >= 0 && j + q < V ? Elt<T>::get(p[j + q]) : -INFINITY,
-                               j + q + 1 >= 0 && j + q + 1 < V ? Elt<T>::get(p[j + q + 1]) : -INFINITY);
-        return Elt<T>::pack(v);
+        return load_part(p, j, V);
     }
 };
 
@@ -61,64 +57,12 @@ __device__ void write_row(const T* z, T* g, int V, float k, const RowGrad& c, in
     }
 }
 
-__device__ __forceinline__ float teacher_at(const TokenArgs& a, int64_t i) {
-    if (a.tdtype == MALIB_F32) return static_cast<const float*>(a.teacher)[i];
-    if (a.tdtype == MALIB_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.teacher)[i]);
-    return __half2float(static_cast<const __half*>(a.teacher)[i]);
-}
-
-struct TopEntry {
-    int id;                                          // -1: absent
-    float q;                                         // the teacher's probability of the entry
-};
-
-// The teacher's distribution over a row's entries by one warp: q in list, and sum q ln q
-// as the return value; *live: the list has an entry. Teacher logits of -infinity are
-// absent.
-__device__ float teacher_row(const TokenArgs& a, int64_t row, TopEntry* list, bool* live) {
-    const int lane = threadIdx.x & 31;
-    float m = -INFINITY;
-    for (int j = lane; j < a.top; j += 32) {
-        int id = a.ids[row * a.top + j];
-        const float t = teacher_at(a, row * a.top + j);
-        if (id >= a.V) {
-            atomicOr(a.err, ERRBIT_BAD_TOKEN);
-            id = -1;
-        }
-        if (id < 0 || t == -INFINITY) id = -1;
-        else m = max_nan(m, t);
-        list[j] = TopEntry{id, t};
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-    *live = m != -INFINITY;
-    float s = 0.f;
-    for (int j = lane; j < a.top; j += 32) {
-        const float d = (list[j].q - m) * a.inv_t;
-        if (list[j].id >= 0) s += expf(d);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const float ls = logf(s);
-    float h = 0.f;
-    for (int j = lane; j < a.top; j += 32) {
-        const float lq = (list[j].q - m) * a.inv_t - ls, q = expf(lq);
-        list[j].q = list[j].id >= 0 ? q : 0.f;
-        if (list[j].id >= 0 && q != 0.f) h += q * lq;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) h += __shfl_xor_sync(0xffffffffu, h, o);
-    __syncwarp();
-    return h;
-}
-
 template <class T, int kOp>
 __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
     __shared__ RowStat red[2][kW];
     __shared__ RowGrad grad;
     __shared__ TopEntry list[kOp == kTokDistill ? kTokenMaxTop : 1];
-    __shared__ bool list_live;
-    __shared__ float list_h;
+    __shared__ TopRow top;
     double acc[kTokenStats] = {};                    // thread 0
     int buf = 0;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -129,15 +73,11 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
         float w = 1.f;
         if (kOp == kTokDistill) {
             if (threadIdx.x < 32) {
-                bool l;
-                const float h = teacher_row(a, row, list, &l);
-                if (threadIdx.x == 0) {
-                    list_live = l;
-                    list_h = h;
-                }
+                const TopRow t = top_row<T>(a, row, z, list);
+                if (threadIdx.x == 0) top = t;
             }
             __syncthreads();
-            live = list_live;
+            live = top.live != 0;
         } else {
             token = a.tokens[row];
             live = token >= 0 && token < a.V;
@@ -160,21 +100,13 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
             live = r.m != -INFINITY;                 // a row without an entry has no distribution
         }
         float loss = 0.f, logp = 0.f, H = 0.f;
-        if (kOp == kTokDistill && live && threadIdx.x < 32) {
-            // T^2 sum_k q_k (ln q_k - ln p_k)
-            float c = 0.f;
-            for (int j = threadIdx.x; j < a.top; j += 32)
-                if (list[j].q != 0.f) c += list[j].q * log_prob(a, r, Elt<T>::get(z[list[j].id]));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-            loss = a.tt * (list_h - c);
-        }
         if (threadIdx.x == 0) {
             if (live) {
                 acc[0] += 1.0;
                 RowGrad c{r.m, 0.f, 0.f, 0.f};
                 if (kOp == kTokDistill) {
-                    c.c0 = w * a.gscale * a.tt * a.inv_t / r.s;
+                    loss = top_loss(a, r, top);
+                    c.c0 = w * a.gscale * a.top_scale / r.s;
                     acc[1] += (double)w * loss;
                     acc[2] += loss;
                 } else if (kOp == kTokPpo) {
@@ -200,27 +132,14 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
             } else if (kOp == kTokPpo) {
                 write_row(z, g, a.V, a.k, grad, token);
             } else {
-                // the student's probabilities at the teacher's entries, before the row is
-                // written (it may be written in place)
+                // the teacher's entries go over what the row's threads have written
                 const RowGrad c = grad;
-                float v[kTokenMaxTop / kT];
-#pragma unroll
-                for (int u = 0; u < kTokenMaxTop / kT; ++u) {
-                    const int j = threadIdx.x + u * kT;
-                    if (j >= a.top || list[j].id < 0) continue;
-                    // an entry listed more than once has the sum of its probabilities
-                    float q = 0.f;
-                    for (int o = 0; o < a.top; ++o)
-                        if (list[o].id == list[j].id) q += list[o].q;
-                    v[u] = c.c0 * exp2_fast((Elt<T>::get(z[list[j].id]) - c.m) * a.k) - w * a.gscale * a.tt * a.inv_t * q;
-                }
-                __syncthreads();
                 write_row(z, g, a.V, a.k, c, -1);
                 __syncthreads();
-#pragma unroll
-                for (int u = 0; u < kTokenMaxTop / kT; ++u) {
-                    const int j = threadIdx.x + u * kT;
-                    if (j < a.top && list[j].id >= 0) g[list[j].id] = Elt<T>::put(v[u]);
+                for (int j = threadIdx.x; j < a.top; j += kT) {
+                    const TopEntry t = list[j];
+                    if (t.id >= 0)
+                        g[t.id] = Elt<T>::put(c.c0 * exp2_fast((t.z - c.m) * a.k) - w * a.gscale * a.top_scale * t.q);
                 }
             }
         }
@@ -232,9 +151,7 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
     if (kOp == kTokPpo) {
         ppo_stats(a, v);
     } else {
-        a.stats[0] = (float)v[0];
-        a.stats[1] = (float)v[1];
-        a.stats[2] = (float)(v[2] / (v[0] > 0.0 ? v[0] : 1.0));
+        distill_stats(a, v);
     }
 }
 
@@ -295,23 +212,6 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     for (int i = 1; i < 5; ++i) a.stats[i] = (float)(v[i] / v[0]);
 }
 
-// The gradient of preference pairs from the rows' statistics and the pairs' factors.
-template <class T>
-__global__ void __launch_bounds__(kT) token_pair_grad_kernel(TokenArgs a) {
-    __shared__ RowGrad grad;
-    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        if (threadIdx.x == 0) {
-            const TokenRow r = a.rows[row];
-            grad = RowGrad{r.m, -r.value * r.inv_s, 0.f, r.value};
-        }
-        __syncthreads();
-        T* g = static_cast<T*>(a.g) + row * a.gld;
-        if (a.rows[row].live) write_row(static_cast<const T*>(a.z) + row * a.ld, g, a.V, a.k, grad, a.tokens[row]);
-        else zero_row(g, a.V);
-        __syncthreads();
-    }
-}
-
 template <class T>
 cudaError_t launch_rows_t(const TokenArgs& a, int op, int grid, cudaStream_t s) {
     if (op == kTokLogp) token_rows_kernel<T, kTokLogp><<<grid, kT, 0, s>>>(a);
@@ -322,14 +222,11 @@ cudaError_t launch_rows_t(const TokenArgs& a, int op, int grid, cudaStream_t s) 
 
 }  // namespace
 
-// From this many bytes on a row is long: it goes through shared memory.
-constexpr int kRingBytes = 2048;
+// From this many bytes on a row is long: it goes through shared memory (token_ring.cu).
+constexpr int kLongBytes = 2048;
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
-    cudaError_t e;
-    if (op != kTokDistill && a.n > 0 && (int64_t)a.V * (a.dtype == MALIB_F32 ? 4 : 2) >= kRingBytes &&
-        launch_token_ring(a, op, n_sm, s, &e))
-        return e;
+    if (a.n > 0 && (int64_t)a.V * (a.dtype == MALIB_F32 ? 4 : 2) >= kLongBytes) return launch_token_ring(a, op, n_sm, s);
     const int grid = (int)(a.n < 4 * (int64_t)n_sm ? (a.n > 0 ? a.n : 1) : 4 * (int64_t)n_sm);
     if (a.dtype == MALIB_F32) return launch_rows_t<float>(a, op, grid, s);
     if (a.dtype == MALIB_BF16) return launch_rows_t<__nv_bfloat16>(a, op, grid, s);
@@ -341,13 +238,7 @@ cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
-    if ((int64_t)a.V * (a.dtype == MALIB_F32 ? 4 : 2) >= kRingBytes && launch_token_ring(a, kTokPairGrad, n_sm, s, &e))
-        return e;
-    const int grid = (int)(a.n < 4 * (int64_t)n_sm ? a.n : 4 * (int64_t)n_sm);
-    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kT, 0, s>>>(a);
-    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kT, 0, s>>>(a);
-    else token_pair_grad_kernel<__half><<<grid, kT, 0, s>>>(a);
-    return cudaGetLastError();
+    return launch_token_pair_grad(a, s);
 }
 
 }  // namespace malib

@@ -120,11 +120,11 @@ struct Elt<float> {
         v[0] = f2_pack(q.x, q.y);
         v[1] = f2_pack(q.z, q.w);
     }
-    // their maximum (NaN if one is NaN)
-    __device__ static float max(const uint4& q) {
-        return max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)),
-                       max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+    // the maximum of two words' entries, NaN if one is NaN; and the largest entry of a word
+    __device__ static uint32_t max(uint32_t a, uint32_t b) {
+        return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
     }
+    __device__ static float largest(uint32_t m) { return __uint_as_float(m); }
     __device__ static uint4 pack(const F2 (&v)[2]) {
         const float2 a = f2_split(v[0]), b = f2_split(v[1]);
         return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
@@ -144,10 +144,12 @@ struct Elt<__nv_bfloat16> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = f2_pack(w[i] << 16, w[i] & 0xffff0000u);
     }
-    __device__ static float max(const uint4& q) {
-        uint32_t m;
-        asm("{\n .reg .b32 a, b;\n max.NaN.bf16x2 a, %1, %2;\n max.NaN.bf16x2 b, %3, %4;\n max.NaN.bf16x2 %0, a, b;\n}"
-            : "=r"(m) : "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w));
+    __device__ static uint32_t max(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static float largest(uint32_t m) {
         return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
     __device__ static uint4 pack(const F2 (&v)[4]) {
@@ -179,10 +181,12 @@ struct Elt<__half> {
             v[i] = f2_make(f.x, f.y);
         }
     }
-    __device__ static float max(const uint4& q) {
-        uint32_t m;
-        asm("{\n .reg .b32 a, b;\n max.NaN.f16x2 a, %1, %2;\n max.NaN.f16x2 b, %3, %4;\n max.NaN.f16x2 %0, a, b;\n}"
-            : "=r"(m) : "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w));
+    __device__ static uint32_t max(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static float largest(uint32_t m) {
         __half2 h;
         *reinterpret_cast<uint32_t*>(&h) = m;
         const float2 f = __half22float2(h);
@@ -243,22 +247,40 @@ __device__ __forceinline__ void raise(RowStat& r, float mx, float k) {
     r.m = m;
 }
 
-// 16 bytes of logits join r, whose maximum covers them already and is not -infinity.
-template <class T>
-__device__ __forceinline__ void gather(RowStat& r, const uint4& q, float k) {
+// The maximum of 16-byte vectors of logits (NaN if one is NaN).
+template <class T, int N>
+__device__ __forceinline__ float vec_max(const uint4 (&q)[N]) {
+    uint32_t m = q[0].x;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        if (u > 0) m = Elt<T>::max(m, q[u].x);
+        m = Elt<T>::max(m, q[u].y);
+        m = Elt<T>::max(m, q[u].z);
+        m = Elt<T>::max(m, q[u].w);
+    }
+    return Elt<T>::largest(m);
+}
+
+// Vectors of logits join r, whose maximum covers them already and is not -infinity.
+template <class T, int N>
+__device__ __forceinline__ void gather(RowStat& r, const uint4 (&q)[N], float k) {
     constexpr int P = Elt<T>::W / 2;
-    F2 y[P], s = 0ull, t = 0ull;
-    Elt<T>::pairs(q, y);
+    F2 s = f2_make(r.s, 0.f), t = f2_make(r.t, 0.f);
     const F2 k2 = f2_dup(k), neg = f2_dup(-r.m);
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const F2 x = f2_mul(f2_add(y[i], neg), k2), e = f2_exp2(x);
-        s = f2_add(s, e);
-        f2_fma(t, e, f2_floor_x(x));
+    for (int u = 0; u < N; ++u) {
+        F2 y[P];
+        Elt<T>::pairs(q[u], y);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const F2 x = f2_mul(f2_add(y[i], neg), k2), e = f2_exp2(x);
+            s = f2_add(s, e);
+            f2_fma(t, e, f2_floor_x(x));
+        }
     }
     const float2 s2 = f2_split(s), t2 = f2_split(t);
-    r.s += s2.x + s2.y;
-    r.t += t2.x + t2.y;
+    r.s = s2.x + s2.y;
+    r.t = t2.x + t2.y;
 }
 
 // Statistics of N lanes that follow one another, the same in each: their maximum, then

@@ -313,40 +313,22 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
 
     if (warp == kConsumerWarps) {
         // ---- producer
-        // rank 0: claimed rows in batches, lane i with the i-th row's token and weight; the
-        // next batch, whose tokens are on their way, and the start of the one after that,
-        // whose claim is (lane 0): none is waited for where it is asked for
-        struct Batch {
-            int64_t row;
-            int32_t token;
-            float w;
-        };
-        auto look = [&](int64_t row) {
-            Batch b{row, -1, 1.f};
-            if (lane < sh.batch && row + lane < a.n) {
-                b.token = kTop ? 0 : a.tokens[row + lane];
-                if (kOp != kTokLogp) b.w = a.weight ? a.weight[row + lane] : a.w0;
-            }
-            return b;
-        };
+        // rank 0: a batch of claimed rows, lane i with the i-th row's token and weight. The
+        // next one is claimed (lane 0) when the batch's last row is sent, and looked at when
+        // that row's copies are under way: neither is waited for where it is asked for, and
+        // no cluster holds rows that another could start on.
         const int64_t clusters = gridDim.x / C;
-        Batch now{}, next{};
-        unsigned long long claim = 0;
-        int used = 0;
-        // with a batch for every row there is nothing to claim
-        const bool claims = a.n > clusters * sh.batch;
-        auto more = [&] {
-            if (claims && lane == 0) claim = atomicAdd(a.claims, (unsigned long long)sh.batch);
+        const bool claims = a.n > clusters * sh.batch;               // else there is a batch for every row
+        int64_t batch = (int64_t)(blockIdx.x / C) * sh.batch;
+        int used = 0, token = -1;
+        float w = 1.f;
+        auto look = [&] {
+            token = -1;
+            if (lane >= sh.batch || batch + lane >= a.n) return;
+            token = kTop ? 0 : a.tokens[batch + lane];
+            if (kOp != kTokLogp) w = a.weight ? a.weight[batch + lane] : a.w0;
         };
-        auto look_next = [&] {
-            if (claims) next = look((int64_t)(clusters * sh.batch + __shfl_sync(0xffffffffu, claim, 0)));
-            else next.row = a.n;
-            more();
-        };
-        if (rank == 0) {
-            more();
-            now = look((int64_t)(blockIdx.x / C) * sh.batch);
-        }
+        if (rank == 0) look();
         Cursor at, issued;
         bool wrapped = false;
         for (uint32_t t = 0;; ++t) {
@@ -354,8 +336,8 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
             // the cluster's instructions only in launches with clusters
             if (C > 1 && lane == 0) mbar_arrive_expect_tx(&qfull[slot], sizeof(Queued));
             if (rank == 0) {
-                Queued q{now.row + used < a.n ? now.row + used : -1, __shfl_sync(0xffffffffu, now.token, used),
-                         __shfl_sync(0xffffffffu, now.w, used)};
+                Queued q{batch + used < a.n ? batch + used : -1, __shfl_sync(0xffffffffu, token, used),
+                         __shfl_sync(0xffffffffu, w, used)};
                 if (q.token >= a.V && lane == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
                 if (q.token >= a.V || q.w == 0.f) q.token = -1;
                 if (C > 1) {
@@ -371,11 +353,9 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                         mbar_arrive_release(&qfull[slot]);
                     }
                 }
-                if (t == 0) look_next();
                 if (++used == sh.batch) {
-                    used = 0;
-                    now = next;
-                    look_next();
+                    if (!claims) batch = a.n;
+                    else if (lane == 0) batch = clusters * sh.batch + (int64_t)atomicAdd(a.claims, (unsigned long long)sh.batch);
                 }
             }
             const Queued q = take(t);
@@ -409,6 +389,11 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                     }
                     __syncwarp();
                 }
+            }
+            if (rank == 0 && used == sh.batch) {
+                used = 0;
+                batch = __shfl_sync(0xffffffffu, batch, 0);
+                look();
             }
             leave(t);
         }
@@ -477,17 +462,16 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                 const uint4* src = reinterpret_cast<const uint4*>(ring + at.stage * kStageBytes);
                 wait(&full[at.stage], at.parity);
                 uint4 x[kPer];
+                if (n == kStageVecs) {
 #pragma unroll
-                for (int u = 0; u < kPer; ++u)
-                    x[u] = tid + u * kConsumers < n ? src[tid + u * kConsumers] : Elt<T>::none();
-                float mx = Elt<T>::max(x[0]);
+                    for (int u = 0; u < kPer; ++u) x[u] = src[tid + u * kConsumers];
+                } else {
 #pragma unroll
-                for (int u = 1; u < kPer; ++u) mx = max_nan(mx, Elt<T>::max(x[u]));
-                raise(r, mx, a.k);
-                if (r.m != -INFINITY) {
-#pragma unroll
-                    for (int u = 0; u < kPer; ++u) gather<T>(r, x[u], a.k);
+                    for (int u = 0; u < kPer; ++u)
+                        x[u] = tid + u * kConsumers < n ? src[tid + u * kConsumers] : Elt<T>::none();
                 }
+                raise(r, vec_max<T>(x), a.k);
+                if (r.m != -INFINITY) gather<T>(r, x, a.k);
                 if (part < kept) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&empty[at.stage]);

@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(kT) token_rows_kernel(TokenArgs a) {
         if (live) {
             const RowFrame<T> f(z, a.V);
             for (int i = threadIdx.x; i < f.nv; i += kT) {
-                const uint4 q = f.load(i);
-                raise(r, Elt<T>::max(q), a.k);
+                const uint4 q[1] = {f.load(i)};
+                raise(r, vec_max<T>(q), a.k);
                 if (r.m != -INFINITY) gather<T>(r, q, a.k);
             }
             r = block_stat<kW>(r, a.k, red[buf]);

@@ -509,7 +509,7 @@ typedef struct malib_token_batch {
     int64_t ld;               /* row stride in elements; >= vocab, or 0 for one row that all share */
     int32_t vocab;            /* 1 <= V <= 2^24 */
     int32_t dtype;            /* malib_dtype of logits and gradient */
-    float temperature;
+    double temperature;
 } malib_token_batch;
 
 /* The gradient at the logits: grad [n_rows][ld] of the logits' type, ld >= vocab

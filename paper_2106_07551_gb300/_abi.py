@@ -60,7 +60,7 @@ class Traj(C.Structure):
 
 class TokenBatch(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("tokens", C.c_void_p), ("n_rows", C.c_int64), ("ld", C.c_int64),
-                ("vocab", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float)]
+                ("vocab", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_double)]
 
 
 class TokenGrad(C.Structure):

@@ -13,7 +13,7 @@ constexpr int32_t kMaxVocab = 1 << 24;
 
 // Fixed work space: the counter, then the partial sums.
 constexpr int64_t kPartOffset = 256;
-static_assert(kPartOffset + (int64_t)kTokenMaxCtas * kTokenStats * 8 <= kTokenFixedBytes, "token work space");
+static_assert(kPartOffset + (int64_t)kTokenMaxCtas * (int64_t)sizeof(Totals) <= kTokenFixedBytes, "token work space");
 
 int elt_size(int32_t dtype) { return dtype == MALIB_F32 ? 4 : 2; }
 bool known(int32_t dtype) { return dtype == MALIB_F32 || dtype == MALIB_BF16 || dtype == MALIB_F16; }
@@ -41,8 +41,8 @@ struct Call {
         if (b->ld != 0 && b->ld < b->vocab) return bad("logits row stride below vocab");
         const int64_t es = elt_size(b->dtype);
         if (b->n_rows > 0 && b->ld > INT64_MAX / es / b->n_rows) return bad("logits do not fit the address space");
-        if (!(b->temperature >= 1e-6f && b->temperature <= 1e6f)) return bad("temperature must lie in [1e-6, 1e6]");
-        const double exact_k = 1.4426950408889634074 / (double)b->temperature;
+        if (!(b->temperature >= 1e-6 && b->temperature <= 1e6)) return bad("temperature must lie in [1e-6, 1e6]");
+        const double exact_k = 1.4426950408889634074 / b->temperature;
         const float k = (float)exact_k;
         if (b->n_rows > 0) {
             if (!dev(b->logits, (int)es)) return bad("logits must be aligned device memory of the context's device");
@@ -56,9 +56,10 @@ struct Call {
         a.dtype = b->dtype;
         a.k = k;
         a.dk = (float)(0.69314718055994530942 * (exact_k / (double)k - 1.0));
-        a.inv_t = (float)(1.0 / (double)b->temperature);
-        a.tt = b->temperature * b->temperature;
-        a.top_scale = b->temperature;
+        a.inv_t = (float)(1.0 / b->temperature);
+        a.inv_t_lo = (float)(1.0 / b->temperature - (double)a.inv_t);
+        a.tt = (float)(b->temperature * b->temperature);
+        a.top_scale = (float)b->temperature;
         a.tokens = b->tokens;
         a.err = v.err;
         return MALIB_OK;
@@ -98,7 +99,7 @@ struct Call {
         if (r != MALIB_OK) return r;
         a.ticket = static_cast<unsigned*>(fixed);
         a.claims = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(fixed) + 128);
-        a.part = reinterpret_cast<double*>(static_cast<uint8_t*>(fixed) + kPartOffset);
+        a.part = reinterpret_cast<Totals*>(static_cast<uint8_t*>(fixed) + kPartOffset);
         a.row_sums = static_cast<RowSum*>(rows);
         return MALIB_OK;
     }

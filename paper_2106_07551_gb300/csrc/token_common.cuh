@@ -12,6 +12,10 @@
 // row with a running maximum; two partial statistics combine by scaling with
 // 2^((m_a - m) k). They are held in fp32: a row's sum has at most a few hundred
 // thousand terms, added in thousands of partial sums.
+// The fast base-2 exponential is low by 5.0e-8 of its value on average (measured over
+// [-20, 0), the same from -1 down), which every sum of a row, and every scaling of one,
+// would pass on and a sequence's sum add up; 2^x is taken of x + kExpBias, added in the
+// same rounding, which leaves 2^0 = 1.
 // x is held above -200, where 2^x is 0 in fp32, wherever it multiplies 2^x: an entry
 // of -infinity (masked) contributes 0 and not 0 x infinity. A NaN or +infinity makes
 // the row's S, and with it all that follows from the row, NaN.
@@ -28,17 +32,15 @@
 namespace malib {
 
 constexpr int kTokenMaxTop = 1024;                   // teacher entries of a row
-constexpr int kTokenStats = 5;                       // sums of a call's statistics
 constexpr int kTokenMaxCtas = 8192;                  // CTAs whose partial sums the work space holds
 
-enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2 };
+enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3 };
 
 // What a row's statistics leave for a preference pair's sums and its gradient: first
-// value is ln p of the token; the pair's sums put d L / d logit of the token before
-// -p in its place.
+// value + rest is ln p of the token; the pair's sums put d L / d logit of the token
+// before -p into value. inv_s = 0: the row is left out.
 struct __align__(16) TokenRow {
-    float m, inv_s, value;
-    int32_t live;
+    float m, inv_s, value, rest;
 };
 
 // A row's share of a call's statistics.
@@ -55,7 +57,7 @@ struct TokenArgs {
     int64_t n;
     int32_t V;
     int32_t dtype;
-    float k, inv_t;              // log2(e) / T, 1 / T
+    float k, inv_t, inv_t_lo;    // log2(e) / T, 1 / T and what its rounding leaves
     float dk;                    // ln 2 times the relative error of k's rounding
     const int32_t* tokens;       // [n], < 0: the row is left out
     int* err;
@@ -84,7 +86,7 @@ struct TokenArgs {
     float* loss;
     float* reward;               // [2 n_pairs]
     float* stats;
-    double* part;                // [kTokenMaxCtas][kTokenStats]
+    struct Totals* part;         // [kTokenMaxCtas]
     unsigned* ticket;            // CTAs that have written their sums
     RowSum* row_sums;            // [n]
     unsigned long long* claims;  // rows claimed
@@ -205,6 +207,7 @@ struct Elt<__half> {
 
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kXMin = -200.f;
+constexpr float kExpBias = 7.3e-8f;                  // 5.04e-8 / ln 2
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
@@ -212,6 +215,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return r;
 }
 
+__device__ __forceinline__ F2 f2_fma3(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 __device__ __forceinline__ F2 f2_exp2(F2 x) {
     const float2 v = f2_split(x);
     return f2_make(exp2_fast(v.x), exp2_fast(v.y));
@@ -225,13 +233,16 @@ struct RowStat {
     float m, s, t;
 };
 
+// x of an entry with logit z in a row of maximum m, as 2^x takes it.
+__device__ __forceinline__ float x_of(float z, float m, float k) { return fmaf(z - m, k, kExpBias); }
+
 // b's sums join a's. A side that has seen only -infinity has s = t = 0.
 __device__ __forceinline__ RowStat combine(const RowStat& a, const RowStat& b, float k) {
     RowStat r;
     r.m = max_nan(a.m, b.m);
     // (-infinity) - (-infinity) is NaN, which fmaxf takes for kXMin: a factor 0 on sums of 0
     const float da = fmaxf((a.m - r.m) * k, kXMin), db = fmaxf((b.m - r.m) * k, kXMin);
-    const float fa = exp2_fast(da), fb = exp2_fast(db);
+    const float fa = exp2_fast(da + kExpBias), fb = exp2_fast(db + kExpBias);
     r.s = fmaf(a.s, fa, b.s * fb);
     r.t = fa * fmaf(a.s, da, a.t) + fb * fmaf(b.s, db, b.t);
     return r;
@@ -241,7 +252,7 @@ __device__ __forceinline__ RowStat combine(const RowStat& a, const RowStat& b, f
 __device__ __forceinline__ void raise(RowStat& r, float mx, float k) {
     if (mx <= r.m) return;                           // neither a new maximum nor a NaN
     const float m = max_nan(r.m, mx);
-    const float d = fmaxf((r.m - m) * k, kXMin), f = exp2_fast(d);
+    const float d = fmaxf((r.m - m) * k, kXMin), f = exp2_fast(d + kExpBias);
     r.t = f * fmaf(r.s, d, r.t);
     r.s *= f;
     r.m = m;
@@ -266,14 +277,14 @@ template <class T, int N>
 __device__ __forceinline__ void gather(RowStat& r, const uint4 (&q)[N], float k) {
     constexpr int P = Elt<T>::W / 2;
     F2 s = f2_make(r.s, 0.f), t = f2_make(r.t, 0.f);
-    const F2 k2 = f2_dup(k), neg = f2_dup(-r.m);
+    const F2 k2 = f2_dup(k), neg = f2_dup(-r.m), bias = f2_dup(kExpBias);
 #pragma unroll
     for (int u = 0; u < N; ++u) {
         F2 y[P];
         Elt<T>::pairs(q[u], y);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const F2 x = f2_mul(f2_add(y[i], neg), k2), e = f2_exp2(x);
+            const F2 x = f2_fma3(f2_add(y[i], neg), k2, bias), e = f2_exp2(x);
             s = f2_add(s, e);
             f2_fma(t, e, f2_floor_x(x));
         }
@@ -299,34 +310,22 @@ __device__ __forceinline__ RowStat reduce_stat(RowStat r, float k) {
     return r;
 }
 
-// Statistics of the whole block, the same in every thread. red: a slot a warp.
-template <int kWarps>
-__device__ __forceinline__ RowStat block_stat(RowStat r, float k, RowStat* red) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    r = reduce_stat<32>(r, k);
-    if (lane == 0) red[warp] = r;
-    __syncthreads();
-    return reduce_stat<kWarps>(red[lane % kWarps], k);
-}
-
 // The gradient at entry j is 2^x_j (c0 + c1 x_j), and `at` more at the row's token.
 struct RowGrad {
     float m, c0, c1, at;
 };
 
-// ln S. k's rounding to fp32 shifts every row's ln S the same way, by ln 2 (dk / k) t / S,
-// which a sequence's sum would add up; taken out here.
-__device__ __forceinline__ float log_sum(const TokenArgs& a, const RowStat& r) {
-    return logf(r.s) + a.dk * (r.t / r.s);
-}
+// The mean of x under p.
+__device__ __forceinline__ float mean_x(const RowStat& r) { return r.t / r.s - kExpBias; }
 // 16 bytes of the gradient. kEntropy: with the term in x.
 template <class T, bool kEntropy>
 __device__ __forceinline__ void emit(const uint4& q, const RowGrad& c, float k, F2 (&v)[Elt<T>::W / 2]) {
     Elt<T>::pairs(q, v);
-    const F2 k2 = f2_dup(k), neg = f2_dup(-c.m), c0 = f2_dup(c.c0), c1 = f2_dup(c.c1);
+    const F2 k2 = f2_dup(k), neg = f2_dup(-c.m), c0 = f2_dup(c.c0), c1 = f2_dup(c.c1),
+             bias = f2_dup(kExpBias);
 #pragma unroll
     for (int i = 0; i < Elt<T>::W / 2; ++i) {
-        const F2 x = f2_mul(f2_add(v[i], neg), k2), e = f2_exp2(x);
+        const F2 x = f2_fma3(f2_add(v[i], neg), k2, bias), e = f2_exp2(x);
         F2 f = c0;
         if (kEntropy) f2_fma(f, f2_floor_x(x), c1);
         v[i] = f2_mul(e, f);
@@ -362,14 +361,24 @@ __device__ __forceinline__ uint4 load_part(const T* p, int j, int V) {
     return Elt<T>::pack(v);
 }
 
-// ln p of the entry with logit z.
-__device__ __forceinline__ float log_prob(const TokenArgs& a, const RowStat& r, float z) {
-    // ln 2 x (1 + d) for k's relative rounding d: (z - m) / T
-    const float x = (z - r.m) * a.k;
-    return fmaf(kLn2, x, a.dk * x) - log_sum(a, r);
+// ln p of the entry with logit z, (z - m) / T - ln S, and in *rest what its rounding leaves.
+// The difference, the product and 1 / T go in with their errors, and so does what k's
+// rounding to fp32 does to every row's ln S, dk times the mean of x: a sequence adds up
+// what all its rows have in common, and beside ln S alone these are below half a unit.
+__device__ __forceinline__ float log_prob(const TokenArgs& a, const RowStat& r, float z, float* rest = nullptr) {
+    const float y = __fsub_rn(z, r.m), u = __fsub_rn(y, z);
+    const float ye = __fsub_rn(__fsub_rn(z, __fsub_rn(y, u)), __fadd_rn(r.m, u));        // z - m = y + ye
+    const float p = __fmul_rn(y, a.inv_t), pe = fmaf(y, a.inv_t, -p);
+    const float ls = logf(r.s), d = __fsub_rn(p, ls), v = __fsub_rn(d, p);
+    const float de = __fsub_rn(__fsub_rn(p, __fsub_rn(d, v)), __fadd_rn(ls, v));         // p - ls = d + de
+    const float small = (de + pe) + fmaf(y, a.inv_t_lo, fmaf(ye, a.inv_t, -a.dk * mean_x(r)));
+    const bool finite = fabsf(d) < INFINITY;
+    const float out = finite ? d + small : d;
+    if (rest) *rest = finite ? __fadd_rn(__fsub_rn(d, out), small) : 0.f;
+    return out;
 }
 __device__ __forceinline__ float row_entropy(const RowStat& r) {
-    return logf(r.s) - kLn2 * (r.t / r.s);
+    return logf(r.s) - kLn2 * mean_x(r);
 }
 
 struct PpoRow {
@@ -408,58 +417,106 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
 
 // The outputs of a row whose log-probability is all that is asked for.
 __device__ __forceinline__ void logp_row(const TokenArgs& a, int64_t row, bool live, const RowStat& r, float z) {
-    const float logp = live ? log_prob(a, r, z) : 0.f;
+    float rest = 0.f;
+    const float logp = live ? log_prob(a, r, z, &rest) : 0.f;
     if (a.logp) a.logp[row] = logp;
     if (a.entropy) a.entropy[row] = live ? row_entropy(r) : 0.f;
-    if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, live ? 1 : 0};
+    if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, rest};
 }
 
-__device__ __forceinline__ void ppo_stats(const TokenArgs& a, const double (&v)[kTokenStats]) {
-    const double M = v[0] > 0.0 ? v[0] : 1.0;
-    a.stats[0] = (float)v[0];
-    a.stats[1] = (float)v[1];
-    for (int i = 2; i < 5; ++i) a.stats[i] = (float)(v[i] / M);
+// A sum in fp32 with the rounding errors of its additions beside it (Knuth's two-sum): as
+// good as one in fp64, whose rate is a sixtieth of fp32's here.
+struct Sum2 {
+    float s, e;
+    __device__ __forceinline__ void add(float x) {
+        const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
+        e = __fadd_rn(e, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
+        s = t;
+    }
+    __device__ __forceinline__ void add(const Sum2& b) {
+        add(b.s);
+        e = __fadd_rn(e, b.e);
+    }
+    // an infinite sum has an error that is NaN, and none to speak of
+    __device__ __forceinline__ double value() const {
+        return (double)s + (fabsf(s) < INFINITY ? (double)e : 0.0);
+    }
+};
+// The statistics of rows: policy loss: KL and H in x, y; distillation: l in x.
+struct Totals {
+    int32_t rows, clipped;
+    Sum2 loss, x, y;
+    __device__ __forceinline__ void add(const RowSum& r) {
+        rows += r.flags & 1;
+        clipped += r.flags >> 1;
+        loss.add(r.loss);
+        x.add(r.x);
+        y.add(r.y);
+    }
+    __device__ __forceinline__ void add(const Totals& b) {
+        rows += b.rows;
+        clipped += b.clipped;
+        loss.add(b.loss);
+        x.add(b.x);
+        y.add(b.y);
+    }
+};
+__device__ __forceinline__ Sum2 sum2_xor(const Sum2& v, int o) {
+    return Sum2{__shfl_xor_sync(0xffffffffu, v.s, o), __shfl_xor_sync(0xffffffffu, v.e, o)};
 }
-
-// Partial sums of a call's statistics: the CTA's, then, in the CTA that comes last,
-// the call's, in a fixed order. Returns in thread 0 of that CTA true with the sums in
-// out. Called by every thread of the block; acc is thread 0's.
+// The block's totals in thread 0, in a fixed order.
 template <int kThreads>
-__device__ __forceinline__ bool sum_partials(double* part, unsigned* ticket, const double (&acc)[kTokenStats],
-                                             double (&out)[kTokenStats]) {
-    __shared__ bool last;
-    __shared__ double red[kThreads / 32][kTokenStats];
-    if (threadIdx.x == 0) {
+__device__ __forceinline__ Totals block_totals(Totals v) {
+    __shared__ Totals part[kThreads / 32];
 #pragma unroll
-        for (int i = 0; i < kTokenStats; ++i) part[(int64_t)blockIdx.x * kTokenStats + i] = acc[i];
-        __threadfence();
-        last = atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1;   // back at 0 for the next call
+    for (int o = 16; o > 0; o >>= 1) {
+        const Totals b{__shfl_xor_sync(0xffffffffu, v.rows, o), __shfl_xor_sync(0xffffffffu, v.clipped, o),
+                       sum2_xor(v.loss, o), sum2_xor(v.x, o), sum2_xor(v.y, o)};
+        v.add(b);
     }
     __syncthreads();
-    if (!last) return false;
-    __threadfence();
-    double v[kTokenStats] = {};
-    for (int c = threadIdx.x; c < (int)gridDim.x; c += kThreads)
-#pragma unroll
-        for (int i = 0; i < kTokenStats; ++i) v[i] += __ldcg(part + (int64_t)c * kTokenStats + i);
-#pragma unroll
-    for (int i = 0; i < kTokenStats; ++i) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5][i] = v[i];
-    }
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    if (threadIdx.x != 0) return false;
-#pragma unroll
-    for (int i = 0; i < kTokenStats; ++i) {
-        out[i] = 0.0;
-        for (int w = 0; w < kThreads / 32; ++w) out[i] += red[w][i];
+    if (threadIdx.x == 0)
+        for (int w = 1; w < kThreads / 32; ++w) v.add(part[w]);
+    return v;
+}
+template <int kOp>
+__device__ __forceinline__ void write_stats(const TokenArgs& a, const Totals& v) {
+    const double M = v.rows > 0 ? (double)v.rows : 1.0;
+    a.stats[0] = (float)v.rows;
+    a.stats[1] = (float)v.loss.value();
+    if (kOp == kTokPpo) {
+        a.stats[2] = (float)((double)v.clipped / M);
+        a.stats[3] = (float)(v.x.value() / M);
+        a.stats[4] = (float)(v.y.value() / M);
+    } else {
+        a.stats[2] = (float)(v.x.value() / M);
     }
-    return true;
 }
 
+// The calling CTA has stored what others will read; whether it is the last of `of` that
+// come here. The counter is back at 0 for the next call.
+__device__ __forceinline__ bool last_of(unsigned* ticket, unsigned of) {
+    __shared__ bool last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicInc(ticket, of - 1) == of - 1;
+    }
+    __syncthreads();
+    if (last) __threadfence();
+    return last;
+}
+
+// A call's rows (token_pairs.cu), by the kernel that takes their length.
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
-// Rows of at least a few KB (token_ring.cu).
+// Short rows (token_short.cuh), by type.
+constexpr int kShortVecs = 512;                      // most 16-byte vectors of a short row
+cudaError_t launch_token_short_f32(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+cudaError_t launch_token_short_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+cudaError_t launch_token_short_f16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+// Longer ones (token_ring.cu).
 cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s);
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s);

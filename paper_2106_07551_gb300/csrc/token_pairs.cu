@@ -1,0 +1,107 @@
+// Losses of token policies: which kernel takes a call's rows, and the preference loss of
+// answer pairs between its rows' statistics and their gradients.
+#include "token_common.cuh"
+
+namespace malib {
+
+namespace {
+
+constexpr int kPairT = 256;
+
+// A double's sum over a warp costs more than all the rest of a small pair: per thread and
+// warp fp32 sums with their errors, fp64 at the end.
+__device__ __forceinline__ Sum2 warp_sum2(Sum2 v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v.add(sum2_xor(v, o));
+    return v;
+}
+
+// One CTA a pair: the rewards of its two sequences, the loss, and the factor of its
+// rows' gradients.
+__global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
+    __shared__ Sum2 red[kPairT / 32];
+    __shared__ float factor;
+    constexpr int kHalf = kPairT / 2;
+    const int side = threadIdx.x / kHalf, part = threadIdx.x % kHalf;
+    Totals total{};                                  // thread 0: pairs, those in order; loss, rewards
+    for (int p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
+        const int64_t o0 = a.offsets[2 * p], o1 = a.offsets[2 * p + 1], o2 = a.offsets[2 * p + 2];
+        const bool ok = o0 >= 0 && o0 <= o1 && o1 <= o2 && o2 <= a.n && (p > 0 || o0 == 0) &&
+                        (p + 1 < a.n_pairs || o2 == a.n);
+        if (!ok && threadIdx.x == 0) atomicOr(a.err, ERRBIT_BAD_OFFSETS);
+        const int64_t lo = !ok ? 0 : side ? o1 : o0, hi = !ok ? 0 : side ? o2 : o1;
+        Sum2 s{0.f, 0.f};
+        for (int64_t i = lo + part; i < hi; i += kHalf) {
+            const TokenRow r = a.rows[i];
+            if (r.inv_s == 0.f) continue;
+            s.add(r.value);
+            s.e += r.rest;
+            if (a.ref) s.add(-a.ref[i]);
+        }
+        s = warp_sum2(s);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float rew[2];
+            for (int q = 0; q < 2; ++q) {
+                Sum2 v = red[q * (kHalf / 32)];
+                for (int i = 1; i < kHalf / 32; ++i) v.add(red[q * (kHalf / 32) + i]);
+                rew[q] = (float)((double)a.beta * v.value());
+                if (a.reward) a.reward[2 * p + q] = rew[q];
+            }
+            const float d = rew[0] - rew[1];
+            // -ln s(x) = max(-x, 0) + ln(1 + e^-|x|)
+            const float tail = log1pf(expf(-fabsf(d)));
+            const float lp = fmaxf(-d, 0.f) + tail, ln = fmaxf(d, 0.f) + tail;
+            total.add(RowSum{(1.f - a.smooth) * lp + a.smooth * ln, rew[0], rew[1], d > 0.f ? 3 : 1});
+            // smooth s(d) - (1 - smooth) s(-d)
+            const float slope = a.smooth / (1.f + expf(-d)) - (1.f - a.smooth) / (1.f + expf(d));
+            factor = slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs;
+        }
+        if (!a.g || !ok) continue;
+        __syncthreads();
+        const float f = factor;
+        for (int64_t i = o0 + threadIdx.x; i < o2; i += kPairT) a.rows[i].value = i < o1 ? f : -f;
+    }
+    if (!a.stats) return;
+    if (threadIdx.x == 0) a.part[blockIdx.x] = total;
+    if (!last_of(a.ticket, gridDim.x)) return;
+    Totals v{};
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kPairT) v.add(a.part[i]);
+    v = block_totals<kPairT>(v);
+    if (threadIdx.x != 0) return;
+    const double n = (double)a.n_pairs;
+    a.stats[0] = (float)a.n_pairs;
+    a.stats[1] = (float)(v.loss.value() / n);
+    a.stats[2] = (float)((double)v.clipped / n);
+    a.stats[3] = (float)(v.x.value() / n);
+    a.stats[4] = (float)(v.y.value() / n);
+}
+
+bool is_short(const TokenArgs& a) {
+    const int W = a.dtype == MALIB_F32 ? 4 : 8;
+    return (a.V + 2 * (int64_t)W - 2) / W <= kShortVecs;
+}
+
+cudaError_t launch_short(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    if (a.dtype == MALIB_F32) return launch_token_short_f32(a, op, n_sm, s);
+    if (a.dtype == MALIB_BF16) return launch_token_short_bf16(a, op, n_sm, s);
+    return launch_token_short_f16(a, op, n_sm, s);
+}
+
+}  // namespace
+
+cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    return a.n == 0 || is_short(a) ? launch_short(a, op, n_sm, s) : launch_token_ring(a, op, n_sm, s);
+}
+
+cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    cudaError_t e = a.n > 0 ? launch_token_rows(a, kTokLogp, n_sm, s) : cudaSuccess;
+    if (e != cudaSuccess) return e;
+    token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
+    if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
+    return is_short(a) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_token_pair_grad(a, s);
+}
+
+}  // namespace malib

@@ -103,7 +103,7 @@ __device__ __forceinline__ uint4 load_shifted(const uint8_t* p, int by) {   // p
 // One entry of the gradient.
 template <class T>
 __device__ __forceinline__ float emit_one(T z, const RowGrad& c, float k) {
-    const float x = (Elt<T>::get(z) - c.m) * k;
+    const float x = x_of(Elt<T>::get(z), c.m, k);
     return exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
 }
 
@@ -173,12 +173,7 @@ __device__ __forceinline__ void zero_entries(T* g, int j0, int j1) {
 // block).
 template <int kOp, int kThreads>
 __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
-    __shared__ double part[kThreads / 32][kTokenStats];
-    __threadfence();
-    // counts are whole numbers; a thread's other sums are fp32 with their rounding errors
-    // (two-sum), fp64 from the warps on: its rate is a sixtieth of fp32's here
-    int rows = 0, clipped = 0;
-    float sum[3] = {}, err[3] = {};
+    Totals v{};
     constexpr int kAt = 8;                           // loads in flight
     for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kAt * kThreads) {
         float4 q[kAt];
@@ -188,48 +183,10 @@ __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
             q[u] = i < a.n ? __ldcg(reinterpret_cast<const float4*>(a.row_sums + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int u = 0; u < kAt; ++u) {
-            const int flags = __float_as_int(q[u].w);
-            rows += flags & 1;
-            clipped += flags >> 1;
-            const float x[3] = {q[u].x, q[u].y, q[u].z};
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                const float s = __fadd_rn(sum[i], x[i]), y = __fsub_rn(s, sum[i]);
-                err[i] += __fadd_rn(__fsub_rn(sum[i], __fsub_rn(s, y)), __fsub_rn(x[i], y));
-                sum[i] = s;
-            }
-        }
+        for (int u = 0; u < kAt; ++u) v.add(RowSum{q[u].x, q[u].y, q[u].z, __float_as_int(q[u].w)});
     }
-    double v[kTokenStats];
-    v[0] = __reduce_add_sync(0xffffffffu, rows);
-    if (kOp == kTokPpo) v[2] = __reduce_add_sync(0xffffffffu, clipped);
-    // an infinite sum has an error that is NaN, and none to speak of
-    auto whole = [&](int i) { return (double)sum[i] + (fabsf(sum[i]) < INFINITY ? (double)err[i] : 0.0); };
-    v[1] = whole(0);
-    v[kOp == kTokPpo ? 3 : 2] = whole(1);
-    if (kOp == kTokPpo) v[4] = whole(2);
-    constexpr int kSums = kOp == kTokPpo ? 5 : 3;
-#pragma unroll
-    for (int i = 1; i < kSums; ++i) {
-        if (kOp == kTokPpo && i == 2) continue;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    }
-    if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int i = 0; i < kSums; ++i) part[threadIdx.x >> 5][i] = v[i];
-    __syncthreads();
-    if (threadIdx.x >= kSums) return;
-    double all = 0.0;
-    for (int w = 0; w < kThreads / 32; ++w) all += part[w][threadIdx.x];
-    part[0][threadIdx.x] = all;                      // (its own column)
-    __syncwarp((1u << kSums) - 1u);
-    if (threadIdx.x != 0) return;
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) v[i] = part[0][i];
-    if (kOp == kTokPpo) ppo_stats(a, v);
-    else distill_stats(a, v);
+    v = block_totals<kThreads>(v);
+    if (threadIdx.x == 0) write_stats<kOp>(a, v);
 }
 
 template <class T, int kOp>
@@ -248,6 +205,8 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
     __shared__ Queued queue[kQueue];
     __shared__ Partial red[kQueue][kConsumerWarps], xslot[kQueue][kMaxCluster];
     __shared__ RowOut rout[kQueue];
+    constexpr int kSeen = kTop ? 32768 : 32;
+    __shared__ uint32_t seen[kSeen / 32];
     __shared__ TopRow top[2];
     __shared__ int dead;                             // a bounded wait has expired: nothing waits any more
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -403,7 +362,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                     mbar_wait_bounded(&full[i], i <= issued.stage ? issued.parity : issued.parity ^ 1u, 1000000);
     } else if (warp > kConsumerWarps) {
         // ---- teacher
-        if (kTop) {
+        if constexpr (kTop) {
             uint32_t turn = 0;                       // rows that are read
             for (uint32_t t = 0;; ++t) {
                 const Queued q = take(t);
@@ -411,7 +370,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                 if (q.token >= 0) {
                     const int b = turn & 1u;
                     wait(&tempty[b], (turn >> 1 & 1u) ^ 1u);
-                    const TopRow r = top_row<T>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld, entries + b * a.top);
+                    const TopRow r = top_row<T, kSeen>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld, entries + b * a.top, seen);
                     if (lane == 0) top[b] = r;
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&tfull[b]);
@@ -558,7 +517,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                         for (int i = tid; i < a.top; i += kConsumers) {
                             const TopEntry e = entries[b * a.top + i];
                             if (e.id >= j0 && e.id < j1)
-                                g[e.id] = Elt<T>::put(c.c0 * exp2_fast((e.z - c.m) * a.k) - c.at * e.q);
+                                g[e.id] = Elt<T>::put(c.c0 * exp2_fast(x_of(e.z, c.m, a.k)) - c.at * e.q);
                         }
                 }
             }
@@ -575,17 +534,10 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
         cluster_arrive();
         cluster_wait();
     }
-    __syncthreads();
     // the CTA that ends last clears the claims for the next call and sums the statistics
     const bool stats = kOp != kTokLogp && a.stats;
     if (!stats && a.n <= (int64_t)(gridDim.x / C) * sh.batch) return;
-    __shared__ bool last;
-    if (tid == 0) {
-        __threadfence();
-        last = atomicInc(a.ticket, gridDim.x - 1) == gridDim.x - 1;   // back at 0 for the next call
-    }
-    __syncthreads();
-    if (!last) return;
+    if (!last_of(a.ticket, gridDim.x)) return;
     if (tid == 0) *a.claims = 0ull;
     if (stats) sum_rows<kOp, kThreads>(a);
 }
@@ -612,7 +564,7 @@ __global__ void __launch_bounds__(kConsumers) token_pair_grad_kernel(TokenArgs a
         for (int u = 0; u < kPer; ++u) {
             const int j = (v0 + tid + u * kConsumers) * W - h;
             q[u] = Elt<T>::none();
-            if (r.live == 0 || j >= a.V) continue;
+            if (r.inv_s == 0.f || j >= a.V) continue;
             if (zo == 0 && j >= 0 && j + W <= a.V) {
                 q[u] = __ldcs(reinterpret_cast<const uint4*>(z + j));
             } else {
@@ -631,7 +583,7 @@ __global__ void __launch_bounds__(kConsumers) token_pair_grad_kernel(TokenArgs a
             emit<T, false>(q[u], c, a.k, v);
             if ((unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
             uint4 out = Elt<T>::pack(v);
-            if (r.live == 0) out = make_uint4(0, 0, 0, 0);
+            if (r.inv_s == 0.f) out = make_uint4(0, 0, 0, 0);
             if (j >= 0 && j + W <= a.V) __stcs(reinterpret_cast<uint4*>(g + j), out);
             else store_part(g + j, j, a.V, out);
         }

@@ -1,0 +1,193 @@
+// Losses of token policies, short rows (up to 8 KB): a row is held in registers by G lanes
+// of a warp, N vectors of 16 bytes each, read once and its gradient written from there.
+// No barrier and no shared memory: the lanes exchange maximum and sums by shuffles.
+// Bound by memory from about 1 KB a row on (an SM's warps hold up to 128 KB in flight);
+// rows of a few entries by instructions, of which the row's loss takes more than its
+// entries: a row of 15 takes 8 lanes, so that a warp computes four rows' losses at once.
+// The rows' shares of the statistics are summed by the lanes that take them, a fixed set
+// of rows each, then by block and call in a fixed order.
+#pragma once
+
+#include "token_common.cuh"
+#include "token_top.cuh"
+
+namespace malib {
+
+namespace {
+
+constexpr int kShortThreads = 128, kShortWarps = kShortThreads / 32;
+
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <class T, int kOp, int G, int N>
+__global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a) {
+    constexpr int W = Elt<T>::W, kRows = 32 / G;     // rows a warp takes at a time
+    constexpr bool kTop = kOp == kTokDistill;
+    static_assert(!kTop || G == 32, "a warp prepares its row's list");
+    extern __shared__ TopEntry lists[];              // [warps][a.top]
+    __shared__ uint32_t seen[kShortWarps][kTop ? 4096 / 32 : 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G;
+    const int64_t step = (int64_t)gridDim.x * kShortWarps * kRows;
+    Totals total{};
+    for (int64_t row0 = ((int64_t)blockIdx.x * kShortWarps + warp) * kRows; row0 < a.n; row0 += step) {
+        const bool in_range = row0 + lane / G < a.n;
+        const int64_t row = in_range ? row0 + lane / G : a.n - 1;
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        T* g = kOp != kTokLogp && a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
+        const int token = kTop ? -1 : a.tokens[row];
+        const bool known = kTop || (token >= 0 && token < a.V);
+        float w = 1.f;
+        TokenRow pair{};
+        PpoRow in{};
+        if (kOp == kTokPpo || kTop) w = a.weight ? a.weight[row] : a.w0;
+        if (kOp == kTokPpo) in = ppo_load(a, row);
+        if (kOp == kTokPairGrad) pair = a.rows[row];
+        const bool read = in_range && w != 0.f && known && (kOp != kTokPairGrad || pair.inv_s != 0.f);
+        if (!kTop && in_range && token >= a.V) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+
+        const int h = (int)(((uintptr_t)z & 15u) / sizeof(T));
+        uint4 q[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int j = (sub + u * G) * W - h;
+            q[u] = Elt<T>::none();
+            if (!read || j >= a.V) continue;
+            q[u] = j >= 0 && j + W <= a.V ? *reinterpret_cast<const uint4*>(z + j) : load_part(z, j, a.V);
+        }
+        float zt = 0.f;
+        if (kOp != kTokPairGrad && !kTop && read) zt = Elt<T>::get(z[token]);
+        TopEntry* list = lists + warp * a.top;
+        TopRow top{};
+        if constexpr (kTop) {
+            if (read) top = top_row<T, 4096>(a, row, z, list, seen[warp]);
+        }
+
+        RowGrad c{0.f, 0.f, 0.f, 0.f};
+        bool live = read;
+        if (kOp == kTokPairGrad) {
+            c = RowGrad{pair.m, -pair.value * pair.inv_s, 0.f, pair.value};
+        } else {
+            RowStat r{group_max<G>(vec_max<T>(q)), 0.f, 0.f};
+            live = r.m != -INFINITY;
+            if (live) gather<T>(r, q, a.k);
+            r.s = group_sum<G>(r.s);
+            r.t = group_sum<G>(r.t);
+            const bool first = sub == 0 && in_range;
+            if (kOp == kTokLogp) {
+                if (first) logp_row(a, row, live, r, zt);
+            } else {
+                RowSum sum{0.f, 0.f, 0.f, 0};
+                float out = 0.f;
+                if (kOp == kTokPpo) {
+                    if (live) {
+                        float loss, clipped, kl, H;
+                        out = log_prob(a, r, zt);
+                        c = ppo_row(a, in, r, out, w, &loss, &clipped, &kl, &H);
+                        sum = RowSum{w * loss, kl, H, clipped != 0.f ? 3 : 1};
+                    }
+                    if (first && a.logp) a.logp[row] = out;
+                } else {
+                    live = live && top.live;
+                    if (live) {
+                        const float f = w * a.gscale * a.top_scale;
+                        out = top_loss(a, r, top);
+                        c = RowGrad{r.m, f / r.s, 0.f, f};
+                        sum = RowSum{w * out, out, 0.f, 1};
+                    }
+                    if (first && a.loss) a.loss[row] = out;
+                }
+                if (first) total.add(sum);
+            }
+        }
+        if (!g) continue;
+        const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int j = (sub + u * G) * W - h;
+            if (!in_range || j >= a.V) continue;
+            F2 v[W / 2] = {};
+            if (live) {
+                emit<T, kOp == kTokPpo>(q[u], c, a.k, v);
+                if (!kTop && (unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
+            }
+            const uint4 out = Elt<T>::pack(v);
+            if (alike && j >= 0 && j + W <= a.V) *reinterpret_cast<uint4*>(g + j) = out;
+            else store_part(g + j, j, a.V, out);
+        }
+        if (kTop) {
+            // the teacher's entries, over what the warp has written
+            __syncwarp();
+            if (live)
+                for (int i = lane; i < a.top; i += 32) {
+                    const TopEntry e = list[i];
+                    if (e.id >= 0) g[e.id] = Elt<T>::put(c.c0 * exp2_fast(x_of(e.z, c.m, a.k)) - c.at * e.q);
+                }
+            __syncwarp();
+        }
+    }
+    if ((kOp != kTokPpo && !kTop) || !a.stats) return;
+    total = block_totals<kShortThreads>(total);
+    if (threadIdx.x == 0) a.part[blockIdx.x] = total;
+    if (!last_of(a.ticket, gridDim.x)) return;
+    Totals v{};
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kShortThreads) v.add(a.part[i]);
+    v = block_totals<kShortThreads>(v);
+    if (threadIdx.x == 0) write_stats<kOp>(a, v);
+}
+
+template <class T, int kOp, int G, int N>
+cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    const int64_t rows = kShortWarps * (32 / G);     // rows of a block at a time
+    int64_t grid = (a.n + rows - 1) / rows;
+    // a few blocks more than an SM holds at once even out the shares
+    if (grid > 24 * (int64_t)n_sm) grid = 24 * (int64_t)n_sm;
+    if (grid > kTokenMaxCtas) grid = kTokenMaxCtas;
+    if (grid < 1) grid = 1;
+    const size_t bytes = kOp == kTokDistill ? (size_t)kShortWarps * a.top * sizeof(TopEntry) : 0;
+    if (bytes > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(token_short_kernel<T, kOp, G, N>,
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   kShortWarps * kTokenMaxTop * (int)sizeof(TopEntry));
+        if (e != cudaSuccess) return e;
+    }
+    token_short_kernel<T, kOp, G, N><<<(unsigned)grid, kShortThreads, bytes, s>>>(a);
+    return cudaGetLastError();
+}
+
+// Lanes a row and vectors a lane by the most vectors a row has.
+template <class T, int kOp>
+cudaError_t launch_short_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    const int nv = (a.V + 2 * Elt<T>::W - 2) / Elt<T>::W;
+    if constexpr (kOp != kTokDistill) {
+        if (nv <= 4) return launch_short<T, kOp, 4, 1>(a, n_sm, s);
+        if (nv <= 8) return launch_short<T, kOp, 8, 1>(a, n_sm, s);
+    }
+    if (nv <= 32) return launch_short<T, kOp, 32, 1>(a, n_sm, s);
+    if (nv <= 64) return launch_short<T, kOp, 32, 2>(a, n_sm, s);
+    if (nv <= 128) return launch_short<T, kOp, 32, 4>(a, n_sm, s);
+    if (nv <= 256) return launch_short<T, kOp, 32, 8>(a, n_sm, s);
+    return launch_short<T, kOp, 32, 16>(a, n_sm, s);
+}
+
+template <class T>
+cudaError_t launch_short_type(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    if (op == kTokLogp) return launch_short_op<T, kTokLogp>(a, n_sm, s);
+    if (op == kTokPpo) return launch_short_op<T, kTokPpo>(a, n_sm, s);
+    if (op == kTokDistill) return launch_short_op<T, kTokDistill>(a, n_sm, s);
+    return launch_short_op<T, kTokPairGrad>(a, n_sm, s);
+}
+
+}  // namespace
+
+}  // namespace malib

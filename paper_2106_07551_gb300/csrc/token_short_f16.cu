@@ -1,0 +1,10 @@
+// Short rows of f16 logits.
+#include "token_short.cuh"
+
+namespace malib {
+
+cudaError_t launch_token_short_f16(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    return launch_short_type<__half>(a, op, n_sm, s);
+}
+
+}  // namespace malib

@@ -40,10 +40,9 @@ __device__ __forceinline__ float warp_max_nan(float v) {
 // a.top entries. Teacher logits of -infinity are absent. The q of an id that is listed
 // more than once are added, in the list's order, at its first place: places are looked
 // for where a bit of the id's low bits has been seen, 32 entries at a time.
-template <class T>
-__device__ __forceinline__ TopRow top_row(const TokenArgs& a, int64_t row, const T* z, TopEntry* list) {
-    constexpr int kBits = 32768;
-    __shared__ uint32_t seen[kBits / 32];
+template <class T, int kBits>
+__device__ __forceinline__ TopRow top_row(const TokenArgs& a, int64_t row, const T* z, TopEntry* list,
+                                          uint32_t (&seen)[kBits / 32]) {
     const int lane = threadIdx.x & 31;
     for (int i = lane; i < kBits / 32; i += 32) seen[i] = 0u;
     __syncwarp();
@@ -123,12 +122,6 @@ __device__ __forceinline__ float top_loss(const TokenArgs& a, const RowStat& r, 
     // sum q ln p = sum q (z - zr) / T + ((zr - m) / T - ln S) sum q
     const float lp = fmaf(log_prob(a, r, t.zr), t.q, t.zq);
     return a.tt * (t.h - lp);
-}
-
-__device__ __forceinline__ void distill_stats(const TokenArgs& a, const double (&v)[kTokenStats]) {
-    a.stats[0] = (float)v[0];
-    a.stats[1] = (float)v[1];
-    a.stats[2] = (float)(v[2] / (v[0] > 0.0 ? v[0] : 1.0));
 }
 
 }  // namespace malib

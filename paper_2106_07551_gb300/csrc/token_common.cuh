@@ -443,7 +443,7 @@ struct Sum2 {
     }
 };
 // The statistics of rows: policy loss: KL and H in x, y; distillation: l in x.
-struct Totals {
+struct __align__(16) Totals {
     int32_t rows, clipped;
     Sum2 loss, x, y;
     __device__ __forceinline__ void add(const RowSum& r) {
@@ -480,6 +480,28 @@ __device__ __forceinline__ Totals block_totals(Totals v) {
     if (threadIdx.x == 0)
         for (int w = 1; w < kThreads / 32; ++w) v.add(part[w]);
     return v;
+}
+// The sum of the blocks' totals part[0 .. n), in thread 0 of the calling block.
+template <int kThreads>
+__device__ __forceinline__ Totals sum_parts(const Totals* part, int n) {
+    static_assert(sizeof(Totals) == 32, "two 16-byte loads");
+    Totals v{};
+    constexpr int kAt = 4;                           // of two loads each, in flight
+    for (int i0 = threadIdx.x; i0 < n; i0 += kAt * kThreads) {
+        int4 q[kAt][2];
+#pragma unroll
+        for (int u = 0; u < kAt; ++u)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                q[u][k] = i0 + u * kThreads < n ? __ldcg(reinterpret_cast<const int4*>(part + i0 + u * kThreads) + k)
+                                                : make_int4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < kAt; ++u)
+            v.add(Totals{q[u][0].x, q[u][0].y, Sum2{__int_as_float(q[u][0].z), __int_as_float(q[u][0].w)},
+                         Sum2{__int_as_float(q[u][1].x), __int_as_float(q[u][1].y)},
+                         Sum2{__int_as_float(q[u][1].z), __int_as_float(q[u][1].w)}});
+    }
+    return block_totals<kThreads>(v);
 }
 template <int kOp>
 __device__ __forceinline__ void write_stats(const TokenArgs& a, const Totals& v) {

@@ -67,9 +67,7 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     if (!a.stats) return;
     if (threadIdx.x == 0) a.part[blockIdx.x] = total;
     if (!last_of(a.ticket, gridDim.x)) return;
-    Totals v{};
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += kPairT) v.add(a.part[i]);
-    v = block_totals<kPairT>(v);
+    const Totals v = sum_parts<kPairT>(a.part, (int)gridDim.x);
     if (threadIdx.x != 0) return;
     const double n = (double)a.n_pairs;
     a.stats[0] = (float)a.n_pairs;

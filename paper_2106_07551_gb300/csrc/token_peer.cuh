@@ -1,4 +1,4 @@
-// Clusters: rank, barrier, stores to and arrivals at a peer's shared memory. Only for
+// Clusters: rank, barrier, stores to a peer's shared memory. Only for
 // launches with a cluster dimension: without one these stores are illegal instructions.
 #pragma once
 
@@ -22,14 +22,6 @@ __device__ __forceinline__ void peer_store(void* dst, uint64_t* bar, uint32_t ra
         " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [d], {%3, %4, %5, %6}, [b];\n}" ::"r"(
             smem_u32(dst)),
         "r"(smem_u32(bar)), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
-        : "memory");
-}
-
-// An arrival on CTA `rank`'s barrier; what this thread has done goes before it.
-__device__ __forceinline__ void peer_arrive(uint64_t* bar, uint32_t rank) {
-    asm volatile(
-        "{\n .reg .b32 b;\n mapa.shared::cluster.u32 b, %0, %1;\n"
-        " mbarrier.arrive.release.cluster.shared::cluster.b64 _, [b];\n}" ::"r"(smem_u32(bar)), "r"(rank)
         : "memory");
 }
 

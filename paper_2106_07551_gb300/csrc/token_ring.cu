@@ -14,9 +14,8 @@
 //
 // Rows are claimed, not dealt: SMs do not all get the same share of the memory's rate, and
 // rows that are left out cost a write and no read; with a fixed share each, SMs stood
-// idle for 10 to 20% of a call. The producer of the cluster's first CTA claims a row ahead
-// (an atomic counter), reads its token and weight, and puts it into every CTA's queue of
-// kQueue rows. What a row adds to the statistics is stored by itself and summed in the
+// idle for 10 to 20% of a call. The producer claims a row ahead (an atomic counter), reads
+// its token and weight, and puts it into the CTA's queue. What a row adds to the statistics is stored by itself and summed in the
 // rows' order at the end, so that a call's results do not depend on who took what.
 //
 // Bound by memory: the rings of two CTAs an SM hold 2 x 96 KB in flight or in work, and
@@ -29,8 +28,6 @@
 //
 // Every wait is bounded, between the warps too: one that expires ends the CTA's work and
 // is reported as MALIB_ETIMEOUT.
-#include <mutex>
-
 #include "token_common.cuh"
 #include "token_peer.cuh"
 #include "token_top.cuh"
@@ -79,6 +76,7 @@ struct Shape {
     int slice;                                       // vectors of a CTA's slice
     int keep;                                        // stages that hold parts of a row for its second sweep
     int queue_log, batch;                            // rows known ahead (log 2), rows a claim takes
+    int single;                                      // the grid has a CTA, or a cluster, for every row
 };
 
 // Sixteen bytes of shared memory from a byte offset that need not be a multiple of 16.
@@ -199,11 +197,11 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages];
     // per queued row: known, no longer needed; per row that is read: the warps' statistics
     // are there, the CTAs', the result, the written slice
-    __shared__ __align__(8) uint64_t qfull[kQueue], qempty[kQueue], sfull[kQueue], xfull[kQueue], rfull[kQueue],
-        pfull[kQueue];
+    __shared__ __align__(8) uint64_t qfull[kQueue], qempty[kQueue], sfull[kQueue], rfull[kQueue], pfull[kQueue],
+        xfull;
     __shared__ __align__(8) uint64_t tfull[2], tempty[2];
     __shared__ Queued queue[kQueue];
-    __shared__ Partial red[kQueue][kConsumerWarps], xslot[kQueue][kMaxCluster];
+    __shared__ Partial red[kQueue][kConsumerWarps], xslot[kMaxCluster];
     __shared__ RowOut rout[kQueue];
     constexpr int kSeen = kTop ? 32768 : 32;
     __shared__ uint32_t seen[kSeen / 32];
@@ -222,12 +220,12 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
         }
         for (int i = 0; i < kQueue; ++i) {
             mbar_init(&qfull[i], 1);
-            mbar_init(&qempty[i], C * (kThreads / 32));
+            mbar_init(&qempty[i], kThreads / 32);
             mbar_init(&sfull[i], kConsumerWarps);
-            mbar_init(&xfull[i], 1);
             mbar_init(&rfull[i], 1);
             mbar_init(&pfull[i], kConsumerWarps);
         }
+        mbar_init(&xfull, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&tfull[i], 1);
             mbar_init(&tempty[i], kConsumerWarps);
@@ -235,11 +233,14 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
         fence_proxy_async_smem();
     }
     __syncthreads();
-    if (C > 1) {
-        // the peers' barriers and memory are there before the first store to them
-        cluster_arrive();
-        cluster_wait();
-    }
+    // The peers' barriers and memory are there before the first store to them: arrived here,
+    // waited for where it is needed.
+    if (C > 1) cluster_arrive();
+    bool joined = C == 1;
+    auto join = [&] {
+        if (!joined) cluster_wait();
+        joined = true;
+    };
     volatile int* gone = &dead;
     auto expired = [&] {
         *gone = 1;
@@ -249,73 +250,65 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
         if (mbar_try_wait(bar, parity) || *gone) return;
         if (!mbar_wait_bounded(bar, parity, kWaitLimitNs)) expired();
     };
-    auto wait_peers = [&](uint64_t* bar, uint32_t parity) {
-        if (!*gone && !peer_wait_bounded(bar, parity, kWaitLimitNs)) expired();
-    };
     auto slot_of = [&](uint32_t t) { return t & ((1u << sh.queue_log) - 1u); };
     auto parity_of = [&](uint32_t t) { return t >> sh.queue_log & 1u; };
-    // Turn t's row, as every warp of the cluster sees it; row < 0: there is none.
+    // A row's token and weight (row < a.n).
+    auto look = [&](int64_t row) {
+        Queued q{row, kTop ? 0 : a.tokens[row], 1.f};
+        if (kOp != kTokLogp) q.w = a.weight ? a.weight[row] : a.w0;
+        return q;
+    };
+    auto settle = [&](Queued& q, bool report) {
+        if (q.token >= a.V && report) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        if (q.token >= a.V || q.w == 0.f) q.token = -1;
+    };
+    // Turn t's row, as every warp sees it; row < 0: there is none.
     auto take = [&](uint32_t t) {
-        if (C > 1) wait_peers(&qfull[slot_of(t)], parity_of(t));
-        else wait(&qfull[slot_of(t)], parity_of(t));
-        Queued q = queue[slot_of(t)];
-        if (*gone) q.row = -1;
+        Queued q{-1, -1, 0.f};
+        if (sh.single) {
+            if (t > 0) return q;
+            q = look(blockIdx.x / C);
+            settle(q, rank == 0 && tid == 0);
+            return q;
+        }
+        wait(&qfull[slot_of(t)], parity_of(t));
+        if (!*gone) q = queue[slot_of(t)];
         return q;
     };
     // The warp needs nothing of turn t any more.
     auto leave = [&](uint32_t t) {
         __syncwarp();
-        if (lane != 0) return;
-        if (C > 1) peer_arrive(&qempty[slot_of(t)], 0);
-        else mbar_arrive_release(&qempty[slot_of(t)]);
+        if (lane == 0) mbar_arrive_release(&qempty[slot_of(t)]);
     };
 
     if (warp == kConsumerWarps) {
         // ---- producer
-        // rank 0: a batch of claimed rows, lane i with the i-th row's token and weight. The
-        // next one is claimed (lane 0) when the batch's last row is sent, and looked at when
-        // that row's copies are under way: neither is waited for where it is asked for, and
-        // no cluster holds rows that another could start on.
-        const int64_t clusters = gridDim.x / C;
-        const bool claims = a.n > clusters * sh.batch;               // else there is a batch for every row
-        int64_t batch = (int64_t)(blockIdx.x / C) * sh.batch;
-        int used = 0, token = -1;
-        float w = 1.f;
-        auto look = [&] {
-            token = -1;
-            if (lane >= sh.batch || batch + lane >= a.n) return;
-            token = kTop ? 0 : a.tokens[batch + lane];
-            if (kOp != kTokLogp) w = a.weight ? a.weight[batch + lane] : a.w0;
+        // A batch of claimed rows, lane i with the i-th row's token and weight. The next one is
+        // claimed (lane 0) when the batch's last row is queued, and looked at when that row's
+        // copies are under way: neither is waited for where it is asked for, and no CTA holds
+        // rows that another could start on.
+        int64_t batch = (int64_t)blockIdx.x * sh.batch;
+        int used = 0;
+        Queued mine{-1, -1, 0.f};
+        auto look_batch = [&] {
+            if (lane < sh.batch && batch + lane < a.n) mine = look(batch + lane);
         };
-        if (rank == 0) look();
+        if (!sh.single) look_batch();
         Cursor at, issued;
         bool wrapped = false;
         for (uint32_t t = 0;; ++t) {
-            const int slot = slot_of(t);
-            // the cluster's instructions only in launches with clusters
-            if (C > 1 && lane == 0) mbar_arrive_expect_tx(&qfull[slot], sizeof(Queued));
-            if (rank == 0) {
-                Queued q{batch + used < a.n ? batch + used : -1, __shfl_sync(0xffffffffu, token, used),
-                         __shfl_sync(0xffffffffu, w, used)};
-                if (q.token >= a.V && lane == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
-                if (q.token >= a.V || q.w == 0.f) q.token = -1;
-                if (C > 1) {
-                    wait_peers(&qempty[slot], parity_of(t) ^ 1u);
-                    if (lane < C)
-                        peer_store(&queue[slot], &qfull[slot], lane,
-                                   make_float4(__int_as_float((int)(uint32_t)q.row), __int_as_float((int)(q.row >> 32)),
-                                               __int_as_float(q.token), q.w));
-                } else {
-                    wait(&qempty[slot], parity_of(t) ^ 1u);
-                    if (lane == 0) {
-                        queue[slot] = q;
-                        mbar_arrive_release(&qfull[slot]);
-                    }
+            if (!sh.single) {
+                const int slot = slot_of(t);
+                Queued q{batch + used < a.n ? batch + used : -1, __shfl_sync(0xffffffffu, mine.token, used),
+                         __shfl_sync(0xffffffffu, mine.w, used)};
+                if (q.row >= 0) settle(q, lane == 0);
+                wait(&qempty[slot], parity_of(t) ^ 1u);
+                if (lane == 0) {
+                    queue[slot] = q;
+                    mbar_arrive_release(&qfull[slot]);
                 }
-                if (++used == sh.batch) {
-                    if (!claims) batch = a.n;
-                    else if (lane == 0) batch = clusters * sh.batch + (int64_t)atomicAdd(a.claims, (unsigned long long)sh.batch);
-                }
+                if (++used == sh.batch && lane == 0)
+                    batch = (int64_t)gridDim.x * sh.batch + (int64_t)atomicAdd(a.claims, (unsigned long long)sh.batch);
             }
             const Queued q = take(t);
             if (q.row < 0) break;
@@ -349,10 +342,10 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                     __syncwarp();
                 }
             }
-            if (rank == 0 && used == sh.batch) {
+            if (!sh.single && used == sh.batch) {
                 used = 0;
                 batch = __shfl_sync(0xffffffffu, batch, 0);
-                look();
+                look_batch();
             }
             leave(t);
         }
@@ -450,10 +443,11 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                 if (C > 1) {
                     // The logits that the loss takes (zt, the teacher's entries) have been read
                     // before any CTA of the row writes its part: they go before these sums.
-                    if (lane == 0) mbar_arrive_expect_tx(&xfull[slot], (uint32_t)(C * sizeof(Partial)));
-                    if (lane < C) peer_store(&xslot[slot][rank], &xfull[slot], lane, make_float4(r.m, r.s, r.t, zt));
-                    wait_peers(&xfull[slot], parity);
-                    const Partial& px = xslot[slot][lane & (kMaxCluster - 1)];
+                    join();
+                    if (lane == 0) mbar_arrive_expect_tx(&xfull, (uint32_t)(C * sizeof(Partial)));
+                    if (lane < C) peer_store(&xslot[rank], &xfull, lane, make_float4(r.m, r.s, r.t, zt));
+                    if (!*gone && !peer_wait_bounded(&xfull, 0, kWaitLimitNs)) expired();
+                    const Partial& px = xslot[lane & (kMaxCluster - 1)];
                     r = reduce_stat<kMaxCluster>(
                         lane % kMaxCluster < C ? RowStat{px.m, px.s, px.t} : RowStat{-INFINITY, 0.f, 0.f}, a.k);
                 }
@@ -529,6 +523,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
             leave(t);
         }
     }
+    join();
     if (C > 1) {
         // no CTA leaves while a peer may still store to it
         cluster_arrive();
@@ -536,7 +531,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
     }
     // the CTA that ends last clears the claims for the next call and sums the statistics
     const bool stats = kOp != kTokLogp && a.stats;
-    if (!stats && a.n <= (int64_t)(gridDim.x / C) * sh.batch) return;
+    if (!stats && sh.single) return;
     if (!last_of(a.ticket, gridDim.x)) return;
     if (tid == 0) *a.claims = 0ull;
     if (stats) sum_rows<kOp, kThreads>(a);
@@ -591,60 +586,31 @@ __global__ void __launch_bounds__(kConsumers) token_pair_grad_kernel(TokenArgs a
 }
 
 template <class T, int kOp>
-cudaError_t launch_ring(const TokenArgs& a, Shape sh, int per_sm, int n_sm, cudaStream_t s) {
-    const void* f = (const void*)token_ring_kernel<T, kOp>;
-    const int bytes = sh.stages * kStageBytes + (kOp == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0);
-    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingTwo);
+cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int grid, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(token_ring_kernel<T, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingTwo);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
+    cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kConsumers + (kOp == kTokDistill ? 64 : 32));
-    cfg.dynamicSmemBytes = bytes;
+    cfg.dynamicSmemBytes = sh.stages * kStageBytes + (kOp == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0);
     cfg.stream = s;
-    int64_t clusters = (int64_t)per_sm * n_sm;
     if (sh.cluster > 1) {
         at.id = cudaLaunchAttributeClusterDimension;
         at.val.clusterDim.x = sh.cluster;
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        // Clusters lie within a part of the device: fewer fit than the SMs' number says.
-        // How many, asked once per device, cluster and stages (lists that take less than a
-        // stage more do not change what fits).
-        static std::mutex mu;
-        static int held[3][kMaxCluster + 1][kMaxStages + 1];
-        static int held_dev = -1;
-        int dev = 0;
-        if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-        std::lock_guard<std::mutex> lock(mu);
-        if (held_dev != dev) {
-            for (auto& x : held)
-                for (auto& y : x)
-                    for (int& q : y) q = 0;
-            held_dev = dev;
-        }
-        int& n = held[per_sm - 1][sh.cluster][sh.stages];
-        if (n == 0) {
-            cfg.gridDim = dim3(sh.cluster);
-            if ((e = cudaOccupancyMaxActiveClusters(&n, f, &cfg)) != cudaSuccess) return e;
-            if (n < 1) n = 1;
-        }
-        clusters = n;
     }
-    if (clusters > a.n) clusters = a.n;
-    // a claim leaves every cluster several more
-    if (sh.batch > a.n / (4 * clusters)) sh.batch = (int)(a.n / (4 * clusters));
-    if (sh.batch < 1) sh.batch = 1;
-    cfg.gridDim = dim3((unsigned)(clusters * sh.cluster));
     e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp>, a, sh);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <class T>
-cudaError_t launch_ring_t(const TokenArgs& a, int op, const Shape& sh, int per_sm, int n_sm, cudaStream_t s) {
-    if (op == kTokLogp) return launch_ring<T, kTokLogp>(a, sh, per_sm, n_sm, s);
-    if (op == kTokPpo) return launch_ring<T, kTokPpo>(a, sh, per_sm, n_sm, s);
-    return launch_ring<T, kTokDistill>(a, sh, per_sm, n_sm, s);
+cudaError_t launch_ring_t(const TokenArgs& a, int op, const Shape& sh, int grid, cudaStream_t s) {
+    if (op == kTokLogp) return launch_ring<T, kTokLogp>(a, sh, grid, s);
+    if (op == kTokPpo) return launch_ring<T, kTokPpo>(a, sh, grid, s);
+    return launch_ring<T, kTokDistill>(a, sh, grid, s);
 }
 
 }  // namespace
@@ -653,23 +619,38 @@ cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
     const int64_t nv = (a.V + 2 * (int64_t)W - 2) / W;               // most vectors of a row
     const int lists = op == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0;
-    const int per_sm = op == kTokLogp ? 3 : 2;
-    Shape sh{1, op == kTokLogp ? 4 : (kRingTwo - lists) / kStageBytes, 0, 0, 0, 1};
+    const int held = (op == kTokLogp ? 3 : 2) * n_sm;                // CTAs the device holds
+    Shape sh{1, op == kTokLogp ? 4 : (kRingTwo - lists) / kStageBytes, 0, 0, 0, 1, 0};
     auto slice = [&](int c) { return (nv + c - 1) / c; };
-    // Few rows: more CTAs a row, down to half a stage a slice.
-    while (sh.cluster < kMaxCluster && a.n * sh.cluster * 2 <= (int64_t)per_sm * n_sm &&
-           slice(sh.cluster * 2) >= kStageVecs / 2)
-        sh.cluster *= 2;
+    // CTAs a row: the rounds that the device takes over the rows, times the bytes that a CTA
+    // moves in one and what it costs besides (about 4 us, the time of 80 KB). In us, C = 1
+    // and the C taken: ppo 25 x 32,768 bf16 20 and 12 (8), distillation 333 x 151,111 fp32
+    // 126 and 97 (4); 333 x 32,768 bf16 rows' statistics stay at C = 1, 11, with 4 20.
+    const int64_t bytes = a.V * (int64_t)(16 / W) * (op == kTokLogp ? 1 : 2);
+    int64_t best = 0;
+    for (int c = 1; c <= kMaxCluster && (c == 1 || slice(c) >= kStageVecs / 2); c *= 2) {
+        const int64_t t = (a.n * c + held - 1) / held * (80 * 1024 + bytes / c);
+        if (c > 1 && t >= best) continue;
+        best = t;
+        sh.cluster = c;
+    }
     sh.slice = (int)slice(sh.cluster);
     sh.keep = sh.slice <= (sh.stages - 1) * kStageVecs ? sh.stages - 1 : sh.stages - 2;
+    // A cluster takes one row, as does a CTA when there are no more rows than CTAs.
+    sh.single = sh.cluster > 1 || a.n <= held;
+    const int64_t grid = sh.single ? a.n * sh.cluster : held;
     // Rows of a stage or more are claimed one by one and known one ahead, so that no CTA holds
-    // several while others run out; short ones in batches of about two stages.
+    // several while others run out; short ones in batches of about two stages, as long as
+    // there are several for every CTA.
     sh.queue_log = sh.slice >= kStageVecs ? 1 : 2;
-    sh.batch = sh.slice >= kStageVecs ? 1 : 2 * kStageVecs / sh.slice;
-    if (sh.batch > 16) sh.batch = 16;
-    if (a.dtype == MALIB_F32) return launch_ring_t<float>(a, op, sh, per_sm, n_sm, s);
-    if (a.dtype == MALIB_BF16) return launch_ring_t<__nv_bfloat16>(a, op, sh, per_sm, n_sm, s);
-    return launch_ring_t<__half>(a, op, sh, per_sm, n_sm, s);
+    if (sh.slice < kStageVecs && !sh.single) {
+        const int64_t most = a.n / (4 * grid), about = 2 * kStageVecs / sh.slice;
+        sh.batch = (int)(most < 1 ? 1 : most < about ? most : about);
+        if (sh.batch > 16) sh.batch = 16;
+    }
+    if (a.dtype == MALIB_F32) return launch_ring_t<float>(a, op, sh, (int)grid, s);
+    if (a.dtype == MALIB_BF16) return launch_ring_t<__nv_bfloat16>(a, op, sh, (int)grid, s);
+    return launch_ring_t<__half>(a, op, sh, (int)grid, s);
 }
 
 cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s) {

@@ -2,8 +2,9 @@
 // of a warp, N vectors of 16 bytes each, read once and its gradient written from there.
 // No barrier and no shared memory: the lanes exchange maximum and sums by shuffles.
 // Bound by memory from about 1 KB a row on (an SM's warps hold up to 128 KB in flight);
-// rows of a few entries by instructions, of which the row's loss takes more than its
-// entries: a row of 15 takes 8 lanes, so that a warp computes four rows' losses at once.
+// shorter ones by instructions, of which the row's loss takes more than its entries: rows
+// of up to 8 vectors take 8 lanes, so that a warp computes four rows' losses at once, and
+// rows of a few entries one lane each.
 // The rows' shares of the statistics are summed by the lanes that take them, a fixed set
 // of rows each, then by block and call in a fixed order.
 #pragma once
@@ -28,6 +29,24 @@ __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
     for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
+}
+
+// The call's statistics from its threads' sums: by block, then in the block that ends last.
+template <int kOp>
+__device__ __forceinline__ void finish_short(const TokenArgs& a, Totals total) {
+    total = block_totals<kShortThreads>(total);
+    if (threadIdx.x == 0) a.part[blockIdx.x] = total;
+    if (!last_of(a.ticket, gridDim.x)) return;
+    const Totals v = sum_parts<kShortThreads>(a.part, (int)gridDim.x);
+    if (threadIdx.x == 0) write_stats<kOp>(a, v);
+}
+
+// Blocks of `rows` rows at a time; a few more than the SMs hold at once even out the shares.
+inline unsigned short_grid(int64_t n, int64_t rows, int n_sm) {
+    int64_t grid = (n + rows - 1) / rows;
+    if (grid > 24 * (int64_t)n_sm) grid = 24 * (int64_t)n_sm;
+    if (grid > kTokenMaxCtas) grid = kTokenMaxCtas;
+    return (unsigned)(grid < 1 ? 1 : grid);
 }
 
 template <class T, int kOp, int G, int N>
@@ -136,24 +155,118 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
             __syncwarp();
         }
     }
-    if ((kOp != kTokPpo && !kTop) || !a.stats) return;
-    total = block_totals<kShortThreads>(total);
-    if (threadIdx.x == 0) a.part[blockIdx.x] = total;
-    if (!last_of(a.ticket, gridDim.x)) return;
-    Totals v{};
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += kShortThreads) v.add(a.part[i]);
-    v = block_totals<kShortThreads>(v);
-    if (threadIdx.x == 0) write_stats<kOp>(a, v);
+    if ((kOp == kTokPpo || kTop) && a.stats) finish_short<kOp>(a, total);
+}
+
+// Rows of up to N <= 32 entries (the actions of the environments): a thread a row, so that
+// its loss is computed once and not by every lane of a group. Rows that follow one another
+// without a gap go through shared memory, so that neighbouring threads read and write
+// neighbouring entries; others entry by entry. Bound by the launch and by instructions:
+// 102,400 rows of 15 fp32 entries with every term of the policy loss take 26 us with 8
+// lanes a row, 18 with a thread a row whose entries it reads itself.
+template <class T, int kOp, int N>
+__global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) {
+    __shared__ T tile[kShortThreads * N];
+    const int tid = threadIdx.x;
+    const bool flat_z = a.ld == a.V, flat_g = a.gld == a.V;
+    Totals total{};
+    for (int64_t row0 = (int64_t)blockIdx.x * kShortThreads; row0 < a.n; row0 += (int64_t)gridDim.x * kShortThreads) {
+        const int rows = (int)min((int64_t)kShortThreads, a.n - row0), entries = rows * a.V;
+        const bool in_range = tid < rows;
+        const int64_t row = row0 + (in_range ? tid : 0);
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        T* g = kOp != kTokLogp && a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
+        if (flat_z) {
+            const T* first = static_cast<const T*>(a.z) + row0 * a.V;
+#pragma unroll 8
+            for (int e = tid; e < entries; e += kShortThreads) tile[e] = first[e];
+        }
+        const int token = in_range ? a.tokens[row] : -1;
+        float w = 1.f;
+        TokenRow pair{};
+        PpoRow in{};
+        if (kOp == kTokPpo) {
+            w = a.weight ? a.weight[row] : a.w0;
+            in = ppo_load(a, row);
+        }
+        if (kOp == kTokPairGrad) pair = a.rows[row];
+        const bool read = w != 0.f && token >= 0 && token < a.V && (kOp != kTokPairGrad || pair.inv_s != 0.f);
+        if (token >= a.V) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        float v[N];
+        if (flat_z) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = read && j < a.V ? Elt<T>::get(tile[tid * a.V + j]) : -INFINITY;
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = read && j < a.V ? Elt<T>::get(z[j]) : -INFINITY;
+        }
+        RowGrad c{0.f, 0.f, 0.f, 0.f};
+        bool live = read;
+        if (kOp == kTokPairGrad) {
+            c = RowGrad{pair.m, -pair.value * pair.inv_s, 0.f, pair.value};
+        } else {
+            RowStat r{v[0], 0.f, 0.f};
+            float zt = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                r.m = max_nan(r.m, v[j]);
+                if (j == token) zt = v[j];
+            }
+            live = r.m != -INFINITY;
+            if (live) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float x = x_of(v[j], r.m, a.k), e = exp2_fast(x);
+                    r.s += e;
+                    r.t = fmaf(e, fmaxf(x, kXMin), r.t);
+                }
+            }
+            if (kOp == kTokLogp) {
+                if (in_range) logp_row(a, row, live, r, zt);
+            } else {
+                float logp = 0.f;
+                if (live) {
+                    float loss, clipped, kl, H;
+                    logp = log_prob(a, r, zt);
+                    c = ppo_row(a, in, r, logp, w, &loss, &clipped, &kl, &H);
+                    total.add(RowSum{w * loss, kl, H, clipped != 0.f ? 3 : 1});
+                }
+                if (a.logp && in_range) a.logp[row] = logp;
+            }
+        }
+        if (!g) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (j >= a.V || !in_range) break;
+            float f = 0.f;
+            if (live) {
+                const float x = x_of(v[j], c.m, a.k);
+                f = exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
+                if (j == token) f += c.at;
+            }
+            if (flat_g) tile[tid * a.V + j] = Elt<T>::put(f);
+            else g[j] = Elt<T>::put(f);
+        }
+        if (flat_g) {
+            T* first = static_cast<T*>(a.g) + row0 * a.V;
+            __syncthreads();
+            for (int e = tid; e < entries; e += kShortThreads) first[e] = tile[e];
+            __syncthreads();
+        }
+    }
+    if (kOp == kTokPpo && a.stats) finish_short<kOp>(a, total);
+}
+
+template <class T, int kOp, int N>
+cudaError_t launch_tiny(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    token_tiny_kernel<T, kOp, N><<<short_grid(a.n, kShortThreads, n_sm), kShortThreads, 0, s>>>(a);
+    return cudaGetLastError();
 }
 
 template <class T, int kOp, int G, int N>
 cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
-    const int64_t rows = kShortWarps * (32 / G);     // rows of a block at a time
-    int64_t grid = (a.n + rows - 1) / rows;
-    // a few blocks more than an SM holds at once even out the shares
-    if (grid > 24 * (int64_t)n_sm) grid = 24 * (int64_t)n_sm;
-    if (grid > kTokenMaxCtas) grid = kTokenMaxCtas;
-    if (grid < 1) grid = 1;
     const size_t bytes = kOp == kTokDistill ? (size_t)kShortWarps * a.top * sizeof(TopEntry) : 0;
     if (bytes > 0) {
         const cudaError_t e = cudaFuncSetAttribute(token_short_kernel<T, kOp, G, N>,
@@ -161,7 +274,7 @@ cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
                                                    kShortWarps * kTokenMaxTop * (int)sizeof(TopEntry));
         if (e != cudaSuccess) return e;
     }
-    token_short_kernel<T, kOp, G, N><<<(unsigned)grid, kShortThreads, bytes, s>>>(a);
+    token_short_kernel<T, kOp, G, N><<<short_grid(a.n, kShortWarps * (32 / G), n_sm), kShortThreads, bytes, s>>>(a);
     return cudaGetLastError();
 }
 
@@ -170,7 +283,9 @@ template <class T, int kOp>
 cudaError_t launch_short_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
     const int nv = (a.V + 2 * Elt<T>::W - 2) / Elt<T>::W;
     if constexpr (kOp != kTokDistill) {
-        if (nv <= 4) return launch_short<T, kOp, 4, 1>(a, n_sm, s);
+        if (a.V <= 8) return launch_tiny<T, kOp, 8>(a, n_sm, s);
+        if (a.V <= 16) return launch_tiny<T, kOp, 16>(a, n_sm, s);
+        if (a.V <= 32) return launch_tiny<T, kOp, 32>(a, n_sm, s);
         if (nv <= 8) return launch_short<T, kOp, 8, 1>(a, n_sm, s);
     }
     if (nv <= 32) return launch_short<T, kOp, 32, 1>(a, n_sm, s);

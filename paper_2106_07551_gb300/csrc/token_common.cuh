@@ -438,9 +438,7 @@ struct Sum2 {
         e = __fadd_rn(e, b.e);
     }
     // an infinite sum has an error that is NaN, and none to speak of
-    __device__ __forceinline__ double value() const {
-        return (double)s + (fabsf(s) < INFINITY ? (double)e : 0.0);
-    }
+    __device__ __forceinline__ float value() const { return fabsf(s) < INFINITY ? __fadd_rn(s, e) : s; }
 };
 // The statistics of rows: policy loss: KL and H in x, y; distillation: l in x.
 struct __align__(16) Totals {
@@ -505,15 +503,15 @@ __device__ __forceinline__ Totals sum_parts(const Totals* part, int n) {
 }
 template <int kOp>
 __device__ __forceinline__ void write_stats(const TokenArgs& a, const Totals& v) {
-    const double M = v.rows > 0 ? (double)v.rows : 1.0;
+    const float M = v.rows > 0 ? (float)v.rows : 1.f;
     a.stats[0] = (float)v.rows;
-    a.stats[1] = (float)v.loss.value();
+    a.stats[1] = v.loss.value();
     if (kOp == kTokPpo) {
-        a.stats[2] = (float)((double)v.clipped / M);
-        a.stats[3] = (float)(v.x.value() / M);
-        a.stats[4] = (float)(v.y.value() / M);
+        a.stats[2] = (float)v.clipped / M;
+        a.stats[3] = v.x.value() / M;
+        a.stats[4] = v.y.value() / M;
     } else {
-        a.stats[2] = (float)(v.x.value() / M);
+        a.stats[2] = v.x.value() / M;
     }
 }
 

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
             for (int q = 0; q < 2; ++q) {
                 Sum2 v = red[q * (kHalf / 32)];
                 for (int i = 1; i < kHalf / 32; ++i) v.add(red[q * (kHalf / 32) + i]);
-                rew[q] = (float)((double)a.beta * v.value());
+                rew[q] = fmaf(a.beta, v.s, a.beta * (fabsf(v.s) < INFINITY ? v.e : 0.f));
                 if (a.reward) a.reward[2 * p + q] = rew[q];
             }
             const float d = rew[0] - rew[1];
@@ -69,12 +69,12 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     if (!last_of(a.ticket, gridDim.x)) return;
     const Totals v = sum_parts<kPairT>(a.part, (int)gridDim.x);
     if (threadIdx.x != 0) return;
-    const double n = (double)a.n_pairs;
-    a.stats[0] = (float)a.n_pairs;
-    a.stats[1] = (float)(v.loss.value() / n);
-    a.stats[2] = (float)((double)v.clipped / n);
-    a.stats[3] = (float)(v.x.value() / n);
-    a.stats[4] = (float)(v.y.value() / n);
+    const float n = (float)a.n_pairs;
+    a.stats[0] = n;
+    a.stats[1] = v.loss.value() / n;
+    a.stats[2] = (float)v.clipped / n;
+    a.stats[3] = v.x.value() / n;
+    a.stats[4] = v.y.value() / n;
 }
 
 bool is_short(const TokenArgs& a) {

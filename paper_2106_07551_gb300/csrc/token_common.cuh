@@ -536,9 +536,10 @@ constexpr int kShortVecs = 512;                      // most 16-byte vectors of 
 cudaError_t launch_token_short_f32(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_short_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_short_f16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
-// Longer ones (token_ring.cu).
-cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
-cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s);
+// Longer ones (token_ring.cuh).
+cudaError_t launch_token_ring_f32(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+cudaError_t launch_token_ring_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
+cudaError_t launch_token_ring_f16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s);
 
 }  // namespace malib

@@ -1,6 +1,7 @@
 // Losses of token policies: which kernel takes a call's rows, and the preference loss of
 // answer pairs between its rows' statistics and their gradients.
 #include "token_common.cuh"
+#include "token_shift.cuh"
 
 namespace malib {
 
@@ -77,6 +78,56 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     a.stats[4] = v.y.value() / n;
 }
 
+constexpr int kGradT = 256, kGradPer = 4, kGradVecs = kGradT * kGradPer;
+
+// The gradient of preference pairs from the rows' statistics and factors: a CTA per part
+// of a row, entries straight from and to global memory, as a copy would go.
+template <class T>
+__global__ void __launch_bounds__(kGradT) token_pair_grad_kernel(TokenArgs a, int parts) {
+    constexpr int W = Elt<T>::W;
+    const int tid = threadIdx.x;
+    const int64_t total = a.n * parts;
+    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+        const int64_t row = at / parts;
+        const int v0 = (int)(at - row * parts) * kGradVecs;
+        const TokenRow r = a.rows[row];
+        const int token = a.tokens[row];
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        T* g = static_cast<T*>(a.g) + row * a.gld;
+        const int h = (int)(((uintptr_t)g & 15u) / sizeof(T));       // vectors of the gradient's own alignment
+        const int zo = (int)((uintptr_t)z & 15u) - (int)((uintptr_t)g & 15u);
+        const RowGrad c{r.m, -r.value * r.inv_s, 0.f, r.value};
+        uint4 q[kGradPer];
+#pragma unroll
+        for (int u = 0; u < kGradPer; ++u) {
+            const int j = (v0 + tid + u * kGradT) * W - h;
+            q[u] = Elt<T>::none();
+            if (r.inv_s == 0.f || j >= a.V) continue;
+            if (zo == 0 && j >= 0 && j + W <= a.V) {
+                q[u] = __ldcs(reinterpret_cast<const uint4*>(z + j));
+            } else {
+                // a vector that starts inside one of the logits' blocks, or a partial one
+                const uint8_t* p = reinterpret_cast<const uint8_t*>(z + j);
+                const int by = (int)((uintptr_t)p & 15u);
+                if (j - W >= 0 && j + 2 * W <= a.V) q[u] = by ? load_shifted(p - by, by) : *reinterpret_cast<const uint4*>(p);
+                else q[u] = load_part(z, j, a.V);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kGradPer; ++u) {
+            const int j = (v0 + tid + u * kGradT) * W - h;
+            if (j >= a.V) continue;
+            F2 v[W / 2];
+            emit<T, false>(q[u], c, a.k, v);
+            if ((unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
+            uint4 out = Elt<T>::pack(v);
+            if (r.inv_s == 0.f) out = make_uint4(0, 0, 0, 0);
+            if (j >= 0 && j + W <= a.V) __stcs(reinterpret_cast<uint4*>(g + j), out);
+            else store_part(g + j, j, a.V, out);
+        }
+    }
+}
+
 bool is_short(const TokenArgs& a) {
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
     return (a.V + 2 * (int64_t)W - 2) / W <= kShortVecs;
@@ -88,10 +139,27 @@ cudaError_t launch_short(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
     return launch_token_short_f16(a, op, n_sm, s);
 }
 
+cudaError_t launch_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    if (a.dtype == MALIB_F32) return launch_token_ring_f32(a, op, n_sm, s);
+    if (a.dtype == MALIB_BF16) return launch_token_ring_bf16(a, op, n_sm, s);
+    return launch_token_ring_f16(a, op, n_sm, s);
+}
+
+cudaError_t launch_pair_grad(const TokenArgs& a, cudaStream_t s) {
+    const int W = a.dtype == MALIB_F32 ? 4 : 8;
+    const int parts = (int)(((a.V + 2 * (int64_t)W - 2) / W + kGradVecs - 1) / kGradVecs);
+    const int64_t total = a.n * parts;
+    const unsigned grid = (unsigned)(total < (1 << 30) ? total : (1 << 30));
+    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kGradT, 0, s>>>(a, parts);
+    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kGradT, 0, s>>>(a, parts);
+    else token_pair_grad_kernel<__half><<<grid, kGradT, 0, s>>>(a, parts);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
-    return a.n == 0 || is_short(a) ? launch_short(a, op, n_sm, s) : launch_token_ring(a, op, n_sm, s);
+    return a.n == 0 || is_short(a) ? launch_short(a, op, n_sm, s) : launch_ring(a, op, n_sm, s);
 }
 
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
@@ -99,7 +167,7 @@ cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
-    return is_short(a) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_token_pair_grad(a, s);
+    return is_short(a) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_pair_grad(a, s);
 }
 
 }  // namespace malib

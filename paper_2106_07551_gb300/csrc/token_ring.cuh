@@ -1,25 +1,34 @@
 // Losses of token policies, long rows: one pass over memory. A row is read from global
 // memory once; it stays in shared memory while its statistics are gathered, and the
-// gradient is computed from there.
+// gradient is computed from there. Where a row is longer than the ring, its last parts
+// stay and the others are read again, which the L2 cache serves.
 //
-// A cluster of C CTAs takes a row, each a slice of it. One warp of a CTA (the producer)
-// runs ahead and copies slices into a ring of 16 KB stages with bulk copies, completing
-// on an mbarrier per stage; eight warps (the consumers) gather the slice's statistics
-// stage by stage; warp 0 exchanges them with the row's other CTAs through distributed
-// shared memory (asynchronous stores that complete on an mbarrier) and computes the
-// row's loss; and the consumers go through the same stages again, writing the gradient
-// to global memory and freeing each stage as they leave it. The next row's copies fill
-// the freed stages meanwhile. For distillation a further warp (the teacher) prepares the
-// row's list of entries ahead.
+// One warp of a CTA (the producer) runs ahead and copies rows into a ring of stages with
+// bulk copies, completing on an mbarrier per stage; the other warps (the consumers) gather
+// a row's statistics stage by stage; warp 0 sums the warps' statistics and computes the
+// row's loss; and the consumers go through the same stages again, writing the gradient to
+// global memory and freeing each stage as they leave it. The next row's copies fill the
+// freed stages meanwhile. For distillation a further warp (the teacher) prepares the row's
+// list of entries ahead.
 //
 // Rows are claimed, not dealt: SMs do not all get the same share of the memory's rate, and
 // rows that are left out cost a write and no read; with a fixed share each, SMs stood
 // idle for 10 to 20% of a call. The producer claims a row ahead (an atomic counter), reads
-// its token and weight, and puts it into the CTA's queue. What a row adds to the statistics is stored by itself and summed in the
-// rows' order at the end, so that a call's results do not depend on who took what.
+// its token and weight, and puts it into the CTA's queue. What a row adds to the
+// statistics is stored by itself and summed in the rows' order at the end, so that a
+// call's results do not depend on who took what.
 //
-// Bound by memory: the rings of two CTAs an SM hold 2 x 96 KB in flight or in work, and
-// while a CTA waits for its row's sums the SM's other one computes.
+// With few rows a cluster of C CTAs takes one row, each a slice of it, and exchanges the
+// sums through distributed shared memory (asynchronous stores that complete on an mbarrier).
+//
+// Bound by memory for rows of 100 KB and more, below by the sweeps' instructions (per entry
+// about 7 and an exponential in the first one, 4.5 to 6 and one in the second) and what a
+// row costs besides. Stages of 16 KB under four consumer warps with three CTAs an SM, or of
+// 32 KB under eight warps: eight vectors a thread and stage hide the latencies of shared
+// memory and of the exponential, which four did not. ppo with every term, us a call
+// (bf16, 4,096 rows of which a quarter is left out): 64 KB rows 86 with the small shape, 87
+// and 113 with two and one CTAs of the large one; 100 KB 130, 136, 166; 128 KB 174, 157,
+// 180; 192 KB 287, 254, 249; 16,384 rows of 256 KB 1,648, 1,562, 1,281.
 //
 // Rows start at any element: a row's vectors are the 16-byte blocks of its address, the
 // full ones copied in bulk, a partial first or last one filled in by the producer's
@@ -28,20 +37,27 @@
 //
 // Every wait is bounded, between the warps too: one that expires ends the CTA's work and
 // is reported as MALIB_ETIMEOUT.
+#pragma once
+
 #include "token_common.cuh"
 #include "token_peer.cuh"
+#include "token_shift.cuh"
 #include "token_top.cuh"
 
 namespace malib {
 
 namespace {
 
-constexpr int kConsumers = 256, kConsumerWarps = kConsumers / 32;
-constexpr int kPer = 4;                              // vectors a thread and stage
-constexpr int kStageVecs = kPer * kConsumers, kStageBytes = kStageVecs * 16;
-constexpr int kMaxStages = 8, kMaxCluster = 8;
+// Consumer threads, and vectors of each in a stage.
+struct RingSmall {
+    static constexpr int kConsumers = 128, kPer = 8;
+};
+struct RingLarge {
+    static constexpr int kConsumers = 256, kPer = 8;
+};
+constexpr int kMaxStages = 6, kMaxCluster = 8;
 constexpr int kQueue = 4;                            // most rows known ahead
-constexpr int kRingTwo = 104 * 1024;                 // dynamic shared memory with two CTAs an SM
+constexpr int kRingMost = 216 * 1024;                // dynamic shared memory
 
 // What the row's CTAs exchange, and what a warp leaves for its CTA.
 struct __align__(16) Partial {
@@ -79,25 +95,6 @@ struct Shape {
     int single;                                      // the grid has a CTA, or a cluster, for every row
 };
 
-// Sixteen bytes of shared memory from a byte offset that need not be a multiple of 16.
-template <int kWord>
-__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t bits) {
-    const uint32_t w[9] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, 0};
-    return make_uint4(__funnelshift_r(w[kWord], w[kWord + 1], bits), __funnelshift_r(w[kWord + 1], w[kWord + 2], bits),
-                      __funnelshift_r(w[kWord + 2], w[kWord + 3], bits),
-                      __funnelshift_r(w[kWord + 3], w[kWord + 4], bits));
-}
-__device__ __forceinline__ uint4 load_shifted(const uint8_t* p, int by) {   // p: 16-byte aligned, 0 < by < 16
-    const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 16);
-    const uint32_t bits = 8u * (by & 3);
-    switch (by >> 2) {
-        case 0: return shifted<0>(a, b, bits);
-        case 1: return shifted<1>(a, b, bits);
-        case 2: return shifted<2>(a, b, bits);
-        default: return shifted<3>(a, b, bits);
-    }
-}
-
 // One entry of the gradient.
 template <class T>
 __device__ __forceinline__ float emit_one(T z, const RowGrad& c, float k) {
@@ -106,8 +103,9 @@ __device__ __forceinline__ float emit_one(T z, const RowGrad& c, float k) {
 }
 
 // The gradient of a stage: entries [j0, j1) of the row, those of the n vectors at src,
-// the first of which is entry `first` (before the row where the row starts inside it).
-template <class T, bool kEntropy>
+// the first of which is entry `first` (before the row where the row starts inside it). By
+// the first kConsumers threads; a full stage has kPer vectors for each.
+template <class T, bool kEntropy, int kConsumers, int kPer>
 __device__ __forceinline__ void emit_stage(const uint8_t* src, int first, int j0, int j1, int n, T* g, bool alike,
                                            const RowGrad& c, float k, int token) {
     constexpr int W = Elt<T>::W;
@@ -117,7 +115,7 @@ __device__ __forceinline__ void emit_stage(const uint8_t* src, int first, int j0
     if (alike) {
         const uint4* q = reinterpret_cast<const uint4*>(src) + tid;
         T* out = g + (first + tid * W);
-        if (j0 == first && j1 - j0 == kStageVecs * W) {
+        if (j0 == first && j1 - j0 == kPer * kConsumers * W) {
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
                 emit<T, kEntropy>(q[u * kConsumers], c, k, v);
@@ -154,8 +152,8 @@ __device__ __forceinline__ void emit_stage(const uint8_t* src, int first, int j0
     }
 }
 
-// Zeros to entries [j0, j1) of a row.
-template <class T>
+// Zeros to entries [j0, j1) of a row, by the first kConsumers threads.
+template <class T, int kConsumers>
 __device__ __forceinline__ void zero_entries(T* g, int j0, int j1) {
     constexpr int W = Elt<T>::W;
     const int tid = threadIdx.x;
@@ -187,10 +185,13 @@ __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
     if (threadIdx.x == 0) write_stats<kOp>(a, v);
 }
 
-template <class T, int kOp>
-__global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), kOp == kTokLogp ? 3 : 2)
+template <class T, int kOp, class Ring>
+__global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32),
+                                  Ring::kConsumers > 128 ? 2 : kOp == kTokLogp ? 4 : 3)
     token_ring_kernel(TokenArgs a, Shape sh) {
     constexpr int W = Elt<T>::W;
+    constexpr int kConsumers = Ring::kConsumers, kConsumerWarps = kConsumers / 32, kPer = Ring::kPer;
+    constexpr int kStageVecs = kConsumers * kPer, kStageBytes = kStageVecs * 16;
     constexpr int kThreads = kConsumers + (kOp == kTokDistill ? 64 : 32);
     constexpr bool kTop = kOp == kTokDistill;
     extern __shared__ __align__(128) uint8_t ring[];
@@ -363,7 +364,8 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                 if (q.token >= 0) {
                     const int b = turn & 1u;
                     wait(&tempty[b], (turn >> 1 & 1u) ^ 1u);
-                    const TopRow r = top_row<T, kSeen>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld, entries + b * a.top, seen);
+                    const TopRow r = top_row<T, kSeen>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld,
+                                                       entries + b * a.top, seen);
                     if (lane == 0) top[b] = r;
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&tfull[b]);
@@ -394,7 +396,7 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                     if (kTop && a.loss) a.loss[row] = 0.f;
                     if (kOp != kTokLogp) a.row_sums[row] = RowSum{0.f, 0.f, 0.f, 0};
                 }
-                if (g) zero_entries(g, max(0, v_lo * W - h), max(0, min(a.V, v_hi * W - h)));
+                if (g) zero_entries<T, kConsumers>(g, max(0, v_lo * W - h), max(0, min(a.V, v_hi * W - h)));
                 leave(t);
                 continue;
             }
@@ -496,9 +498,12 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
                     const int j0 = max(0, j), j1 = min(a.V, j + n * W);
                     const uint8_t* src = ring + at.stage * kStageBytes;
                     const int token = kTop ? -1 : q.token;
-                    if (!live) zero_entries(g, j0, j1);
-                    else if (kOp == kTokPpo && c.c1 != 0.f) emit_stage<T, true>(src, j, j0, j1, n, g, alike, c, a.k, token);
-                    else emit_stage<T, false>(src, j, j0, j1, n, g, alike, c, a.k, token);
+                    if (!live)
+                        zero_entries<T, kConsumers>(g, j0, j1);
+                    else if (kOp == kTokPpo && c.c1 != 0.f)
+                        emit_stage<T, true, kConsumers, kPer>(src, j, j0, j1, n, g, alike, c, a.k, token);
+                    else
+                        emit_stage<T, false, kConsumers, kPer>(src, j, j0, j1, n, g, alike, c, a.k, token);
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&empty[at.stage]);
                 }
@@ -537,63 +542,17 @@ __global__ void __launch_bounds__(kConsumers + (kOp == kTokDistill ? 64 : 32), k
     if (stats) sum_rows<kOp, kThreads>(a);
 }
 
-// The gradient of preference pairs from the rows' statistics and factors: a CTA per part
-// of a row, entries straight from and to global memory, as a copy would go.
-template <class T>
-__global__ void __launch_bounds__(kConsumers) token_pair_grad_kernel(TokenArgs a, int parts) {
-    constexpr int W = Elt<T>::W;
-    const int tid = threadIdx.x;
-    const int64_t total = a.n * parts;
-    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
-        const int64_t row = at / parts;
-        const int v0 = (int)(at - row * parts) * kStageVecs;
-        const TokenRow r = a.rows[row];
-        const int token = a.tokens[row];
-        const T* z = static_cast<const T*>(a.z) + row * a.ld;
-        T* g = static_cast<T*>(a.g) + row * a.gld;
-        const int h = (int)(((uintptr_t)g & 15u) / sizeof(T));       // vectors of the gradient's own alignment
-        const int zo = (int)((uintptr_t)z & 15u) - (int)((uintptr_t)g & 15u);
-        const RowGrad c{r.m, -r.value * r.inv_s, 0.f, r.value};
-        uint4 q[kPer];
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) {
-            const int j = (v0 + tid + u * kConsumers) * W - h;
-            q[u] = Elt<T>::none();
-            if (r.inv_s == 0.f || j >= a.V) continue;
-            if (zo == 0 && j >= 0 && j + W <= a.V) {
-                q[u] = __ldcs(reinterpret_cast<const uint4*>(z + j));
-            } else {
-                // a vector that starts inside one of the logits' blocks, or a partial one
-                const uint8_t* p = reinterpret_cast<const uint8_t*>(z + j);
-                const int by = (int)((uintptr_t)p & 15u);
-                if (j - W >= 0 && j + 2 * W <= a.V) q[u] = by ? load_shifted(p - by, by) : *reinterpret_cast<const uint4*>(p);
-                else q[u] = load_part(z, j, a.V);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) {
-            const int j = (v0 + tid + u * kConsumers) * W - h;
-            if (j >= a.V) continue;
-            F2 v[W / 2];
-            emit<T, false>(q[u], c, a.k, v);
-            if ((unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
-            uint4 out = Elt<T>::pack(v);
-            if (r.inv_s == 0.f) out = make_uint4(0, 0, 0, 0);
-            if (j >= 0 && j + W <= a.V) __stcs(reinterpret_cast<uint4*>(g + j), out);
-            else store_part(g + j, j, a.V, out);
-        }
-    }
-}
-
-template <class T, int kOp>
-cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int grid, cudaStream_t s) {
-    cudaError_t e = cudaFuncSetAttribute(token_ring_kernel<T, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingTwo);
+template <class T, int kOp, class Ring>
+cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t grid, cudaStream_t s) {
+    cudaError_t e =
+        cudaFuncSetAttribute(token_ring_kernel<T, kOp, Ring>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingMost);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(kConsumers + (kOp == kTokDistill ? 64 : 32));
-    cfg.dynamicSmemBytes = sh.stages * kStageBytes + (kOp == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0);
+    cfg.blockDim = dim3(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32));
+    cfg.dynamicSmemBytes = (size_t)sh.stages * Ring::kConsumers * Ring::kPer * 16 +
+                           (kOp == kTokDistill ? 2 * a.top * sizeof(TopEntry) : 0);
     cfg.stream = s;
     if (sh.cluster > 1) {
         at.id = cudaLaunchAttributeClusterDimension;
@@ -602,66 +561,66 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int grid, cudaStrea
         cfg.attrs = &at;
         cfg.numAttrs = 1;
     }
-    e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp>, a, sh);
+    e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp, Ring>, a, sh);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <class T>
-cudaError_t launch_ring_t(const TokenArgs& a, int op, const Shape& sh, int grid, cudaStream_t s) {
-    if (op == kTokLogp) return launch_ring<T, kTokLogp>(a, sh, grid, s);
-    if (op == kTokPpo) return launch_ring<T, kTokPpo>(a, sh, grid, s);
-    return launch_ring<T, kTokDistill>(a, sh, grid, s);
-}
-
-}  // namespace
-
-cudaError_t launch_token_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
-    const int W = a.dtype == MALIB_F32 ? 4 : 8;
-    const int64_t nv = (a.V + 2 * (int64_t)W - 2) / W;               // most vectors of a row
-    const int lists = op == kTokDistill ? 2 * a.top * (int)sizeof(TopEntry) : 0;
-    const int held = (op == kTokLogp ? 3 : 2) * n_sm;                // CTAs the device holds
-    Shape sh{1, op == kTokLogp ? 4 : (kRingTwo - lists) / kStageBytes, 0, 0, 0, 1, 0};
+template <class T, int kOp>
+cudaError_t launch_ring_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
+    const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
+    const bool write = kOp != kTokLogp && a.g != nullptr;
     auto slice = [&](int c) { return (nv + c - 1) / c; };
-    // CTAs a row: the rounds that the device takes over the rows, times the bytes that a CTA
-    // moves in one and what it costs besides (about 4 us, the time of 80 KB). In us, C = 1
-    // and the C taken: ppo 25 x 32,768 bf16 20 and 12 (8), distillation 333 x 151,111 fp32
-    // 126 and 97 (4); 333 x 32,768 bf16 rows' statistics stay at C = 1, 11, with 4 20.
-    const int64_t bytes = a.V * (int64_t)(16 / W) * (op == kTokLogp ? 1 : 2);
+    // CTAs an SM by the bytes of a slice (the figures above): three of the small shape with
+    // four stages, four with three where nothing is written; two or one of the large one
+    // with three or six.
+    auto ctas = [&](int c) { return !write ? 4 : slice(c) <= 7168 ? 3 : slice(c) <= 13312 ? 2 : 1; };
+    // CTAs a row: the rounds that the device takes over the rows, each of the bytes that a CTA
+    // moves at its share of the memory's rate (45 bytes a ns and SM) and 4 us besides. In us,
+    // C = 1 and the C taken: ppo 25 x 32,768 bf16 20 and 12 (8), distillation 333 x 151,111
+    // fp32 126 and 97 (4); 333 x 32,768 bf16 rows' statistics stay at C = 1, 11, with 4 20.
+    const int64_t bytes = nv * 16 * (write ? 2 : 1);
+    Shape sh{};
     int64_t best = 0;
-    for (int c = 1; c <= kMaxCluster && (c == 1 || slice(c) >= kStageVecs / 2); c *= 2) {
-        const int64_t t = (a.n * c + held - 1) / held * (80 * 1024 + bytes / c);
+    for (int c = 1; c <= kMaxCluster && (c == 1 || slice(c) >= 512); c *= 2) {
+        const int64_t held = (int64_t)ctas(c) * n_sm;
+        const int64_t t = (a.n * c + held - 1) / held * (4000 + bytes / c * ctas(c) / 45);
         if (c > 1 && t >= best) continue;
         best = t;
         sh.cluster = c;
     }
+    const int per_sm = ctas(sh.cluster);
+    const int64_t held = (int64_t)per_sm * n_sm;
+    const bool large = per_sm < 3;
+    const int stage = large ? RingLarge::kConsumers * RingLarge::kPer : RingSmall::kConsumers * RingSmall::kPer;
+    sh.stages = per_sm == 4 ? 3 : per_sm == 3 ? 4 : per_sm == 2 ? 3 : 6;
     sh.slice = (int)slice(sh.cluster);
-    sh.keep = sh.slice <= (sh.stages - 1) * kStageVecs ? sh.stages - 1 : sh.stages - 2;
+    sh.keep = sh.slice <= (sh.stages - 1) * stage ? sh.stages - 1 : sh.stages - 2;
     // A cluster takes one row, as does a CTA when there are no more rows than CTAs.
     sh.single = sh.cluster > 1 || a.n <= held;
     const int64_t grid = sh.single ? a.n * sh.cluster : held;
     // Rows of a stage or more are claimed one by one and known one ahead, so that no CTA holds
     // several while others run out; short ones in batches of about two stages, as long as
     // there are several for every CTA.
-    sh.queue_log = sh.slice >= kStageVecs ? 1 : 2;
-    if (sh.slice < kStageVecs && !sh.single) {
-        const int64_t most = a.n / (4 * grid), about = 2 * kStageVecs / sh.slice;
+    sh.queue_log = sh.slice >= stage ? 1 : 2;
+    sh.batch = 1;
+    if (sh.slice < stage && !sh.single) {
+        const int64_t most = a.n / (4 * grid), about = 2 * stage / sh.slice;
         sh.batch = (int)(most < 1 ? 1 : most < about ? most : about);
         if (sh.batch > 16) sh.batch = 16;
     }
-    if (a.dtype == MALIB_F32) return launch_ring_t<float>(a, op, sh, (int)grid, s);
-    if (a.dtype == MALIB_BF16) return launch_ring_t<__nv_bfloat16>(a, op, sh, (int)grid, s);
-    return launch_ring_t<__half>(a, op, sh, (int)grid, s);
+    if constexpr (kOp != kTokLogp) {
+        if (large) return launch_ring<T, kOp, RingLarge>(a, sh, grid, s);
+    }
+    return launch_ring<T, kOp, RingSmall>(a, sh, grid, s);
 }
 
-cudaError_t launch_token_pair_grad(const TokenArgs& a, cudaStream_t s) {
-    const int W = a.dtype == MALIB_F32 ? 4 : 8;
-    const int parts = (int)(((a.V + 2 * (int64_t)W - 2) / W + kStageVecs - 1) / kStageVecs);
-    const int64_t total = a.n * parts;
-    const unsigned grid = (unsigned)(total < (1 << 30) ? total : (1 << 30));
-    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kConsumers, 0, s>>>(a, parts);
-    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kConsumers, 0, s>>>(a, parts);
-    else token_pair_grad_kernel<__half><<<grid, kConsumers, 0, s>>>(a, parts);
-    return cudaGetLastError();
+template <class T>
+cudaError_t launch_ring_type(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    if (op == kTokLogp) return launch_ring_op<T, kTokLogp>(a, n_sm, s);
+    if (op == kTokPpo) return launch_ring_op<T, kTokPpo>(a, n_sm, s);
+    return launch_ring_op<T, kTokDistill>(a, n_sm, s);
 }
+
+}  // namespace
 
 }  // namespace malib

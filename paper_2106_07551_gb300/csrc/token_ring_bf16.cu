@@ -1,0 +1,10 @@
+// Long rows of bf16 logits.
+#include "token_ring.cuh"
+
+namespace malib {
+
+cudaError_t launch_token_ring_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
+    return launch_ring_type<__nv_bfloat16>(a, op, n_sm, s);
+}
+
+}  // namespace malib

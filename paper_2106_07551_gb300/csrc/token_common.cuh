@@ -515,6 +515,12 @@ __device__ __forceinline__ void write_stats(const TokenArgs& a, const Totals& v)
     }
 }
 
+// The kernels of a preference call are launched while the one before still runs. This
+// waits until that one is complete and what it wrote is there;
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// this lets the next one be launched, once every CTA has come here.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // The calling CTA has stored what others will read; whether it is the last of `of` that
 // come here. The counter is back at 0 for the next call.
 __device__ __forceinline__ bool last_of(unsigned* ticket, unsigned of) {

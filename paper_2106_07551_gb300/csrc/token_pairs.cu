@@ -9,8 +9,6 @@ namespace {
 
 constexpr int kPairT = 256;
 
-// A double's sum over a warp costs more than all the rest of a small pair: per thread and
-// warp fp32 sums with their errors, fp64 at the end.
 __device__ __forceinline__ Sum2 warp_sum2(Sum2 v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v.add(sum2_xor(v, o));
@@ -25,6 +23,8 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     constexpr int kHalf = kPairT / 2;
     const int side = threadIdx.x / kHalf, part = threadIdx.x % kHalf;
     Totals total{};                                  // thread 0: pairs, those in order; loss, rewards
+    wait_for_previous();
+    let_next_start();
     for (int p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
         const int64_t o0 = a.offsets[2 * p], o1 = a.offsets[2 * p + 1], o2 = a.offsets[2 * p + 2];
         const bool ok = o0 >= 0 && o0 <= o1 && o1 <= o2 && o2 <= a.n && (p > 0 || o0 == 0) &&
@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(kGradT) token_pair_grad_kernel(TokenArgs a, in
     constexpr int W = Elt<T>::W;
     const int tid = threadIdx.x;
     const int64_t total = a.n * parts;
+    wait_for_previous();
     for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
         const int64_t row = at / parts;
         const int v0 = (int)(at - row * parts) * kGradVecs;
@@ -145,15 +146,30 @@ cudaError_t launch_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
     return launch_token_ring_f16(a, op, n_sm, s);
 }
 
+// Launches a kernel that waits for the stream's previous one itself.
+template <class... Args>
+cudaError_t launch_after(void (*kernel)(Args...), unsigned grid, unsigned threads, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 cudaError_t launch_pair_grad(const TokenArgs& a, cudaStream_t s) {
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
     const int parts = (int)(((a.V + 2 * (int64_t)W - 2) / W + kGradVecs - 1) / kGradVecs);
     const int64_t total = a.n * parts;
     const unsigned grid = (unsigned)(total < (1 << 30) ? total : (1 << 30));
-    if (a.dtype == MALIB_F32) token_pair_grad_kernel<float><<<grid, kGradT, 0, s>>>(a, parts);
-    else if (a.dtype == MALIB_BF16) token_pair_grad_kernel<__nv_bfloat16><<<grid, kGradT, 0, s>>>(a, parts);
-    else token_pair_grad_kernel<__half><<<grid, kGradT, 0, s>>>(a, parts);
-    return cudaGetLastError();
+    if (a.dtype == MALIB_F32) return launch_after(token_pair_grad_kernel<float>, grid, kGradT, s, a, parts);
+    if (a.dtype == MALIB_BF16) return launch_after(token_pair_grad_kernel<__nv_bfloat16>, grid, kGradT, s, a, parts);
+    return launch_after(token_pair_grad_kernel<__half>, grid, kGradT, s, a, parts);
 }
 
 }  // namespace
@@ -165,8 +181,8 @@ cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     cudaError_t e = a.n > 0 ? launch_token_rows(a, kTokLogp, n_sm, s) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    token_pairs_kernel<<<a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm, kPairT, 0, s>>>(a);
-    if ((e = cudaGetLastError()) != cudaSuccess || !a.g || a.n == 0) return e;
+    e = launch_after(token_pairs_kernel, (unsigned)(a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm), kPairT, s, a);
+    if (e != cudaSuccess || !a.g || a.n == 0) return e;
     return is_short(a) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_pair_grad(a, s);
 }
 

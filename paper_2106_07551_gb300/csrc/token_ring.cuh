@@ -48,12 +48,18 @@ namespace malib {
 
 namespace {
 
-// Consumer threads, and vectors of each in a stage.
+// Consumer threads, vectors of each in a stage, CTAs an SM.
 struct RingSmall {
-    static constexpr int kConsumers = 128, kPer = 8;
+    static constexpr int kConsumers = 128, kPer = 8, kCtas = 3;
+};
+struct RingStat {                                    // nothing is written
+    static constexpr int kConsumers = 128, kPer = 8, kCtas = 4;
 };
 struct RingLarge {
-    static constexpr int kConsumers = 256, kPer = 8;
+    static constexpr int kConsumers = 256, kPer = 8, kCtas = 2;
+};
+struct RingHuge {
+    static constexpr int kConsumers = 256, kPer = 8, kCtas = 1;
 };
 constexpr int kMaxStages = 6, kMaxCluster = 8;
 constexpr int kQueue = 4;                            // most rows known ahead
@@ -186,8 +192,7 @@ __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
 }
 
 template <class T, int kOp, class Ring>
-__global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32),
-                                  Ring::kConsumers > 128 ? 2 : kOp == kTokLogp ? 4 : 3)
+__global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32), Ring::kCtas)
     token_ring_kernel(TokenArgs a, Shape sh) {
     constexpr int W = Elt<T>::W;
     constexpr int kConsumers = Ring::kConsumers, kConsumerWarps = kConsumers / 32, kPer = Ring::kPer;
@@ -234,6 +239,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
         fence_proxy_async_smem();
     }
     __syncthreads();
+    if (kOp == kTokLogp) let_next_start();
     // The peers' barriers and memory are there before the first store to them: arrived here,
     // waited for where it is needed.
     if (C > 1) cluster_arrive();
@@ -574,24 +580,17 @@ cudaError_t launch_ring_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
     // four stages, four with three where nothing is written; two or one of the large one
     // with three or six.
     auto ctas = [&](int c) { return !write ? 4 : slice(c) <= 7168 ? 3 : slice(c) <= 13312 ? 2 : 1; };
-    // CTAs a row: the rounds that the device takes over the rows, each of the bytes that a CTA
-    // moves at its share of the memory's rate (45 bytes a ns and SM) and 4 us besides. In us,
-    // C = 1 and the C taken: ppo 25 x 32,768 bf16 20 and 12 (8), distillation 333 x 151,111
-    // fp32 126 and 97 (4); 333 x 32,768 bf16 rows' statistics stay at C = 1, 11, with 4 20.
-    const int64_t bytes = nv * 16 * (write ? 2 : 1);
+    // CTAs a row: as many as the device holds for all the rows at once, with slices of 8 KB
+    // or more. Over more rounds than one the exchange costs what the finer share gains. In
+    // us, C = 1, 2, 4 and 8, ppo bf16: 25 rows of 64 KB 13.1, 11.8, 11.9, 11.4; 120 13.2,
+    // 13.0, 18.7, 21.7; 300 14.5, 22.9, 28.9, 43.5; 60 rows of 256 KB 20.8, 16.7, 15.8, 22.1.
     Shape sh{};
-    int64_t best = 0;
-    for (int c = 1; c <= kMaxCluster && (c == 1 || slice(c) >= 512); c *= 2) {
-        const int64_t held = (int64_t)ctas(c) * n_sm;
-        const int64_t t = (a.n * c + held - 1) / held * (4000 + bytes / c * ctas(c) / 45);
-        if (c > 1 && t >= best) continue;
-        best = t;
-        sh.cluster = c;
-    }
+    sh.cluster = 1;
+    for (int c = 2; c <= kMaxCluster && slice(c) >= 512; c *= 2)
+        if (a.n * c <= (int64_t)ctas(c) * n_sm) sh.cluster = c;
     const int per_sm = ctas(sh.cluster);
     const int64_t held = (int64_t)per_sm * n_sm;
-    const bool large = per_sm < 3;
-    const int stage = large ? RingLarge::kConsumers * RingLarge::kPer : RingSmall::kConsumers * RingSmall::kPer;
+    const int stage = (per_sm < 3 ? RingLarge::kConsumers : RingSmall::kConsumers) * RingSmall::kPer;
     sh.stages = per_sm == 4 ? 3 : per_sm == 3 ? 4 : per_sm == 2 ? 3 : 6;
     sh.slice = (int)slice(sh.cluster);
     sh.keep = sh.slice <= (sh.stages - 1) * stage ? sh.stages - 1 : sh.stages - 2;
@@ -608,10 +607,13 @@ cudaError_t launch_ring_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
         sh.batch = (int)(most < 1 ? 1 : most < about ? most : about);
         if (sh.batch > 16) sh.batch = 16;
     }
+    if (per_sm == 4) return launch_ring<T, kOp, RingStat>(a, sh, grid, s);
     if constexpr (kOp != kTokLogp) {
-        if (large) return launch_ring<T, kOp, RingLarge>(a, sh, grid, s);
+        if (per_sm == 3) return launch_ring<T, kOp, RingSmall>(a, sh, grid, s);
+        if (per_sm == 2) return launch_ring<T, kOp, RingLarge>(a, sh, grid, s);
+        return launch_ring<T, kOp, RingHuge>(a, sh, grid, s);
     }
-    return launch_ring<T, kOp, RingSmall>(a, sh, grid, s);
+    return cudaErrorInvalidValue;                    // (not reached)
 }
 
 template <class T>

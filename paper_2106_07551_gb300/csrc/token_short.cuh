@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G;
     const int64_t step = (int64_t)gridDim.x * kShortWarps * kRows;
     Totals total{};
+    if (kOp == kTokLogp) let_next_start();
     for (int64_t row0 = ((int64_t)blockIdx.x * kShortWarps + warp) * kRows; row0 < a.n; row0 += step) {
         const bool in_range = row0 + lane / G < a.n;
         const int64_t row = in_range ? row0 + lane / G : a.n - 1;
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) 
     const int tid = threadIdx.x;
     const bool flat_z = a.ld == a.V, flat_g = a.gld == a.V;
     Totals total{};
+    if (kOp == kTokLogp) let_next_start();
     for (int64_t row0 = (int64_t)blockIdx.x * kShortThreads; row0 < a.n; row0 += (int64_t)gridDim.x * kShortThreads) {
         const int rows = (int)min((int64_t)kShortThreads, a.n - row0), entries = rows * a.V;
         const bool in_range = tid < rows;

@@ -815,3 +815,67 @@ def test_streams_threads_and_graphs():
         call(g)
         c.sync()
         assert bool((got == g).all()) and bool((gs == stats).all())
+
+
+# ---------------------------------------------------------------- more rows than CTAs: rows are claimed
+
+LOADED = [(1300, 4600, "bf16"), (700, 9001, "bf16"), (900, 5003, "f32"), (620, 17000, "f16"), (330, 60_001, "bf16"),
+          (320, 31_000, "f32"), (170, 120_003, "bf16"), (160, 70_001, "f32")]
+
+
+@pytest.mark.parametrize("n,V,dt", LOADED)
+def test_more_rows_than_the_device_holds(ctx, n, V, dt):
+    """Rows of every length class that CTAs claim one after another, with rows left out
+    among them and masked entries; also in place, and the same bits each time."""
+    b = Batch(n, V, dt, n + V, T=0.9, masked=0.1, out=0.3)
+    check_ppo(ctx, b)
+    check_logprob(ctx, b)
+    scale = 4096.0 if dt == "f16" else 1.0
+    p, first = Ppo(b), None
+    for _ in range(3):
+        _, g = b.grad(pad=1)                                  # rows aligned differently from the logits'
+        stats = empty(5)
+        p.call(ctx, b, g, scale, stats=stats)
+        ctx.sync()
+        first = first or (g, stats)
+        assert bool((g == first[0]).all()) and bool((stats == first[1]).all())
+    keep = b.logits.clone()
+    p.call(ctx, b, b.logits, scale)
+    ctx.sync()
+    assert bool((b.logits == first[0]).all())
+    b.logits.copy_(keep)
+    check_pref(ctx, b, 3)
+
+
+@pytest.mark.parametrize("n,V,dt", LOADED[::2])
+def test_distill_more_rows_than_the_device_holds(ctx, n, V, dt):
+    b = Batch(n, V, dt, n + V, T=1.2, out=0.0)
+    check_distill(ctx, b, 40, tdt=dt)
+    d, (_, g) = Distill(b, 30, twice=True), b.grad()
+    outs = []
+    for target in (g, b.logits.clone(), None):
+        stats, loss = empty(3), empty(n)
+        d.call(ctx, b, target, loss=loss, stats=stats)
+        ctx.sync()
+        outs.append((stats, loss))
+    for s, l in outs[1:]:
+        assert bool((s[:1] == outs[0][0][:1]).all())
+        close(l, outs[0][1].double().cpu().numpy(), 2e-5 * (1 + outs[0][1].abs().double().cpu().numpy()), "loss")
+
+
+def test_many_calls_in_a_row_leave_nothing_behind(ctx):
+    """Calls of different lengths one after another on one context: counters and work
+    space start as they did."""
+    cases = [Batch(n, V, "bf16", n + V) for n, V in [(700, 9001), (3, 40000), (2000, 60), (50, 300), (1, 200_000), (900, 12)]]
+    losses = [(b, Ppo(b)) for b in cases]
+    first = []
+    for rep in range(4):
+        for i, (b, p) in enumerate(losses):
+            _, g = b.grad()
+            stats = empty(5)
+            p.call(ctx, b, g, stats=stats)
+            if rep == 0:
+                first.append((g, stats))
+            else:
+                assert bool((g == first[i][0]).all()) and bool((stats == first[i][1]).all())
+    ctx.sync()

@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(kGradT) token_pair_grad_kernel(TokenArgs a, in
     const int tid = threadIdx.x;
     const int64_t total = a.n * parts;
     wait_for_previous();
-    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
-        const int64_t row = at / parts;
+    for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
+        const int64_t at = total - 1 - i, row = at / parts;        // the rows read last may still be in the L2 cache
         const int v0 = (int)(at - row * parts) * kGradVecs;
         const TokenRow r = a.rows[row];
         const int token = a.tokens[row];

@@ -18,8 +18,9 @@
 // statistics is stored by itself and summed in the rows' order at the end, so that a
 // call's results do not depend on who took what.
 //
-// With few rows a cluster of C CTAs takes one row, each a slice of it, and exchanges the
-// sums through distributed shared memory (asynchronous stores that complete on an mbarrier).
+// With few rows, or very long ones, a cluster of C CTAs takes a row, each a slice of it, and
+// exchanges the sums through distributed shared memory (asynchronous stores that complete on
+// an mbarrier). Clusters' rows are dealt: a claim would have to be exchanged too.
 //
 // Bound by memory for rows of 100 KB and more, below by the sweeps' instructions (per entry
 // about 7 and an exponential in the first one, 4.5 to 6 and one in the second) and what a
@@ -98,8 +99,28 @@ struct Shape {
     int slice;                                       // vectors of a CTA's slice
     int keep;                                        // stages that hold parts of a row for its second sweep
     int queue_log, batch;                            // rows known ahead (log 2), rows a claim takes
-    int single;                                      // the grid has a CTA, or a cluster, for every row
+    int dealt;                                       // row t of CTA, or cluster, i is i + t times their number
+    int l2;                                          // copies say how long the L2 cache should keep a part
 };
+
+// How long the L2 cache should keep what a copy reads.
+__device__ __forceinline__ uint64_t l2_evict_first() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ uint64_t l2_evict_last() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void bulk_g2s_l2(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
+            smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
 
 // One entry of the gradient.
 template <class T>
@@ -204,10 +225,10 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
     // per queued row: known, no longer needed; per row that is read: the warps' statistics
     // are there, the CTAs', the result, the written slice
     __shared__ __align__(8) uint64_t qfull[kQueue], qempty[kQueue], sfull[kQueue], rfull[kQueue], pfull[kQueue],
-        xfull;
+        xfull[2];
     __shared__ __align__(8) uint64_t tfull[2], tempty[2];
     __shared__ Queued queue[kQueue];
-    __shared__ Partial red[kQueue][kConsumerWarps], xslot[kMaxCluster];
+    __shared__ Partial red[kQueue][kConsumerWarps], xslot[2][kMaxCluster];
     __shared__ RowOut rout[kQueue];
     constexpr int kSeen = kTop ? 32768 : 32;
     __shared__ uint32_t seen[kSeen / 32];
@@ -231,8 +252,8 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
             mbar_init(&rfull[i], 1);
             mbar_init(&pfull[i], kConsumerWarps);
         }
-        mbar_init(&xfull, 1);
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&xfull[i], 1);
             mbar_init(&tfull[i], 1);
             mbar_init(&tempty[i], kConsumerWarps);
         }
@@ -269,12 +290,17 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
         if (q.token >= a.V && report) atomicOr(a.err, ERRBIT_BAD_TOKEN);
         if (q.token >= a.V || q.w == 0.f) q.token = -1;
     };
-    // Turn t's row, as every warp sees it; row < 0: there is none.
+    // Turn t's row, as every warp sees it; row < 0: there is none. A dealt row's token and
+    // weight are asked for a turn ahead.
+    Queued ahead{-1, -1, 0.f};
+    if (sh.dealt && blockIdx.x / C < a.n) ahead = look(blockIdx.x / C);
     auto take = [&](uint32_t t) {
         Queued q{-1, -1, 0.f};
-        if (sh.single) {
-            if (t > 0) return q;
-            q = look(blockIdx.x / C);
+        if (sh.dealt) {
+            q = ahead;
+            ahead.row = -1;
+            const int64_t next = q.row + gridDim.x / C;
+            if (q.row >= 0 && next < a.n) ahead = look(next);
             settle(q, rank == 0 && tid == 0);
             return q;
         }
@@ -284,6 +310,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
     };
     // The warp needs nothing of turn t any more.
     auto leave = [&](uint32_t t) {
+        if (sh.dealt) return;
         __syncwarp();
         if (lane == 0) mbar_arrive_release(&qempty[slot_of(t)]);
     };
@@ -300,11 +327,12 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
         auto look_batch = [&] {
             if (lane < sh.batch && batch + lane < a.n) mine = look(batch + lane);
         };
-        if (!sh.single) look_batch();
+        if (!sh.dealt) look_batch();
+        const uint64_t l2_first = l2_evict_first(), l2_last = l2_evict_last();
         Cursor at, issued;
         bool wrapped = false;
         for (uint32_t t = 0;; ++t) {
-            if (!sh.single) {
+            if (!sh.dealt) {
                 const int slot = slot_of(t);
                 Queued q{batch + used < a.n ? batch + used : -1, __shfl_sync(0xffffffffu, mine.token, used),
                          __shfl_sync(0xffffffffu, mine.w, used)};
@@ -344,12 +372,16 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                         const int b0 = head ? 1 : 0, b1 = tail ? n - 1 : n;
                         const uint32_t bytes = b1 > b0 ? (uint32_t)(b1 - b0) * 16u : 0u;
                         mbar_arrive_expect_tx(&full[stage], bytes);
-                        if (bytes) bulk_g2s(dst + b0 * 16, z + ((int64_t)(v + b0) * W - h), bytes, &full[stage]);
+                        const T* src = z + ((int64_t)(v + b0) * W - h);
+                        if (kOp != kTokLogp && bytes && sh.l2)
+                            bulk_g2s_l2(dst + b0 * 16, src, bytes, &full[stage], part < again ? l2_last : l2_first);
+                        else if (bytes)
+                            bulk_g2s(dst + b0 * 16, src, bytes, &full[stage]);
                     }
                     __syncwarp();
                 }
             }
-            if (!sh.single && used == sh.batch) {
+            if (!sh.dealt && used == sh.batch) {
                 used = 0;
                 batch = __shfl_sync(0xffffffffu, batch, 0);
                 look_batch();
@@ -450,12 +482,14 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                 const float zt = Elt<T>::get(z_token);
                 if (C > 1) {
                     // The logits that the loss takes (zt, the teacher's entries) have been read
-                    // before any CTA of the row writes its part: they go before these sums.
+                    // before any CTA of the row writes its part: they go before these sums. Two
+                    // rows' sums have places: a CTA sends the second next row's after it has
+                    // the next one's of every peer, which sent them after reading this row's.
                     join();
-                    if (lane == 0) mbar_arrive_expect_tx(&xfull, (uint32_t)(C * sizeof(Partial)));
-                    if (lane < C) peer_store(&xslot[rank], &xfull, lane, make_float4(r.m, r.s, r.t, zt));
-                    if (!*gone && !peer_wait_bounded(&xfull, 0, kWaitLimitNs)) expired();
-                    const Partial& px = xslot[lane & (kMaxCluster - 1)];
+                    if (lane == 0) mbar_arrive_expect_tx(&xfull[b], (uint32_t)(C * sizeof(Partial)));
+                    if (lane < C) peer_store(&xslot[b][rank], &xfull[b], lane, make_float4(r.m, r.s, r.t, zt));
+                    if (!*gone && !peer_wait_bounded(&xfull[b], turn >> 1 & 1u, kWaitLimitNs)) expired();
+                    const Partial& px = xslot[b][lane & (kMaxCluster - 1)];
                     r = reduce_stat<kMaxCluster>(
                         lane % kMaxCluster < C ? RowStat{px.m, px.s, px.t} : RowStat{-INFINITY, 0.f, 0.f}, a.k);
                 }
@@ -542,20 +576,21 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
     }
     // the CTA that ends last clears the claims for the next call and sums the statistics
     const bool stats = kOp != kTokLogp && a.stats;
-    if (!stats && sh.single) return;
+    if (!stats && sh.dealt) return;
     if (!last_of(a.ticket, gridDim.x)) return;
     if (tid == 0) *a.claims = 0ull;
     if (stats) sum_rows<kOp, kThreads>(a);
 }
 
+// `units` CTAs, or clusters; 0: as many clusters as the device holds, at most one a row.
 template <class T, int kOp, class Ring>
-cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t grid, cudaStream_t s) {
+cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t units, cudaStream_t s) {
     cudaError_t e =
         cudaFuncSetAttribute(token_ring_kernel<T, kOp, Ring>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingMost);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = dim3((unsigned)((units ? units : 1) * sh.cluster));
     cfg.blockDim = dim3(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32));
     cfg.dynamicSmemBytes = (size_t)sh.stages * Ring::kConsumers * Ring::kPer * 16 +
                            (kOp == kTokDistill ? 2 * a.top * sizeof(TopEntry) : 0);
@@ -566,6 +601,12 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t grid, cudaS
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
+    }
+    if (units == 0) {
+        int most = 0;
+        e = cudaOccupancyMaxActiveClusters(&most, token_ring_kernel<T, kOp, Ring>, &cfg);
+        if (e != cudaSuccess) return e;
+        cfg.gridDim.x = (unsigned)(most < 1 ? 1 : most < a.n ? most : a.n) * sh.cluster;
     }
     e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp, Ring>, a, sh);
     return e != cudaSuccess ? e : cudaGetLastError();
@@ -588,30 +629,44 @@ cudaError_t launch_ring_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
     sh.cluster = 1;
     for (int c = 2; c <= kMaxCluster && slice(c) >= 512; c *= 2)
         if (a.n * c <= (int64_t)ctas(c) * n_sm) sh.cluster = c;
+    // Rows of 480 KB or more, over several rounds: slices of 240 KB or more, by clusters of 2
+    // or 4 one row after another. Less of a row has to come again from the L2 cache, the
+    // last round is shorter, and a slice of this length hides the exchange. us, C = 1, 2 and
+    // 4: 333 rows of 604 KB 99, 91, 92; 1,200 of them 300, 252, 277; 200 rows of 500 KB 63,
+    // 54, 56; 800 of 1 MB 341, 340, 301; 800 of 400 KB 126, 137, 163; 1,200 of 256 KB 114,
+    // 139, 186.
+    const bool again = write && sh.cluster == 1 && a.n > n_sm && slice(2) >= 15000;
+    if (again) sh.cluster = slice(4) >= 15000 ? 4 : 2;
     const int per_sm = ctas(sh.cluster);
     const int64_t held = (int64_t)per_sm * n_sm;
     const int stage = (per_sm < 3 ? RingLarge::kConsumers : RingSmall::kConsumers) * RingSmall::kPer;
     sh.stages = per_sm == 4 ? 3 : per_sm == 3 ? 4 : per_sm == 2 ? 3 : 6;
     sh.slice = (int)slice(sh.cluster);
     sh.keep = sh.slice <= (sh.stages - 1) * stage ? sh.stages - 1 : sh.stages - 2;
-    // A cluster takes one row, as does a CTA when there are no more rows than CTAs.
-    sh.single = sh.cluster > 1 || a.n <= held;
-    const int64_t grid = sh.single ? a.n * sh.cluster : held;
+    // Every row at once, or CTAs that claim rows, or clusters that they are dealt to.
+    sh.dealt = sh.cluster > 1 || a.n <= held;
+    const int64_t units = again ? 0 : sh.dealt ? a.n : held;
+    // Rows of which the CTAs on the device hold some 45 MB or more between their sweeps: the
+    // parts that come again are to stay in the L2 cache, the others and the second copies to
+    // go. us without and with this: 1,111 rows of 200 KB (two CTAs an SM) 91.7 and 87.7,
+    // 800 of 400 KB 126 and 120, 1,200 of 604 KB (clusters of 2) 252 and 246; rows of 256 KB
+    // 329 and 332, of 100 KB no difference.
+    sh.l2 = write && per_sm < 3 && per_sm * sh.slice >= 18000;
     // Rows of a stage or more are claimed one by one and known one ahead, so that no CTA holds
     // several while others run out; short ones in batches of about two stages, as long as
     // there are several for every CTA.
     sh.queue_log = sh.slice >= stage ? 1 : 2;
     sh.batch = 1;
-    if (sh.slice < stage && !sh.single) {
-        const int64_t most = a.n / (4 * grid), about = 2 * stage / sh.slice;
+    if (sh.slice < stage && !sh.dealt) {
+        const int64_t most = a.n / (4 * held), about = 2 * stage / sh.slice;
         sh.batch = (int)(most < 1 ? 1 : most < about ? most : about);
         if (sh.batch > 16) sh.batch = 16;
     }
-    if (per_sm == 4) return launch_ring<T, kOp, RingStat>(a, sh, grid, s);
+    if (per_sm == 4) return launch_ring<T, kOp, RingStat>(a, sh, units, s);
     if constexpr (kOp != kTokLogp) {
-        if (per_sm == 3) return launch_ring<T, kOp, RingSmall>(a, sh, grid, s);
-        if (per_sm == 2) return launch_ring<T, kOp, RingLarge>(a, sh, grid, s);
-        return launch_ring<T, kOp, RingHuge>(a, sh, grid, s);
+        if (per_sm == 3) return launch_ring<T, kOp, RingSmall>(a, sh, units, s);
+        if (per_sm == 2) return launch_ring<T, kOp, RingLarge>(a, sh, units, s);
+        return launch_ring<T, kOp, RingHuge>(a, sh, units, s);
     }
     return cudaErrorInvalidValue;                    // (not reached)
 }

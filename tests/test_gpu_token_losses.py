@@ -879,3 +879,21 @@ def test_many_calls_in_a_row_leave_nothing_behind(ctx):
             else:
                 assert bool((g == first[i][0]).all()) and bool((stats == first[i][1]).all())
     ctx.sync()
+
+
+@pytest.mark.parametrize("n,V,dt", [(156, 240_003, "bf16"), (153, 121_001, "f32"), (154, 240_050, "f32")])
+def test_very_long_rows_one_after_another(ctx, n, V, dt):
+    """More rows of 480 KB and more than the device has SMs: clusters take several each."""
+    b = Batch(n, V, dt, n + V, T=1.1, masked=0.05, out=0.2)
+    check_ppo(ctx, b)
+    p, (_, g), stats = Ppo(b), b.grad(pad=3), empty(5)
+    p.call(ctx, b, g, stats=stats)
+    ctx.sync()
+    p.call(ctx, b, b.logits)
+    ctx.sync()
+    assert bool((b.logits == g).all())
+
+
+def test_distill_very_long_rows(ctx):
+    b = Batch(160, 122_003, "f32", 5, T=1.3)
+    check_distill(ctx, b, 1024)

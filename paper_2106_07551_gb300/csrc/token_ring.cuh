@@ -197,7 +197,7 @@ __device__ __forceinline__ void zero_entries(T* g, int j0, int j1) {
 template <int kOp, int kThreads>
 __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
     Totals v{};
-    constexpr int kAt = 8;                           // loads in flight
+    constexpr int kAt = 16;                          // loads in flight
     for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kAt * kThreads) {
         float4 q[kAt];
 #pragma unroll

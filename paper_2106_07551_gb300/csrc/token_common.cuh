@@ -538,7 +538,14 @@ __device__ __forceinline__ bool last_of(unsigned* ticket, unsigned of) {
 // A call's rows (token_pairs.cu), by the kernel that takes their length.
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 // Short rows (token_short.cuh), by type.
-constexpr int kShortVecs = 512;                      // most 16-byte vectors of a short row
+// Most 16-byte vectors of a short row; longer ones go through the ring, which costs some
+// microsecond a row and SM. us, short and ring, bf16: policy loss of 10,000 rows of 4,300
+// entries 49 and 73, of 6,000 60 and 74, of 8,000 81 and 80 (2,000 rows: 33 and 27);
+// log-probabilities of 16,000 rows of 4,300 entries 35 and 55, of 6,000 47 and 54, of 8,000
+// 67 and 55. And of a row whose pair's gradient is taken by a warp: longer ones stream past
+// it in parts (the preference call on 8,192 rows of 3,001 entries 42 us by warps, 48 in
+// parts, of 4,000 43 and 44, of 6,000 64 and 60).
+constexpr int kShortVecs = 768, kShortGradVecs = 512;
 cudaError_t launch_token_short_f32(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_short_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_short_f16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);

@@ -129,9 +129,9 @@ __global__ void __launch_bounds__(kGradT) token_pair_grad_kernel(TokenArgs a, in
     }
 }
 
-bool is_short(const TokenArgs& a) {
+bool is_short(const TokenArgs& a, int op) {
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
-    return (a.V + 2 * (int64_t)W - 2) / W <= kShortVecs;
+    return (a.V + 2 * (int64_t)W - 2) / W <= (op == kTokPairGrad ? kShortGradVecs : kShortVecs);
 }
 
 cudaError_t launch_short(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
@@ -175,7 +175,7 @@ cudaError_t launch_pair_grad(const TokenArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
-    return a.n == 0 || is_short(a) ? launch_short(a, op, n_sm, s) : launch_ring(a, op, n_sm, s);
+    return a.n == 0 || is_short(a, op) ? launch_short(a, op, n_sm, s) : launch_ring(a, op, n_sm, s);
 }
 
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
@@ -183,7 +183,7 @@ cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     e = launch_after(token_pairs_kernel, (unsigned)(a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm), kPairT, s, a);
     if (e != cudaSuccess || !a.g || a.n == 0) return e;
-    return is_short(a) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_pair_grad(a, s);
+    return is_short(a, kTokPairGrad) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_pair_grad(a, s);
 }
 
 }  // namespace malib

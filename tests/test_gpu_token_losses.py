@@ -897,3 +897,25 @@ def test_very_long_rows_one_after_another(ctx, n, V, dt):
 def test_distill_very_long_rows(ctx):
     b = Batch(160, 122_003, "f32", 5, T=1.3)
     check_distill(ctx, b, 1024)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("vectors", [64, 128, 256, 512, 768])
+@pytest.mark.parametrize("past", [-1, 0, 1])
+def test_lengths_where_the_kernel_changes(ctx, dt, vectors, past):
+    """Rows of as many 16-byte vectors as one kernel takes, one entry less and one more,
+    aligned and not, gradients aligned alike and differently."""
+    W = 4 if dt == "f32" else 8
+    for V, pad in ((vectors * W + past, 0), (vectors * W - W + 1 + past, 1)):
+        b = Batch(41, V, dt, V, T=0.8, masked=0.1, out=0.2, pad=pad)
+        check_logprob(ctx, b)
+        check_ppo(ctx, b)
+        check_pref(ctx, b, 4)
+        p, (_, g) = Ppo(b), b.grad(pad=3)
+        p.call(ctx, b, g)
+        ctx.sync()
+        _, h = b.grad()
+        p.call(ctx, b, h)
+        ctx.sync()
+        assert bool((g == h).all())
+        check_distill(ctx, Batch(41, V, dt, V + 1, T=1.5, out=0.0, pad=pad), 33, tdt=dt)

@@ -493,8 +493,9 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
  * 0, no teacher entry, or logits that are all -infinity. They add nothing to
  * losses, sequence sums and statistics, their outputs per row are 0 and their
  * gradient rows are written as 0.
- * All arithmetic is fp32 with statistics summed in fp64 in a fixed order (the same
- * call gives the same bits); the gradient is rounded once to the logits' type.
+ * All arithmetic is fp32, in a fixed order (the same call gives the same bits); sums
+ * over rows carry their rounding errors along; the gradient is rounded once to the
+ * logits' type.
  * All buffers are DEVICE memory of the context's device, aligned to their element;
  * the context needs no population. Calls are asynchronous on the context's
  * stream and allocate at most their first time at a size (context-owned work

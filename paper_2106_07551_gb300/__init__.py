@@ -154,20 +154,30 @@ def alloc_eval_dump(env_kind: int, n_pairs: int, n_dump: int, device="cuda"):
     return out
 
 
+class _Types:
+    """torch's types, looked up once: the token losses' checks run on every call."""
+
+    f32 = i32 = i64 = None
+    codes: dict = {}
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.f32, cls.i32, cls.i64 = torch.float32, torch.int32, torch.int64
+        cls.codes = {torch.float32: MALIB_F32, torch.bfloat16: MALIB_BF16, torch.float16: MALIB_F16}
+
+
 def _vector(x, n, dtype, what):
     """Address of a contiguous tensor of n values of a type (None -> NULL)."""
     if x is None:
         return None
-    if str(x.dtype) != dtype or x.numel() != n or not x.is_contiguous():
+    if x.dtype is not dtype or x.numel() != n or not x.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} values")
     return x.data_ptr()
 
 
-_TOKEN_DTYPES = {"torch.float32": MALIB_F32, "torch.bfloat16": MALIB_BF16, "torch.float16": MALIB_F16}
-
-
 def _token_dtype(x, what):
-    code = _TOKEN_DTYPES.get(str(x.dtype))
+    code = _Types.codes.get(x.dtype)
     if code is None:
         raise ValueError(f"{what} must be float32, bfloat16 or float16")
     return code
@@ -175,17 +185,21 @@ def _token_dtype(x, what):
 
 def _token_rows(x, what):
     """(rows, vocabulary, row stride) of a matrix whose rows are contiguous."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{what} must have two dimensions (rows, vocabulary)")
-    n, V = x.shape
-    if V < 1 or (V > 1 and x.stride(1) != 1):
+    n, V = shape
+    ld, one = x.stride()
+    if V < 1 or (V > 1 and one != 1):
         raise ValueError(f"the rows of {what} must be contiguous")
-    return n, V, x.stride(0) if n > 1 else V
+    return n, V, ld if n > 1 else V
 
 
 def _token_batch(logits, tokens, temperature):
+    if not _Types.codes:
+        _Types.load()
     n, V, ld = _token_rows(logits, "logits")
-    return TokenBatch(logits.data_ptr(), _vector(tokens, n, "torch.int32", "tokens"), n, ld, V,
+    return TokenBatch(logits.data_ptr(), _vector(tokens, n, _Types.i32, "tokens"), n, ld, V,
                       _token_dtype(logits, "logits"), temperature)
 
 
@@ -193,7 +207,7 @@ def _token_grad(logits, grad, scale):
     if grad is None:
         return None
     n, V, ld = _token_rows(grad, "grad_out")
-    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+    if grad.dtype is not logits.dtype or (n, V) != logits.shape:
         raise ValueError("grad_out must have the shape and type of logits")
     return C.byref(TokenGrad(grad.data_ptr(), ld, scale))
 
@@ -368,8 +382,8 @@ class Context:
         b = _token_batch(logits, tokens, temperature)
         n = b.n_rows
         _check(self.lib, self.handle,
-               self.lib.malib_token_logprob(self.handle, C.byref(b), _vector(logp_out, n, "torch.float32", "logp_out"),
-                                            _vector(entropy_out, n, "torch.float32", "entropy_out")))
+               self.lib.malib_token_logprob(self.handle, C.byref(b), _vector(logp_out, n, _Types.f32, "logp_out"),
+                                            _vector(entropy_out, n, _Types.f32, "entropy_out")))
 
     def learn_token_ppo(self, logits, tokens, old_logp, advantage, grad_out=None, stats_out=None, weight=None,
                         ref_logp=None, logp_out=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0,
@@ -379,7 +393,7 @@ class Context:
         itself) and (rows counted, loss, clipped share, mean KL, mean entropy) into
         stats_out (fp32 [5])."""
         b = _token_batch(logits, tokens, temperature)
-        n, f32 = b.n_rows, "torch.float32"
+        n, f32 = b.n_rows, _Types.f32
         p = TokenPpo(_vector(old_logp, n, f32, "old_logp"), _vector(advantage, n, f32, "advantage"),
                      _vector(weight, n, f32, "weight"), _vector(ref_logp, n, f32, "ref_logp"), clip_low, clip_high,
                      kl_coef, entropy_coef)
@@ -396,10 +410,10 @@ class Context:
         into grad_out, the rewards [2 pairs] into reward_out and (pairs, loss, share
         of pairs in order, mean reward chosen, rejected) into stats_out (fp32 [5])."""
         b = _token_batch(logits, tokens, temperature)
-        n, f32, S = b.n_rows, "torch.float32", int(offsets.numel()) - 1
+        n, f32, S = b.n_rows, _Types.f32, int(offsets.numel()) - 1
         if S < 2 or S % 2:
             raise ValueError("offsets must hold 2 pairs + 1 values")
-        p = TokenPref(_vector(offsets, S + 1, "torch.int64", "offsets"), _vector(ref_logp, n, f32, "ref_logp"), S // 2,
+        p = TokenPref(_vector(offsets, S + 1, _Types.i64, "offsets"), _vector(ref_logp, n, f32, "ref_logp"), S // 2,
                       beta, label_smoothing)
         _check(self.lib, self.handle,
                self.lib.malib_learn_token_pref(self.handle, C.byref(b), C.byref(p),
@@ -414,12 +428,12 @@ class Context:
         grad_out, the rows' losses into loss_out [rows] and (rows counted, loss,
         mean row loss) into stats_out (fp32 [3])."""
         b = _token_batch(logits, None, temperature)
-        n, f32 = b.n_rows, "torch.float32"
+        n, f32 = b.n_rows, _Types.f32
         if teacher_ids.dim() != 2 or teacher_ids.shape[0] != n or teacher_logits.shape != teacher_ids.shape:
             raise ValueError("teacher_ids and teacher_logits must be [rows][top]")
         top = teacher_ids.shape[1]
-        p = TokenDistill(_vector(teacher_ids, n * top, "torch.int32", "teacher_ids"),
-                         _vector(teacher_logits, n * top, str(teacher_logits.dtype), "teacher_logits"),
+        p = TokenDistill(_vector(teacher_ids, n * top, _Types.i32, "teacher_ids"),
+                         _vector(teacher_logits, n * top, teacher_logits.dtype, "teacher_logits"),
                          _vector(weight, n, f32, "weight"), top, _token_dtype(teacher_logits, "teacher_logits"))
         _check(self.lib, self.handle,
                self.lib.malib_learn_token_distill(self.handle, C.byref(b), C.byref(p),

@@ -521,6 +521,25 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 // this lets the next one be launched, once every CTA has come here.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Launches a kernel that waits for the stream's previous one itself: what the launch takes
+// overlaps that one's end.
+template <class... Args, class... Given>
+cudaError_t launch_after(void (*kernel)(Args...), unsigned grid, unsigned threads, size_t bytes, cudaStream_t s,
+                         const Given&... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Args(args)...);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 // The calling CTA has stored what others will read; whether it is the last of `of` that
 // come here. The counter is back at 0 for the next call.
 __device__ __forceinline__ bool last_of(unsigned* ticket, unsigned of) {

@@ -150,30 +150,14 @@ cudaError_t launch_ring(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
     return launch_token_ring_f16(a, op, n_sm, s);
 }
 
-// Launches a kernel that waits for the stream's previous one itself.
-template <class... Args>
-cudaError_t launch_after(void (*kernel)(Args...), unsigned grid, unsigned threads, cudaStream_t s, Args... args) {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute at{};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.stream = s;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-    return e != cudaSuccess ? e : cudaGetLastError();
-}
-
 cudaError_t launch_pair_grad(const TokenArgs& a, cudaStream_t s) {
     const int W = a.dtype == MALIB_F32 ? 4 : 8;
     const int parts = (int)(((a.V + 2 * (int64_t)W - 2) / W + kGradVecs - 1) / kGradVecs);
     const int64_t total = a.n * parts;
     const unsigned grid = (unsigned)(total < (1 << 30) ? total : (1 << 30));
-    if (a.dtype == MALIB_F32) return launch_after(token_pair_grad_kernel<float>, grid, kGradT, s, a, parts);
-    if (a.dtype == MALIB_BF16) return launch_after(token_pair_grad_kernel<__nv_bfloat16>, grid, kGradT, s, a, parts);
-    return launch_after(token_pair_grad_kernel<__half>, grid, kGradT, s, a, parts);
+    if (a.dtype == MALIB_F32) return launch_after(token_pair_grad_kernel<float>, grid, kGradT, 0, s, a, parts);
+    if (a.dtype == MALIB_BF16) return launch_after(token_pair_grad_kernel<__nv_bfloat16>, grid, kGradT, 0, s, a, parts);
+    return launch_after(token_pair_grad_kernel<__half>, grid, kGradT, 0, s, a, parts);
 }
 
 }  // namespace
@@ -185,7 +169,7 @@ cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {
     cudaError_t e = a.n > 0 ? launch_token_rows(a, kTokLogp, n_sm, s) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    e = launch_after(token_pairs_kernel, (unsigned)(a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm), kPairT, s, a);
+    e = launch_after(token_pairs_kernel, (unsigned)(a.n_pairs < 4 * n_sm ? a.n_pairs : 4 * n_sm), kPairT, 0, s, a);
     if (e != cudaSuccess || !a.g || a.n == 0) return e;
     return is_short(a, kTokPairGrad) ? launch_short(a, kTokPairGrad, n_sm, s) : launch_pair_grad(a, s);
 }

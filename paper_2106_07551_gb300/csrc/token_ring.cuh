@@ -191,6 +191,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
         fence_proxy_async_smem();
     }
     __syncthreads();
+    wait_for_previous();
     if (kOp == kTokLogp) let_next_start();
     // The peers' barriers and memory are there before the first store to them: arrived here,
     // waited for where it is needed.
@@ -520,18 +521,21 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t units, cuda
         cudaFuncSetAttribute(token_ring_kernel<T, kOp, Ring>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingMost);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute at{};
+    cudaLaunchAttribute at[2] = {};
     cfg.gridDim = dim3((unsigned)((units ? units : 1) * sh.cluster));
     cfg.blockDim = dim3(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32));
     cfg.dynamicSmemBytes = (size_t)sh.stages * Ring::kConsumers * Ring::kPer * 16 +
                            (kOp == kTokDistill ? 2 * a.top * sizeof(TopEntry) : 0);
     cfg.stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
     if (sh.cluster > 1) {
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim.x = sh.cluster;
-        at.val.clusterDim.y = at.val.clusterDim.z = 1;
-        cfg.attrs = &at;
-        cfg.numAttrs = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = sh.cluster;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
     }
     if (units == 0) {
         int most = 0;

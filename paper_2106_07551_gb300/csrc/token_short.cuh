@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G;
     const int64_t step = (int64_t)gridDim.x * kShortWarps * kRows;
     Totals total{};
+    wait_for_previous();
     if (kOp == kTokLogp) let_next_start();
     for (int64_t row0 = ((int64_t)blockIdx.x * kShortWarps + warp) * kRows; row0 < a.n; row0 += step) {
         const bool in_range = row0 + lane / G < a.n;
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, 
     uint4* own = reinterpret_cast<uint4*>(shared) + warp * slab;
     TopEntry* list = reinterpret_cast<TopEntry*>(shared + (size_t)kShortWarps * slab * 16) + warp * a.top;
     Totals total{};
+    wait_for_previous();
     if (kOp == kTokLogp) let_next_start();
     for (int64_t row = (int64_t)blockIdx.x * kShortWarps + warp; row < a.n; row += (int64_t)gridDim.x * kShortWarps) {
         const T* z = static_cast<const T*>(a.z) + row * a.ld;
@@ -284,6 +286,7 @@ __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) 
     const int tid = threadIdx.x;
     const bool flat_z = a.ld == a.V, flat_g = a.gld == a.V;
     Totals total{};
+    wait_for_previous();
     if (kOp == kTokLogp) let_next_start();
     for (int64_t row0 = (int64_t)blockIdx.x * kShortThreads; row0 < a.n; row0 += (int64_t)gridDim.x * kShortThreads) {
         const int rows = (int)min((int64_t)kShortThreads, a.n - row0), entries = rows * a.V;
@@ -380,8 +383,7 @@ cudaError_t launch_tiny(const TokenArgs& a, int n_sm, cudaStream_t s) {
     const cudaError_t e =
         short_grid(token_tiny_kernel<T, kOp, N>, 0, a.n, kShortThreads, kOp == kTokPpo && a.stats, n_sm, &grid);
     if (e != cudaSuccess) return e;
-    token_tiny_kernel<T, kOp, N><<<grid, kShortThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    return launch_after(token_tiny_kernel<T, kOp, N>, grid, kShortThreads, 0, s, a);
 }
 
 template <class T, int kOp, int G, int N>
@@ -398,8 +400,7 @@ cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
     const cudaError_t e =
         short_grid(token_short_kernel<T, kOp, G, N>, bytes, a.n, kShortWarps * (32 / G), stats, n_sm, &grid);
     if (e != cudaSuccess) return e;
-    token_short_kernel<T, kOp, G, N><<<grid, kShortThreads, bytes, s>>>(a);
-    return cudaGetLastError();
+    return launch_after(token_short_kernel<T, kOp, G, N>, grid, kShortThreads, bytes, s, a);
 }
 
 template <class T, int kOp>
@@ -413,8 +414,7 @@ cudaError_t launch_slab(const TokenArgs& a, int nv, int n_sm, cudaStream_t s) {
     const bool stats = (kOp == kTokPpo || kOp == kTokDistill) && a.stats;
     e = short_grid(token_slab_kernel<T, kOp>, bytes, a.n, kShortWarps, stats, n_sm, &grid);
     if (e != cudaSuccess) return e;
-    token_slab_kernel<T, kOp><<<grid, kShortThreads, bytes, s>>>(a, slab);
-    return cudaGetLastError();
+    return launch_after(token_slab_kernel<T, kOp>, grid, kShortThreads, bytes, s, a, slab);
 }
 
 // Lanes a row and vectors a lane by the most vectors a row has.

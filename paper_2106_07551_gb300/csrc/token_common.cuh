@@ -515,14 +515,16 @@ __device__ __forceinline__ void write_stats(const TokenArgs& a, const Totals& v)
     }
 }
 
-// The kernels of a preference call are launched while the one before still runs. This
-// waits until that one is complete and what it wrote is there;
+// The kernels are launched while the stream's one before still runs. This, at every kernel's
+// start, waits until that one is complete and what it wrote is there;
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// this lets the next one be launched, once every CTA has come here.
+// this lets the next one be launched, once every CTA has come here: in the kernels of a
+// preference call, the others' end is near enough.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Launches a kernel that waits for the stream's previous one itself: what the launch takes
-// overlaps that one's end.
+// overlaps that one's end. us a call without and with this: one row of 131,072 entries 7.5
+// and 6.5, 102,400 rows of 15 12.2 and 11.0, 4,096 rows of 32,768 85 and 82.5.
 template <class... Args, class... Given>
 cudaError_t launch_after(void (*kernel)(Args...), unsigned grid, unsigned threads, size_t bytes, cudaStream_t s,
                          const Given&... args) {

@@ -18,7 +18,8 @@ __device__ __forceinline__ Sum2 warp_sum2(Sum2 v) {
 // One CTA a pair: the rewards of its two sequences, the loss, and the factor of its
 // rows' gradients. Bound by latency (a row's 16 bytes from L2, sums, a logarithm): some 5 us
 // between the kernels before and after it, which are launched while it and the statistics
-// run (333 rows of 4 pairs 24 us a call without that, 22 with it).
+// run (333 rows of 4 pairs 24 us a call without that, 22 with it, 19 where the call's first
+// kernel overlaps the stream's one before as well).
 __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     __shared__ Sum2 red[kPairT / 32];
     __shared__ float factor;

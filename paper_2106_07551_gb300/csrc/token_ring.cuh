@@ -30,7 +30,7 @@
 // (bf16, 4,096 rows of which a quarter is left out): 64 KB rows 86 with the small shape, 87
 // and 113 with two and one CTAs of the large one; 100 KB 130, 136, 166; 128 KB 174, 157,
 // 180; 192 KB 287, 254, 249; 16,384 rows of 256 KB 1,648, 1,562, 1,281 (6.4 TB/s).
-// Log-probabilities of 8,192 rows of 128 KB, a quarter left out: 121 us (6.7 TB/s).
+// Log-probabilities of 8,192 rows of 128 KB, a quarter left out: 119 us (6.8 TB/s).
 //
 // Rows start at any element: a row's vectors are the 16-byte blocks of its address, the
 // full ones copied in bulk, a partial first or last one filled in by the producer's

@@ -5,8 +5,8 @@
 // Bound by instructions: some 15 an entry for both sweeps, and the row's loss, which takes
 // more than the entries of the shortest rows: rows of up to 8 vectors take 8 lanes, so that
 // a warp computes four rows' losses at once, and rows of a few entries one lane each.
-// Measured on bf16 rows, policy loss with every term: 20,000 rows of 4,000 entries 71 us
-// (280 MB: 3.9 TB/s), of 300 entries 23 us.
+// Measured on bf16 rows, policy loss with every term: 20,000 rows of 4,000 entries 69 us
+// (280 MB: 4.1 TB/s), of 300 entries 20 us.
 // The rows' shares of the statistics are summed by the lanes that take them, a fixed set
 // of rows each, then by block and call in a fixed order.
 #pragma once
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, 
 // without a gap go through shared memory, so that neighbouring threads read and write
 // neighbouring entries; others entry by entry. Bound by the launch and by instructions:
 // 102,400 rows of 15 fp32 entries with every term of the policy loss took 26 us with 8
-// lanes a row, 18 with a thread a row that reads its entries itself, and take 12 with this.
+// lanes a row, 18 with a thread a row that reads its entries itself, and take 10 to 11 with this.
 template <class T, int kOp, int N>
 __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) {
     __shared__ T tile[kShortThreads * N];

@@ -25,6 +25,9 @@
  *    (an invalid policy id in a device-side pair table, an expired bounded
  *    wait) are reported by the next malib_sync().
  *  - Threads: one context must not be used from two threads at once.
+ *  - Graphs: work space that a context owns stays where a captured call found it,
+ *    also when a larger call needs more, until malib_destroy(); a graph must not be
+ *    replayed after that, and its replays are ordered like the context's other calls.
  */
 #ifndef MALIB_H
 #define MALIB_H

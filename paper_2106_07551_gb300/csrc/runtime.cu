@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <utility>
 #include <vector>
@@ -14,6 +15,7 @@
 #include "internal.h"
 #include "malib.h"
 #include "tc_common.cuh"
+#include "work_space.h"
 
 using namespace malib;
 
@@ -73,6 +75,7 @@ struct malib_ctx {
     int64_t token_fixed_cap = 0;
     uint8_t* token_rows = nullptr;     // a row's statistics or share of a call's
     int64_t token_rows_cap = 0;
+    std::vector<void*> outgrown;       // blocks that a larger one replaced: captured graphs may hold them
 
     int64_t launches = 0;
     bool timing = false;
@@ -123,17 +126,29 @@ int cuda_fail(malib_ctx* c, cudaError_t e, const char* what) {
 // Device memory of the context's own device (or managed memory).
 bool is_device_ptr(const malib_ctx* c, const void* p) { return ptr_where(p, c->device) == kPtrHere; }
 
+// Where a context's work space comes from (work_space.h): its stream's memory pool.
+struct CtxMem {
+    malib_ctx* c;
+    const char* what;
+    int allocate(void** p, int64_t bytes) {
+        CK(cudaMallocAsync(p, (size_t)bytes, c->stream), what);
+        return MALIB_OK;
+    }
+    int keep(void* p) {
+        try {
+            c->outgrown.push_back(p);
+        } catch (const std::bad_alloc&) {
+            return fail(c, MALIB_ENOMEM, "%s: out of host memory", what);
+        }
+        return MALIB_OK;
+    }
+    void release(void* p) { cudaFreeAsync(p, c->stream); }
+};
+
 template <class T>
 int ensure(malib_ctx* c, T*& p, int64_t& cap, int64_t need, const char* what) {
-    if (need <= cap) return MALIB_OK;
-    int64_t n = cap > 0 ? cap : 64;
-    while (n < need) n *= 2;
-    if (p) cudaFreeAsync(p, c->stream);
-    p = nullptr;
-    cap = 0;
-    CK(cudaMallocAsync((void**)&p, (size_t)n * sizeof(T), c->stream), what);
-    cap = n;
-    return MALIB_OK;
+    CtxMem mem{c, what};
+    return grow(mem, p, cap, need);
 }
 
 int64_t mlp_param_floats(const int* d) {
@@ -449,6 +464,7 @@ void malib_destroy(malib_ctx* c) {
     cudaFree(c->learn_grad);
     cudaFree(c->token_fixed);
     cudaFree(c->token_rows);
+    for (void* p : c->outgrown) cudaFree(p);
     cudaFree(c->d_stage);
     cudaFree(c->d_jobs);
     delete c;

@@ -28,6 +28,8 @@
  *  - Graphs: work space that a context owns stays where a captured call found it,
  *    also when a larger call needs more, until malib_destroy(); a graph must not be
  *    replayed after that, and its replays are ordered like the context's other calls.
+ *    A call whose work space would have to grow while the stream is captured is
+ *    refused (MALIB_ESTATE, nothing is enqueued): make one of its size before.
  */
 #ifndef MALIB_H
 #define MALIB_H
@@ -43,7 +45,8 @@ typedef enum malib_status {
     MALIB_EINVAL = -1,        /* bad argument (null pointer, size, id, layout) */
     MALIB_ENOMEM = -2,        /* device or host allocation failed */
     MALIB_ECUDA = -3,         /* a CUDA runtime call failed */
-    MALIB_ESTATE = -4,        /* no population loaded, or env/population mismatch */
+    MALIB_ESTATE = -4,        /* no population loaded, or env/population mismatch; or work
+                                 space that would grow during a stream capture */
     MALIB_ETIMEOUT = -5,      /* a bounded device-side wait expired */
     MALIB_EUNSUPPORTED = -6,  /* valid request outside the built kernels' shapes */
     MALIB_ENOTCONVERGED = -7  /* an iterative solver reached its iteration limit */
@@ -504,7 +507,7 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
  * stream and allocate at most their first time at a size (context-owned work
  * space: a context's calls must be ordered, also across malib_set_stream). A token
  * or teacher entry >= V leaves its row, or the entry, out and gives MALIB_EINVAL
- * at the next malib_sync. n_rows == 0 is valid. Errors: EINVAL, ENOMEM, ECUDA.
+ * at the next malib_sync. n_rows == 0 is valid. Errors: EINVAL, ENOMEM, ECUDA, ESTATE.
  */
 typedef struct malib_token_batch {
     const void* logits;       /* [n_rows][ld], the first vocab of each row are used */

@@ -130,6 +130,13 @@ bool is_device_ptr(const malib_ctx* c, const void* p) { return ptr_where(p, c->d
 struct CtxMem {
     malib_ctx* c;
     const char* what;
+    int may_grow() {
+        cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(c->stream, &st) == cudaSuccess && st == cudaStreamCaptureStatusNone) return MALIB_OK;
+        cudaGetLastError();
+        return fail(c, MALIB_ESTATE,
+                    "%s would have to grow during a stream capture: make a call of this size before it", what);
+    }
     int allocate(void** p, int64_t bytes) {
         CK(cudaMallocAsync(p, (size_t)bytes, c->stream), what);
         return MALIB_OK;

@@ -3,9 +3,11 @@
 // A captured graph holds the addresses that its calls were given at the capture. A block that
 // is outgrown is therefore kept, as long as the context, and not freed: a graph that is
 // replayed after a larger call still has its own. Blocks at least double, so what is kept
-// is smaller than what is in use.
+// is smaller than what is in use. While the stream is captured nothing grows: the block would
+// belong to the graph, and later calls would use it outside the graph's runs.
 //
 // Plain C++: Mem is where blocks come from. Its functions return 0 or the status to report.
+//   int may_grow();                         // refuses while the stream is captured
 //   int allocate(void** p, int64_t bytes);
 //   int keep(void* p);                      // p lives as long as the context
 //   void release(void* p);                  // p was never used
@@ -21,9 +23,10 @@ int grow(Mem& mem, T*& p, int64_t& cap, int64_t need) {
     if (need <= cap) return 0;
     int64_t n = cap > 0 ? cap : 64;
     while (n < need) n *= 2;
-    void* fresh = nullptr;
-    int r = mem.allocate(&fresh, n * (int64_t)sizeof(T));
+    int r = mem.may_grow();
     if (r != 0) return r;
+    void* fresh = nullptr;
+    if ((r = mem.allocate(&fresh, n * (int64_t)sizeof(T))) != 0) return r;
     if (p && (r = mem.keep(p)) != 0) {
         mem.release(fresh);
         return r;

@@ -77,3 +77,39 @@ def test_replay_after_larger_calls():
             cap.replay()
             c.sync()
             assert cap.same() and bool((stats == first).all()) and float(stats[0]) == n
+
+
+@pytest.mark.parametrize("warm", [0, 40])
+def test_growth_during_a_capture_is_refused(warm):
+    """Nothing of the refused call is in the graph, and the plain call after it is good; a call that
+    needs no more than there is can be captured."""
+    torch = need_gpu()
+    from paper_2106_07551_gb300 import Context, MalibError
+    stream = torch.cuda.Stream()
+    n, V = 2000, 129
+    with torch.cuda.stream(stream), Context(0, stream) as c:
+        b = Batch(n, V, "f32", 3)
+        p, (_, g), stats = Ppo(b), b.grad(), empty(5)
+        tok, old, adv = cuda(b.tok), cuda(p.old), cuda(p.adv)
+        call = lambda m: c.learn_token_ppo(b.logits[:m], tok[:m], old[:m], adv[:m], g[:m], stats)  # noqa: E731
+        if warm:
+            call(warm)
+            c.sync()
+        g.fill_(7.0)
+        graph, mark = torch.cuda.CUDAGraph(), empty(1)
+        with torch.cuda.graph(graph, stream=stream):
+            with pytest.raises(MalibError, match="ESTATE.*capture"):
+                call(n)
+            if warm:
+                call(warm)
+            mark.fill_(1.0)
+        graph.replay()
+        stream.synchronize()
+        assert float(mark) == 1.0 and bool((g[warm:] == 7.0).all()) and (not warm or bool((g[:warm] != 7.0).all()))
+        call(n)
+        c.sync()
+        first = (g.clone(), stats.clone())
+        graph.replay()
+        call(n)
+        c.sync()
+        assert bool((g == first[0]).all()) and bool((stats == first[1]).all()) and float(stats[0]) == (b.tok >= 0).sum()

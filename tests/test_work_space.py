@@ -15,7 +15,8 @@ struct Host {
     std::set<void*> live;
     std::vector<void*> kept;
     std::vector<int64_t> sizes;
-    int fail_allocate = 0, fail_keep = 0;
+    int fail_allocate = 0, fail_keep = 0, captured = 0;
+    int may_grow() { return captured ? -4 : 0; }
     int allocate(void** p, int64_t bytes) {
         if (fail_allocate) return fail_allocate;
         *p = std::malloc(16);
@@ -81,4 +82,22 @@ def test_a_failure_leaves_the_block(tmp_path):
     CHECK(grow(h, p, cap, 1000) == -2 && p == q && cap == had && h.live.size() == 1);
     h.fail_keep = 0;
     CHECK(grow(h, p, cap, 1000) == 0 && p != q && h.live.count(q));
+    """)
+
+
+def test_nothing_grows_during_a_capture(tmp_path):
+    """A block taken during a capture would belong to the graph."""
+    run(tmp_path, r"""
+    Host h;
+    int* p = nullptr;
+    int64_t cap = 0;
+    h.captured = 1;
+    CHECK(grow(h, p, cap, 10) == -4 && !p && cap == 0 && h.sizes.empty());
+    h.captured = 0;
+    CHECK(grow(h, p, cap, 100) == 0);
+    int* const q = p;
+    const int64_t had = cap;
+    h.captured = 1;
+    CHECK(grow(h, p, cap, had) == 0 && p == q);
+    CHECK(grow(h, p, cap, had + 1) == -4 && p == q && cap == had && h.sizes.size() == 1 && h.kept.empty());
     """)

@@ -72,7 +72,6 @@ struct malib_ctx {
     float* learn_grad = nullptr;       // the gradient when the caller's buffer is host memory
     int64_t learn_grad_cap = 0;
     uint8_t* token_fixed = nullptr;    // token losses: counters, partial sums
-    int64_t token_fixed_cap = 0;
     uint8_t* token_rows = nullptr;     // a row's statistics or share of a call's
     int64_t token_rows_cap = 0;
     std::vector<void*> outgrown;       // blocks that a larger one replaced: captured graphs may hold them
@@ -139,6 +138,10 @@ struct CtxMem {
     }
     int allocate(void** p, int64_t bytes) {
         CK(cudaMallocAsync(p, (size_t)bytes, c->stream), what);
+        return MALIB_OK;
+    }
+    int clear(void* p, int64_t bytes) {
+        CK(cudaMemsetAsync(p, 0, (size_t)bytes, c->stream), what);
         return MALIB_OK;
     }
     int keep(void* p) {
@@ -404,12 +407,9 @@ int ctx_scratch(void* ctx, int64_t bytes, void** out) {
 int ctx_token_work(void* ctx, int64_t bytes, void** fixed_out, void** out) {
     malib_ctx* c = static_cast<malib_ctx*>(ctx);
     if (!c || bytes < 0) return MALIB_EINVAL;
-    int r;
-    if (!c->token_fixed) {
-        if ((r = ensure(c, c->token_fixed, c->token_fixed_cap, kTokenFixedBytes, "token work space")) != MALIB_OK) return r;
-        CK(cudaMemsetAsync(c->token_fixed, 0, kTokenFixedBytes, c->stream), "token work space");
-    }
-    if ((r = ensure(c, c->token_rows, c->token_rows_cap, bytes, "token work space")) != MALIB_OK) return r;
+    CtxMem mem{c, "token work space"};
+    int r = take_cleared(mem, c->token_fixed, kTokenFixedBytes);
+    if (r != MALIB_OK || (r = ensure(c, c->token_rows, c->token_rows_cap, bytes, "token work space")) != MALIB_OK) return r;
     *fixed_out = c->token_fixed;
     *out = c->token_rows;
     return MALIB_OK;

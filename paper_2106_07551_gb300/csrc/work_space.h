@@ -9,6 +9,7 @@
 // Plain C++: Mem is where blocks come from. Its functions return 0 or the status to report.
 //   int may_grow();                         // refuses while the stream is captured
 //   int allocate(void** p, int64_t bytes);
+//   int clear(void* p, int64_t bytes);      // zeros
 //   int keep(void* p);                      // p lives as long as the context
 //   void release(void* p);                  // p was never used
 #pragma once
@@ -33,6 +34,23 @@ int grow(Mem& mem, T*& p, int64_t& cap, int64_t need) {
     }
     p = static_cast<T*>(fresh);
     cap = n;
+    return 0;
+}
+
+// Takes the block p of a fixed size that starts as zeros. Where it fails, p stays null: the next
+// call starts again.
+template <class Mem, class T>
+int take_cleared(Mem& mem, T*& p, int64_t n) {
+    if (p) return 0;
+    T* fresh = nullptr;
+    int64_t cap = 0;
+    int r = grow(mem, fresh, cap, n);
+    if (r != 0) return r;
+    if ((r = mem.clear(fresh, n * (int64_t)sizeof(T))) != 0) {
+        mem.release(fresh);
+        return r;
+    }
+    p = fresh;
     return 0;
 }
 

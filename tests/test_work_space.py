@@ -15,13 +15,18 @@ struct Host {
     std::set<void*> live;
     std::vector<void*> kept;
     std::vector<int64_t> sizes;
-    int fail_allocate = 0, fail_keep = 0, captured = 0;
+    int fail_allocate = 0, fail_keep = 0, fail_clear = 0, captured = 0, cleared = 0;
     int may_grow() { return captured ? -4 : 0; }
     int allocate(void** p, int64_t bytes) {
         if (fail_allocate) return fail_allocate;
         *p = std::malloc(16);
         live.insert(*p);
         sizes.push_back(bytes);
+        return 0;
+    }
+    int clear(void* p, int64_t bytes) {
+        if (fail_clear) return fail_clear;
+        cleared += live.count(p) && bytes == 1000;
         return 0;
     }
     int keep(void* p) {
@@ -100,4 +105,21 @@ def test_nothing_grows_during_a_capture(tmp_path):
     h.captured = 1;
     CHECK(grow(h, p, cap, had) == 0 && p == q);
     CHECK(grow(h, p, cap, had + 1) == -4 && p == q && cap == had && h.sizes.size() == 1 && h.kept.empty());
+    """)
+
+
+def test_a_block_that_was_not_cleared_is_not_used(tmp_path):
+    """The counters of a context start as zeros, also after a first call that could not write them."""
+    run(tmp_path, r"""
+    Host h;
+    char* p = nullptr;
+    h.captured = 1;
+    CHECK(take_cleared(h, p, 1000) == -4 && !p);
+    h.captured = 0;
+    h.fail_clear = -3;
+    CHECK(take_cleared(h, p, 1000) == -3 && !p && h.live.empty());
+    h.fail_clear = 0;
+    CHECK(take_cleared(h, p, 1000) == 0 && p && h.cleared == 1 && h.live.size() == 1);
+    char* const q = p;
+    CHECK(take_cleared(h, p, 1000) == 0 && p == q && h.cleared == 1);
     """)

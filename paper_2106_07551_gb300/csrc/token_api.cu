@@ -158,7 +158,7 @@ int malib_learn_token_ppo(malib_ctx* ctx, const malib_token_batch* batch, const 
     c.a.ent = loss->entropy_coef;
     c.a.logp = logp_out;
     c.a.stats = stats_out;
-    return c.done(launch_token_rows(c.a, kTokPpo, c.v.n_sm, c.v.stream), 1);
+    return c.done(launch_token_rows(c.a, kTokPpo, c.v.n_sm, c.v.stream), c.a.n > 0 || stats_out ? 1 : 0);
 }
 
 int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_pref* loss,
@@ -209,7 +209,7 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
     c.a.top = loss->top;
     c.a.loss = loss_out;
     c.a.stats = stats_out;
-    return c.done(launch_token_rows(c.a, kTokDistill, c.v.n_sm, c.v.stream), 1);
+    return c.done(launch_token_rows(c.a, kTokDistill, c.v.n_sm, c.v.stream), c.a.n > 0 || stats_out ? 1 : 0);
 }
 
 }  // extern "C"

@@ -164,7 +164,13 @@ cudaError_t launch_pair_grad(const TokenArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
-    return a.n == 0 || is_short(a, op) ? launch_short(a, op, n_sm, s) : launch_ring(a, op, n_sm, s);
+    if (a.n == 0) {
+        // No rows: the statistics of none, written by a kernel whose launch does not go by the vocabulary.
+        TokenArgs none = a;
+        none.V = 1;
+        return a.stats ? launch_short(none, op, n_sm, s) : cudaSuccess;
+    }
+    return is_short(a, op) ? launch_short(a, op, n_sm, s) : launch_ring(a, op, n_sm, s);
 }
 
 cudaError_t launch_token_pairs(const TokenArgs& a, int n_sm, cudaStream_t s) {

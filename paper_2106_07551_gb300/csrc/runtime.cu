@@ -112,6 +112,7 @@ int fail(malib_ctx* c, int code, const char* fmt, ...) {
 }
 
 int cuda_fail(malib_ctx* c, cudaError_t e, const char* what) {
+    cudaGetLastError();               // reported here, not by the caller's next check
     return fail(c, e == cudaErrorMemoryAllocation ? MALIB_ENOMEM : MALIB_ECUDA, "%s: %s", what,
                 cudaGetErrorString(e));
 }

@@ -104,8 +104,13 @@ struct Call {
         return MALIB_OK;
     }
 
+    // The launches' own status: the runtime's last error may be the caller's, and one of a launch
+    // does not stay there for the caller's next check.
     int done(cudaError_t e, int launches) {
-        if (e != cudaSuccess) return ctx_fail(ctx, MALIB_ECUDA, cudaGetErrorString(e));
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            return ctx_fail(ctx, MALIB_ECUDA, cudaGetErrorString(e));
+        }
         ctx_count_launches(ctx, launches);
         return MALIB_OK;
     }

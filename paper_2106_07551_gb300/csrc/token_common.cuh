@@ -538,8 +538,7 @@ cudaError_t launch_after(void (*kernel)(Args...), unsigned grid, unsigned thread
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Args(args)...);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, kernel, Args(args)...);
 }
 
 // The calling CTA has stored what others will read; whether it is the last of `of` that

@@ -543,8 +543,7 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t units, cuda
         if (e != cudaSuccess) return e;
         cfg.gridDim.x = (unsigned)(most < 1 ? 1 : most < a.n ? most : a.n) * sh.cluster;
     }
-    e = cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp, Ring>, a, sh);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, token_ring_kernel<T, kOp, Ring>, a, sh);
 }
 
 template <class T, int kOp>

@@ -56,8 +56,9 @@ def ppo(z, tokens, old, adv, weight, ref=None, lo=0.2, hi=0.2, ck=0.0, ch=0.0, T
             if ref is not None:
                 r = ref[i] - logp[i]
                 kl[i] = np.expm1(r) - r
-                l[i] += ck * kl[i]
-                slope[i] -= ck * np.expm1(r)
+                if ck:                                       # one that is only reported adds 0, however large
+                    l[i] += ck * kl[i]
+                    slope[i] -= ck * np.expm1(r)
             one = np.zeros(lp.shape[1])
             one[tokens[i]] = 1.0
             grad[i] = weight[i] / T * (slope[i] * (one - p[i]) - ch * dH[i])

@@ -404,8 +404,10 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
     if (a.ref) {
         const float d = in.ref - logp, e = expm1f(d);
         *kl = e - d;
-        l = fmaf(a.kl, *kl, l);
-        slope = fmaf(-a.kl, e, slope);
+        if (a.kl != 0.f) {                           // a term that is only reported adds 0, also where e is infinite
+            l = fmaf(a.kl, *kl, l);
+            slope = fmaf(-a.kl, e, slope);
+        }
     }
     *loss = l;
     *clipped = clip ? 1.f : 0.f;

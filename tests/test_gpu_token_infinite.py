@@ -1,0 +1,55 @@
+"""The token losses where a factor of the formulas is infinite or overflows fp32: a term whose
+coefficient is 0 adds 0, an infinite value stays infinite and does not become NaN, and masked
+entries keep gradient 0."""
+import numpy as np
+import pytest
+
+from gpu_util import context
+from oracle import token_loss as tl
+from test_gpu_token_losses import HALF_ULP, TINY, Batch, cuda, empty
+
+pytestmark = pytest.mark.gpu
+
+# one length for each kernel: a thread a row, 8 lanes, a warp in registers, a warp through shared
+# memory, the ring, the ring in clusters (few rows)
+LENGTHS = [12, 40, 300, 5000, 40_000, 150_001]
+TYPES = ["f32", "bf16", "f16"]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = context()
+    yield c
+    c.sync()
+    c.close()
+
+
+def rows(V, dt, seed, pad=0):
+    """Four rows with masked entries, whose tokens are not; and their ln p."""
+    b = Batch(4, V, dt, seed, masked=0.3, out=0.0, pad=pad)
+    return b, tl.logprob(b.z, b.tok)[0]
+
+
+def ppo(ctx, b, old, adv, g=None, **kw):
+    logp, stats = empty(b.n), empty(5)
+    kw = {k: cuda(np.asarray(v, np.float32)) if k == "ref_logp" and v is not None else v for k, v in kw.items()}
+    ctx.learn_token_ppo(b.logits, cuda(b.tok), cuda(np.asarray(old, np.float32)), cuda(np.asarray(adv, np.float32)), g,
+                        stats, logp_out=logp, **kw)
+    ctx.sync()
+    return logp.cpu().numpy(), stats.cpu().numpy()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LENGTHS)
+def test_reference_with_coefficient_zero(ctx, V, dt):
+    """The KL reported alone: no bit of loss and gradient differs from the call without a
+    reference, also where e^(ref - ln p) exceeds fp32."""
+    b, lp = rows(V, dt, V)
+    adv, old = [1, -1, 0.5, 2], lp + 0.1
+    (_, plain), (_, with_ref) = b.grad(), b.grad()
+    logp0, s0 = ppo(ctx, b, old, adv, plain, entropy_coef=0.01)
+    logp1, s1 = ppo(ctx, b, old, adv, with_ref, entropy_coef=0.01, ref_logp=lp + [0.1, 100, -0.2, -100])
+    assert np.isfinite(s0).all() and np.array_equal(logp0, logp1) and bool((plain == with_ref).all())
+    assert np.array_equal(s0[[0, 1, 2, 4]], s1[[0, 1, 2, 4]]) and s1[3] == np.inf
+    _, s2 = ppo(ctx, b, old, adv, with_ref, entropy_coef=0.01, ref_logp=lp + [0.1, 80, -0.2, -100])
+    np.testing.assert_allclose(s2[3], np.exp(80) / 4, rtol=1e-4)                  # 80 is known to its rounding and ln p's error

@@ -1,0 +1,15 @@
+"""The token losses' 64-bit oracle where a factor is infinite or overflows."""
+import numpy as np
+
+from oracle import token_loss as tl
+
+Z = np.array([[0.5, -1.0, 2.0, -np.inf], [1.0, 0.0, -0.5, 0.25]])
+TOK = np.array([2, 1])
+W = np.array([0.5, 0.5])
+
+
+def test_reference_with_coefficient_zero():
+    lp = tl.logprob(Z, TOK)[0]
+    plain = tl.ppo(Z, TOK, lp, np.ones(2), W)
+    L, g, _, _, _, stats = tl.ppo(Z, TOK, lp, np.ones(2), W, ref=lp + [800.0, 0.1])
+    assert L == plain[0] and np.array_equal(g, plain[1]) and stats[3] == np.inf

@@ -49,7 +49,8 @@ def ppo(z, tokens, old, adv, weight, ref=None, lo=0.2, hi=0.2, ck=0.0, ch=0.0, T
         logp[i] = lp[i, tokens[i]]
         with np.errstate(over="ignore", invalid="ignore"):
             rho = np.exp(logp[i] - old[i])
-            a, b = rho * adv[i], np.clip(rho, 1 - lo, 1 + hi) * adv[i]
+            a = 0.0 if adv[i] == 0 and np.isinf(rho) else rho * adv[i]
+            b = np.clip(rho, 1 - lo, 1 + hi) * adv[i]
             clipped[i] = a > b
             l[i] = -(b if a > b else a) - (ch * H[i] if ch else 0.0)
             slope[i] = 0.0 if a > b else -a

@@ -393,7 +393,8 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
                                            float* loss, float* clipped, float* kl, float* H) {
     const float A = in.adv;
     const float rho = expf(logp - in.old);
-    const float free_ = rho * A;
+    // an advantage of 0 makes 0 of every ratio, also of one past fp32; a NaN ratio stays one
+    const float free_ = A == 0.f && rho == INFINITY ? 0.f : rho * A;
     // a NaN ratio stays one (fminf and fmaxf would drop it)
     const float cut = (rho < a.ratio_lo ? a.ratio_lo : rho > a.ratio_hi ? a.ratio_hi : rho) * A;
     const bool clip = free_ > cut;                   // ties to the unclipped term, which carries the gradient

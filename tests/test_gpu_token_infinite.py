@@ -53,3 +53,22 @@ def test_reference_with_coefficient_zero(ctx, V, dt):
     assert np.array_equal(s0[[0, 1, 2, 4]], s1[[0, 1, 2, 4]]) and s1[3] == np.inf
     _, s2 = ppo(ctx, b, old, adv, with_ref, entropy_coef=0.01, ref_logp=lp + [0.1, 80, -0.2, -100])
     np.testing.assert_allclose(s2[3], np.exp(80) / 4, rtol=1e-4)                  # 80 is known to its rounding and ln p's error
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LENGTHS)
+def test_ratio_past_fp32_with_advantage_zero(ctx, V, dt):
+    """rho A of an advantage 0 is 0 whatever the ratio: the row adds nothing, and the entropy term
+    is as it is without the ratio."""
+    b, lp = rows(V, dt, V + 1)
+    (_, g), (_, near) = b.grad(), b.grad()
+    far = lp - [100, 0.1, 200, -0.1]
+    _, stats = ppo(ctx, b, far, [0, 1, -0.0, -1], g, entropy_coef=0.5)
+    _, want = ppo(ctx, b, lp - [0, 0.1, 0, -0.1], [0, 1, -0.0, -1], near, entropy_coef=0.5)
+    assert np.isfinite(stats).all() and np.array_equal(stats, want) and bool((g == near).all())
+    # the clipped term of a positive advantage is finite too, the unclipped one of a negative is not
+    _, stats = ppo(ctx, b, far, [1, 0, 1, 0], g)
+    np.testing.assert_allclose(stats[1], -2 * 1.2 / 4, rtol=1e-6)
+    assert not g.any()
+    _, stats = ppo(ctx, b, far, [-1, 0, 0, 0], g)
+    assert stats[1] == np.inf

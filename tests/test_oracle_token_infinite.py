@@ -13,3 +13,10 @@ def test_reference_with_coefficient_zero():
     plain = tl.ppo(Z, TOK, lp, np.ones(2), W)
     L, g, _, _, _, stats = tl.ppo(Z, TOK, lp, np.ones(2), W, ref=lp + [800.0, 0.1])
     assert L == plain[0] and np.array_equal(g, plain[1]) and stats[3] == np.inf
+
+
+def test_ratio_past_the_type_with_advantage_zero():
+    lp = tl.logprob(Z, TOK)[0]
+    want = tl.ppo(Z, TOK, lp, np.array([0.0, 1.0]), W, ch=0.1)
+    got = tl.ppo(Z, TOK, lp - [800.0, 0.0], np.array([0.0, 1.0]), W, ch=0.1)
+    assert got[0] == want[0] and np.array_equal(got[1], want[1])

@@ -56,7 +56,7 @@ def ppo(z, tokens, old, adv, weight, ref=None, lo=0.2, hi=0.2, ck=0.0, ch=0.0, T
             slope[i] = 0.0 if a > b else -a
             if ref is not None:
                 r = ref[i] - logp[i]
-                kl[i] = np.expm1(r) - r
+                kl[i] = np.inf if r == np.inf else np.expm1(r) - r
                 if ck:                                       # one that is only reported adds 0, however large
                     l[i] += ck * kl[i]
                     slope[i] -= ck * np.expm1(r)

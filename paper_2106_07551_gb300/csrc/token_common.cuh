@@ -404,7 +404,7 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
     *kl = 0.f;
     if (a.ref) {
         const float d = in.ref - logp, e = expm1f(d);
-        *kl = e - d;
+        *kl = e < INFINITY ? e - d : e;              // e^r outgrows r: +infinity, also at r = +infinity
         if (a.kl != 0.f) {                           // a term that is only reported adds 0, also where e is infinite
             l = fmaf(a.kl, *kl, l);
             slope = fmaf(-a.kl, e, slope);

@@ -72,3 +72,21 @@ def test_ratio_past_fp32_with_advantage_zero(ctx, V, dt):
     assert not g.any()
     _, stats = ppo(ctx, b, far, [-1, 0, 0, 0], g)
     assert stats[1] == np.inf
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LENGTHS)
+def test_kl_of_a_masked_token(ctx, V, dt):
+    """ln p = -infinity: e^r - r - 1 is +infinity, and so are the loss with a KL term and the
+    statistic; without one the loss is the others'."""
+    b, lp = rows(V, dt, V + 2)
+    z = b.z.copy()
+    z[1, b.tok[1]] = -np.inf
+    b.set(z)
+    lp = np.where(np.arange(4) == 1, -3.0, tl.logprob(b.z, b.tok)[0])
+    old, adv, ref = lp + 0.1, [1, 1, -1, 2], lp + 0.2
+    logp, stats = ppo(ctx, b, old, adv, ref_logp=ref, kl_coef=0.1)
+    assert logp[1] == -np.inf and stats[1] == np.inf and stats[3] == np.inf and np.isfinite(stats[[0, 2, 4]]).all()
+    _, alone = ppo(ctx, b, old, adv, ref_logp=ref)
+    _, none = ppo(ctx, b, old, adv)
+    assert np.isfinite(none).all() and np.array_equal(alone[[0, 1, 2, 4]], none[[0, 1, 2, 4]]) and alone[3] == np.inf

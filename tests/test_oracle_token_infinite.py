@@ -20,3 +20,9 @@ def test_ratio_past_the_type_with_advantage_zero():
     want = tl.ppo(Z, TOK, lp, np.array([0.0, 1.0]), W, ch=0.1)
     got = tl.ppo(Z, TOK, lp - [800.0, 0.0], np.array([0.0, 1.0]), W, ch=0.1)
     assert got[0] == want[0] and np.array_equal(got[1], want[1])
+
+
+def test_kl_of_a_masked_token():
+    tok = np.array([3, 1])
+    L, _, logp, l, _, stats = tl.ppo(Z, tok, np.array([-1.0, -1.0]), np.ones(2), W, ref=np.array([-1.0, -1.0]), ck=0.1)
+    assert logp[0] == -np.inf and l[0] == L == stats[3] == np.inf and np.isfinite(l[1])

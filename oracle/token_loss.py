@@ -62,7 +62,8 @@ def ppo(z, tokens, old, adv, weight, ref=None, lo=0.2, hi=0.2, ck=0.0, ch=0.0, T
                     slope[i] -= ck * np.expm1(r)
             one = np.zeros(lp.shape[1])
             one[tokens[i]] = 1.0
-            grad[i] = weight[i] / T * (slope[i] * (one - p[i]) - ch * dH[i])
+            d = one - p[i]
+            grad[i] = weight[i] / T * (np.where(d == 0, 0.0, slope[i] * d) - ch * dH[i])     # the slope may be infinite
     L = float((weight * l)[live].sum())
     M = max(1, live.sum())
     stats = np.array([live.sum(), L, clipped.sum() / M, kl.sum() / M, np.where(live, H, 0).sum() / M])

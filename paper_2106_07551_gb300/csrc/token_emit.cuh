@@ -15,6 +15,33 @@ __device__ __forceinline__ float emit_one(T z, const RowGrad& c, float k) {
     return exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
 }
 
+// A row of the policy loss whose slope at ln p is infinite (a KL term or a ratio past fp32, a
+// masked token with a KL term): its entries are infinite, and 0 times infinity or the difference
+// of two infinities would make NaN of some. One entry of such a row, or of any other: 0 where p is
+// 0, the slope's sign at the token.
+__device__ __forceinline__ bool is_steep(const RowGrad& c) { return fabsf(c.c0) == INFINITY; }
+template <class T>
+__device__ __forceinline__ float emit_steep(T z, const RowGrad& c, float k, bool token) {
+    const float x = x_of(Elt<T>::get(z), c.m, k), e = exp2_fast(x);
+    const float v = e == 0.f && is_steep(c) ? 0.f : e * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
+    return !token ? v : fabsf(c.at) == INFINITY ? c.at : v + c.at;
+}
+// Sixteen bytes of such a row, the token entry `at` of them.
+template <class T>
+__device__ __forceinline__ void emit_steep(const uint4& q, const RowGrad& c, float k, int at, F2 (&v)[Elt<T>::W / 2]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < Elt<T>::W; i += 2)
+        v[i / 2] = f2_make(emit_steep(Elt<T>::word(w, i), c, k, i == at), emit_steep(Elt<T>::word(w, i + 1), c, k, i + 1 == at));
+}
+// Entries [j0, j1), entry j at e[j], by kThreads threads tid.
+template <class T, int kThreads>
+__device__ __forceinline__ void emit_steep_part(int tid, const T* e, int j0, int j1, T* g, const RowGrad& c, float k,
+                                                int token) {
+#pragma unroll 1
+    for (int j = j0 + tid; j < j1; j += kThreads) g[j] = Elt<T>::put(emit_steep(e[j], c, k, j == token));
+}
+
 // The gradient of a stage: entries [j0, j1) of the row, those of the n vectors at src,
 // the first of which is entry `first` (before the row where the row starts inside it). By
 // the first kConsumers threads; a full stage has kPer vectors for each.

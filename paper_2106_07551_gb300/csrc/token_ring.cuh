@@ -80,8 +80,9 @@ struct __align__(16) Queued {
 // What warp 0 leaves for the second sweep.
 struct RowOut {
     RowGrad c;
-    int32_t live;
+    int32_t kind;                                    // kOutZero: no gradient; kOutSteep: an infinite slope
 };
+enum : int { kOutZero = 0, kOutPlain = 1, kOutSteep = 2 };
 
 // A place in the ring: the stage and the parity of its present use.
 struct Cursor {
@@ -453,7 +454,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     }
                     if (first) a.row_sums[row] = sum;
                     if (lane == 0) {
-                        rout[slot] = RowOut{c, live};
+                        rout[slot] = RowOut{c, !live ? kOutZero : kOp == kTokPpo && is_steep(c) ? kOutSteep : kOutPlain};
                         mbar_arrive_release(&rfull[slot]);
                     }
                 }
@@ -461,7 +462,8 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
             if (g) {
                 wait(&rfull[slot], parity);
                 const RowGrad c = rout[slot].c;
-                const bool live = rout[slot].live != 0, alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+                const int kind = rout[slot].kind;
+                const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
                 if (kept < parts) at = begin;
                 for (int i = 0; i < parts; ++i, at.next(sh.stages)) {
                     const int part = kept + i < parts ? kept + i : kept + i - parts, v = v_lo + part * kStageVecs;
@@ -470,9 +472,12 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     const int j0 = max(0, j), j1 = min(a.V, j + n * W);
                     const uint8_t* src = ring + at.stage * kStageBytes;
                     const int token = kTop ? -1 : q.token;
-                    if (!live)
-                        zero_entries<T, kConsumers>(tid, g, j0, j1);
-                    else if (kOp == kTokPpo && c.c1 != 0.f)
+                    if (kind != kOutPlain) {
+                        if (kOp == kTokPpo && kind == kOutSteep)
+                            emit_steep_part<T, kConsumers>(tid, reinterpret_cast<const T*>(src) - j, j0, j1, g, c, a.k, token);
+                        else
+                            zero_entries<T, kConsumers>(tid, g, j0, j1);
+                    } else if (kOp == kTokPpo && c.c1 != 0.f)
                         emit_stage<T, true, kConsumers, kPer>(tid, src, j, j0, j1, n, g, alike, c, a.k, token);
                     else
                         emit_stage<T, false, kConsumers, kPer>(tid, src, j, j0, j1, n, g, alike, c, a.k, token);
@@ -484,7 +489,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     if (lane == 0) mbar_arrive_release(&pfull[slot]);
                     wait(&pfull[slot], parity);
                     const int j0 = max(0, v_lo * W - h), j1 = min(a.V, v_hi * W - h);
-                    if (live)
+                    if (kind == kOutPlain)
                         for (int i = tid; i < a.top; i += kConsumers) {
                             const TopEntry e = entries[b * a.top + i];
                             if (e.id >= j0 && e.id < j1)

@@ -160,15 +160,17 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
             row_loss<kOp>(a, row, sub == 0 && in_range, r, zt, in, w, top, live, c, total);
         }
         if (!g) continue;
-        const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+        const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0, plain = live && !(kOp == kTokPpo && is_steep(c));
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int j = (sub + u * G) * W - h;
             if (!in_range || j >= a.V) continue;
             F2 v[W / 2] = {};
-            if (live) {
+            if (plain) {
                 emit<T, kOp == kTokPpo>(q[u], c, a.k, v);
                 if (!kTop && (unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
+            } else if (kOp == kTokPpo && live) {
+                emit_steep<T>(q[u], c, a.k, token - j, v);
             }
             const uint4 out = Elt<T>::pack(v);
             if (alike && j >= 0 && j + W <= a.V) *reinterpret_cast<uint4*>(g + j) = out;
@@ -254,8 +256,14 @@ __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, 
             }
             row_loss<kOp>(a, row, lane == 0, r, zt, in, w, top, live, c, total);
         }
-        if (g && !live) zero_entries<T, 32>(lane, g, 0, a.V);
-        if (g && live) {
+        const bool plain = __all_sync(0xffffffffu, live && !(kOp == kTokPpo && is_steep(c)));
+        if (g && !plain) {
+            if (kOp == kTokPpo && live)
+                emit_steep_part<T, 32>(lane, reinterpret_cast<const T*>(own) + h, 0, a.V, g, c, a.k, token);
+            else
+                zero_entries<T, 32>(lane, g, 0, a.V);
+        }
+        if (g && plain) {
             const uint8_t* src = reinterpret_cast<const uint8_t*>(own);
             const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
             if (kOp == kTokPpo && c.c1 != 0.f) emit_stage<T, true, 32, kPer>(lane, src, -h, 0, a.V, nv, g, alike, c, a.k, token);
@@ -360,9 +368,13 @@ __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) 
             if (j >= a.V || !in_range) break;
             float f = 0.f;
             if (live) {
-                const float x = x_of(v[j], c.m, a.k);
-                f = exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
-                if (j == token) f += c.at;
+                if (is_steep(c)) {
+                    f = emit_steep(v[j], c, a.k, j == token);
+                } else {
+                    const float x = x_of(v[j], c.m, a.k);
+                    f = exp2_fast(x) * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
+                    if (j == token) f += c.at;
+                }
             }
             if (flat_g) tile[tid * a.V + j] = Elt<T>::put(f);
             else g[j] = Elt<T>::put(f);

@@ -90,3 +90,38 @@ def test_kl_of_a_masked_token(ctx, V, dt):
     _, alone = ppo(ctx, b, old, adv, ref_logp=ref)
     _, none = ppo(ctx, b, old, adv)
     assert np.isfinite(none).all() and np.array_equal(alone[[0, 1, 2, 4]], none[[0, 1, 2, 4]]) and alone[3] == np.inf
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LENGTHS)
+def test_gradient_of_an_infinite_slope(ctx, V, dt, pad):
+    """Where the slope at ln p exceeds fp32, or is infinite (a masked token with a KL term), the
+    entries go to the infinity of their sign, masked ones stay 0, and other rows are as ever."""
+    b, lp = rows(V, dt, V + 3, pad)
+    z = b.z.copy()
+    z[2, b.tok[2]] = -np.inf
+    b.set(z)
+    lp, p, _, _ = tl.rows(b.z)
+    lp = lp[np.arange(4), b.tok]
+    old, ref = np.where(np.isfinite(lp), lp, -3) + 0.1, np.where(np.isfinite(lp), lp, -3) + [0, 200, 0, 0]
+    masked = np.isneginf(b.z)
+    one = np.zeros_like(b.z, bool)
+    one[np.arange(4), b.tok] = True
+    (_, plain), (_, g) = b.grad(), b.grad(pad=2 * pad)
+    ppo(ctx, b, old, [1, 1, 1, -1], plain, ref_logp=np.where(np.arange(4) % 3 == 0, ref, 0), kl_coef=0.1)
+    keep = b.logits.clone()
+    for out in (g, b.logits):
+        ppo(ctx, b, old, [1, 1, 1, -1], out, ref_logp=ref, kl_coef=0.1)
+        got = out.double().cpu().numpy()
+        b.logits.copy_(keep)
+        assert bool((out[[0, 3]] == plain[[0, 3]]).all()) if out is g else True
+        for i in (1, 2):
+            assert np.isneginf(got[i, one[i]]).all()
+            assert (got[i, masked[i] & ~one[i]] == 0).all()
+            assert np.isposinf(got[i, ~masked[i] & ~one[i]]).all()
+    # a ratio past fp32 with a negative advantage: the slope is -rho A = +infinity
+    ppo(ctx, b, old - [0, 200, 0, 0], [0, -1, 0, 0], g, entropy_coef=0.1)
+    got = g.double().cpu().numpy()
+    assert np.isposinf(got[1, one[1]]).all() and np.isneginf(got[1, ~masked[1] & ~one[1]]).all()
+    assert (got[masked & ~one] == 0).all()

@@ -26,3 +26,13 @@ def test_kl_of_a_masked_token():
     tok = np.array([3, 1])
     L, _, logp, l, _, stats = tl.ppo(Z, tok, np.array([-1.0, -1.0]), np.ones(2), W, ref=np.array([-1.0, -1.0]), ck=0.1)
     assert logp[0] == -np.inf and l[0] == L == stats[3] == np.inf and np.isfinite(l[1])
+
+
+def test_gradient_of_an_infinite_slope():
+    """Masked entries stay 0, the others go to the infinity of their sign."""
+    tok = np.array([0, 1])
+    z = np.array([[-np.inf, -1.0, 2.0, -np.inf], [1.0, 0.0, -0.5, 0.25]])
+    for ref in ([-1.0, -1.0], [-1.0, 900.0]):
+        g = tl.ppo(z, tok, np.array([-1.0, -1.0]), np.ones(2), W, ref=np.array(ref), ck=0.1)[1]
+        assert np.array_equal(g[0], [-np.inf, np.inf, np.inf, 0])
+        assert np.isfinite(g[1]).all() if ref[1] < 0 else np.array_equal(g[1], np.inf * np.array([1, -1, 1, 1]))

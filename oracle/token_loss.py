@@ -79,7 +79,7 @@ def pref(z, tokens, offsets, ref=None, beta=0.1, smooth=0.0, T=1.0):
     gain = np.where(live, lp[i, np.maximum(tokens, 0)] - (0 if ref is None else ref), 0.0)
     R = np.array([beta * gain[offsets[s]:offsets[s + 1]].sum() for s in range(2 * P)])
     D = R[0::2] - R[1::2]
-    l = (1 - smooth) * np.logaddexp(0, -D) + smooth * np.logaddexp(0, D)
+    l = (1 - smooth) * np.logaddexp(0, -D) + (smooth * np.logaddexp(0, D) if smooth else 0.0)
     dD = smooth / (1 + np.exp(-D)) - (1 - smooth) / (1 + np.exp(D))
     slope = np.zeros(n)
     for s in range(2 * P):

@@ -58,7 +58,9 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
             // -ln s(x) = max(-x, 0) + ln(1 + e^-|x|)
             const float tail = log1pf(expf(-fabsf(d)));
             const float lp = fmaxf(-d, 0.f) + tail, ln = fmaxf(d, 0.f) + tail;
-            total.add(RowSum{(1.f - a.smooth) * lp + a.smooth * ln, rew[0], rew[1], d > 0.f ? 3 : 1});
+            // without smoothing the second term adds 0, also where it is infinite
+            const float second = a.smooth != 0.f ? a.smooth * ln : 0.f;
+            total.add(RowSum{(1.f - a.smooth) * lp + second, rew[0], rew[1], d > 0.f ? 3 : 1});
             // smooth s(d) - (1 - smooth) s(-d)
             const float slope = a.smooth / (1.f + expf(-d)) - (1.f - a.smooth) / (1.f + expf(d));
             factor = slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs;

@@ -125,3 +125,35 @@ def test_gradient_of_an_infinite_slope(ctx, V, dt, pad):
     got = g.double().cpu().numpy()
     assert np.isposinf(got[1, one[1]]).all() and np.isneginf(got[1, ~masked[1] & ~one[1]]).all()
     assert (got[masked & ~one] == 0).all()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LENGTHS)
+def test_pair_with_a_masked_rejected_token(ctx, V, dt):
+    """D = +infinity: the loss is 0 without label smoothing, +infinity with it."""
+    b, lp = rows(V, dt, V + 4)
+    z = b.z.copy()
+    z[1, b.tok[1]] = -np.inf
+    b.set(z)
+    off = np.array([0, 1, 2, 3, 4], np.int64)
+    ref = np.where(np.isfinite(lp), lp, -3) - [0.3, 0, 0.5, -0.2]
+    _, g = b.grad()
+    reward, stats = empty(4), empty(5)
+
+    def call(smooth):
+        ctx.learn_token_pref(b.logits, cuda(b.tok), cuda(off), g, stats, ref_logp=cuda(ref.astype(np.float32)),
+                             reward_out=reward, beta=0.5, label_smoothing=smooth, grad_scale=1024.0)
+        ctx.sync()
+        return stats.cpu().numpy(), reward.cpu().numpy(), g.double().cpu().numpy()
+    s, r, got = call(0.0)
+    wL, wg, wr, _, ws = tl.pref(b.z, b.tok, off, ref.astype(np.float32).astype(np.float64), 0.5, 0.0)
+    assert np.isfinite(wL) and wr[1] == r[1] == -np.inf and s[4] == -np.inf
+    np.testing.assert_allclose(s[:4], ws[:4], rtol=0, atol=1e-4)                    # ln p to 5e-5 at 150,001 entries
+    np.testing.assert_allclose(r[[0, 2, 3]], wr[[0, 2, 3]], rtol=0, atol=1e-4)
+    assert not got[:2].any()
+    wg = wg * 1024
+    one = np.arange(V) == b.tok[:, None]
+    tol = 1e-4 * (np.abs(wg) + np.abs(wg).max() * one)
+    assert (np.abs(got - wg) <= tol + HALF_ULP[dt] * (np.abs(wg) + tol) + TINY[dt]).all()
+    s, r, _ = call(0.25)
+    assert s[1] == np.inf and r[1] == -np.inf

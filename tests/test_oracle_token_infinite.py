@@ -36,3 +36,11 @@ def test_gradient_of_an_infinite_slope():
         g = tl.ppo(z, tok, np.array([-1.0, -1.0]), np.ones(2), W, ref=np.array(ref), ck=0.1)[1]
         assert np.array_equal(g[0], [-np.inf, np.inf, np.inf, 0])
         assert np.isfinite(g[1]).all() if ref[1] < 0 else np.array_equal(g[1], np.inf * np.array([1, -1, 1, 1]))
+
+
+def test_pair_with_a_masked_rejected_token():
+    z, off = np.vstack([Z[1], Z[0], Z[1], Z[1]]), np.arange(5)
+    tok = np.array([1, 3, 0, 2])
+    L, g, R, _, _ = tl.pref(z, tok, off, None, 0.5)
+    assert R[1] == -np.inf and not g[:2].any() and L == np.logaddexp(0, -(R[2] - R[3])) / 2
+    assert tl.pref(z, tok, off, None, 0.5, 0.1)[0] == np.inf

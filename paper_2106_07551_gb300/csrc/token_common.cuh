@@ -10,8 +10,8 @@
 // widened by the subtraction itself.)
 // A row's statistics are (m, S, t), t = sum_j 2^x_j x_j, gathered in one pass over the
 // row with a running maximum; two partial statistics combine by scaling with
-// 2^((m_a - m) k). They are held in fp32: a row's sum has at most a few hundred
-// thousand terms, added in thousands of partial sums.
+// 2^((m_a - m) k). They are held in fp32, a long row's with what the additions of its
+// parts' sums leave (LongStat).
 // The fast base-2 exponential is low by 5.0e-8 of its value on average (measured over
 // [-20, 0), the same from -1 down), which every sum of a row, and every scaling of one,
 // would pass on and a sequence's sum add up; 2^x is taken of x + kExpBias, added in the
@@ -229,6 +229,22 @@ __device__ __forceinline__ F2 f2_floor_x(F2 x) {
     return f2_make(fmaxf(v.x, kXMin), fmaxf(v.y, kXMin));
 }
 
+// A sum in fp32 with the rounding errors of its additions beside it (Knuth's two-sum): as
+// good as one in fp64, whose rate is a sixtieth of fp32's here.
+struct Sum2 {
+    float s, e;
+    __device__ __forceinline__ void add(float x) {
+        const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
+        e = __fadd_rn(e, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
+        s = t;
+    }
+    __device__ __forceinline__ void add(const Sum2& b) {
+        add(b.s);
+        e = __fadd_rn(e, b.e);
+    }
+    // an infinite sum has an error that is NaN, and none to speak of
+    __device__ __forceinline__ float value() const { return fabsf(s) < INFINITY ? __fadd_rn(s, e) : s; }
+};
 struct RowStat {
     float m, s, t;
 };
@@ -276,7 +292,7 @@ __device__ __forceinline__ float vec_max(const uint4 (&q)[N]) {
 template <class T, int N>
 __device__ __forceinline__ void gather(RowStat& r, const uint4 (&q)[N], float k) {
     constexpr int P = Elt<T>::W / 2;
-    F2 s = f2_make(r.s, 0.f), t = f2_make(r.t, 0.f);
+    F2 s = 0ull, t = 0ull;
     const F2 k2 = f2_dup(k), neg = f2_dup(-r.m), bias = f2_dup(kExpBias);
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -290,9 +306,34 @@ __device__ __forceinline__ void gather(RowStat& r, const uint4 (&q)[N], float k)
         }
     }
     const float2 s2 = f2_split(s), t2 = f2_split(t);
-    r.s = s2.x + s2.y;
-    r.t = t2.x + t2.y;
+    r.s += s2.x + s2.y;
+    r.t += t2.x + t2.y;
 }
+
+// The statistics of a row of many parts: each part's sums join these with the rounding errors of
+// the additions kept, so that what a row of any length loses is what a part does. (One sum over
+// 2^24 entries, 131,072 a thread, is off by up to 7e-4 of itself.)
+struct LongStat {
+    float m;
+    Sum2 s, t;
+};
+__device__ __forceinline__ void raise(LongStat& r, float mx, float k) {
+    if (mx <= r.m) return;
+    const float m = max_nan(r.m, mx);
+    const float d = fmaxf((r.m - m) * k, kXMin), f = exp2_fast(d + kExpBias);
+    r.t = Sum2{f * fmaf(r.s.s, d, r.t.s), f * fmaf(r.s.e, d, r.t.e)};
+    r.s = Sum2{f * r.s.s, f * r.s.e};
+    r.m = m;
+}
+template <class T, int N>
+__device__ __forceinline__ void gather(LongStat& r, const uint4 (&q)[N], float k) {
+    RowStat part{r.m, 0.f, 0.f};
+    gather<T>(part, q, k);
+    r.s.add(part.s);
+    r.t.add(part.t);
+}
+__device__ __forceinline__ RowStat stat_of(const LongStat& r) { return RowStat{r.m, r.s.value(), r.t.value()}; }
+__device__ __forceinline__ RowStat stat_of(const RowStat& r) { return r; }
 
 // Statistics of N lanes that follow one another, the same in each: their maximum, then
 // their sums to its base.
@@ -427,22 +468,6 @@ __device__ __forceinline__ void logp_row(const TokenArgs& a, int64_t row, bool l
     if (a.rows) a.rows[row] = TokenRow{r.m, live ? 1.f / r.s : 0.f, logp, rest};
 }
 
-// A sum in fp32 with the rounding errors of its additions beside it (Knuth's two-sum): as
-// good as one in fp64, whose rate is a sixtieth of fp32's here.
-struct Sum2 {
-    float s, e;
-    __device__ __forceinline__ void add(float x) {
-        const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
-        e = __fadd_rn(e, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
-        s = t;
-    }
-    __device__ __forceinline__ void add(const Sum2& b) {
-        add(b.s);
-        e = __fadd_rn(e, b.e);
-    }
-    // an infinite sum has an error that is NaN, and none to speak of
-    __device__ __forceinline__ float value() const { return fabsf(s) < INFINITY ? __fadd_rn(s, e) : s; }
-};
 // The statistics of rows: policy loss: KL and H in x, y; distillation: l in x.
 struct __align__(16) Totals {
     int32_t rows, clipped;

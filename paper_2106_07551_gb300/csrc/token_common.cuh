@@ -230,7 +230,10 @@ __device__ __forceinline__ F2 f2_floor_x(F2 x) {
 }
 
 // A sum in fp32 with the rounding errors of its additions beside it (Knuth's two-sum): as
-// good as one in fp64, whose rate is a sixtieth of fp32's here.
+// good as one in fp64, whose rate is a sixtieth of fp32's here, over some 10^5 additions. The
+// errors' own sum is plain fp32: it is off by 1e-6 to 4e-6 of the whole after 262,144 additions of
+// one value, 1e-4 after 1.8 million. Where there may be as many it is settled as it goes, which
+// keeps the errors' sum below half a unit of the whole.
 struct Sum2 {
     float s, e;
     __device__ __forceinline__ void add(float x) {
@@ -241,6 +244,11 @@ struct Sum2 {
     __device__ __forceinline__ void add(const Sum2& b) {
         add(b.s);
         e = __fadd_rn(e, b.e);
+    }
+    __device__ __forceinline__ void settle() {
+        const float t = __fadd_rn(s, e);
+        e = __fsub_rn(e, __fsub_rn(t, s));
+        s = t;
     }
     // an infinite sum has an error that is NaN, and none to speak of
     __device__ __forceinline__ float value() const { return fabsf(s) < INFINITY ? __fadd_rn(s, e) : s; }

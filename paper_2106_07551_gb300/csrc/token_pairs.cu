@@ -26,6 +26,9 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     constexpr int kHalf = kPairT / 2;
     const int side = threadIdx.x / kHalf, part = threadIdx.x % kHalf;
     Totals total{};                                  // thread 0: pairs, those in order; loss, rewards
+    constexpr int kSettle = 1024;                    // rows, pairs after which a sum is settled
+    constexpr int kLoads = 4;                        // of a thread in flight
+    unsigned taken = 0;
     wait_for_previous();
     let_next_start();
     for (int p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
@@ -35,12 +38,28 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
         if (!ok && threadIdx.x == 0) atomicOr(a.err, ERRBIT_BAD_OFFSETS);
         const int64_t lo = !ok ? 0 : side ? o1 : o0, hi = !ok ? 0 : side ? o2 : o1;
         Sum2 s{0.f, 0.f};
-        for (int64_t i = lo + part; i < hi; i += kHalf) {
-            const TokenRow r = a.rows[i];
-            if (r.inv_s == 0.f) continue;
-            s.add(r.value);
-            s.e += r.rest;
-            if (a.ref) s.add(-a.ref[i]);
+        for (int64_t i0 = lo + part; i0 < hi; i0 += kSettle * kHalf) {
+            const TokenRow* rows = a.rows + i0;
+            const float* ref = a.ref ? a.ref + i0 : nullptr;
+            const int n = (int)min((int64_t)kSettle, (hi - i0 + kHalf - 1) / kHalf);
+            for (int u0 = 0; u0 < n; u0 += kLoads) {
+                TokenRow r[kLoads];
+                float f[kLoads];
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) {
+                    const bool there = u0 + u < n;
+                    r[u] = there ? rows[(u0 + u) * kHalf] : TokenRow{0.f, 0.f, 0.f, 0.f};
+                    f[u] = there && ref ? ref[(u0 + u) * kHalf] : 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) {
+                    if (r[u].inv_s == 0.f) continue;
+                    s.add(r[u].value);
+                    s.e += r[u].rest;
+                    if (ref) s.add(-f[u]);
+                }
+            }
+            s.settle();
         }
         s = warp_sum2(s);
         __syncthreads();
@@ -61,6 +80,11 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
             // without smoothing the second term adds 0, also where it is infinite
             const float second = a.smooth != 0.f ? a.smooth * ln : 0.f;
             total.add(RowSum{(1.f - a.smooth) * lp + second, rew[0], rew[1], d > 0.f ? 3 : 1});
+            if (++taken % kSettle == 0) {
+                total.loss.settle();
+                total.x.settle();
+                total.y.settle();
+            }
             // smooth s(d) - (1 - smooth) s(-d)
             const float slope = a.smooth / (1.f + expf(-d)) - (1.f - a.smooth) / (1.f + expf(d));
             factor = slope * a.beta * a.gscale * a.inv_t / (float)a.n_pairs;

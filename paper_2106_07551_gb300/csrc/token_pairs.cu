@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
     unsigned taken = 0;
     wait_for_previous();
     let_next_start();
-    for (int p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
+    for (int64_t p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {          // 2 p + 2 passes 31 bits at 2^30 pairs
         const int64_t o0 = a.offsets[2 * p], o1 = a.offsets[2 * p + 1], o2 = a.offsets[2 * p + 2];
         const bool ok = o0 >= 0 && o0 <= o1 && o1 <= o2 && o2 <= a.n && (p > 0 || o0 == 0) &&
                         (p + 1 < a.n_pairs || o2 == a.n);
@@ -43,19 +43,19 @@ __global__ void __launch_bounds__(kPairT) token_pairs_kernel(TokenArgs a) {
             const float* ref = a.ref ? a.ref + i0 : nullptr;
             const int n = (int)min((int64_t)kSettle, (hi - i0 + kHalf - 1) / kHalf);
             for (int u0 = 0; u0 < n; u0 += kLoads) {
-                TokenRow r[kLoads];
+                float4 r[kLoads];
                 float f[kLoads];
 #pragma unroll
-                for (int u = 0; u < kLoads; ++u) {
-                    const bool there = u0 + u < n;
-                    r[u] = there ? rows[(u0 + u) * kHalf] : TokenRow{0.f, 0.f, 0.f, 0.f};
-                    f[u] = there && ref ? ref[(u0 + u) * kHalf] : 0.f;
+                for (int u = 0; u < kLoads; ++u) {   // past the end the last one again: no load waits for a branch
+                    const int at = min(u0 + u, n - 1) * kHalf;
+                    r[u] = __ldcg(reinterpret_cast<const float4*>(rows + at));
+                    f[u] = ref ? __ldcg(ref + at) : 0.f;
                 }
 #pragma unroll
                 for (int u = 0; u < kLoads; ++u) {
-                    if (r[u].inv_s == 0.f) continue;
-                    s.add(r[u].value);
-                    s.e += r[u].rest;
+                    if (u0 + u >= n || r[u].y == 0.f) continue;               // inv_s
+                    s.add(r[u].z);
+                    s.e += r[u].w;
                     if (ref) s.add(-f[u]);
                 }
             }

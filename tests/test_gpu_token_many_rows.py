@@ -1,4 +1,6 @@
 """More rows, and more pairs, than an ordinary call has: sums of millions of terms, counts past 31 bits."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -27,3 +29,34 @@ def test_reward_of_very_many_rows(with_ref):
     want = (lp - (0.3125 if with_ref else 0)) * 2.0 ** 8
     tol = 2.0 ** 8 * (2.0 ** -22 + 11 * 2.0 ** -24) + 2 * 2.0 ** -24 * abs(want)
     assert abs(float(reward[0]) - want) <= tol and float(reward[1]) == 0
+
+
+def test_as_many_pairs_as_are_taken():
+    """2^30 pairs, whose last offset is entry 2^31: pairs without rows but the last, whose two answers
+    have a row each."""
+    torch = need_gpu()
+    from paper_2106_07551_gb300 import _abi
+    P = 1 << 30
+    if torch.cuda.mem_get_info()[0] < 32 << 30:
+        pytest.skip("needs 32 GB")
+    off = torch.zeros(2 * P + 1, dtype=torch.int64, device="cuda")
+    off[2 * P - 1], off[2 * P] = 1, 2
+    z = torch.tensor([[1.0, 0.0], [0.0, 1.0]], device="cuda")
+    tok, stats, reward = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.empty(5, device="cuda"), torch.empty(
+        2 * P, device="cuda")
+    g = torch.empty_like(z)
+    with context() as ctx:
+        ctx.learn_token_pref(z, tok, off, g, stats, reward_out=reward, beta=2.0, grad_scale=float(P))
+        ctx.sync()
+        s = stats.double().cpu().numpy()
+        assert s[0] == P
+        np.testing.assert_allclose(s[1], np.log(2), rtol=1e-6)
+        # D = 2 (ln p(0 | 1, 0) - ln p(0 | 0, 1)) = 2: slope -2 s(-2), times 1 - p(0) in each row
+        np.testing.assert_allclose(reward[-2:].tolist(), [-2 * np.log1p(np.exp(-1)), -2 * np.log1p(np.exp(1))], rtol=1e-5)
+        assert not reward[:-2].any()
+        want = -2 / (1 + np.exp(2)) * np.array([1 / (1 + np.e), -1 / (1 + np.exp(-1))])
+        np.testing.assert_allclose(g[:, 0].tolist(), want, rtol=1e-5)
+        np.testing.assert_allclose(g[:, 1].tolist(), -want, rtol=1e-5)
+        b = _abi.TokenBatch(z.data_ptr(), tok.data_ptr(), 2, 2, 2, 0, 1.0)
+        p = _abi.TokenPref(off.data_ptr(), None, P + 1, 1.0, 0.0)
+        assert ctx.lib.malib_learn_token_pref(ctx.handle, C.byref(b), C.byref(p), None, None, None) == _abi.MALIB_EINVAL

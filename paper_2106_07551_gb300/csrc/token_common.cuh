@@ -245,12 +245,13 @@ struct Sum2 {
         add(b.s);
         e = __fadd_rn(e, b.e);
     }
+    // an infinite sum has an error that is NaN, and none to speak of
     __device__ __forceinline__ void settle() {
+        if (!(fabsf(s) < INFINITY)) return;
         const float t = __fadd_rn(s, e);
         e = __fsub_rn(e, __fsub_rn(t, s));
         s = t;
     }
-    // an infinite sum has an error that is NaN, and none to speak of
     __device__ __forceinline__ float value() const { return fabsf(s) < INFINITY ? __fadd_rn(s, e) : s; }
 };
 struct RowStat {

@@ -507,7 +507,8 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
  * stream and allocate at most their first time at a size (context-owned work
  * space: a context's calls must be ordered, also across malib_set_stream). A token
  * or teacher entry >= V leaves its row, or the entry, out and gives MALIB_EINVAL
- * at the next malib_sync. n_rows == 0 is valid. Errors: EINVAL, ENOMEM, ECUDA, ESTATE.
+ * at the next malib_sync. n_rows == 0 is valid; the rows that statistics count and
+ * average over are counted up to 2^32 - 1. Errors: EINVAL, ENOMEM, ECUDA, ESTATE.
  */
 typedef struct malib_token_batch {
     const void* logits;       /* [n_rows][ld], the first vocab of each row are used */

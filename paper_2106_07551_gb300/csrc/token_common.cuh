@@ -479,7 +479,7 @@ __device__ __forceinline__ void logp_row(const TokenArgs& a, int64_t row, bool l
 
 // The statistics of rows: policy loss: KL and H in x, y; distillation: l in x.
 struct __align__(16) Totals {
-    int32_t rows, clipped;
+    uint32_t rows, clipped;                          // (64 bits here cost 2 % of 20,000 rows of 300 entries)
     Sum2 loss, x, y;
     __device__ __forceinline__ void add(const RowSum& r) {
         rows += r.flags & 1;
@@ -532,7 +532,7 @@ __device__ __forceinline__ Totals sum_parts(const Totals* part, int n) {
                                                 : make_int4(0, 0, 0, 0);
 #pragma unroll
         for (int u = 0; u < kAt; ++u)
-            v.add(Totals{q[u][0].x, q[u][0].y, Sum2{__int_as_float(q[u][0].z), __int_as_float(q[u][0].w)},
+            v.add(Totals{(uint32_t)q[u][0].x, (uint32_t)q[u][0].y, Sum2{__int_as_float(q[u][0].z), __int_as_float(q[u][0].w)},
                          Sum2{__int_as_float(q[u][1].x), __int_as_float(q[u][1].y)},
                          Sum2{__int_as_float(q[u][1].z), __int_as_float(q[u][1].w)}});
     }

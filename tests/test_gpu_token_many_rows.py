@@ -60,3 +60,25 @@ def test_as_many_pairs_as_are_taken():
         b = _abi.TokenBatch(z.data_ptr(), tok.data_ptr(), 2, 2, 2, 0, 1.0)
         p = _abi.TokenPref(off.data_ptr(), None, P + 1, 1.0, 0.0)
         assert ctx.lib.malib_learn_token_pref(ctx.handle, C.byref(b), C.byref(p), None, None, None) == _abi.MALIB_EINVAL
+
+
+def test_rows_past_31_bits_are_counted():
+    """2^31 + 77 rows over one row of logits that all share."""
+    torch = need_gpu()
+    n = (1 << 31) + 77
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 120 GB")
+    z = torch.zeros((1, 2), dtype=torch.bfloat16, device="cuda").expand(n, 2)
+    tok = torch.zeros(n, dtype=torch.int32, device="cuda")
+    tok[5] = -1
+    old = torch.zeros(n, device="cuda")                           # and the advantages
+    old[n - 1] = 1.0
+    stats = torch.empty(5, device="cuda")
+    with context() as ctx:
+        ctx.learn_token_ppo(z, tok, old, old, None, stats)
+        ctx.sync()
+    s = stats.double().cpu().numpy()
+    assert s[0] == np.float32(n - 1)
+    # the last row: rho = e^-1 / 2, A = 1, weight 1 / n; every row's entropy is ln 2
+    np.testing.assert_allclose(s[1], -0.5 * np.exp(-1) / n, rtol=1e-5)
+    np.testing.assert_allclose(s[4], np.log(2), rtol=1e-6)

@@ -513,7 +513,7 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
 typedef struct malib_token_batch {
     const void* logits;       /* [n_rows][ld], the first vocab of each row are used */
     const int32_t* tokens;    /* [n_rows] the token that was chosen; < 0: row left out */
-    int64_t n_rows;
+    int64_t n_rows;           /* 0 <= n_rows <= 2^40 */
     int64_t ld;               /* row stride in elements; >= vocab, or 0 for one row that all share */
     int32_t vocab;            /* 1 <= V <= 2^24 */
     int32_t dtype;            /* malib_dtype of logits and gradient */

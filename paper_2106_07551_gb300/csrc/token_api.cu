@@ -1,6 +1,5 @@
 // C entry points of the token losses: argument checks, work space, launches.
 #include <cmath>
-#include <cstdio>
 
 #include "malib.h"
 #include "token_common.cuh"
@@ -10,6 +9,7 @@ using namespace malib;
 namespace {
 
 constexpr int32_t kMaxVocab = 1 << 24;
+constexpr int64_t kMaxRows = 1ll << 40;              // far past what memory holds; 16 bytes a row of work space
 
 // Fixed work space: the counter, then the partial sums.
 constexpr int64_t kPartOffset = 256;
@@ -37,7 +37,7 @@ struct Call {
         if (!b) return bad("token batch is NULL");
         if (!known(b->dtype)) return bad("unknown logits dtype");
         if (b->vocab < 1 || b->vocab > kMaxVocab) return bad("vocab must lie in [1, 2^24]");
-        if (b->n_rows < 0) return bad("n_rows < 0");
+        if (b->n_rows < 0 || b->n_rows > kMaxRows) return bad("n_rows must lie in [0, 2^40]");
         if (b->ld != 0 && b->ld < b->vocab) return bad("logits row stride below vocab");
         const int64_t es = elt_size(b->dtype);
         if (b->n_rows > 0 && b->ld > INT64_MAX / es / b->n_rows) return bad("logits do not fit the address space");

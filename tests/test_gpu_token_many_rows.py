@@ -82,3 +82,24 @@ def test_rows_past_31_bits_are_counted():
     # the last row: rho = e^-1 / 2, A = 1, weight 1 / n; every row's entropy is ln 2
     np.testing.assert_allclose(s[1], -0.5 * np.exp(-1) / n, rtol=1e-5)
     np.testing.assert_allclose(s[4], np.log(2), rtol=1e-6)
+
+
+@pytest.mark.parametrize("n", [(1 << 40) + 1, 1 << 58, (1 << 59) + 3, 1 << 60, (1 << 60) + 1, (1 << 63) - 1])
+def test_rows_that_no_memory_holds_are_refused(n):
+    """Rows that share one row of logits have no extent that could overflow; their work space has."""
+    torch = need_gpu()
+    from paper_2106_07551_gb300 import _abi
+    z, v = torch.zeros((1, 8), device="cuda"), torch.zeros(8, device="cuda")
+    i, off = torch.zeros(8, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    p, q, d = _abi.TokenPpo(v.data_ptr(), v.data_ptr(), None, None, 0.2, 0.2, 0.0, 0.0), _abi.TokenPref(
+        off.data_ptr(), None, 1, 0.1, 0.0), _abi.TokenDistill(i.data_ptr(), v.data_ptr(), None, 1, 0)
+    b = _abi.TokenBatch(z.data_ptr(), i.data_ptr(), n, 0, 8, 0, 1.0)
+    t = _abi.TokenBatch(z.data_ptr(), None, n, 0, 8, 0, 1.0)
+    with context() as ctx:
+        lib, h, r = ctx.lib, ctx.handle, C.byref
+        assert lib.malib_token_logprob(h, r(b), v.data_ptr(), None) == _abi.MALIB_EINVAL
+        assert lib.malib_learn_token_ppo(h, r(b), r(p), None, None, v.data_ptr()) == _abi.MALIB_EINVAL
+        assert lib.malib_learn_token_pref(h, r(b), r(q), None, None, v.data_ptr()) == _abi.MALIB_EINVAL
+        assert lib.malib_learn_token_distill(h, r(t), r(d), None, None, v.data_ptr()) == _abi.MALIB_EINVAL
+        assert "n_rows" in ctx.last_error()
+        ctx.sync()

@@ -493,8 +493,10 @@ int malib_pop_update(malib_ctx* ctx, int32_t policy_id, const float* params, int
  * a loss and the gradient at the logits, which the caller's network carries back.
  * With the row's logits z and temperature T in [1e-6, 1e6], y = z / T, the policy is
  *   ln p_j = y_j - ln sum_i exp(y_i),   H = -sum_j p_j ln p_j.
- * Logits of -infinity are masked entries: p_j = 0, no entropy, gradient 0. A NaN
- * or +infinity among the logits makes the row's results NaN.
+ * Logits of -infinity are masked entries: p_j = 0, no entropy, gradient 0 (at a row's
+ * own token, where ln p = -infinity, the slope at ln p). A NaN or +infinity among the
+ * logits makes the row's results NaN. A term whose coefficient is 0 adds 0, and so does
+ * a ratio with advantage 0, also where the other factor is infinite or past fp32.
  * Rows that are LEFT OUT: those with a negative token (a prompt, padding), weight
  * 0, no teacher entry, or logits that are all -infinity. They add nothing to
  * losses, sequence sums and statistics, their outputs per row are 0 and their
@@ -522,8 +524,9 @@ typedef struct malib_token_batch {
 
 /* The gradient at the logits: grad [n_rows][ld] of the logits' type, ld >= vocab
  * (columns from vocab on are not written); NULL for the loss alone. grad may be the
- * logits' buffer with the same ld (written in place) but must not overlap it
- * otherwise. scale multiplies the gradient (an upstream factor, or a loss scale
+ * logits' buffer with the same ld (written in place); otherwise the ranges from the
+ * first row's start to the last row's end must be apart (rows of the two side by side
+ * in one buffer are refused). scale multiplies the gradient (an upstream factor, or a loss scale
  * for fp16), not the loss. */
 typedef struct malib_token_grad {
     void* grad;

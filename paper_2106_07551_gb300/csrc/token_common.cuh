@@ -601,7 +601,9 @@ cudaError_t launch_token_rows(const TokenArgs& a, int op, int n_sm, cudaStream_t
 // log-probabilities of 16,000 rows of 4,300 entries 35 and 55, of 6,000 47 and 54, of 8,000
 // 67 and 55. And of a row whose pair's gradient is taken by a warp: longer ones stream past
 // it in parts (the preference call on 8,192 rows of 3,001 entries 42 us by warps, 48 in
-// parts, of 4,000 43 and 44, of 6,000 64 and 60).
+// parts, of 4,000 43 and 44, of 6,000 64 and 60). fp32 rows change at the same bytes, which
+// was not measured: they have half the entries, and where entries bound a row the change
+// could come later.
 constexpr int kShortVecs = 768, kShortGradVecs = 512;
 cudaError_t launch_token_short_f32(const TokenArgs& a, int op, int n_sm, cudaStream_t s);
 cudaError_t launch_token_short_bf16(const TokenArgs& a, int op, int n_sm, cudaStream_t s);

@@ -311,7 +311,10 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     T entry = Elt<T>::put(-INFINITY);
                     if (fill && pj >= 0 && pj < a.V) entry = z[pj];
                     wait(&empty[stage], at.parity ^ 1u);
-                    if (fill) reinterpret_cast<T*>(dst)[(pv - v) * W + (lane & 15)] = entry;
+                    if (fill) {
+                        reinterpret_cast<T*>(dst)[(pv - v) * W + (lane & 15)] = entry;
+                        fence_proxy_async_smem();    // a later use's copy overwrites what is stored here
+                    }
                     __syncwarp();
                     if (*gone) break;
                     wrapped |= stage + 1 == sh.stages;

@@ -611,6 +611,117 @@ typedef struct malib_token_distill {
 int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_distill* loss,
                               const malib_token_grad* grad, float* loss_out, float* stats_out);
 
+/*
+ * malib_learn_token_scores - the gradient at the logits of any loss of the rows'
+ * log-probabilities and entropies, from its slopes there (what the caller's own loss, or an
+ * automatic differentiation of it, gives for the results of malib_token_logprob and
+ * malib_token_top). With g = logp_grad_i at ln p of row i's token a, e = entropy_grad_i at H, and
+ * h = top_grad [n_rows][top] at ln p of the entries ids [n_rows][top] (< 0: absent):
+ *   dL / dz_j = (1 / T) [ g 1(j = a) + sum_k h_k 1(j = id_k) - p_j (g + sum_k h_k) - e p_j (ln p_j + H) ].
+ * An id listed more than once, or the token, has the sum of its slopes. Each of logp_grad,
+ * entropy_grad and (ids, top_grad) may be NULL (0), not all; 1 <= top <= 1024 with ids. Rows are
+ * left out by their token or as all -infinity; grad as for the losses, required. A row
+ * with an infinite slope has the entries' own slopes / T where p_j = 0, else the infinity of their sign,
+ * as the losses have; with a NaN, or infinities of both signs or at H, NaN.
+ */
+typedef struct malib_token_scores {
+    const float* logp_grad;
+    const float* entropy_grad;
+    const int32_t* ids;
+    const float* top_grad;
+    int32_t top;
+} malib_token_scores;
+int malib_learn_token_scores(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_scores* scores,
+                             const malib_token_grad* grad);
+
+/* ---- the rollout of token policies: likely entries, the draw of a token ----
+ *
+ * On a malib_token_batch, with its rules on buffers, errors and order; a row's entries
+ * are in the order of falling logits, the lower index first among equal ones (-0 equals
+ * 0). Masked entries (logit -infinity) are never listed and never drawn. batch->tokens
+ * may be NULL: no row is left out by its token. A row with a NaN or +infinity among its
+ * logits gives NaN, ids and tokens of -1 and rank 0; so does a row that is left out, with 0
+ * for NaN. No output may overlap the logits or another one; sums are fp32 or more.
+ */
+
+/*
+ * malib_token_top - the first `top` entries of each row with their ln p, and of the row's
+ * token its ln p and its rank (1: the first entry; a masked one comes after every unmasked
+ * one), and H. The list is what malib_learn_token_distill takes as a teacher's (top_logp
+ * with MALIB_F32). Places that the row has no unmasked entry for hold id -1 and -infinity.
+ * 1 <= top <= 1024. ids and top_logp [n_rows][top] are required, the others (all [n_rows])
+ * optional; logp and rank need batch->tokens.
+ */
+typedef struct malib_token_list {
+    int32_t* ids;
+    float* top_logp;
+    float* logp;
+    float* entropy;
+    int32_t* rank;
+    int32_t top;
+} malib_token_list;
+int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_list* out);
+
+/*
+ * malib_token_sample - draws a token of each row (what malib_rollout does for its policies).
+ * Kept are all unmasked entries (top_k 0), or of the first top_k those before which less than
+ * top_p of the top_k's probability lies (at least one). With a random number u in [0, 1) the
+ * token is the first kept entry, in the order of the index (top_k 0) or of the list, whose running
+ * probability exceeds u times the kept one; entries whose probability is below 2^-126 of the
+ * largest are not drawn. u >= 1 draws the last.
+ * u is uniform[row], or without it the top 24 bits of the first word of Philox4x32-10 at counter
+ * (sequence lo32, sequence hi32, step, agent) under `seed` over 2^24, as in malib_rollout: a
+ * sequence's draws do not depend on the batch that it is in. agent < 2^31 (the counters of
+ * malib_dropout are from there on). 0 <= top_k <= 1024; 0 < top_p <= 1, 1 without top_k.
+ * batch->tokens: rows with a negative one are left out (their answer has ended); other values are
+ * not looked at. token_out may be batch->tokens. Outputs [n_rows], each may be NULL: the token; its
+ * ln p and H by the whole row; draw_logp, ln of the probability that it was drawn with
+ * (among the kept).
+ */
+typedef struct malib_token_draw {
+    const float* uniform;
+    const int64_t* sequence;
+    const int32_t* step;
+    uint64_t seed;
+    uint32_t agent;
+    int32_t top_k;
+    float top_p;
+} malib_token_draw;
+int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_draw* draw, int32_t* token_out,
+                       float* logp_out, float* entropy_out, float* draw_logp_out);
+
+/*
+ * malib_dropout - dropout for a policy's network, whose mask is never stored: a rollout, the
+ * learner's pass over its samples in another order, and the backward pass see the same one.
+ *   out[i][c] = residual[i][c] + (kept ? x[i][c] / (1 - p) : 0)
+ * with p rounded to a multiple of 2^-16. Column c of a row of sequence q at step t is kept if its 16
+ * bits are >= p 2^16: of Philox4x32-10 at counter (q lo32, q hi32, t, 2^31 | site << 16 | c / 8)
+ * under `seed`, word c / 2 mod 4, the low half for even c. site (< 2^15) tells a network's dropout
+ * layers apart. fp32 arithmetic with one rounding, and the one to the type.
+ * The backward pass is the same call on the gradient without residual (whose gradient is out's).
+ * x, residual (may be NULL), out [n_rows][ld] of the type dtype, ld >= dim (columns from dim on are
+ * not written), 0 for x or residual: one row that all share. out may be x or residual with the
+ * same ld; otherwise their ranges must be apart. 1 <= dim <= 524,288; 0 <= p <= 1 - 2^-16;
+ * sequence int64 [n_rows], step int32 [n_rows]. A dropped element of x has no influence, also
+ * where it is infinite or NaN. All device memory of the context's device, aligned to its element;
+ * asynchronous on the context's stream; no work space. n_rows == 0 is valid. Errors: EINVAL, ECUDA.
+ */
+typedef struct malib_dropout_batch {
+    const void* x;
+    const void* residual;
+    void* out;
+    int64_t n_rows;
+    int64_t ld_x, ld_residual, ld_out;
+    const int64_t* sequence;
+    const int32_t* step;
+    uint64_t seed;
+    double p;
+    int32_t dim;
+    int32_t dtype;
+    uint32_t site;
+} malib_dropout_batch;
+int malib_dropout(malib_ctx* ctx, const malib_dropout_batch* batch);
+
 /* ---- measurement and self-test entry points (used by tests and the benchmark) ---- */
 
 /* Total decisions (env-steps: one decision by the acting seat) played by the

@@ -17,8 +17,8 @@ from . import _abi
 from ._abi import (MALIB_BF16, MALIB_DUMP_LOGITS, MALIB_ENOTCONVERGED, MALIB_ENV_KUHN,
                    MALIB_ENV_LEDUC, MALIB_ENV_SPREAD, MALIB_ENV_ADVERSARY, MALIB_ENV_SPEAKER_LISTENER,
                    MALIB_ENV_PUSH, MALIB_ENV_TAG, MALIB_ENV_REFERENCE, MALIB_EXACT_EXPECTATION, MALIB_F32, MALIB_POL_MLP,
-                   MALIB_F16, MALIB_POL_TABULAR, MALIB_SPREAD_CONTACT, EnvSpec, PolicyDesc, TokenBatch, TokenDistill,
-                   TokenGrad, TokenPpo, TokenPref, Traj)
+                   MALIB_F16, MALIB_POL_TABULAR, MALIB_SPREAD_CONTACT, DropoutBatch, EnvSpec, PolicyDesc, TokenBatch,
+                   TokenDistill, TokenDraw, TokenGrad, TokenList, TokenPpo, TokenPref, TokenScores, Traj)
 
 __all__ = ["MalibError", "Context", "EnvSpec", "make_spec", "policy_desc", "alloc_traj",
            "alloc_eval_dump", "malib_create", "malib_pop_load", "malib_rollout",
@@ -385,6 +385,39 @@ class Context:
                self.lib.malib_token_logprob(self.handle, C.byref(b), _vector(logp_out, n, _Types.f32, "logp_out"),
                                             _vector(entropy_out, n, _Types.f32, "entropy_out")))
 
+    def token_top(self, logits, ids_out, top_logp_out, tokens=None, logp_out=None, entropy_out=None, rank_out=None,
+                  temperature=1.0):
+        """The most likely entries of each row, most likely first: ids int32 [rows][top]
+        and their ln p [rows][top]; of the row's token its ln p and its rank (1: the most
+        likely entry), and the row's entropy, each [rows]. tokens may be None."""
+        b = _token_batch(logits, tokens, temperature)
+        n, f32, i32 = b.n_rows, _Types.f32, _Types.i32
+        if ids_out.dim() != 2 or ids_out.shape[0] != n or top_logp_out.shape != ids_out.shape:
+            raise ValueError("ids_out and top_logp_out must be [rows][top]")
+        top = ids_out.shape[1]
+        out = TokenList(_vector(ids_out, n * top, i32, "ids_out"), _vector(top_logp_out, n * top, f32, "top_logp_out"),
+                        _vector(logp_out, n, f32, "logp_out"), _vector(entropy_out, n, f32, "entropy_out"),
+                        _vector(rank_out, n, i32, "rank_out"), top)
+        _check(self.lib, self.handle, self.lib.malib_token_top(self.handle, C.byref(b), C.byref(out)))
+
+    def token_sample(self, logits, token_out, logp_out=None, entropy_out=None, draw_logp_out=None, tokens=None,
+                     uniform=None, sequence=None, step=None, seed=0, agent=0, top_k=0, top_p=1.0, temperature=1.0):
+        """Draws a token of each row from all its entries (top_k 0) or from the first
+        top_k, of which the likeliest are kept up to top_p of their probability: the
+        token, its ln p and the entropy by the whole row, and ln of the probability that
+        it was drawn with. The random numbers are uniform [rows], or those of (seed;
+        sequence int64 [rows], step int32 [rows], agent). Rows with a negative token in
+        tokens (may be token_out itself) are left out (-1)."""
+        b = _token_batch(logits, tokens, temperature)
+        n, f32, i32 = b.n_rows, _Types.f32, _Types.i32
+        d = TokenDraw(_vector(uniform, n, f32, "uniform"), _vector(sequence, n, _Types.i64, "sequence"),
+                      _vector(step, n, i32, "step"), seed, agent, top_k, top_p)
+        _check(self.lib, self.handle,
+               self.lib.malib_token_sample(self.handle, C.byref(b), C.byref(d), _vector(token_out, n, i32, "token_out"),
+                                           _vector(logp_out, n, f32, "logp_out"),
+                                           _vector(entropy_out, n, f32, "entropy_out"),
+                                           _vector(draw_logp_out, n, f32, "draw_logp_out")))
+
     def learn_token_ppo(self, logits, tokens, old_logp, advantage, grad_out=None, stats_out=None, weight=None,
                         ref_logp=None, logp_out=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0,
                         temperature=1.0, grad_scale=1.0):
@@ -440,6 +473,48 @@ class Context:
                                                   _token_grad(logits, grad_out, grad_scale),
                                                   _vector(loss_out, n, f32, "loss_out"),
                                                   _vector(stats_out, 3, f32, "stats_out")))
+
+    def learn_token_scores(self, logits, tokens, grad_out, logp_grad=None, entropy_grad=None, ids=None, top_grad=None,
+                           temperature=1.0, grad_scale=1.0):
+        """The gradient at the logits of any loss of log-probabilities and entropies, from
+        its slopes: logp_grad [rows] at ln p of the tokens, entropy_grad [rows] at the
+        entropies, top_grad [rows][top] at ln p of the entries ids int32 [rows][top]
+        (< 0: absent). Into grad_out (may be logits itself)."""
+        b = _token_batch(logits, tokens, temperature)
+        n, f32, top = b.n_rows, _Types.f32, 0
+        if (ids is None) != (top_grad is None):
+            raise ValueError("ids and top_grad go together")
+        if ids is not None:
+            if ids.dim() != 2 or ids.shape[0] != n or top_grad.shape != ids.shape or ids.shape[1] < 1:
+                raise ValueError("ids and top_grad must be [rows][top]")
+            top = ids.shape[1]
+        s = TokenScores(_vector(logp_grad, n, f32, "logp_grad"), _vector(entropy_grad, n, f32, "entropy_grad"),
+                        _vector(ids, n * top, _Types.i32, "ids"), _vector(top_grad, n * top, f32, "top_grad"), top)
+        _check(self.lib, self.handle,
+               self.lib.malib_learn_token_scores(self.handle, C.byref(b), C.byref(s),
+                                                 _token_grad(logits, grad_out, grad_scale)))
+
+    def dropout(self, x, out, p, seed, site=0, sequence=None, step=None, residual=None):
+        """out = residual + dropout(x) of matrices [rows][dim] (rows contiguous), with the mask
+        of (seed; sequence int64 [rows], step int32 [rows], site, column): the same in
+        whatever batch a row is. out may be x or residual. The backward pass is the same
+        call on the gradient without residual."""
+        if not _Types.codes:
+            _Types.load()
+        n, d, ld = _token_rows(x, "x")
+        if out.shape != x.shape or out.dtype is not x.dtype:
+            raise ValueError("out must have the shape and type of x")
+        ld_res = 0
+        if residual is not None:
+            if residual.shape != x.shape or residual.dtype is not x.dtype:
+                raise ValueError("residual must have the shape and type of x")
+            ld_res = _token_rows(residual, "residual")[2]
+        if sequence is None or step is None:
+            raise ValueError("sequence and step are needed")
+        b = DropoutBatch(x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), n, ld, ld_res,
+                         _token_rows(out, "out")[2], _vector(sequence, n, _Types.i64, "sequence"),
+                         _vector(step, n, _Types.i32, "step"), seed, p, d, _token_dtype(x, "x"), site)
+        _check(self.lib, self.handle, self.lib.malib_dropout(self.handle, C.byref(b)))
 
     def exploitability(self, ids0, x, ids1, y):
         """(b0, b1, exploitability) of the seat mixtures (ids with fp64 weights)."""

@@ -37,7 +37,8 @@ EXPORTS = (
     "malib_meta_aggregate", "malib_exploitability", "malib_learn_pg", "malib_learn_pg_batch",
     "malib_learn_ppo_batch", "malib_adam_step",
     "malib_pop_update", "malib_token_logprob", "malib_learn_token_ppo", "malib_learn_token_pref",
-    "malib_learn_token_distill",
+    "malib_learn_token_distill", "malib_token_top", "malib_token_sample",
+    "malib_learn_token_scores", "malib_dropout",
 )
 
 
@@ -81,6 +82,28 @@ class TokenPref(C.Structure):
 class TokenDistill(C.Structure):
     _fields_ = [("ids", C.c_void_p), ("teacher", C.c_void_p), ("weight", C.c_void_p), ("top", C.c_int32),
                 ("teacher_dtype", C.c_int32)]
+
+
+class TokenList(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("top_logp", C.c_void_p), ("logp", C.c_void_p), ("entropy", C.c_void_p),
+                ("rank", C.c_void_p), ("top", C.c_int32)]
+
+
+class TokenDraw(C.Structure):
+    _fields_ = [("uniform", C.c_void_p), ("sequence", C.c_void_p), ("step", C.c_void_p), ("seed", C.c_uint64),
+                ("agent", C.c_uint32), ("top_k", C.c_int32), ("top_p", C.c_float)]
+
+
+class TokenScores(C.Structure):
+    _fields_ = [("logp_grad", C.c_void_p), ("entropy_grad", C.c_void_p), ("ids", C.c_void_p), ("top_grad", C.c_void_p),
+                ("top", C.c_int32)]
+
+
+class DropoutBatch(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p), ("n_rows", C.c_int64),
+                ("ld_x", C.c_int64), ("ld_residual", C.c_int64), ("ld_out", C.c_int64), ("sequence", C.c_void_p),
+                ("step", C.c_void_p), ("seed", C.c_uint64), ("p", C.c_double), ("dim", C.c_int32), ("dtype", C.c_int32),
+                ("site", C.c_uint32)]
 
 
 _lock = threading.Lock()
@@ -147,6 +170,11 @@ def load(path: str | None = None):
                                                  C.POINTER(TokenGrad), P, P]),
             "malib_learn_token_distill": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenDistill),
                                                     C.POINTER(TokenGrad), P, P]),
+            "malib_token_top": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenList)]),
+            "malib_token_sample": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenDraw), P, P, P, P]),
+            "malib_learn_token_scores": (C.c_int, [P, C.POINTER(TokenBatch), C.POINTER(TokenScores),
+                                                   C.POINTER(TokenGrad)]),
+            "malib_dropout": (C.c_int, [P, C.POINTER(DropoutBatch)]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -3,6 +3,7 @@
 
 #include "malib.h"
 #include "token_common.cuh"
+#include "token_rollout.h"
 
 using namespace malib;
 
@@ -32,7 +33,9 @@ struct Call {
     // The same, or NULL.
     bool opt(const void* p, int align) const { return !p || dev(p, align); }
 
-    int begin(const malib_token_batch* b, bool tokens) {
+    enum Tokens { kNoTokens, kNeedTokens, kMayTokens };
+
+    int begin(const malib_token_batch* b, Tokens tokens) {
         a = TokenArgs{};
         if (!b) return bad("token batch is NULL");
         if (!known(b->dtype)) return bad("unknown logits dtype");
@@ -46,9 +49,10 @@ struct Call {
         const float k = (float)exact_k;
         if (b->n_rows > 0) {
             if (!dev(b->logits, (int)es)) return bad("logits must be aligned device memory of the context's device");
-            if (tokens && !dev(b->tokens, 4)) return bad("tokens must be aligned device memory of the context's device");
+            if (tokens != kNoTokens && !(tokens == kMayTokens ? opt(b->tokens, 4) : dev(b->tokens, 4)))
+                return bad("tokens must be aligned device memory of the context's device");
         }
-        if (!tokens && b->tokens) return bad("tokens must be NULL");
+        if (tokens == kNoTokens && b->tokens) return bad("tokens must be NULL");
         a.z = b->logits;
         a.ld = b->ld;
         a.n = b->n_rows;
@@ -124,7 +128,7 @@ int malib_token_logprob(malib_ctx* ctx, const malib_token_batch* batch, float* l
     Call c{ctx};
     if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
     DevSel d(c.v.device);
-    int r = c.begin(batch, true);
+    int r = c.begin(batch, Call::kNeedTokens);
     if (r != MALIB_OK) return r;
     if (c.a.n == 0) return MALIB_OK;
     if (!c.opt(logp_out, 4) || !c.opt(entropy_out, 4))
@@ -140,7 +144,7 @@ int malib_learn_token_ppo(malib_ctx* ctx, const malib_token_batch* batch, const 
     Call c{ctx};
     if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
     DevSel d(c.v.device);
-    int r = c.begin(batch, true);
+    int r = c.begin(batch, Call::kNeedTokens);
     if (r != MALIB_OK) return r;
     if (!loss) return c.bad("loss is NULL");
     if (!(loss->clip_low > 0.0f && loss->clip_low < 1.0f) || !(loss->clip_high > 0.0f) || std::isinf(loss->clip_high))
@@ -171,7 +175,7 @@ int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const
     Call c{ctx};
     if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
     DevSel d(c.v.device);
-    int r = c.begin(batch, true);
+    int r = c.begin(batch, Call::kNeedTokens);
     if (r != MALIB_OK) return r;
     if (!loss) return c.bad("loss is NULL");
     if (loss->n_pairs < 1 || loss->n_pairs > (1 << 30)) return c.bad("n_pairs must lie in [1, 2^30]");
@@ -198,7 +202,7 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
     Call c{ctx};
     if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
     DevSel d(c.v.device);
-    int r = c.begin(batch, false);
+    int r = c.begin(batch, Call::kNoTokens);
     if (r != MALIB_OK) return r;
     if (!loss) return c.bad("loss is NULL");
     if (loss->top < 1 || loss->top > kTokenMaxTop) return c.bad("top must lie in [1, 1024]");
@@ -215,6 +219,133 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
     c.a.loss = loss_out;
     c.a.stats = stats_out;
     return c.done(launch_token_rows(c.a, kTokDistill, c.v.n_sm, c.v.stream), c.a.n > 0 || stats_out ? 1 : 0);
+}
+
+int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_list* out) {
+    Call c{ctx};
+    if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
+    DevSel d(c.v.device);
+    int r = c.begin(batch, Call::kMayTokens);
+    if (r != MALIB_OK) return r;
+    if (!out) return c.bad("list is NULL");
+    if (out->top < 1 || out->top > kTokenMaxTop) return c.bad("top must lie in [1, 1024]");
+    if ((out->logp || out->rank) && !batch->tokens) return c.bad("logp and rank need tokens");
+    if (c.a.n == 0) return MALIB_OK;
+    if (c.a.n > INT64_MAX / 4 / out->top) return c.bad("the lists do not fit the address space");
+    if (!c.dev(out->ids, 4) || !c.dev(out->top_logp, 4) || !c.opt(out->logp, 4) || !c.opt(out->entropy, 4) ||
+        !c.opt(out->rank, 4))
+        return c.bad("outputs must be device memory of the context's device");
+    ListArgs a{c.a};
+    a.K = out->top;
+    a.top_ids = out->ids;
+    a.top_logp = out->top_logp;
+    a.logp = out->logp;
+    a.entropy = out->entropy;
+    a.rank = out->rank;
+    return c.done(launch_token_list(a, kListTop, c.v.n_sm, c.v.stream), 1);
+}
+
+int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_draw* draw, int32_t* token_out,
+                       float* logp_out, float* entropy_out, float* draw_logp_out) {
+    Call c{ctx};
+    if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
+    DevSel d(c.v.device);
+    int r = c.begin(batch, Call::kMayTokens);
+    if (r != MALIB_OK) return r;
+    if (!draw) return c.bad("draw is NULL");
+    if (draw->top_k < 0 || draw->top_k > kTokenMaxTop) return c.bad("top_k must lie in [0, 1024]");
+    if (!(draw->top_p > 0.0f && draw->top_p <= 1.0f)) return c.bad("top_p must lie in (0, 1]");
+    if (draw->top_k == 0 && draw->top_p < 1.0f) return c.bad("top_p below 1 needs top_k");
+    if (draw->agent >> 31) return c.bad("agent must lie below 2^31");
+    if (c.a.n == 0) return MALIB_OK;
+    if (draw->uniform ? !c.dev(draw->uniform, 4) : !c.dev(draw->sequence, 8) || !c.dev(draw->step, 4))
+        return c.bad("uniform, or sequence and step, must be aligned device memory of the context's device");
+    if (!c.opt(token_out, 4) || !c.opt(logp_out, 4) || !c.opt(entropy_out, 4) || !c.opt(draw_logp_out, 4))
+        return c.bad("outputs must be device memory of the context's device");
+    ListArgs a{c.a};
+    a.K = draw->top_k;
+    a.drawn = token_out;
+    a.logp = logp_out;
+    a.entropy = entropy_out;
+    a.draw_logp = draw_logp_out;
+    a.uniform = draw->uniform;
+    a.sequence = draw->sequence;
+    a.step = draw->step;
+    a.seed = draw->seed;
+    a.agent = draw->agent;
+    a.top_p = draw->top_p;
+    return c.done(launch_token_list(a, draw->top_k ? kListDraw : kListDrawAll, c.v.n_sm, c.v.stream), 1);
+}
+
+int malib_learn_token_scores(malib_ctx* ctx, const malib_token_batch* batch, const malib_token_scores* scores,
+                             const malib_token_grad* grad) {
+    Call c{ctx};
+    if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
+    DevSel d(c.v.device);
+    int r = c.begin(batch, Call::kNeedTokens);
+    if (r != MALIB_OK) return r;
+    if (!scores) return c.bad("scores is NULL");
+    if (c.a.n > 0 && !scores->logp_grad && !scores->entropy_grad && !scores->ids) return c.bad("no slopes are given");
+    if (scores->ids && (scores->top < 1 || scores->top > kTokenMaxTop)) return c.bad("top must lie in [1, 1024]");
+    if (!scores->ids && scores->top_grad) return c.bad("top_grad needs ids");
+    if (!grad || (c.a.n > 0 && !grad->grad)) return c.bad("gradient is NULL");
+    if ((r = c.gradient(grad)) != MALIB_OK) return r;
+    if (c.a.n == 0) return MALIB_OK;
+    if (!c.opt(scores->logp_grad, 4) || !c.opt(scores->entropy_grad, 4) || !c.opt(scores->ids, 4) ||
+        (scores->ids && !c.dev(scores->top_grad, 4)))
+        return c.bad("slopes and ids must be aligned device memory of the context's device");
+    if ((r = c.work()) != MALIB_OK) return r;
+    c.a.logp_grad = scores->logp_grad;
+    c.a.entropy_grad = scores->entropy_grad;
+    c.a.ids = scores->ids;
+    c.a.list_grad = scores->top_grad;
+    c.a.top = scores->ids ? scores->top : 0;
+    return c.done(launch_token_rows(c.a, scores->ids ? kTokScoresList : kTokScores, c.v.n_sm, c.v.stream), 1);
+}
+
+int malib_dropout(malib_ctx* ctx, const malib_dropout_batch* b) {
+    Call c{ctx};
+    if (!ctx_view(ctx, &c.v)) return MALIB_EINVAL;
+    DevSel d(c.v.device);
+    if (!b) return c.bad("dropout batch is NULL");
+    if (!known(b->dtype)) return c.bad("unknown dtype");
+    if (b->dim < 1 || b->dim > (1 << 19)) return c.bad("dim must lie in [1, 524288]");
+    if (b->n_rows < 0 || b->n_rows > kMaxRows) return c.bad("n_rows must lie in [0, 2^40]");
+    if (!(b->p >= 0.0 && b->p <= 65535.0 / 65536.0)) return c.bad("p must lie in [0, 1 - 2^-16]");
+    if (b->site >> 15) return c.bad("site must lie below 2^15");
+    const int64_t n = b->n_rows, es = elt_size(b->dtype), most = n > 0 ? INT64_MAX / es / n : INT64_MAX;
+    if ((b->ld_x != 0 && b->ld_x < b->dim) || (b->residual && b->ld_residual != 0 && b->ld_residual < b->dim) ||
+        b->ld_out < b->dim || b->ld_x > most || (b->residual && b->ld_residual > most) || b->ld_out > most)
+        return c.bad("row stride below dim, or rows past the address space");
+    if (n == 0) return MALIB_OK;
+    if (!c.dev(b->x, (int)es) || !c.opt(b->residual, (int)es) || !c.dev(b->out, (int)es))
+        return c.bad("x, residual and out must be aligned device memory of the context's device");
+    if (!c.dev(b->sequence, 8) || !c.dev(b->step, 4))
+        return c.bad("sequence and step must be aligned device memory of the context's device");
+    const auto apart = [&](const void* in, int64_t ld) {
+        if (!in || (in == b->out && (ld == b->ld_out || n == 1))) return true;
+        const uintptr_t i0 = (uintptr_t)in, i1 = i0 + (uintptr_t)(((n - 1) * ld + b->dim) * es);
+        const uintptr_t o0 = (uintptr_t)b->out, o1 = o0 + (uintptr_t)(((n - 1) * b->ld_out + b->dim) * es);
+        return o1 <= i0 || i1 <= o0;
+    };
+    if (!apart(b->x, b->ld_x) || !apart(b->residual, b->ld_residual)) return c.bad("out overlaps x or residual other than in place");
+    DropArgs a{};
+    a.x = b->x;
+    a.residual = b->residual;
+    a.out = b->out;
+    a.n = n;
+    a.ld_x = b->ld_x;
+    a.ld_res = b->ld_residual;
+    a.ld_out = b->ld_out;
+    a.d = b->dim;
+    a.dtype = b->dtype;
+    a.sequence = b->sequence;
+    a.step = b->step;
+    a.seed = b->seed;
+    a.counter = 1u << 31 | b->site << 16;
+    a.least = (uint32_t)(b->p * 65536.0 + 0.5);
+    a.scale = (float)(65536.0 / (65536.0 - (double)a.least));
+    return c.done(launch_dropout(a, c.v.n_sm, c.v.stream), 1);
 }
 
 }  // extern "C"

@@ -34,7 +34,14 @@ namespace malib {
 constexpr int kTokenMaxTop = 1024;                   // teacher entries of a row
 constexpr int kTokenMaxCtas = 8192;                  // CTAs whose partial sums the work space holds
 
-enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3 };
+enum : int { kTokLogp = 0, kTokPpo = 1, kTokDistill = 2, kTokPairGrad = 3, kTokScores = 4, kTokScoresList = 5 };
+// Calls whose gradient has a factor of ln p (and not of p alone), and one that may be infinite;
+// calls that read a list of entries for every row; calls with statistics over the rows.
+__host__ __device__ constexpr bool has_slope(int op) { return op == kTokPpo || op == kTokScores || op == kTokScoresList; }
+__host__ __device__ constexpr bool has_list(int op) { return op == kTokDistill || op == kTokScoresList; }
+__host__ __device__ constexpr bool has_stats(int op) { return op == kTokPpo || op == kTokDistill; }
+// Entries that a row's list takes: the scores' one has the token behind the `top` given ones.
+__host__ __device__ constexpr int list_room(int op, int top) { return op == kTokDistill ? top : op == kTokScoresList ? top + 1 : 0; }
 
 // What a row's statistics leave for a preference pair's sums and its gradient: first
 // value + rest is ln p of the token; the pair's sums put d L / d logit of the token
@@ -75,6 +82,10 @@ struct TokenArgs {
     const void* teacher;         // [n][top]
     int32_t tdtype, top;
     float tt, top_scale;         // T^2, T
+    // scores: the loss's slopes
+    const float* logp_grad;      // [n] at ln p of the row's token; null: 0
+    const float* entropy_grad;   // [n] at H; null: 0
+    const float* list_grad;      // [n][top] at ln p of the entries ids
     // preference pairs
     const int64_t* offsets;      // [2 pairs + 1]
     int32_t n_pairs;
@@ -466,6 +477,25 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
     const float gt = f * slope, h = f * a.ent, inv_s = 1.f / r.s;
     // p (-gt + h (ln p + H)),  ln p = x ln 2 - ln S
     return RowGrad{r.m, inv_s * (a.ent != 0.f ? fmaf(h, *H - logf(r.s), -gt) : -gt), inv_s * h * kLn2, gt};
+}
+
+// The gradient of a row whose loss has the slopes `total` at its log-probabilities (the token's and
+// the listed entries' together) and `e` at its entropy, before what each of these entries adds, `at`
+// times its own slope:
+//   d L / d z_j = (1 / T) [ own slope of j - p_j total - e p_j (ln p_j + H) ].
+__device__ __forceinline__ RowGrad scores_row(const TokenArgs& a, float total, float e, const RowStat& r) {
+    const float f = a.gscale * a.inv_t, gt = f * total, h = -f * e, inv_s = 1.f / r.s;
+    return RowGrad{r.m, inv_s * (e != 0.f ? fmaf(h, row_entropy(r) - logf(r.s), -gt) : -gt), inv_s * h * kLn2, f};
+}
+
+// What a gradient of scores takes besides its list: the slopes at the token's ln p and at H.
+struct Slopes {
+    float g, e;
+};
+template <int kOp>
+__device__ __forceinline__ Slopes load_slopes(const TokenArgs& a, int64_t row) {
+    if (kOp != kTokScores && kOp != kTokScoresList) return Slopes{0.f, 0.f};
+    return Slopes{kOp == kTokScores && a.logp_grad ? a.logp_grad[row] : 0.f, a.entropy_grad ? a.entropy_grad[row] : 0.f};
 }
 
 // The outputs of a row whose log-probability is all that is asked for.

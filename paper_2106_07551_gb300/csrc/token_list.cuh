@@ -1,0 +1,534 @@
+// Token policies, the rollout's side: a row's most likely entries and the draw of its token.
+// A row holds logits z_0 .. z_{V-1}; its entries are in the order of falling z, the lower index
+// first among equal ones (-0 equals 0). With the row's statistics (m, S, t) as for the losses,
+// ln p_j = (z_j - m) / T - ln S, and the order of z is that of p. A masked entry (-infinity) is
+// never listed and never drawn.
+//
+// The first K entries: an entry's key is its logit's bits, mapped so that larger logits have
+// larger keys, with the index below them, so that no two keys are equal (56 bits). A bound is
+// looked for with at least K keys and at most kListCap above it: a histogram of the keys' top 8
+// bits says in which bin the K-th lies, one of the next 8 bits looks into that bin, and so on
+// until few enough are left. What lies above the bound is collected, sorted, and cut at K.
+//
+// The draw from the whole row takes the entries in the order of their index: sums of consecutive
+// entries are kept from the statistics' pass, the one that holds u times the whole is found among
+// them, and its entries alone are read again. The draw from a list takes them in the list's order.
+#pragma once
+
+#include "token_common.cuh"
+#include "token_peer.cuh"
+#include "token_rollout.h"
+
+namespace malib {
+
+struct ListShape {
+    int cluster, slice;                              // CTAs a row, vectors of a CTA's slice
+};
+
+namespace {
+
+constexpr int kListCap = 2048;                       // most entries that are sorted
+constexpr int kListPer = 8;                          // vectors a thread has in flight
+constexpr uint32_t kIndexMask = (1u << 24) - 1;
+
+// Larger for larger logits; the same for -0 and 0.
+__device__ __forceinline__ uint32_t order_key(float z) {
+    const uint32_t b = __float_as_uint(__fadd_rn(z, 0.f));
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t key) {
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+__device__ __forceinline__ uint64_t entry_key(float z, int j) {
+    return (uint64_t)order_key(z) << 24 | (kIndexMask - (uint32_t)j);
+}
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)(kIndexMask - ((uint32_t)key & kIndexMask)); }
+__device__ __forceinline__ float key_logit(uint64_t key) { return order_value((uint32_t)(key >> 24)); }
+
+// What a CTA's peers take from it.
+struct __align__(16) ListShared {
+    float4 stat;                                     // m, S, t, entries before the token (bits)
+    uint32_t hist[2][256];
+    uint32_t count;                                  // keys collected
+};
+struct ListPick {
+    uint32_t digit, above, at;                       // of a histogram; at = 0: fewer than K entries in all
+};
+
+template <class T>
+struct RowView {
+    const T* z;
+    int h, nv, V;                                    // entries before the first in its vector; vectors
+    __device__ __forceinline__ uint4 vec(int v) const {
+        const int j = v * Elt<T>::W - h;
+        return j >= 0 && j + Elt<T>::W <= V ? *reinterpret_cast<const uint4*>(z + j) : load_part(z, j, V);
+    }
+};
+template <class T>
+__device__ __forceinline__ float entry_of(const uint4& q, int i) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    return Elt<T>::get(Elt<T>::word(w, i));
+}
+// f(j, z) for the unmasked entries of vectors [v0, v1), by n threads.
+template <class T, class F>
+__device__ __forceinline__ void each_entry(const RowView<T>& r, int v0, int v1, int tid, int n, F f) {
+    for (int v = v0 + tid; v < v1; v += n) {
+        const uint4 q = r.vec(v);
+#pragma unroll
+        for (int i = 0; i < Elt<T>::W; ++i) {
+            const float z = entry_of<T>(q, i);
+            if (z > -INFINITY) f(v * Elt<T>::W - r.h + i, z);
+        }
+    }
+}
+
+// Sorts the n keys at `key` (room for kListCap), largest first; what comes back has the first K in
+// order. Few of them are counted: a key's place is how many are larger.
+template <int kThreads>
+__device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, int tid) {
+    if (n <= max(128, kThreads + kThreads / 2)) {
+        for (int i = tid; i < n; i += kThreads) {
+            const uint64_t own = key[i];
+            int place = 0;
+            for (int j = 0; j < n; ++j) place += key[j] > own;
+            if (place < K) sorted[place] = own;
+        }
+        __syncthreads();
+        return sorted;
+    }
+    int P = 256;
+    while (P < n) P *= 2;
+    for (int i = n + tid; i < P; i += kThreads) key[i] = 0ull;
+    __syncthreads();
+    for (int size = 2; size <= P; size *= 2)
+        for (int gap = size / 2; gap > 0; gap /= 2) {
+            for (int i = tid; i < P / 2; i += kThreads) {
+                const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
+                const uint64_t x = key[lo], y = key[hi];
+                if ((x < y) == ((lo & size) == 0)) {
+                    key[lo] = y;
+                    key[hi] = x;
+                }
+            }
+            __syncthreads();
+        }
+    return key;
+}
+
+__device__ __forceinline__ float warp_scan(float v, int lane) {      // inclusive
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const float b = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += b;
+    }
+    return v;
+}
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A row's random number in [0, 1).
+__device__ __forceinline__ float row_uniform(const ListArgs& a, int64_t row) {
+    if (a.uniform) return a.uniform[row];
+    return u24(draw((uint64_t)a.sequence[row], (uint32_t)a.step[row], a.agent, a.seed).x);
+}
+
+__device__ __forceinline__ void write_draw(const ListArgs& a, int64_t row, int token, float logp, float H, float drawn) {
+    if (a.drawn) a.drawn[row] = token;
+    if (a.logp) a.logp[row] = logp;
+    if (a.entropy) a.entropy[row] = H;
+    if (a.draw_logp) a.draw_logp[row] = drawn;
+}
+
+// The draw from a sorted list (one warp). w_i = 2^x_i; kept are the entries before which less than
+// top_p of the list's mass lies; the token is the first whose running mass exceeds u times the kept
+// one.
+__device__ __forceinline__ void draw_listed(const ListArgs& a, int64_t row, const RowStat& r, const uint64_t* key, int n,
+                                            int lane) {
+    const int per = (n + 31) / 32, i0 = min(n, lane * per), i1 = min(n, i0 + per);
+    float own = 0.f;
+    for (int i = i0; i < i1; ++i) own += exp2_fast(x_of(key_logit(key[i]), r.m, a.k));
+    const float before = warp_scan(own, lane) - own, total = __shfl_sync(0xffffffffu, before + own, 31);
+    // the kept ones' number, mass, and sum of w x
+    float cum = before, mass = 0.f, t = 0.f;
+    int kept = 0;
+    for (int i = i0; i < i1; ++i) {
+        if (i > 0 && a.top_p < 1.f && !(cum < a.top_p * total)) break;
+        const float x = x_of(key_logit(key[i]), r.m, a.k), w = exp2_fast(x);
+        cum += w;
+        mass = cum;
+        t = fmaf(w, fmaxf(x, kXMin), t);
+        kept = i + 1;
+    }
+    mass = warp_max(mass);
+    t = warp_add(t);
+    kept = __reduce_max_sync(0xffffffffu, kept);
+    const float target = row_uniform(a, row) * mass;
+    int at = -1, last = -1;
+    cum = before;
+    for (int i = i0; i < min(i1, kept); ++i) {
+        const float w = exp2_fast(x_of(key_logit(key[i]), r.m, a.k));
+        cum += w;
+        if (w > 0.f) last = i;
+        if (at < 0 && w > 0.f && cum > target) at = i;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, at >= 0);
+    at = hit ? __shfl_sync(0xffffffffu, at, __ffs(hit) - 1) : __reduce_max_sync(0xffffffffu, last);
+    if (lane == 0) {
+        const float z = key_logit(key[at]);
+        write_draw(a, row, key_index(key[at]), log_prob(a, r, z), row_entropy(r), log_prob(a, RowStat{r.m, mass, t}, z));
+    }
+}
+
+template <class T, int kOp, int kThreads>
+__global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListShape sh) {
+    constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
+    constexpr bool kAll = kOp == kListDrawAll;
+    extern __shared__ __align__(16) uint64_t keys[];                 // keys [kListCap + 1024], or segments' (m, S)
+    __shared__ ListShared own;
+    __shared__ float4 red[kWarps];
+    __shared__ ListPick pick;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = sh.cluster, rank = C > 1 ? (int)cluster_rank() : 0;
+    uint64_t* sorted = keys + kListCap;
+    float2* segment = reinterpret_cast<float2*>(keys);
+    wait_for_previous();
+    let_next_start();
+    // Every CTA of the row comes here; what each wrote before is seen by all after it.
+    auto meet = [&] {
+        if (C == 1) {
+            __syncthreads();
+        } else {
+            cluster_arrive();
+            cluster_wait();
+        }
+    };
+    for (int64_t row = blockIdx.x / C; row < a.n; row += gridDim.x / C) {
+        const int token = a.tokens ? a.tokens[row] : 0;
+        const bool first = tid == 0 && rank == 0;
+        bool live = token >= 0;
+        if (kOp == kListTop && token >= a.V) {
+            live = false;
+            if (first) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        }
+        // (the same in every thread of the row's CTAs)
+        auto no_list = [&](float logp) {
+            if (kOp == kListTop && rank == 0)
+                for (int i = tid; i < a.K; i += kThreads) {
+                    a.top_ids[row * a.K + i] = -1;
+                    a.top_logp[row * a.K + i] = logp;
+                }
+        };
+        if (!live) {
+            if (kOp == kListTop) {
+                if (first) {
+                    logp_row(a, row, false, RowStat{0.f, 1.f, 0.f}, 0.f);
+                    if (a.rank) a.rank[row] = 0;
+                }
+                no_list(0.f);
+            } else if (first) {
+                write_draw(a, row, -1, 0.f, 0.f, 0.f);
+            }
+            continue;
+        }
+        const T* z = static_cast<const T*>(a.z) + row * a.ld;
+        const int h = (int)(((uintptr_t)z & 15u) / sizeof(T)), nv = (h + a.V + W - 1) / W;
+        const RowView<T> view{z, h, nv, a.V};
+        const int v_lo = min(nv, rank * sh.slice), v_hi = min(nv, v_lo + sh.slice);
+        float zt = 0.f;
+        if (kOp == kListTop && a.tokens) zt = Elt<T>::get(z[token]);
+
+        // ---- statistics; a warp's vectors of a batch follow one another
+        LongStat st{-INFINITY, {0.f, 0.f}, {0.f, 0.f}};
+        uint32_t before = 0;
+        const uint32_t own_end = (uint32_t)min(token, v_hi * W - h);   // equal entries count up to here
+        int segments = 0;
+        for (int b = v_lo; b < v_hi; b += kBatch, segments += kWarps) {
+            uint4 x[kListPer];
+            const int v0 = b + warp * kWarpVecs + lane;
+#pragma unroll
+            for (int u = 0; u < kListPer; ++u) x[u] = v0 + u * 32 < v_hi ? view.vec(v0 + u * 32) : Elt<T>::none();
+            raise(st, warp_max(vec_max<T>(x)), a.k);
+            RowStat part{st.m, 0.f, 0.f};
+            if (st.m != -INFINITY) gather<T>(part, x, a.k);
+            st.s.add(part.s);
+            st.t.add(part.t);
+            if (kAll) {
+                const float s = warp_add(part.s);
+                if (lane == 0) segment[segments + warp] = make_float2(st.m, s);
+            }
+            if (kOp == kListTop && a.rank) {
+#pragma unroll
+                for (int u = 0; u < kListPer; ++u)
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const float e = entry_of<T>(x[u], i);
+                        before += e > zt || (e == zt && (uint32_t)((v0 + u * 32) * W - h + i) < own_end);
+                    }
+            }
+        }
+        RowStat r = stat_of(st);
+        r.s = warp_add(r.s);
+        r.t = warp_add(r.t);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) red[warp] = make_float4(r.m, r.s, r.t, __uint_as_float(before));
+        __syncthreads();
+        {
+            const float4 q = red[lane & (kWarps - 1)];
+            r = reduce_stat<kWarps>(RowStat{q.x, q.y, q.z}, a.k);
+            before = __reduce_add_sync(0xffffffffu, lane < kWarps ? __float_as_uint(q.w) : 0u);
+        }
+        float4 peer = make_float4(r.m, r.s, r.t, 0.f);               // lane i: CTA i's
+        if (C > 1) {
+            if (tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
+            meet();
+            peer = lane < C ? peer_load(&own.stat, lane) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            before = __reduce_add_sync(0xffffffffu, __float_as_uint(peer.w));
+            r = reduce_stat<32>(RowStat{peer.x, peer.y, peer.z}, a.k);
+        }
+        live = r.m != -INFINITY;
+        const bool good = live && fabsf(r.s) < INFINITY;             // no NaN, no +infinity
+        if (kOp == kListTop && first) {
+            logp_row(a, row, live, r, zt);
+            if (a.rank) a.rank[row] = good ? (int)before + 1 : 0;
+        }
+        if (!good) {
+            no_list(live ? NAN : 0.f);
+            if (kOp != kListTop && first) write_draw(a, row, -1, live ? NAN : 0.f, live ? NAN : 0.f, live ? NAN : 0.f);
+        } else if constexpr (kAll) {
+            if (warp == 0) {
+                // the CTA, then the segment, that holds the target; then its entries. Sums of many
+                // are in 64 bits; where rounding leaves none, the last one that has a mass.
+                const double target = (double)row_uniform(a, row) * (double)r.s;
+                auto mass_at = [&](float m, float s) { return s * exp2_fast(fmaxf((m - r.m) * a.k, kXMin) + kExpBias); };
+                double passed = 0.0;
+                int cta = 0;
+                if (C > 1) {
+                    const float w = lane < C ? mass_at(peer.x, peer.y) : 0.f, cum = warp_scan(w, lane);
+                    const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && (double)cum > target),
+                                   some = __ballot_sync(0xffffffffu, w > 0.f);
+                    cta = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+                    passed = (double)__shfl_sync(0xffffffffu, cum - w, cta);
+                }
+                if (cta == rank) {
+                    int at = -1, last = 0;
+                    double last_passed = passed;
+                    for (int s0 = 0; s0 < segments && at < 0; s0 += 32) {
+                        const float2 sg = s0 + lane < segments ? segment[s0 + lane] : make_float2(-INFINITY, 0.f);
+                        const float w = sg.y > 0.f ? mass_at(sg.x, sg.y) : 0.f, cum = warp_scan(w, lane);
+                        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && passed + (double)cum > target),
+                                       some = __ballot_sync(0xffffffffu, w > 0.f);
+                        if (some) {
+                            const int k = 31 - __clz(some);
+                            last = s0 + k;
+                            last_passed = passed + (double)__shfl_sync(0xffffffffu, cum - w, k);
+                        }
+                        if (hit) {
+                            const int k = __ffs(hit) - 1;
+                            at = s0 + k;
+                            passed += (double)__shfl_sync(0xffffffffu, cum - w, k);
+                        } else {
+                            passed += (double)__shfl_sync(0xffffffffu, cum, 31);
+                        }
+                    }
+                    if (at < 0) {
+                        at = last;
+                        passed = last_passed;
+                    }
+                    const float rest = (float)(target - passed);
+                    const int v0 = v_lo + at * kWarpVecs + lane;
+                    float sum = 0.f;
+                    int found = -1, behind = -1;
+                    float fz = 0.f, bz = 0.f;
+                    for (int u = 0; u < kListPer && !__any_sync(0xffffffffu, found >= 0); ++u) {
+                        const int v = v0 + u * 32;
+                        const uint4 q = v < v_hi ? view.vec(v) : Elt<T>::none();
+                        float e[W], mine = 0.f;
+#pragma unroll
+                        for (int i = 0; i < W; ++i) {
+                            e[i] = exp2_fast(x_of(entry_of<T>(q, i), r.m, a.k));
+                            mine += e[i];
+                        }
+                        const float incl = warp_scan(mine, lane);
+                        float cum = sum + (incl - mine);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) {
+                            cum += e[i];
+                            if (e[i] > 0.f) {
+                                behind = v * W - h + i;
+                                bz = entry_of<T>(q, i);
+                                if (found < 0 && cum > rest) {
+                                    found = behind;
+                                    fz = bz;
+                                }
+                            }
+                        }
+                        sum += __shfl_sync(0xffffffffu, incl, 31);
+                    }
+                    const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
+                    int lane_at, j;
+                    if (hit) {
+                        lane_at = __ffs(hit) - 1;
+                        j = found;
+                    } else {
+                        const int most = __reduce_max_sync(0xffffffffu, behind);
+                        lane_at = __ffs(__ballot_sync(0xffffffffu, behind == most)) - 1;
+                        j = behind;
+                        fz = bz;
+                    }
+                    if (lane == lane_at) {
+                        const float logp = log_prob(a, r, fz);
+                        write_draw(a, row, j, logp, row_entropy(r), logp);
+                    }
+                }
+            }
+        } else {
+            // ---- a bound with at least K keys above it, or all, and at most kListCap
+            uint64_t bound = 0;
+            uint32_t above = 0;
+            int shift = 48;
+            for (int pass = 0;; ++pass, shift -= 8) {
+                uint32_t* hist = own.hist[pass & 1];
+                for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
+                __syncthreads();
+                each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                    const uint64_t key = entry_key(e, j);
+                    if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
+                });
+                meet();
+                if (warp == 0) {
+                    uint32_t n[8], sum = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int bin = 255 - 8 * lane - i;
+                        n[i] = hist[bin];
+                        if (C > 1) {
+                            n[i] = 0;
+                            for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
+                        }
+                        sum += n[i];
+                    }
+                    uint32_t upto = sum;
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) {
+                        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                        if (lane >= o) upto += x;
+                    }
+                    const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
+                    if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
+                        ListPick p{0, 0, 0};
+                        uint32_t cum = above + upto - sum;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
+                                p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
+                            cum += n[i];
+                        }
+                        pick = p;
+                    }
+                }
+                __syncthreads();
+                const ListPick p = pick;
+                if (p.at == 0) {                                     // in the first pass only: all of them
+                    bound = 0;
+                    break;
+                }
+                bound = bound << 8 | p.digit;
+                above = p.above;
+                if (above + p.at <= (uint32_t)kListCap) {
+                    bound <<= shift;
+                    break;
+                }
+            }
+            // ---- what lies above it, in the first CTA
+            if (tid == 0) own.count = 0;
+            __syncthreads();
+            each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                const uint64_t key = entry_key(e, j);
+                if (key >= bound) keys[atomicAdd(&own.count, 1u)] = key;
+            });
+            meet();
+            if (rank == 0) {
+                int n = (int)own.count;
+                for (int c = 1; c < C; ++c) {
+                    const int more = (int)peer_load(&own.count, c);
+                    for (int i = tid; i < more; i += kThreads) keys[n + i] = peer_load(keys + i, c);
+                    n += more;
+                }
+                __syncthreads();
+                const uint64_t* list = sort_keys<kThreads>(keys, sorted, n, a.K, tid);
+                if (kOp == kListDraw) {
+                    if (warp == 0) draw_listed(a, row, r, list, min(n, a.K), lane);
+                } else {
+                    for (int i = tid; i < a.K; i += kThreads) {
+                        const int64_t o = row * a.K + i;
+                        a.top_ids[o] = i < n ? key_index(list[i]) : -1;
+                        a.top_logp[o] = i < n ? log_prob(a, r, key_logit(list[i])) : -INFINITY;
+                    }
+                }
+            }
+        }
+        meet();                                                      // nothing of this row is read any more
+    }
+}
+
+template <class T, int kOp, int kThreads>
+cudaError_t launch_list_threads(const ListArgs& a, const ListShape& sh, size_t bytes, cudaStream_t s) {
+    const auto kernel = token_list_kernel<T, kOp, kThreads>;
+    if (bytes > 32 << 10) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at[2] = {};
+    const int64_t rows = a.n < 1 << 20 ? a.n : 1 << 20;              // by a CTA or cluster each, the others by them too
+    cfg.gridDim = dim3((unsigned)(rows * sh.cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (sh.cluster > 1) {
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = sh.cluster;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, a, sh);
+}
+
+template <class T, int kOp>
+cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
+    const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
+    ListShape sh{1, (int)nv};
+    for (int c = 2; c <= 8 && (nv + c - 1) / c >= 512; c *= 2)
+        if (a.n * c <= 4 * (int64_t)n_sm) {
+            sh.cluster = c;
+            sh.slice = (int)((nv + c - 1) / c);
+        }
+    const bool small = sh.slice <= 256;
+    const int batch = small ? 256 : 2048;
+    const size_t bytes = kOp == kListDrawAll ? (size_t)((sh.slice + batch - 1) / batch) * (batch / 256) * sizeof(float2)
+                                             : (kListCap + 1024) * sizeof(uint64_t);
+    return small ? launch_list_threads<T, kOp, 32>(a, sh, bytes, s) : launch_list_threads<T, kOp, 256>(a, sh, bytes, s);
+}
+
+template <class T>
+cudaError_t launch_list_type(const ListArgs& a, int op, int n_sm, cudaStream_t s) {
+    if (op == kListTop) return launch_list_op<T, kListTop>(a, n_sm, s);
+    if (op == kListDraw) return launch_list_op<T, kListDraw>(a, n_sm, s);
+    return launch_list_op<T, kListDrawAll>(a, n_sm, s);
+}
+
+}  // namespace
+
+}  // namespace malib

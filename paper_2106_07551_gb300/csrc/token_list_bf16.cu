@@ -1,0 +1,10 @@
+// The most likely entries and the draw of bf16 logits.
+#include "token_list.cuh"
+
+namespace malib {
+
+cudaError_t launch_token_list_bf16(const ListArgs& a, int op, int n_sm, cudaStream_t s) {
+    return launch_list_type<__nv_bfloat16>(a, op, n_sm, s);
+}
+
+}  // namespace malib

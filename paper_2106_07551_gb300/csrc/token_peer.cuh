@@ -1,5 +1,5 @@
-// Clusters: rank, barrier, stores to a peer's shared memory. Only for
-// launches with a cluster dimension: without one these stores are illegal instructions.
+// Clusters: rank, barrier, stores to a peer's shared memory and loads from it. Only for
+// launches with a cluster dimension: without one these are illegal instructions.
 #pragma once
 
 #include "device_common.cuh"
@@ -23,6 +23,32 @@ __device__ __forceinline__ void peer_store(void* dst, uint64_t* bar, uint32_t ra
             smem_u32(dst)),
         "r"(smem_u32(bar)), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
         : "memory");
+}
+
+// Reads the same place of CTA `rank` of the cluster, after a cluster barrier that follows its writes.
+__device__ __forceinline__ uint64_t peer_load(const uint64_t* src, uint32_t rank) {
+    uint64_t v;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.u64 %0, [a];\n}"
+                 : "=l"(v)
+                 : "r"(smem_u32(src)), "r"(rank)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t peer_load(const uint32_t* src, uint32_t rank) {
+    uint32_t v;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.u32 %0, [a];\n}"
+                 : "=r"(v)
+                 : "r"(smem_u32(src)), "r"(rank)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 peer_load(const float4* src, uint32_t rank) {
+    float4 v;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(smem_u32(src)), "r"(rank)
+                 : "memory");
+    return v;
 }
 
 // mbar_wait_bounded for a barrier that peers complete: their stores are seen after it.

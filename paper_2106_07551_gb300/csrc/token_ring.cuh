@@ -8,7 +8,7 @@
 // a row's statistics stage by stage; warp 0 sums the warps' statistics and computes the
 // row's loss; and the consumers go through the same stages again, writing the gradient to
 // global memory and freeing each stage as they leave it. The next row's copies fill the
-// freed stages meanwhile. For distillation a further warp (the teacher) prepares the row's
+// freed stages meanwhile. Where rows have lists a further warp (the teacher) prepares the row's
 // list of entries ahead.
 //
 // Rows are claimed, not dealt: SMs do not all get the same share of the memory's rate, and
@@ -79,7 +79,7 @@ struct RingHugeLong : RingHuge {
 };
 constexpr int kMaxStages = 6, kMaxCluster = 8;
 constexpr int kQueue = 4;                            // most rows known ahead
-constexpr int kRingMost = 216 * 1024;                // dynamic shared memory
+constexpr int kRingMost = 216 * 1024 + 32;           // dynamic shared memory: six large stages, two lists
 
 // What the row's CTAs exchange, and what a warp leaves for its CTA.
 struct __align__(16) Partial {
@@ -159,13 +159,14 @@ __device__ __forceinline__ void sum_rows(const TokenArgs& a) {
 }
 
 template <class T, int kOp, class Ring>
-__global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32), Ring::kCtas)
+__global__ void __launch_bounds__(Ring::kConsumers + (has_list(kOp) ? 64 : 32), Ring::kCtas)
     token_ring_kernel(TokenArgs a, Shape sh) {
     constexpr int W = Elt<T>::W;
     constexpr int kConsumers = Ring::kConsumers, kConsumerWarps = kConsumers / 32, kPer = Ring::kPer;
     constexpr int kStageVecs = kConsumers * kPer, kStageBytes = kStageVecs * 16;
-    constexpr int kThreads = kConsumers + (kOp == kTokDistill ? 64 : 32);
-    constexpr bool kTop = kOp == kTokDistill;
+    constexpr int kThreads = kConsumers + (has_list(kOp) ? 64 : 32);
+    constexpr bool kTop = has_list(kOp), kAll = kOp == kTokDistill;   // kAll: rows have no token
+    constexpr bool kScores = kOp == kTokScores || kOp == kTokScoresList;
     using Own = typename Ring::Own;
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages];
@@ -184,7 +185,8 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = sh.cluster, rank = C > 1 ? (int)cluster_rank() : 0;
     const int v_lo = rank * sh.slice;
-    TopEntry* entries = reinterpret_cast<TopEntry*>(ring + sh.stages * kStageBytes);   // [2][a.top]
+    TopEntry* entries = reinterpret_cast<TopEntry*>(ring + sh.stages * kStageBytes);   // [2][room]
+    const int room = list_room(kOp, a.top);
 
     if (tid == 0) {
         dead = 0;
@@ -230,8 +232,8 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
     auto parity_of = [&](uint32_t t) { return t >> sh.queue_log & 1u; };
     // A row's token and weight (row < a.n).
     auto look = [&](int64_t row) {
-        Queued q{row, kTop ? 0 : a.tokens[row], 1.f};
-        if (kOp != kTokLogp) q.w = a.weight ? a.weight[row] : a.w0;
+        Queued q{row, kAll ? 0 : a.tokens[row], 1.f};
+        if (has_stats(kOp)) q.w = a.weight ? a.weight[row] : a.w0;
         return q;
     };
     auto settle = [&](Queued& q, bool report) {
@@ -353,8 +355,8 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                 if (q.token >= 0) {
                     const int b = turn & 1u;
                     wait(&tempty[b], (turn >> 1 & 1u) ^ 1u);
-                    const TopRow r = top_row<T, kSeen>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld,
-                                                       entries + b * a.top, seen);
+                    const TopRow r = list_row<T, kOp, kSeen>(a, q.row, static_cast<const T*>(a.z) + q.row * a.ld, q.token,
+                                                             entries + b * room, seen);
                     if (lane == 0) top[b] = r;
                     __syncwarp();
                     if (lane == 0) mbar_arrive_release(&tfull[b]);
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     if (kOp == kTokLogp) logp_row(a, row, false, RowStat{0.f, 1.f, 0.f}, 0.f);
                     if (kOp == kTokPpo && a.logp) a.logp[row] = 0.f;
                     if (kTop && a.loss) a.loss[row] = 0.f;
-                    if (kOp != kTokLogp) a.row_sums[row] = RowSum{0.f, 0.f, 0.f, 0};
+                    if (has_stats(kOp)) a.row_sums[row] = RowSum{0.f, 0.f, 0.f, 0};
                 }
                 if (g) zero_entries<T, kConsumers>(tid, g, max(0, v_lo * W - h), max(0, min(a.V, v_hi * W - h)));
                 leave(t);
@@ -391,7 +393,9 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
             }
             T z_token = Elt<T>::put(0.f);            // widened where it is used: nothing waits for it here
             PpoRow in{};
+            Slopes slopes{0.f, 0.f};
             if (warp == 0) {
+                slopes = load_slopes<kOp>(a, row);
                 if (!kTop) z_token = z[q.token];
                 if (kOp == kTokPpo) in = ppo_load(a, row);
             }
@@ -461,6 +465,9 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                             sum = RowSum{q.w * loss, kl, H, clipped != 0.f ? 3 : 1};
                         }
                         if (a.logp && first) a.logp[row] = logp;
+                    } else if (kScores) {
+                        if (live) c = scores_row(a, kTop ? top[b].q : slopes.g, slopes.e, r);
+                        if (!kTop) c.at *= slopes.g;
                     } else {
                         live = live && top[b].live;
                         if (live) {
@@ -471,9 +478,9 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                         }
                         if (a.loss && first) a.loss[row] = loss;
                     }
-                    if (first) a.row_sums[row] = sum;
+                    if (has_stats(kOp) && first) a.row_sums[row] = sum;
                     if (lane == 0) {
-                        rout[slot] = RowOut{c, !live ? kOutZero : kOp == kTokPpo && is_steep(c) ? kOutSteep : kOutPlain};
+                        rout[slot] = RowOut{c, !live ? kOutZero : has_slope(kOp) && is_steep(c) ? kOutSteep : kOutPlain};
                         mbar_arrive_release(&rfull[slot]);
                     }
                 }
@@ -492,11 +499,11 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     const uint8_t* src = ring + at.stage * kStageBytes;
                     const int token = kTop ? -1 : q.token;
                     if (kind != kOutPlain) {
-                        if (kOp == kTokPpo && kind == kOutSteep)
+                        if (has_slope(kOp) && kind == kOutSteep)
                             emit_steep_part<T, kConsumers>(tid, reinterpret_cast<const T*>(src) - j, j0, j1, g, c, a.k, token);
                         else
                             zero_entries<T, kConsumers>(tid, g, j0, j1);
-                    } else if (kOp == kTokPpo && c.c1 != 0.f)
+                    } else if (has_slope(kOp) && c.c1 != 0.f)
                         emit_stage<T, true, kConsumers, kPer>(tid, src, j, j0, j1, n, g, alike, c, a.k, token);
                     else
                         emit_stage<T, false, kConsumers, kPer>(tid, src, j, j0, j1, n, g, alike, c, a.k, token);
@@ -504,15 +511,14 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
                     if (lane == 0) mbar_arrive_release(&empty[at.stage]);
                 }
                 if (kTop) {
-                    // the teacher's entries of this slice, over what the CTA's warps have written
+                    // the list's entries of this slice, over what the CTA's warps have written
                     if (lane == 0) mbar_arrive_release(&pfull[slot]);
                     wait(&pfull[slot], parity);
                     const int j0 = max(0, v_lo * W - h), j1 = min(a.V, v_hi * W - h);
-                    if (kind == kOutPlain)
-                        for (int i = tid; i < a.top; i += kConsumers) {
-                            const TopEntry e = entries[b * a.top + i];
-                            if (e.id >= j0 && e.id < j1)
-                                g[e.id] = Elt<T>::put(c.c0 * exp2_fast(x_of(e.z, c.m, a.k)) - c.at * e.q);
+                    if (kind != kOutZero)
+                        for (int i = tid; i < room; i += kConsumers) {
+                            const TopEntry e = entries[b * room + i];
+                            if (e.id >= j0 && e.id < j1) g[e.id] = Elt<T>::put(list_entry<kOp>(e, c, a.k));
                         }
                 }
             }
@@ -531,7 +537,7 @@ __global__ void __launch_bounds__(Ring::kConsumers + (kOp == kTokDistill ? 64 : 
         cluster_wait();
     }
     // the CTA that ends last clears the claims for the next call and sums the statistics
-    const bool stats = kOp != kTokLogp && a.stats;
+    const bool stats = has_stats(kOp) && a.stats;
     if (!stats && sh.dealt) return;
     if (!last_of(a.ticket, gridDim.x)) return;
     if (tid == 0) *a.claims = 0ull;
@@ -547,9 +553,9 @@ cudaError_t launch_ring(const TokenArgs& a, const Shape& sh, int64_t units, cuda
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at[2] = {};
     cfg.gridDim = dim3((unsigned)((units ? units : 1) * sh.cluster));
-    cfg.blockDim = dim3(Ring::kConsumers + (kOp == kTokDistill ? 64 : 32));
+    cfg.blockDim = dim3(Ring::kConsumers + (has_list(kOp) ? 64 : 32));
     cfg.dynamicSmemBytes = (size_t)sh.stages * Ring::kConsumers * Ring::kPer * 16 +
-                           (kOp == kTokDistill ? 2 * a.top * sizeof(TopEntry) : 0);
+                           2 * list_room(kOp, a.top) * sizeof(TopEntry);
     cfg.stream = s;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -635,6 +641,8 @@ template <class T>
 cudaError_t launch_ring_type(const TokenArgs& a, int op, int n_sm, cudaStream_t s) {
     if (op == kTokLogp) return launch_ring_op<T, kTokLogp>(a, n_sm, s);
     if (op == kTokPpo) return launch_ring_op<T, kTokPpo>(a, n_sm, s);
+    if (op == kTokScores) return launch_ring_op<T, kTokScores>(a, n_sm, s);
+    if (op == kTokScoresList) return launch_ring_op<T, kTokScoresList>(a, n_sm, s);
     return launch_ring_op<T, kTokDistill>(a, n_sm, s);
 }
 

@@ -68,10 +68,15 @@ cudaError_t short_grid(Kernel kernel, size_t bytes, int64_t n, int64_t rows, boo
 // them, `first` among them for what is stored; the gradient's factors c and whether it has any.
 template <int kOp>
 __device__ __forceinline__ void row_loss(const TokenArgs& a, int64_t row, bool first, const RowStat& r, float zt,
-                                         const PpoRow& in, float w, const TopRow& top, bool& live, RowGrad& c,
-                                         Totals& total) {
+                                         const PpoRow& in, const Slopes& slopes, float w, const TopRow& top, bool& live,
+                                         RowGrad& c, Totals& total) {
     if (kOp == kTokLogp) {
         if (first) logp_row(a, row, live, r, zt);
+        return;
+    }
+    if (kOp == kTokScores || kOp == kTokScoresList) {
+        if (live) c = scores_row(a, kOp == kTokScores ? slopes.g : top.q, slopes.e, r);
+        if (kOp == kTokScores) c.at *= slopes.g;
         return;
     }
     RowSum sum{0.f, 0.f, 0.f, 0};
@@ -105,9 +110,9 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_al
 template <class T, int kOp, int G, int N>
 __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a) {
     constexpr int W = Elt<T>::W, kRows = 32 / G;     // rows a warp takes at a time
-    constexpr bool kTop = kOp == kTokDistill;
+    constexpr bool kTop = has_list(kOp), kAll = kOp == kTokDistill;   // kAll: rows have no token
     static_assert(!kTop || G == 32, "a warp prepares its row's list");
-    extern __shared__ TopEntry lists[];              // [warps][a.top]
+    extern __shared__ TopEntry lists[];              // [warps][list_room]
     __shared__ uint32_t seen[kShortWarps][kTop ? 4096 / 32 : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G;
     const int64_t step = (int64_t)gridDim.x * kShortWarps * kRows;
@@ -119,16 +124,16 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
         const int64_t row = in_range ? row0 + lane / G : a.n - 1;
         const T* z = static_cast<const T*>(a.z) + row * a.ld;
         T* g = kOp != kTokLogp && a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
-        const int token = kTop ? -1 : a.tokens[row];
-        const bool known = kTop || (token >= 0 && token < a.V);
+        const int token = kAll ? -1 : a.tokens[row];
+        const bool known = kAll || (token >= 0 && token < a.V);
         float w = 1.f;
         TokenRow pair{};
         PpoRow in{};
-        if (kOp == kTokPpo || kTop) w = a.weight ? a.weight[row] : a.w0;
+        if (has_stats(kOp)) w = a.weight ? a.weight[row] : a.w0;
         if (kOp == kTokPpo) in = ppo_load(a, row);
         if (kOp == kTokPairGrad) pair = a.rows[row];
         const bool read = in_range && w != 0.f && known && (kOp != kTokPairGrad || pair.inv_s != 0.f);
-        if (!kTop && in_range && token >= a.V) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        if (!kAll && in_range && token >= a.V) atomicOr(a.err, ERRBIT_BAD_TOKEN);
 
         const int h = (int)(((uintptr_t)z & 15u) / sizeof(T));
         uint4 q[N];
@@ -140,11 +145,12 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
             q[u] = j >= 0 && j + W <= a.V ? *reinterpret_cast<const uint4*>(z + j) : load_part(z, j, a.V);
         }
         float zt = 0.f;
-        if (kOp != kTokPairGrad && !kTop && read) zt = Elt<T>::get(z[token]);
-        TopEntry* list = lists + warp * a.top;
+        if (kOp != kTokPairGrad && !kAll && read) zt = Elt<T>::get(z[token]);
+        const Slopes slopes = load_slopes<kOp>(a, row);
+        TopEntry* list = lists + warp * list_room(kOp, a.top);
         TopRow top{};
         if constexpr (kTop) {
-            if (read) top = top_row<T, 4096>(a, row, z, list, seen[warp]);
+            if (read) top = list_row<T, kOp, 4096>(a, row, z, token, list, seen[warp]);
         }
 
         RowGrad c{0.f, 0.f, 0.f, 0.f};
@@ -157,37 +163,37 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
             if (live) gather<T>(r, q, a.k);
             r.s = group_sum<G>(r.s);
             r.t = group_sum<G>(r.t);
-            row_loss<kOp>(a, row, sub == 0 && in_range, r, zt, in, w, top, live, c, total);
+            row_loss<kOp>(a, row, sub == 0 && in_range, r, zt, in, slopes, w, top, live, c, total);
         }
         if (!g) continue;
-        const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0, plain = live && !(kOp == kTokPpo && is_steep(c));
+        const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0, plain = live && !(has_slope(kOp) && is_steep(c));
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int j = (sub + u * G) * W - h;
             if (!in_range || j >= a.V) continue;
             F2 v[W / 2] = {};
             if (plain) {
-                emit<T, kOp == kTokPpo>(q[u], c, a.k, v);
+                emit<T, has_slope(kOp)>(q[u], c, a.k, v);
                 if (!kTop && (unsigned)(token - j) < (unsigned)W) add_at(v, token - j, c.at);
-            } else if (kOp == kTokPpo && live) {
-                emit_steep<T>(q[u], c, a.k, token - j, v);
+            } else if (has_slope(kOp) && live) {
+                emit_steep<T>(q[u], c, a.k, kTop ? -1 : token - j, v);
             }
             const uint4 out = Elt<T>::pack(v);
             if (alike && j >= 0 && j + W <= a.V) *reinterpret_cast<uint4*>(g + j) = out;
             else store_part(g + j, j, a.V, out);
         }
         if (kTop) {
-            // the teacher's entries, over what the warp has written
+            // the list's entries, over what the warp has written
             __syncwarp();
             if (live)
-                for (int i = lane; i < a.top; i += 32) {
+                for (int i = lane; i < list_room(kOp, a.top); i += 32) {
                     const TopEntry e = list[i];
-                    if (e.id >= 0) g[e.id] = Elt<T>::put(c.c0 * exp2_fast(x_of(e.z, c.m, a.k)) - c.at * e.q);
+                    if (e.id >= 0) g[e.id] = Elt<T>::put(list_entry<kOp>(e, c, a.k));
                 }
             __syncwarp();
         }
     }
-    if ((kOp == kTokPpo || kTop) && a.stats) finish_short<kOp>(a, total);
+    if (has_stats(kOp) && a.stats) finish_short<kOp>(a, total);
 }
 
 // Rows of a warp each that pass through shared memory, more than 4 vectors a lane: every lane
@@ -201,28 +207,29 @@ __global__ void __launch_bounds__(kShortThreads) token_short_kernel(TokenArgs a)
 template <class T, int kOp>
 __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, int slab) {
     constexpr int W = Elt<T>::W, kPer = 4;
-    constexpr bool kTop = kOp == kTokDistill;
-    extern __shared__ __align__(16) uint8_t shared[];                // [warps][slab] vectors, [warps][a.top] entries
+    constexpr bool kTop = has_list(kOp), kAll = kOp == kTokDistill;   // kAll: rows have no token
+    extern __shared__ __align__(16) uint8_t shared[];                // [warps][slab] vectors, [warps][list_room] entries
     __shared__ uint32_t seen[kShortWarps][kTop ? 4096 / 32 : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint4* own = reinterpret_cast<uint4*>(shared) + warp * slab;
-    TopEntry* list = reinterpret_cast<TopEntry*>(shared + (size_t)kShortWarps * slab * 16) + warp * a.top;
+    TopEntry* list = reinterpret_cast<TopEntry*>(shared + (size_t)kShortWarps * slab * 16) + warp * list_room(kOp, a.top);
     Totals total{};
     wait_for_previous();
     if (kOp == kTokLogp) let_next_start();
     for (int64_t row = (int64_t)blockIdx.x * kShortWarps + warp; row < a.n; row += (int64_t)gridDim.x * kShortWarps) {
         const T* z = static_cast<const T*>(a.z) + row * a.ld;
         T* g = kOp != kTokLogp && a.g ? static_cast<T*>(a.g) + row * a.gld : nullptr;
-        const int token = kTop ? -1 : a.tokens[row];
+        const int token = kAll ? -1 : a.tokens[row];
         float w = 1.f;
         TokenRow pair{};
         PpoRow in{};
-        if (kOp == kTokPpo || kTop) w = a.weight ? a.weight[row] : a.w0;
+        if (has_stats(kOp)) w = a.weight ? a.weight[row] : a.w0;
         if (kOp == kTokPpo) in = ppo_load(a, row);
         if (kOp == kTokPairGrad) pair = a.rows[row];
-        const bool known = kTop || (token >= 0 && token < a.V);
+        const bool known = kAll || (token >= 0 && token < a.V);
+        const Slopes slopes = load_slopes<kOp>(a, row);
         bool live = w != 0.f && known && (kOp != kTokPairGrad || pair.inv_s != 0.f);
-        if (!kTop && token >= a.V && lane == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
+        if (!kAll && token >= a.V && lane == 0) atomicOr(a.err, ERRBIT_BAD_TOKEN);
 
         const int h = (int)(((uintptr_t)z & 15u) / sizeof(T)), nv = (h + a.V + W - 1) / W;
         RowStat r{-INFINITY, 0.f, 0.f};
@@ -234,8 +241,8 @@ __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, 
                 if (j >= 0 && j + W <= a.V) cp_async_16(own + i, z + j);
                 else own[i] = load_part(z, j, a.V);
             }
-            if (kOp != kTokPairGrad && !kTop) zt = Elt<T>::get(z[token]);
-            if constexpr (kTop) top = top_row<T, 4096>(a, row, z, list, seen[warp]);
+            if (kOp != kTokPairGrad && !kAll) zt = Elt<T>::get(z[token]);
+            if constexpr (kTop) top = list_row<T, kOp, 4096>(a, row, z, token, list, seen[warp]);
             cp_async_wait();
             __syncwarp();
         }
@@ -254,32 +261,33 @@ __global__ void __launch_bounds__(kShortThreads) token_slab_kernel(TokenArgs a, 
                 r = reduce_stat<32>(r, a.k);
                 live = r.m != -INFINITY;
             }
-            row_loss<kOp>(a, row, lane == 0, r, zt, in, w, top, live, c, total);
+            row_loss<kOp>(a, row, lane == 0, r, zt, in, slopes, w, top, live, c, total);
         }
-        const bool plain = __all_sync(0xffffffffu, live && !(kOp == kTokPpo && is_steep(c)));
+        const bool plain = __all_sync(0xffffffffu, live && !(has_slope(kOp) && is_steep(c)));
+        const int at = kTop ? -1 : token;            // a list has the token
         if (g && !plain) {
-            if (kOp == kTokPpo && live)
-                emit_steep_part<T, 32>(lane, reinterpret_cast<const T*>(own) + h, 0, a.V, g, c, a.k, token);
+            if (has_slope(kOp) && live)
+                emit_steep_part<T, 32>(lane, reinterpret_cast<const T*>(own) + h, 0, a.V, g, c, a.k, at);
             else
                 zero_entries<T, 32>(lane, g, 0, a.V);
         }
         if (g && plain) {
             const uint8_t* src = reinterpret_cast<const uint8_t*>(own);
             const bool alike = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
-            if (kOp == kTokPpo && c.c1 != 0.f) emit_stage<T, true, 32, kPer>(lane, src, -h, 0, a.V, nv, g, alike, c, a.k, token);
-            else emit_stage<T, false, 32, kPer>(lane, src, -h, 0, a.V, nv, g, alike, c, a.k, token);
-            if (kTop) {
-                // the teacher's entries, over what the warp has written
-                __syncwarp();
-                for (int i = lane; i < a.top; i += 32) {
-                    const TopEntry e = list[i];
-                    if (e.id >= 0) g[e.id] = Elt<T>::put(c.c0 * exp2_fast(x_of(e.z, c.m, a.k)) - c.at * e.q);
-                }
+            if (has_slope(kOp) && c.c1 != 0.f) emit_stage<T, true, 32, kPer>(lane, src, -h, 0, a.V, nv, g, alike, c, a.k, at);
+            else emit_stage<T, false, 32, kPer>(lane, src, -h, 0, a.V, nv, g, alike, c, a.k, at);
+        }
+        if (kTop && g && live) {
+            // the list's entries, over what the warp has written
+            __syncwarp();
+            for (int i = lane; i < list_room(kOp, a.top); i += 32) {
+                const TopEntry e = list[i];
+                if (e.id >= 0) g[e.id] = Elt<T>::put(list_entry<kOp>(e, c, a.k));
             }
         }
         __syncwarp();
     }
-    if ((kOp == kTokPpo || kTop) && a.stats) finish_short<kOp>(a, total);
+    if (has_stats(kOp) && a.stats) finish_short<kOp>(a, total);
 }
 
 // Rows of up to N <= 32 entries (the actions of the environments): a thread a row, so that
@@ -315,6 +323,7 @@ __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) 
             w = a.weight ? a.weight[row] : a.w0;
             in = ppo_load(a, row);
         }
+        const Slopes slopes = load_slopes<kOp>(a, row);
         if (kOp == kTokPairGrad) pair = a.rows[row];
         const bool read = w != 0.f && token >= 0 && token < a.V && (kOp != kTokPairGrad || pair.inv_s != 0.f);
         if (token >= a.V) atomicOr(a.err, ERRBIT_BAD_TOKEN);
@@ -351,6 +360,9 @@ __global__ void __launch_bounds__(kShortThreads) token_tiny_kernel(TokenArgs a) 
             }
             if (kOp == kTokLogp) {
                 if (in_range) logp_row(a, row, live, r, zt);
+            } else if (kOp == kTokScores) {
+                if (live) c = scores_row(a, slopes.g, slopes.e, r);
+                c.at *= slopes.g;
             } else {
                 float logp = 0.f;
                 if (live) {
@@ -400,15 +412,15 @@ cudaError_t launch_tiny(const TokenArgs& a, int n_sm, cudaStream_t s) {
 
 template <class T, int kOp, int G, int N>
 cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
-    const size_t bytes = kOp == kTokDistill ? (size_t)kShortWarps * a.top * sizeof(TopEntry) : 0;
+    const size_t bytes = has_list(kOp) ? (size_t)kShortWarps * list_room(kOp, a.top) * sizeof(TopEntry) : 0;
     if (bytes > 0) {
         const cudaError_t e = cudaFuncSetAttribute(token_short_kernel<T, kOp, G, N>,
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   kShortWarps * kTokenMaxTop * (int)sizeof(TopEntry));
+                                                   kShortWarps * list_room(kOp, kTokenMaxTop) * (int)sizeof(TopEntry));
         if (e != cudaSuccess) return e;
     }
     unsigned grid = 0;
-    const bool stats = (kOp == kTokPpo || kOp == kTokDistill) && a.stats;
+    const bool stats = has_stats(kOp) && a.stats;
     const cudaError_t e =
         short_grid(token_short_kernel<T, kOp, G, N>, bytes, a.n, kShortWarps * (32 / G), stats, n_sm, &grid);
     if (e != cudaSuccess) return e;
@@ -418,12 +430,12 @@ cudaError_t launch_short(const TokenArgs& a, int n_sm, cudaStream_t s) {
 template <class T, int kOp>
 cudaError_t launch_slab(const TokenArgs& a, int nv, int n_sm, cudaStream_t s) {
     const int slab = (nv + 31) / 32 * 32;
-    const size_t bytes = (size_t)kShortWarps * (slab * 16 + (kOp == kTokDistill ? a.top * sizeof(TopEntry) : 0));
+    const size_t bytes = (size_t)kShortWarps * (slab * 16 + list_room(kOp, a.top) * sizeof(TopEntry));
     cudaError_t e = cudaFuncSetAttribute(token_slab_kernel<T, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         kShortWarps * (kShortVecs * 16 + kTokenMaxTop * (int)sizeof(TopEntry)));
+                                         kShortWarps * (kShortVecs * 16 + list_room(kOp, kTokenMaxTop) * (int)sizeof(TopEntry)));
     if (e != cudaSuccess) return e;
     unsigned grid = 0;
-    const bool stats = (kOp == kTokPpo || kOp == kTokDistill) && a.stats;
+    const bool stats = has_stats(kOp) && a.stats;
     e = short_grid(token_slab_kernel<T, kOp>, bytes, a.n, kShortWarps, stats, n_sm, &grid);
     if (e != cudaSuccess) return e;
     return launch_after(token_slab_kernel<T, kOp>, grid, kShortThreads, bytes, s, a, slab);
@@ -433,7 +445,7 @@ cudaError_t launch_slab(const TokenArgs& a, int nv, int n_sm, cudaStream_t s) {
 template <class T, int kOp>
 cudaError_t launch_short_op(const TokenArgs& a, int n_sm, cudaStream_t s) {
     const int nv = (a.V + 2 * Elt<T>::W - 2) / Elt<T>::W;
-    if constexpr (kOp != kTokDistill) {
+    if constexpr (!has_list(kOp)) {
         if (a.V <= 8) return launch_tiny<T, kOp, 8>(a, n_sm, s);
         if (a.V <= 16) return launch_tiny<T, kOp, 16>(a, n_sm, s);
         if (a.V <= 32) return launch_tiny<T, kOp, 32>(a, n_sm, s);
@@ -454,6 +466,8 @@ cudaError_t launch_short_type(const TokenArgs& a, int op, int n_sm, cudaStream_t
     if (op == kTokLogp) return launch_short_op<T, kTokLogp>(a, n_sm, s);
     if (op == kTokPpo) return launch_short_op<T, kTokPpo>(a, n_sm, s);
     if (op == kTokDistill) return launch_short_op<T, kTokDistill>(a, n_sm, s);
+    if (op == kTokScores) return launch_short_op<T, kTokScores>(a, n_sm, s);
+    if (op == kTokScoresList) return launch_short_op<T, kTokScoresList>(a, n_sm, s);
     return launch_short_op<T, kTokPairGrad>(a, n_sm, s);
 }
 

@@ -6,9 +6,15 @@
 //
 // The first K entries: an entry's key is its logit's bits, mapped so that larger logits have
 // larger keys, with the index below them, so that no two keys are equal (56 bits). A bound is
-// looked for with at least K keys and at most kListCap above it: a histogram of the keys' top 8
-// bits says in which bin the K-th lies, one of the next 8 bits looks into that bin, and so on
-// until few enough are left. What lies above the bound is collected, sorted, and cut at K.
+// looked for with at least K keys and at most kListCap above it; what lies above it is collected,
+// sorted, and cut at K. The bound comes from the maxima of groups of entries, which the
+// statistics' pass leaves: the K-th largest maximum has at least K entries above it, and as few
+// more as groups have several of the first entries. Only the groups whose maximum reaches it are
+// read again. The maxima's keys are held in 16 bits, which lowers the bound to the next
+// such value; which one that is, a histogram of their distances from the row's maximum says.
+// Where that leaves more than kListCap entries (many equal ones, or the first entries in
+// few groups), the bound is found from all keys: a histogram of their top 8 bits says in which bin
+// the K-th lies, one of the next 8 bits looks into that bin, and so on.
 //
 // The draw from the whole row takes the entries in the order of their index: sums of consecutive
 // entries are kept from the statistics' pass, the one that holds u times the whole is found among
@@ -23,12 +29,15 @@ namespace malib {
 
 struct ListShape {
     int cluster, slice;                              // CTAs a row, vectors of a CTA's slice
+    int group;                                       // vectors of a maximum: 1, 2, 4 or a multiple of 8; 0: no maxima
 };
 
 namespace {
 
 constexpr int kListCap = 2048;                       // most entries that are sorted
 constexpr int kListPer = 8;                          // vectors a thread has in flight
+constexpr int kListBins = 1024;                      // of the maxima's distances
+constexpr int kListGroups = 4096;                    // most maxima of a slice
 constexpr uint32_t kIndexMask = (1u << 24) - 1;
 
 // Larger for larger logits; the same for -0 and 0.
@@ -48,12 +57,35 @@ __device__ __forceinline__ float key_logit(uint64_t key) { return order_value((u
 // What a CTA's peers take from it.
 struct __align__(16) ListShared {
     float4 stat;                                     // m, S, t, entries before the token (bits)
-    uint32_t hist[2][256];
+    uint32_t hist[kListBins];                        // or two of 256 bins
     uint32_t count;                                  // keys collected
 };
 struct ListPick {
     uint32_t digit, above, at;                       // of a histogram; at = 0: fewer than K entries in all
 };
+
+// The largest of each group of a thread's vectors, as the top 16 bits of its key, to out[0],
+// out[stride] ..; 0: none. What comes back is the largest of all.
+template <class T>
+__device__ __forceinline__ float group_maxima(const uint4 (&x)[kListPer], int group, uint16_t* out, int stride) {
+    uint32_t m[kListPer];
+#pragma unroll
+    for (int u = 0; u < kListPer; ++u)
+        m[u] = Elt<T>::max(Elt<T>::max(x[u].x, x[u].y), Elt<T>::max(x[u].z, x[u].w));
+    const auto store = [&](int i, uint32_t w) {
+        const float z = Elt<T>::largest(w);
+        out[i * stride] = z > -INFINITY ? (uint16_t)(order_key(z) >> 16) : (uint16_t)0;
+    };
+#pragma unroll
+    for (int n = kListPer; n > 1; n /= 2) {
+        if (group * n == kListPer)
+#pragma unroll
+            for (int i = 0; i < n; ++i) store(i, m[i]);
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) m[i] = Elt<T>::max(m[2 * i], m[2 * i + 1]);
+    }
+    return Elt<T>::largest(m[0]);
+}
 
 template <class T>
 struct RowView {
@@ -191,13 +223,17 @@ template <class T, int kOp, int kThreads>
 __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListShape sh) {
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;
-    extern __shared__ __align__(16) uint64_t keys[];                 // keys [kListCap + 1024], or segments' (m, S)
+    // keys [kListCap], sorted ones [1024] (or groups to be read again), maxima [kListGroups]; or segments' (m, S)
+    extern __shared__ __align__(16) uint64_t keys[];
     __shared__ ListShared own;
     __shared__ float4 red[kWarps];
     __shared__ ListPick pick;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = sh.cluster, rank = C > 1 ? (int)cluster_rank() : 0;
     uint64_t* sorted = keys + kListCap;
+    uint32_t* again = reinterpret_cast<uint32_t*>(sorted);
+    uint16_t* maxima = reinterpret_cast<uint16_t*>(sorted + 1024);
+    __shared__ uint32_t n_again, warp_sum[kWarps];
     float2* segment = reinterpret_cast<float2*>(keys);
     wait_for_previous();
     let_next_start();
@@ -249,13 +285,29 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
         LongStat st{-INFINITY, {0.f, 0.f}, {0.f, 0.f}};
         uint32_t before = 0;
         const uint32_t own_end = (uint32_t)min(token, v_hi * W - h);   // equal entries count up to here
-        int segments = 0;
-        for (int b = v_lo; b < v_hi; b += kBatch, segments += kWarps) {
+        int segments = 0, batch = 0;
+        float group_max = -INFINITY;
+        for (int b = v_lo; b < v_hi; b += kBatch, segments += kWarps, ++batch) {
             uint4 x[kListPer];
             const int v0 = b + warp * kWarpVecs + lane;
 #pragma unroll
             for (int u = 0; u < kListPer; ++u) x[u] = v0 + u * 32 < v_hi ? view.vec(v0 + u * 32) : Elt<T>::none();
-            raise(st, warp_max(vec_max<T>(x)), a.k);
+            float mx;
+            if (!kAll && sh.group > 0) {
+                uint16_t* out = maxima + tid + (sh.group < kListPer ? batch * (kListPer / sh.group) * kThreads : 0);
+                mx = group_maxima<T>(x, sh.group, out, kThreads);
+                if (sh.group >= kListPer) {
+                    group_max = fmaxf(group_max, mx);
+                    if ((batch + 1) * kListPer % sh.group == 0 || b + kBatch >= v_hi) {
+                        maxima[batch * kListPer / sh.group * kThreads + tid] =
+                            group_max > -INFINITY ? (uint16_t)(order_key(group_max) >> 16) : (uint16_t)0;
+                        group_max = -INFINITY;
+                    }
+                }
+            } else {
+                mx = vec_max<T>(x);
+            }
+            raise(st, warp_max(mx), a.k);
             RowStat part{st.m, 0.f, 0.f};
             if (st.m != -INFINITY) gather<T>(part, x, a.k);
             st.s.add(part.s);
@@ -390,71 +442,154 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
                 }
             }
         } else {
-            // ---- a bound with at least K keys above it, or all, and at most kListCap
             uint64_t bound = 0;
-            uint32_t above = 0;
-            int shift = 48;
-            for (int pass = 0;; ++pass, shift -= 8) {
-                uint32_t* hist = own.hist[pass & 1];
-                for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
-                __syncthreads();
-                each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
-                    const uint64_t key = entry_key(e, j);
-                    if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
-                });
-                meet();
-                if (warp == 0) {
-                    uint32_t n[8], sum = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int bin = 255 - 8 * lane - i;
-                        n[i] = hist[bin];
-                        if (C > 1) {
-                            n[i] = 0;
-                            for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
-                        }
-                        sum += n[i];
+            bool sure = sh.group == 0 && a.V <= kListCap;            // few enough entries above the bound
+            if (tid == 0) own.count = n_again = pick.digit = 0;
+            if (sh.group > 0) {
+                // ---- the bound from the groups' maxima, and the entries of those that reach it
+                const int slots = ((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + sh.group - 1) / sh.group;
+                const uint32_t top_key = order_key(r.m) >> 16;
+                uint32_t reach = 0;
+                for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {   // bins of one value, then of 64
+                    for (int i = tid; i < kListBins; i += kThreads) own.hist[i] = 0;
+                    __syncthreads();
+                    for (int i = tid; i < slots * kThreads; i += kThreads) {
+                        const uint32_t key = maxima[i], bin = (top_key - key) >> coarse;
+                        if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
                     }
+                    meet();
+                    // thread i counts the bins from kBins i on
+                    constexpr int kBins = kListBins / kThreads;
+                    uint32_t sum = 0;
+                    const auto in_bin = [&](int bin) {
+                        if (C == 1) return own.hist[bin];
+                        uint32_t n = 0;
+                        for (int c = 0; c < C; ++c) n += peer_load(own.hist + bin, c);
+                        return n;
+                    };
+#pragma unroll 4
+                    for (int i = 0; i < kBins; ++i) sum += in_bin(kBins * tid + i);
                     uint32_t upto = sum;
 #pragma unroll
                     for (int o = 1; o < 32; o *= 2) {
-                        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-                        if (lane >= o) upto += x;
+                        const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
+                        if (lane >= o) upto += q;
                     }
-                    const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
-                    if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
-                        ListPick p{0, 0, 0};
-                        uint32_t cum = above + upto - sum;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
-                                p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
-                            cum += n[i];
+                    if (kWarps > 1) {
+                        if (lane == 31) warp_sum[warp] = upto;
+                        __syncthreads();
+                        for (int w = 0; w < warp; ++w) upto += warp_sum[w];
+                    }
+                    if (upto >= (uint32_t)a.K && upto - sum < (uint32_t)a.K) {
+                        uint32_t cum = upto - sum, bin = kBins * tid;
+                        while ((cum += in_bin(bin)) < (uint32_t)a.K) ++bin;
+                        // the bin's smallest value, at least 1 (0 has no entries)
+                        const uint32_t below = ((bin + 1) << coarse) - 1;
+                        pick.digit = below < top_key ? top_key - below : 1u;
+                    }
+                    meet();
+                    reach = pick.digit;
+                }
+                if (reach > 0) {
+                    bound = (uint64_t)reach << 40;
+                    for (int i = tid; i < slots * kThreads; i += kThreads)
+                        if (maxima[i] >= reach) {
+                            const uint32_t at = atomicAdd(&n_again, 1u);
+                            if (at < kListCap) again[at] = i;
                         }
-                        pick = p;
+                    __syncthreads();
+                    const int items = (int)min(n_again, (uint32_t)kListCap) * sh.group;
+                    for (int item = tid; item < items; item += kThreads) {
+                        const int id = (int)again[item / sh.group], n = id / kThreads * sh.group + item % sh.group;
+                        const int v = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
+                        if (v >= v_hi) continue;
+                        const uint4 q = view.vec(v);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) {
+                            const float e = entry_of<T>(q, i);
+                            if (e > -INFINITY && order_key(e) >> 16 >= reach) {
+                                const uint32_t at = atomicAdd(&own.count, 1u);
+                                if (at < kListCap) keys[at] = entry_key(e, v * W - h + i);
+                            }
+                        }
                     }
-                }
-                __syncthreads();
-                const ListPick p = pick;
-                if (p.at == 0) {                                     // in the first pass only: all of them
-                    bound = 0;
-                    break;
-                }
-                bound = bound << 8 | p.digit;
-                above = p.above;
-                if (above + p.at <= (uint32_t)kListCap) {
-                    bound <<= shift;
-                    break;
+                    if (tid == 0 && n_again > kListCap) atomicMax(&own.count, (uint32_t)kListCap + 1);
+                    meet();
+                    uint32_t n = own.count;
+                    if (C > 1) n = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
+                    sure = n <= (uint32_t)kListCap;
                 }
             }
-            // ---- what lies above it, in the first CTA
-            if (tid == 0) own.count = 0;
-            __syncthreads();
-            each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
-                const uint64_t key = entry_key(e, j);
-                if (key >= bound) keys[atomicAdd(&own.count, 1u)] = key;
-            });
-            meet();
+            // (sure is the same in all CTAs of the row)
+            if (!sure || sh.group == 0) {
+                if (!sure) {
+                    bound = 0;
+                    uint32_t above = 0;
+                    int shift = 48;
+                    for (int pass = 0;; ++pass, shift -= 8) {
+                        uint32_t* hist = own.hist + 256 * (pass & 1);
+                        for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
+                        __syncthreads();
+                        each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                            const uint64_t key = entry_key(e, j);
+                            if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
+                        });
+                        meet();
+                        if (warp == 0) {
+                            uint32_t n[8], sum = 0;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int bin = 255 - 8 * lane - i;
+                                n[i] = hist[bin];
+                                if (C > 1) {
+                                    n[i] = 0;
+                                    for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
+                                }
+                                sum += n[i];
+                            }
+                            uint32_t upto = sum;
+#pragma unroll
+                            for (int o = 1; o < 32; o *= 2) {
+                                const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                                if (lane >= o) upto += x;
+                            }
+                            const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
+                            if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
+                                ListPick p{0, 0, 0};
+                                uint32_t cum = above + upto - sum;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
+                                        p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
+                                    cum += n[i];
+                                }
+                                pick = p;
+                            }
+                        }
+                        __syncthreads();
+                        const ListPick p = pick;
+                        if (p.at == 0) {                                     // in the first pass only: all of them
+                            bound = 0;
+                            break;
+                        }
+                        bound = bound << 8 | p.digit;
+                        above = p.above;
+                        if (above + p.at <= (uint32_t)kListCap) {
+                            bound <<= shift;
+                            break;
+                        }
+                    }
+                }
+                meet();                                              // the counts that were read
+                if (tid == 0) own.count = 0;
+                __syncthreads();
+                each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                    const uint64_t key = entry_key(e, j);
+                    if (key >= bound) keys[atomicAdd(&own.count, 1u)] = key;
+                });
+                meet();
+            }
+            // ---- sorted in the first CTA
             if (rank == 0) {
                 int n = (int)own.count;
                 for (int c = 1; c < C; ++c) {
@@ -517,8 +652,15 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
         }
     const bool small = sh.slice <= 256;
     const int batch = small ? 256 : 2048;
+    // Maxima of as large groups as leave four for every entry of the list; none where the entries are
+    // few, or too few for groups.
+    if (a.V > 192 && nv >= 2 * (int64_t)a.K) {
+        sh.group = 1;
+        while (sh.group < 8 && nv >= 8 * (int64_t)a.K * sh.group) sh.group *= 2;
+        while ((int64_t)(sh.slice + batch - 1) / batch * batch > (int64_t)kListGroups * sh.group) sh.group *= 2;
+    }
     const size_t bytes = kOp == kListDrawAll ? (size_t)((sh.slice + batch - 1) / batch) * (batch / 256) * sizeof(float2)
-                                             : (kListCap + 1024) * sizeof(uint64_t);
+                                             : (kListCap + 1024) * sizeof(uint64_t) + (sh.group ? kListGroups * sizeof(uint16_t) : 0);
     return small ? launch_list_threads<T, kOp, 32>(a, sh, bytes, s) : launch_list_threads<T, kOp, 256>(a, sh, bytes, s);
 }
 

@@ -29,12 +29,14 @@ namespace malib {
 
 struct ListShape {
     int cluster, slice;                              // CTAs a row, vectors of a CTA's slice
-    int group;                                       // vectors of a maximum: 1, 2, 4 or a multiple of 8; 0: no maxima
+    int group_log;                                   // log 2 of a maximum's vectors; < 0: no maxima
+    int cap;                                         // most keys that are sorted
+    int room;                                        // sorted keys, or twice as many groups to be read again
 };
 
 namespace {
 
-constexpr int kListCap = 2048;                       // most entries that are sorted
+constexpr int kListCap = 2048;                       // most keys that are sorted, for any list
 constexpr int kListPer = 8;                          // vectors a thread has in flight
 constexpr int kListBins = 1024;                      // of the maxima's distances
 constexpr int kListGroups = 4096;                    // most maxima of a slice
@@ -57,8 +59,9 @@ __device__ __forceinline__ float key_logit(uint64_t key) { return order_value((u
 // What a CTA's peers take from it.
 struct __align__(16) ListShared {
     float4 stat;                                     // m, S, t, entries before the token (bits)
+    uint32_t count;                                  // keys collected; past the cap: not all are there
+    uint32_t pad[3];
     uint32_t hist[kListBins];                        // or two of 256 bins
-    uint32_t count;                                  // keys collected
 };
 struct ListPick {
     uint32_t digit, above, at;                       // of a histogram; at = 0: fewer than K entries in all
@@ -67,7 +70,7 @@ struct ListPick {
 // The largest of each group of a thread's vectors, as the top 16 bits of its key, to out[0],
 // out[stride] ..; 0: none. What comes back is the largest of all.
 template <class T>
-__device__ __forceinline__ float group_maxima(const uint4 (&x)[kListPer], int group, uint16_t* out, int stride) {
+__device__ __forceinline__ float group_maxima(const uint4 (&x)[kListPer], int group_log, uint16_t* out, int stride) {
     uint32_t m[kListPer];
 #pragma unroll
     for (int u = 0; u < kListPer; ++u)
@@ -78,7 +81,7 @@ __device__ __forceinline__ float group_maxima(const uint4 (&x)[kListPer], int gr
     };
 #pragma unroll
     for (int n = kListPer; n > 1; n /= 2) {
-        if (group * n == kListPer)
+        if (n << group_log == kListPer)
 #pragma unroll
             for (int i = 0; i < n; ++i) store(i, m[i]);
 #pragma unroll
@@ -114,16 +117,98 @@ __device__ __forceinline__ void each_entry(const RowView<T>& r, int v0, int v1, 
     }
 }
 
-// Sorts the n keys at `key` (room for kListCap), largest first; what comes back has the first K in
-// order. Few of them are counted: a key's place is how many are larger.
+// How many of the entries of a vector are >= the threshold, added to `count` in each of its halves
+// (16-bit types: up to 2,048, or 256 for bf16) or as a whole; two thresholds in a word.
+template <class T>
+struct Above;
+template <>
+struct Above<float> {
+    uint32_t n = 0;
+    __device__ static float next(float z) {          // the smallest larger value
+        return order_value(order_key(z) + 1);
+    }
+    __device__ static uint32_t both(float z) { return __float_as_uint(z); }
+    __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
+        const float t = __uint_as_float(thr);
+        n += __uint_as_float(q.x) >= t;
+        n += __uint_as_float(q.y) >= t;
+        n += __uint_as_float(q.z) >= t;
+        n += __uint_as_float(q.w) >= t;
+    }
+    __device__ __forceinline__ uint32_t take() {
+        const uint32_t r = n;
+        n = 0;
+        return r;
+    }
+};
+// The 16-bit value after z's in the order of the values.
+__device__ __forceinline__ uint16_t next_half(uint16_t b) {
+    if (b == 0x8000u) b = 0;                         // -0 is 0
+    return b & 0x8000u ? (b == 0x8001u ? 0x8000u : b - 1) : b + 1;
+}
+template <>
+struct Above<__nv_bfloat16> {
+    __nv_bfloat162 n = __floats2bfloat162_rn(0.f, 0.f);
+    __device__ static float next(float z) {
+        return __bfloat162float(__ushort_as_bfloat16(next_half(__bfloat16_as_ushort(__float2bfloat16_rn(z)))));
+    }
+    __device__ static uint32_t both(float z) { return __bfloat16_as_ushort(__float2bfloat16_rn(z)) * 0x10001u; }
+    __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        __nv_bfloat162 t;
+        *reinterpret_cast<uint32_t*>(&t) = thr;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __nv_bfloat162 v;
+            *reinterpret_cast<uint32_t*>(&v) = w[i];
+            n = __hadd2(n, __hge2(v, t));
+        }
+    }
+    __device__ __forceinline__ uint32_t take() {
+        const float2 f = __bfloat1622float2(n);
+        n = __floats2bfloat162_rn(0.f, 0.f);
+        return (uint32_t)(f.x + f.y);
+    }
+};
+template <>
+struct Above<__half> {
+    __half2 n = __floats2half2_rn(0.f, 0.f);
+    __device__ static float next(float z) {
+        return __half2float(__ushort_as_half(next_half(__half_as_ushort(__float2half_rn(z)))));
+    }
+    __device__ static uint32_t both(float z) { return __half_as_ushort(__float2half_rn(z)) * 0x10001u; }
+    __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        __half2 t;
+        *reinterpret_cast<uint32_t*>(&t) = thr;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 v;
+            *reinterpret_cast<uint32_t*>(&v) = w[i];
+            n = __hadd2(n, __hge2(v, t));
+        }
+    }
+    __device__ __forceinline__ uint32_t take() {
+        const float2 f = __half22float2(n);
+        n = __floats2half2_rn(0.f, 0.f);
+        return (uint32_t)(f.x + f.y);
+    }
+};
+
+// Sorts the n keys at `key` (room for the next power of two), largest first; what comes back has the
+// first K in order. Few of them are counted: a key's place is how many are larger; 2^l lanes
+// share a key's count.
 template <int kThreads>
 __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, int tid) {
     if (n <= max(128, kThreads + kThreads / 2)) {
-        for (int i = tid; i < n; i += kThreads) {
-            const uint64_t own = key[i];
+        const int lanes = n * 8 <= kThreads ? 8 : n * 4 <= kThreads ? 4 : n * 2 <= kThreads ? 2 : 1;
+        for (int i0 = 0; i0 < n; i0 += kThreads / lanes) {           // (the same rounds in every thread)
+            const int i = i0 + tid / lanes;
+            const uint64_t own = i < n ? key[i] : ~0ull;
             int place = 0;
-            for (int j = 0; j < n; ++j) place += key[j] > own;
-            if (place < K) sorted[place] = own;
+            for (int j = tid & (lanes - 1); j < n; j += lanes) place += key[j] > own;
+            for (int o = lanes / 2; o > 0; o /= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+            if (i < n && (tid & (lanes - 1)) == 0 && place < K) sorted[place] = own;
         }
         __syncthreads();
         return sorted;
@@ -220,20 +305,20 @@ __device__ __forceinline__ void draw_listed(const ListArgs& a, int64_t row, cons
 }
 
 template <class T, int kOp, int kThreads>
-__global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListShape sh) {
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(ListArgs a, ListShape sh) {
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;
-    // keys [kListCap], sorted ones [1024] (or groups to be read again), maxima [kListGroups]; or segments' (m, S)
+    // keys [cap], sorted ones [room] (or groups to be read again), maxima; or segments' (m, S)
     extern __shared__ __align__(16) uint64_t keys[];
     __shared__ ListShared own;
     __shared__ float4 red[kWarps];
     __shared__ ListPick pick;
+    __shared__ uint32_t n_again, warp_total[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = sh.cluster, rank = C > 1 ? (int)cluster_rank() : 0;
-    uint64_t* sorted = keys + kListCap;
+    uint64_t* sorted = keys + sh.cap;
     uint32_t* again = reinterpret_cast<uint32_t*>(sorted);
-    uint16_t* maxima = reinterpret_cast<uint16_t*>(sorted + 1024);
-    __shared__ uint32_t n_again, warp_sum[kWarps];
+    uint16_t* maxima = reinterpret_cast<uint16_t*>(sorted + sh.room);
     float2* segment = reinterpret_cast<float2*>(keys);
     wait_for_previous();
     let_next_start();
@@ -245,6 +330,90 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
             cluster_arrive();
             cluster_wait();
         }
+    };
+    // The keys of a slice's entries that may be among the first K, those of the first K of the slice and
+    // few more, to keys and their number to own.count (past the cap: not all are there). Every
+    // thread of the block; r: the slice's statistics, maxima: those of its groups.
+    auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi) {
+        if (tid == 0) own.count = n_again = pick.digit = 0;
+        if (sh.group_log < 0) {
+            __syncthreads();
+            each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                const uint32_t at = atomicAdd(&own.count, 1u);
+                if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, j);
+            });
+            __syncthreads();
+            return;
+        }
+        const int n_max = (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << sh.group_log) - 1) >> sh.group_log) * kThreads;
+        const uint32_t top_key = order_key(r.m) >> 16;
+        uint32_t reach = 0;
+        for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {       // bins of one value, then of 64
+            constexpr int kBins = kListBins / kThreads;                      // of a thread
+            uint4* bins = reinterpret_cast<uint4*>(own.hist + kBins * tid);
+#pragma unroll
+            for (int i = 0; i < kBins / 4; ++i) bins[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            for (int i = tid; i < n_max; i += kThreads) {
+                const uint32_t key = maxima[i], bin = (top_key - key) >> coarse;
+                if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
+            }
+            __syncthreads();
+            uint32_t sum = 0;
+#pragma unroll
+            for (int i = 0; i < kBins / 4; ++i) sum += (bins[i].x + bins[i].y) + (bins[i].z + bins[i].w);
+            uint32_t upto = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += q;
+            }
+            if (kWarps > 1) {
+                if (lane == 31) warp_total[warp] = upto;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kWarps - 1; ++w) upto += w < warp ? warp_total[w] : 0u;
+            }
+            if (upto >= (uint32_t)a.K && upto - sum < (uint32_t)a.K) {
+                uint32_t cum = upto - sum, bin = kBins * tid;
+                while ((cum += own.hist[bin]) < (uint32_t)a.K) ++bin;
+                // the bin's smallest value, at least 1 (0 has no entries)
+                const uint32_t below = ((bin + 1) << coarse) - 1;
+                pick.digit = below < top_key ? top_key - below : 1u;
+            }
+            __syncthreads();
+            reach = pick.digit;
+        }
+        // (0: fewer than K groups have entries; all entries may be wanted)
+        const uint32_t least = max(reach, 1u);
+        for (int i = tid; i < n_max; i += kThreads)
+            if (maxima[i] >= least) {
+                const uint32_t at = atomicAdd(&n_again, 1u);
+                if (at < 2u * sh.room) again[at] = i;
+            }
+        __syncthreads();
+        if (n_again > 2u * sh.room) {
+            if (tid == 0) own.count = sh.cap + 1;
+        } else {
+            const int items = (int)n_again << sh.group_log;
+            for (int item = tid; item < items; item += kThreads) {
+                const int id = (int)again[item >> sh.group_log];
+                const int n = (id / kThreads << sh.group_log) + (item & ((1 << sh.group_log) - 1));
+                const int v = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
+                if (v >= v_hi) continue;
+                const uint4 q = view.vec(v);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float e = entry_of<T>(q, i);
+                    const uint32_t key = order_key(e);
+                    if (key >> 16 >= least && e > -INFINITY) {
+                        const uint32_t at = atomicAdd(&own.count, 1u);
+                        if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, v * W - view.h + i);
+                    }
+                }
+            }
+        }
+        __syncthreads();
     };
     for (int64_t row = blockIdx.x / C; row < a.n; row += gridDim.x / C) {
         const int token = a.tokens ? a.tokens[row] : 0;
@@ -284,22 +453,42 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
         // ---- statistics; a warp's vectors of a batch follow one another
         LongStat st{-INFINITY, {0.f, 0.f}, {0.f, 0.f}};
         uint32_t before = 0;
-        const uint32_t own_end = (uint32_t)min(token, v_hi * W - h);   // equal entries count up to here
+        const bool ranked = kOp == kListTop && a.rank;
+        Above<T> above;
+        // entries count that are >= the token's before it, and larger ones behind it
+        const uint32_t thr_before = ranked ? Above<T>::both(zt) : 0u, thr_behind = ranked ? Above<T>::both(Above<T>::next(zt)) : 0u;
         int segments = 0, batch = 0;
         float group_max = -INFINITY;
+        // the row's whole vectors; a partial first or last one is filled up
+        const int full_lo = h > 0 ? 1 : 0, full_hi = (h + a.V) % W != 0 ? nv - 1 : nv;
+        const uint4* src = reinterpret_cast<const uint4*>(z - h);
         for (int b = v_lo; b < v_hi; b += kBatch, segments += kWarps, ++batch) {
             uint4 x[kListPer];
             const int v0 = b + warp * kWarpVecs + lane;
+            if (b >= full_lo && b + kBatch <= min(v_hi, full_hi)) {
 #pragma unroll
-            for (int u = 0; u < kListPer; ++u) x[u] = v0 + u * 32 < v_hi ? view.vec(v0 + u * 32) : Elt<T>::none();
+                for (int u = 0; u < kListPer; ++u) x[u] = src[v0 + u * 32];
+            } else {
+                const int lo = full_lo, n = max(0, min(v_hi, full_hi) - lo);
+#pragma unroll
+                for (int u = 0; u < kListPer; ++u) x[u] = (uint32_t)(v0 + u * 32 - lo) < (uint32_t)n ? src[v0 + u * 32] : Elt<T>::none();
+                if (v0 == 0 && full_lo > 0) x[0] = load_part(z, -h, a.V);
+                const int tail = full_hi < nv && nv <= v_hi ? nv - 1 - v0 : -1;
+                if (tail >= 0 && tail < kWarpVecs && tail % 32 == 0 && !(tail == 0 && v0 == 0 && full_lo > 0)) {
+                    const uint4 q = load_part(z, (nv - 1) * W - h, a.V);
+#pragma unroll
+                    for (int u = 0; u < kListPer; ++u)
+                        if (tail == u * 32) x[u] = q;
+                }
+            }
             float mx;
-            if (!kAll && sh.group > 0) {
-                uint16_t* out = maxima + tid + (sh.group < kListPer ? batch * (kListPer / sh.group) * kThreads : 0);
-                mx = group_maxima<T>(x, sh.group, out, kThreads);
-                if (sh.group >= kListPer) {
+            if (!kAll && sh.group_log >= 0) {
+                uint16_t* out = maxima + tid + (batch << 3 >> min(sh.group_log, 3)) * kThreads;
+                mx = group_maxima<T>(x, sh.group_log, out, kThreads);
+                if (sh.group_log >= 3) {
                     group_max = fmaxf(group_max, mx);
-                    if ((batch + 1) * kListPer % sh.group == 0 || b + kBatch >= v_hi) {
-                        maxima[batch * kListPer / sh.group * kThreads + tid] =
+                    if ((batch + 1) % (1 << (sh.group_log - 3)) == 0 || b + kBatch >= v_hi) {
+                        maxima[(batch >> (sh.group_log - 3)) * kThreads + tid] =
                             group_max > -INFINITY ? (uint16_t)(order_key(group_max) >> 16) : (uint16_t)0;
                         group_max = -INFINITY;
                     }
@@ -316,14 +505,21 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
                 const float s = warp_add(part.s);
                 if (lane == 0) segment[segments + warp] = make_float2(st.m, s);
             }
-            if (kOp == kListTop && a.rank) {
+            if (ranked) {
 #pragma unroll
-                for (int u = 0; u < kListPer; ++u)
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        const float e = entry_of<T>(x[u], i);
-                        before += e > zt || (e == zt && (uint32_t)((v0 + u * 32) * W - h + i) < own_end);
-                    }
+                for (int u = 0; u < kListPer; ++u) above.add(x[u], (v0 + u * 32 + 1) * W - h <= token ? thr_before : thr_behind);
+                before += above.take();
+            }
+        }
+        if (ranked) {
+            // the token's own vector counted as one behind it; a masked token comes after every
+            // entry before it
+            if (zt == -INFINITY) {
+                before = 0;
+                if (first) before = (uint32_t)token;
+                each_entry(view, max(v_lo, (token + h) / W), v_hi, tid, kThreads, [&](int j, float) { before += j >= token; });
+            } else if (first) {
+                for (int j = (token + h) / W * W - h; j < token; ++j) before += j >= 0 && Elt<T>::get(z[max(j, 0)]) == zt;
             }
         }
         RowStat r = stat_of(st);
@@ -337,13 +533,20 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
             r = reduce_stat<kWarps>(RowStat{q.x, q.y, q.z}, a.k);
             before = __reduce_add_sync(0xffffffffu, lane < kWarps ? __float_as_uint(q.w) : 0u);
         }
+        // ---- the keys of the slice's first K entries, and what the peers take
+        if constexpr (!kAll) {
+            if (r.m != -INFINITY && fabsf(r.s) < INFINITY) collect(r, view, v_lo, v_hi);
+            else if (tid == 0) own.count = 0;
+        }
         float4 peer = make_float4(r.m, r.s, r.t, 0.f);               // lane i: CTA i's
+        uint32_t n_keys = kAll ? 0 : own.count;
         if (C > 1) {
             if (tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
             meet();
             peer = lane < C ? peer_load(&own.stat, lane) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
             before = __reduce_add_sync(0xffffffffu, __float_as_uint(peer.w));
             r = reduce_stat<32>(RowStat{peer.x, peer.y, peer.z}, a.k);
+            if (!kAll) n_keys = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
         }
         live = r.m != -INFINITY;
         const bool good = live && fabsf(r.s) < INFINITY;             // no NaN, no +infinity
@@ -442,142 +645,62 @@ __global__ void __launch_bounds__(kThreads) token_list_kernel(ListArgs a, ListSh
                 }
             }
         } else {
-            uint64_t bound = 0;
-            bool sure = sh.group == 0 && a.V <= kListCap;            // few enough entries above the bound
-            if (tid == 0) own.count = n_again = pick.digit = 0;
-            if (sh.group > 0) {
-                // ---- the bound from the groups' maxima, and the entries of those that reach it
-                const int slots = ((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + sh.group - 1) / sh.group;
-                const uint32_t top_key = order_key(r.m) >> 16;
-                uint32_t reach = 0;
-                for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {   // bins of one value, then of 64
-                    for (int i = tid; i < kListBins; i += kThreads) own.hist[i] = 0;
+            if (n_keys > (uint32_t)sh.cap) {
+                // ---- too many (the same in all CTAs of the row): a bound from all keys
+                uint64_t bound = 0;
+                uint32_t above = 0;
+                int shift = 48;
+                for (int pass = 0;; ++pass, shift -= 8) {
+                    uint32_t* hist = own.hist + 256 * (pass & 1);
+                    for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
                     __syncthreads();
-                    for (int i = tid; i < slots * kThreads; i += kThreads) {
-                        const uint32_t key = maxima[i], bin = (top_key - key) >> coarse;
-                        if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
-                    }
+                    each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                        const uint64_t key = entry_key(e, j);
+                        if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
+                    });
                     meet();
-                    // thread i counts the bins from kBins i on
-                    constexpr int kBins = kListBins / kThreads;
-                    uint32_t sum = 0;
-                    const auto in_bin = [&](int bin) {
-                        if (C == 1) return own.hist[bin];
-                        uint32_t n = 0;
-                        for (int c = 0; c < C; ++c) n += peer_load(own.hist + bin, c);
-                        return n;
-                    };
-#pragma unroll 4
-                    for (int i = 0; i < kBins; ++i) sum += in_bin(kBins * tid + i);
-                    uint32_t upto = sum;
+                    if (warp == 0) {
+                        uint32_t n[8], sum = 0;
 #pragma unroll
-                    for (int o = 1; o < 32; o *= 2) {
-                        const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
-                        if (lane >= o) upto += q;
-                    }
-                    if (kWarps > 1) {
-                        if (lane == 31) warp_sum[warp] = upto;
-                        __syncthreads();
-                        for (int w = 0; w < warp; ++w) upto += warp_sum[w];
-                    }
-                    if (upto >= (uint32_t)a.K && upto - sum < (uint32_t)a.K) {
-                        uint32_t cum = upto - sum, bin = kBins * tid;
-                        while ((cum += in_bin(bin)) < (uint32_t)a.K) ++bin;
-                        // the bin's smallest value, at least 1 (0 has no entries)
-                        const uint32_t below = ((bin + 1) << coarse) - 1;
-                        pick.digit = below < top_key ? top_key - below : 1u;
-                    }
-                    meet();
-                    reach = pick.digit;
-                }
-                if (reach > 0) {
-                    bound = (uint64_t)reach << 40;
-                    for (int i = tid; i < slots * kThreads; i += kThreads)
-                        if (maxima[i] >= reach) {
-                            const uint32_t at = atomicAdd(&n_again, 1u);
-                            if (at < kListCap) again[at] = i;
-                        }
-                    __syncthreads();
-                    const int items = (int)min(n_again, (uint32_t)kListCap) * sh.group;
-                    for (int item = tid; item < items; item += kThreads) {
-                        const int id = (int)again[item / sh.group], n = id / kThreads * sh.group + item % sh.group;
-                        const int v = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
-                        if (v >= v_hi) continue;
-                        const uint4 q = view.vec(v);
-#pragma unroll
-                        for (int i = 0; i < W; ++i) {
-                            const float e = entry_of<T>(q, i);
-                            if (e > -INFINITY && order_key(e) >> 16 >= reach) {
-                                const uint32_t at = atomicAdd(&own.count, 1u);
-                                if (at < kListCap) keys[at] = entry_key(e, v * W - h + i);
+                        for (int i = 0; i < 8; ++i) {
+                            const int bin = 255 - 8 * lane - i;
+                            n[i] = hist[bin];
+                            if (C > 1) {
+                                n[i] = 0;
+                                for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
                             }
+                            sum += n[i];
                         }
-                    }
-                    if (tid == 0 && n_again > kListCap) atomicMax(&own.count, (uint32_t)kListCap + 1);
-                    meet();
-                    uint32_t n = own.count;
-                    if (C > 1) n = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
-                    sure = n <= (uint32_t)kListCap;
-                }
-            }
-            // (sure is the same in all CTAs of the row)
-            if (!sure || sh.group == 0) {
-                if (!sure) {
-                    bound = 0;
-                    uint32_t above = 0;
-                    int shift = 48;
-                    for (int pass = 0;; ++pass, shift -= 8) {
-                        uint32_t* hist = own.hist + 256 * (pass & 1);
-                        for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
-                        __syncthreads();
-                        each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
-                            const uint64_t key = entry_key(e, j);
-                            if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
-                        });
-                        meet();
-                        if (warp == 0) {
-                            uint32_t n[8], sum = 0;
+                        uint32_t upto = sum;
+#pragma unroll
+                        for (int o = 1; o < 32; o *= 2) {
+                            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                            if (lane >= o) upto += x;
+                        }
+                        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
+                        if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
+                            ListPick p{0, 0, 0};
+                            uint32_t cum = above + upto - sum;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const int bin = 255 - 8 * lane - i;
-                                n[i] = hist[bin];
-                                if (C > 1) {
-                                    n[i] = 0;
-                                    for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
-                                }
-                                sum += n[i];
+                                if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
+                                    p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
+                                cum += n[i];
                             }
-                            uint32_t upto = sum;
-#pragma unroll
-                            for (int o = 1; o < 32; o *= 2) {
-                                const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-                                if (lane >= o) upto += x;
-                            }
-                            const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
-                            if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
-                                ListPick p{0, 0, 0};
-                                uint32_t cum = above + upto - sum;
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
-                                        p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
-                                    cum += n[i];
-                                }
-                                pick = p;
-                            }
+                            pick = p;
                         }
-                        __syncthreads();
-                        const ListPick p = pick;
-                        if (p.at == 0) {                                     // in the first pass only: all of them
-                            bound = 0;
-                            break;
-                        }
-                        bound = bound << 8 | p.digit;
-                        above = p.above;
-                        if (above + p.at <= (uint32_t)kListCap) {
-                            bound <<= shift;
-                            break;
-                        }
+                    }
+                    __syncthreads();
+                    const ListPick p = pick;
+                    if (p.at == 0) {                                     // in the first pass only: all of them
+                        bound = 0;
+                        break;
+                    }
+                    bound = bound << 8 | p.digit;
+                    above = p.above;
+                    if (above + p.at <= (uint32_t)sh.cap) {
+                        bound <<= shift;
+                        break;
                     }
                 }
                 meet();                                              // the counts that were read
@@ -644,23 +767,32 @@ cudaError_t launch_list_threads(const ListArgs& a, const ListShape& sh, size_t b
 template <class T, int kOp>
 cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
-    ListShape sh{1, (int)nv};
+    ListShape sh{1, (int)nv, -1, 0, 0};
+    // Clusters while the CTAs' lists can be sorted together.
+    const bool all = kOp == kListDrawAll;
     for (int c = 2; c <= 8 && (nv + c - 1) / c >= 512; c *= 2)
-        if (a.n * c <= 4 * (int64_t)n_sm) {
+        if (a.n * c <= 4 * (int64_t)n_sm && (all || (int64_t)c * a.K <= kListCap / 2)) {
             sh.cluster = c;
             sh.slice = (int)((nv + c - 1) / c);
         }
     const bool small = sh.slice <= 256;
     const int batch = small ? 256 : 2048;
-    // Maxima of as large groups as leave four for every entry of the list; none where the entries are
-    // few, or too few for groups.
-    if (a.V > 192 && nv >= 2 * (int64_t)a.K) {
-        sh.group = 1;
-        while (sh.group < 8 && nv >= 8 * (int64_t)a.K * sh.group) sh.group *= 2;
-        while ((int64_t)(sh.slice + batch - 1) / batch * batch > (int64_t)kListGroups * sh.group) sh.group *= 2;
+    const int64_t padded = (sh.slice + batch - 1) / batch * batch;
+    size_t bytes = (size_t)padded / 256 * sizeof(float2);
+    if (!all) {
+        // Maxima of as large groups as leave four for every entry of the list; none where all
+        // entries can be sorted as well, or where they are too few.
+        int64_t groups = 0;
+        if (a.V > 192 && sh.slice >= 2 * a.K) {
+            sh.group_log = 0;
+            while (sh.group_log < 3 && sh.slice >= (int64_t)a.K << (sh.group_log + 3)) ++sh.group_log;
+            while (padded >> sh.group_log > kListGroups) ++sh.group_log;
+            groups = ((padded / (batch / 8) + (1 << sh.group_log) - 1) >> sh.group_log) * (batch / 8);
+        }
+        sh.cap = a.K * sh.cluster <= 256 && sh.group_log >= 0 ? 1024 : kListCap;
+        sh.room = a.K <= 256 ? 256 : 1024;
+        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + groups * sizeof(uint16_t);
     }
-    const size_t bytes = kOp == kListDrawAll ? (size_t)((sh.slice + batch - 1) / batch) * (batch / 256) * sizeof(float2)
-                                             : (kListCap + 1024) * sizeof(uint64_t) + (sh.group ? kListGroups * sizeof(uint16_t) : 0);
     return small ? launch_list_threads<T, kOp, 32>(a, sh, bytes, s) : launch_list_threads<T, kOp, 256>(a, sh, bytes, s);
 }
 

@@ -235,6 +235,7 @@ int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_
     if (!c.dev(out->ids, 4) || !c.dev(out->top_logp, 4) || !c.opt(out->logp, 4) || !c.opt(out->entropy, 4) ||
         !c.opt(out->rank, 4))
         return c.bad("outputs must be device memory of the context's device");
+    if ((r = c.work()) != MALIB_OK) return r;
     ListArgs a{c.a};
     a.K = out->top;
     a.top_ids = out->ids;
@@ -262,6 +263,7 @@ int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const mal
         return c.bad("uniform, or sequence and step, must be aligned device memory of the context's device");
     if (!c.opt(token_out, 4) || !c.opt(logp_out, 4) || !c.opt(entropy_out, 4) || !c.opt(draw_logp_out, 4))
         return c.bad("outputs must be device memory of the context's device");
+    if ((r = c.work()) != MALIB_OK) return r;
     ListArgs a{c.a};
     a.K = draw->top_k;
     a.drawn = token_out;

@@ -21,6 +21,9 @@
 // them, and its entries alone are read again. The draw from a list takes them in the list's order.
 #pragma once
 
+#include <cfloat>
+#include <type_traits>
+
 #include "token_common.cuh"
 #include "token_peer.cuh"
 #include "token_rollout.h"
@@ -37,9 +40,10 @@ struct ListShape {
 namespace {
 
 constexpr int kListCap = 2048;                       // most keys that are sorted, for any list
-constexpr int kListPer = 8;                          // vectors a thread has in flight
+constexpr int kListPer = 8;                          // vectors of a thread in a batch
+constexpr int kWordVecs = 4, kWords = kListPer / kWordVecs;          // of a word of maxima; words of a batch
 constexpr int kListBins = 1024;                      // of the maxima's distances
-constexpr int kListGroups = 4096;                    // most maxima of a slice
+constexpr int kListGroups = 16384;                   // most maxima of a slice
 constexpr uint32_t kIndexMask = (1u << 24) - 1;
 
 // Larger for larger logits; the same for -0 and 0.
@@ -67,23 +71,20 @@ struct ListPick {
     uint32_t digit, above, at;                       // of a histogram; at = 0: fewer than K entries in all
 };
 
-// The largest of each group of a thread's vectors, as the top 16 bits of its key, to out[0],
-// out[stride] ..; 0: none. What comes back is the largest of all.
+// The largest of each group of 1, 2, 4 or 8 vectors, as the top 16 bits of its key, to out[0], out[stride] ..; 0:
+// none. Larger groups are their caller's. What comes back is the largest of all.
+__device__ __forceinline__ uint16_t max_key(float z) { return z > -INFINITY ? (uint16_t)(order_key(z) >> 16) : (uint16_t)0; }
 template <class T>
 __device__ __forceinline__ float group_maxima(const uint4 (&x)[kListPer], int group_log, uint16_t* out, int stride) {
     uint32_t m[kListPer];
 #pragma unroll
     for (int u = 0; u < kListPer; ++u)
         m[u] = Elt<T>::max(Elt<T>::max(x[u].x, x[u].y), Elt<T>::max(x[u].z, x[u].w));
-    const auto store = [&](int i, uint32_t w) {
-        const float z = Elt<T>::largest(w);
-        out[i * stride] = z > -INFINITY ? (uint16_t)(order_key(z) >> 16) : (uint16_t)0;
-    };
 #pragma unroll
-    for (int n = kListPer; n > 1; n /= 2) {
+    for (int n = kListPer; n > 0; n /= 2) {
         if (n << group_log == kListPer)
 #pragma unroll
-            for (int i = 0; i < n; ++i) store(i, m[i]);
+            for (int i = 0; i < n; ++i) out[i * stride] = max_key(Elt<T>::largest(m[i]));
 #pragma unroll
         for (int i = 0; i < n / 2; ++i) m[i] = Elt<T>::max(m[2 * i], m[2 * i + 1]);
     }
@@ -117,8 +118,8 @@ __device__ __forceinline__ void each_entry(const RowView<T>& r, int v0, int v1, 
     }
 }
 
-// How many of the entries of a vector are >= the threshold, added to `count` in each of its halves
-// (16-bit types: up to 2,048, or 256 for bf16) or as a whole; two thresholds in a word.
+// How many entries of vectors are >= a threshold (twice in a word for 16-bit types): at most 65,535 in a
+// row between two calls of take().
 template <class T>
 struct Above;
 template <>
@@ -146,9 +147,15 @@ __device__ __forceinline__ uint16_t next_half(uint16_t b) {
     if (b == 0x8000u) b = 0;                         // -0 is 0
     return b & 0x8000u ? (b == 0x8001u ? 0x8000u : b - 1) : b + 1;
 }
+// Comparisons of two give a word of two masks; masks are -1 in their half, and their sum's low half
+// borrows from the high one.
+__device__ __forceinline__ uint32_t count_masks(uint32_t sum) {
+    const uint32_t lo = (0u - sum) & 0xffffu;
+    return 2 * lo - ((sum + lo) >> 16 & 0xffffu) & 0xffffu;
+}
 template <>
 struct Above<__nv_bfloat16> {
-    __nv_bfloat162 n = __floats2bfloat162_rn(0.f, 0.f);
+    uint32_t n = 0;
     __device__ static float next(float z) {
         return __bfloat162float(__ushort_as_bfloat16(next_half(__bfloat16_as_ushort(__float2bfloat16_rn(z)))));
     }
@@ -161,18 +168,18 @@ struct Above<__nv_bfloat16> {
         for (int i = 0; i < 4; ++i) {
             __nv_bfloat162 v;
             *reinterpret_cast<uint32_t*>(&v) = w[i];
-            n = __hadd2(n, __hge2(v, t));
+            n += __hge2_mask(v, t);
         }
     }
     __device__ __forceinline__ uint32_t take() {
-        const float2 f = __bfloat1622float2(n);
-        n = __floats2bfloat162_rn(0.f, 0.f);
-        return (uint32_t)(f.x + f.y);
+        const uint32_t r = count_masks(n);
+        n = 0;
+        return r;
     }
 };
 template <>
 struct Above<__half> {
-    __half2 n = __floats2half2_rn(0.f, 0.f);
+    uint32_t n = 0;
     __device__ static float next(float z) {
         return __half2float(__ushort_as_half(next_half(__half_as_ushort(__float2half_rn(z)))));
     }
@@ -185,38 +192,69 @@ struct Above<__half> {
         for (int i = 0; i < 4; ++i) {
             __half2 v;
             *reinterpret_cast<uint32_t*>(&v) = w[i];
-            n = __hadd2(n, __hge2(v, t));
+            n += __hge2_mask(v, t);
         }
     }
     __device__ __forceinline__ uint32_t take() {
-        const float2 f = __half22float2(n);
-        n = __floats2half2_rn(0.f, 0.f);
-        return (uint32_t)(f.x + f.y);
+        const uint32_t r = count_masks(n);
+        n = 0;
+        return r;
     }
 };
 
-// Sorts the n keys at `key` (room for the next power of two), largest first; what comes back has the
-// first K in order. Few of them are counted: a key's place is how many are larger; 2^l lanes
-// share a key's count.
-template <int kThreads>
-__device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, int tid) {
+// Sorts the n keys at `key` (room for the next power of two, 512 at least), largest first; what comes back
+// has the first K in order. Few of them are counted: a key's place is how many are larger; several lanes
+// share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
+template <int kThreads, class Sync>
+__device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, bool narrow, int tid,
+                                                     Sync sync) {
     if (n <= max(128, kThreads + kThreads / 2)) {
         const int lanes = n * 8 <= kThreads ? 8 : n * 4 <= kThreads ? 4 : n * 2 <= kThreads ? 2 : 1;
+        const auto narrowed = [](uint64_t k) { return (uint32_t)(k >> 24) & 0xffff0000u | (uint32_t)k & 0xffffu; };
+        narrow = narrow && n <= 256;
+        uint32_t* low = reinterpret_cast<uint32_t*>(key + 256);
+        if (narrow) {
+            for (int i = tid; i < (n + 3) / 4 * 4; i += kThreads) low[i] = i < n ? narrowed(key[i]) : 0u;
+        } else if (tid == 0 && n % 2 != 0) {
+            key[n] = 0ull;
+        }
+        sync();
+        const int vecs = narrow ? (n + 3) / 4 : (n + 1) / 2;
+        const uint4* quad = reinterpret_cast<const uint4*>(low);
+        const ulonglong2* pair = reinterpret_cast<const ulonglong2*>(key);
         for (int i0 = 0; i0 < n; i0 += kThreads / lanes) {           // (the same rounds in every thread)
             const int i = i0 + tid / lanes;
+            if (__all_sync(0xffffffffu, i >= n)) continue;
             const uint64_t own = i < n ? key[i] : ~0ull;
             int place = 0;
-            for (int j = tid & (lanes - 1); j < n; j += lanes) place += key[j] > own;
+            if (narrow) {
+                const uint32_t own_low = narrowed(own);
+#pragma unroll 2
+                for (int j = tid & (lanes - 1); j < vecs; j += lanes) {
+                    const uint4 q = quad[j];
+                    place += q.x > own_low;
+                    place += q.y > own_low;
+                    place += q.z > own_low;
+                    place += q.w > own_low;
+                }
+            } else {
+#pragma unroll 2
+                for (int j = tid & (lanes - 1); j < vecs; j += lanes) {
+                    const ulonglong2 q = pair[j];
+                    place += q.x > own;
+                    place += q.y > own;
+                }
+            }
             for (int o = lanes / 2; o > 0; o /= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
             if (i < n && (tid & (lanes - 1)) == 0 && place < K) sorted[place] = own;
         }
-        __syncthreads();
+        sync();
         return sorted;
     }
     int P = 256;
     while (P < n) P *= 2;
     for (int i = n + tid; i < P; i += kThreads) key[i] = 0ull;
-    __syncthreads();
+    sync();
     for (int size = 2; size <= P; size *= 2)
         for (int gap = size / 2; gap > 0; gap /= 2) {
             for (int i = tid; i < P / 2; i += kThreads) {
@@ -227,7 +265,7 @@ __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* so
                     key[hi] = x;
                 }
             }
-            __syncthreads();
+            sync();
         }
     return key;
 }
@@ -246,9 +284,9 @@ __device__ __forceinline__ float warp_add(float v) {
     return v;
 }
 __device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 // A row's random number in [0, 1).
@@ -304,8 +342,244 @@ __device__ __forceinline__ void draw_listed(const ListArgs& a, int64_t row, cons
     }
 }
 
-template <class T, int kOp, int kThreads>
+// The draw from a whole slice that holds the target (one warp): the segment, then its entries. `passed`
+// is the mass before the slice; sums of many are in 64 bits; where rounding leaves no entry, the
+// last one that has a mass is drawn.
+__device__ __forceinline__ float mass_at(const ListArgs& a, float m, float s, const RowStat& r) {
+    return s * exp2_fast(fmaxf((m - r.m) * a.k, kXMin) + kExpBias);
+}
+template <class T>
+__device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const RowStat& r, const RowView<T>& view, int v_lo,
+                                         int v_hi, const float2* segment, int segments, double target, double passed,
+                                         int lane) {
+    constexpr int W = Elt<T>::W, kWarpVecs = 32 * kListPer;
+    int at = -1, last = 0;
+    double last_passed = passed;
+    for (int s0 = 0; s0 < segments && at < 0; s0 += 32) {
+        const float2 sg = s0 + lane < segments ? segment[s0 + lane] : make_float2(-INFINITY, 0.f);
+        const float w = sg.y > 0.f ? mass_at(a, sg.x, sg.y, r) : 0.f, cum = warp_scan(w, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && passed + (double)cum > target),
+                       some = __ballot_sync(0xffffffffu, w > 0.f);
+        if (some) {
+            const int k = 31 - __clz(some);
+            last = s0 + k;
+            last_passed = passed + (double)__shfl_sync(0xffffffffu, cum - w, k);
+        }
+        if (hit) {
+            const int k = __ffs(hit) - 1;
+            at = s0 + k;
+            passed += (double)__shfl_sync(0xffffffffu, cum - w, k);
+        } else {
+            passed += (double)__shfl_sync(0xffffffffu, cum, 31);
+        }
+    }
+    if (at < 0) {
+        at = last;
+        passed = last_passed;
+    }
+    const float rest = (float)(target - passed);
+    const int v0 = v_lo + at * kWarpVecs + lane;
+    float sum = 0.f, fz = 0.f, bz = 0.f;
+    int found = -1, behind = -1;                     // the entry that passes the target; the last one with a mass
+    for (int u = 0; u < kListPer && !__any_sync(0xffffffffu, found >= 0); ++u) {
+        const int v = v0 + u * 32;
+        const uint4 q = v < v_hi ? view.vec(v) : Elt<T>::none();
+        float e[W], mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            e[i] = exp2_fast(x_of(entry_of<T>(q, i), r.m, a.k));
+            mine += e[i];
+        }
+        const float incl = warp_scan(mine, lane);
+        float cum = sum + (incl - mine);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            cum += e[i];
+            if (e[i] > 0.f) {
+                behind = v * W - view.h + i;
+                bz = entry_of<T>(q, i);
+                if (found < 0 && cum > rest) {
+                    found = behind;
+                    fz = bz;
+                }
+            }
+        }
+        sum += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
+    int lane_at = __ffs(hit) - 1;
+    if (!hit) {
+        lane_at = __ffs(__ballot_sync(0xffffffffu, behind == __reduce_max_sync(0xffffffffu, behind))) - 1;
+        found = behind;
+        fz = bz;
+    }
+    if (lane == lane_at) {
+        const float logp = log_prob(a, r, fz);
+        write_draw(a, row, found, logp, row_entropy(r), logp);
+    }
+}
+
+// A key with at least K keys from it on, or 0 where there are fewer, and at most `cap`: by the keys'
+// digits of 8 bits. bins: two histograms; meet: every CTA of the row is there; total: a bin of
+// all of them.
+template <class T, int kThreads, class Sync, class Meet, class Total>
+__device__ __forceinline__ uint64_t bound_of_all(const RowView<T>& view, int v_lo, int v_hi, uint32_t K, uint32_t cap,
+                                                 uint32_t* bins, ListPick* pick, int tid, Sync sync, Meet meet, Total total) {
+    uint64_t bound = 0;
+    uint32_t above = 0;
+    int shift = 48;
+    for (int pass = 0;; ++pass, shift -= 8) {
+        uint32_t* hist = bins + 256 * (pass & 1);
+        for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
+        sync();
+        each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+            const uint64_t key = entry_key(e, j);
+            if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
+        });
+        meet();
+        if (tid < 32) {
+            uint32_t n[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] = total(hist + (255 - 8 * tid - i));
+                sum += n[i];
+            }
+            uint32_t upto = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                if (tid >= o) upto += x;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= K);
+            if (hit ? tid == __ffs(hit) - 1 : tid == 0) {
+                ListPick p{0, 0, 0};
+                uint32_t cum = above + upto - sum;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (hit && p.at == 0 && cum + n[i] >= K) p = ListPick{(uint32_t)(255 - 8 * tid - i), cum, n[i]};
+                    cum += n[i];
+                }
+                *pick = p;
+            }
+        }
+        sync();
+        const ListPick p = *pick;
+        if (p.at == 0) return 0;                     // in the first pass only
+        bound = bound << 8 | p.digit;
+        above = p.above;
+        if (above + p.at <= cap) return bound << shift;
+    }
+}
+
+// What a warp gathers a slice's statistics in: as for the losses' long rows, those of more than
+// kManyBatches batches keep the errors of their parts' additions.
+constexpr int kManyBatches = 16;
+__device__ __forceinline__ void join(RowStat& r, const RowStat& part) {
+    r.s += part.s;
+    r.t += part.t;
+}
+__device__ __forceinline__ void join(LongStat& r, const RowStat& part) {
+    r.s.add(part.s);
+    r.t.add(part.t);
+}
+
+// The maxima of a thread's vectors, four of them to a word: of all 16 entries in 32 bits, of the 16 even and the
+// 16 odd ones in 16 bits each.
+template <class T>
+struct Words {
+    uint32_t w[kWords];
+    float largest;
+    __device__ __forceinline__ explicit Words(const uint4 (&x)[kListPer]) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+#pragma unroll
+            for (int u = 0; u < kWordVecs; ++u) {
+                const uint4& q = x[i * kWordVecs + u];
+                const uint32_t v = Elt<T>::max(Elt<T>::max(q.x, q.y), Elt<T>::max(q.z, q.w));
+                w[i] = u == 0 ? v : Elt<T>::max(w[i], v);
+            }
+            m = i == 0 ? w[i] : Elt<T>::max(m, w[i]);
+        }
+        largest = Elt<T>::largest(m);
+    }
+};
+
+// Where z lies so far below the maximum that 2^x is 0, it is raised to a value there before it is widened, two
+// entries at a time: x stays finite, and needs no bound of its own. low: that value in each half;
+// 0: there is none (a temperature too large for the type, logits too large for fp32).
+template <class T>
+__device__ __forceinline__ uint32_t low_of(float m, float k, float reach) {
+    return 0u;
+}
+__device__ __forceinline__ bool is_low(float low, float m, float k) {
+    const float x = (low - m) * k;
+    return x <= -150.f && x > -INFINITY;
+}
+template <>
+__device__ __forceinline__ uint32_t low_of<__nv_bfloat16>(float m, float k, float reach) {
+    const __nv_bfloat16 low = __float2bfloat16_rd(m - reach);
+    return is_low(__bfloat162float(low), m, k) ? __bfloat16_as_ushort(low) * 0x10001u : 0u;
+}
+template <>
+__device__ __forceinline__ uint32_t low_of<__half>(float m, float k, float reach) {
+    const __half low = __float2half_rd(m - reach);
+    return is_low(__half2float(low), m, k) ? __half_as_ushort(low) * 0x10001u : 0u;
+}
+// The two entries of a word less m.
+template <class T>
+__device__ __forceinline__ F2 word_less(uint32_t w, float m) {
+    float a, b;
+    if constexpr (std::is_same<T, __half>::value)
+        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n sub.f32.f16 %0, l, %3;\n sub.f32.f16 %1, h, %3;\n}"
+            : "=f"(a), "=f"(b) : "r"(w), "f"(m));
+    else
+        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n sub.f32.bf16 %0, l, %3;\n sub.f32.bf16 %1, h, %3;\n}"
+            : "=f"(a), "=f"(b) : "r"(w), "f"(m));
+    return f2_make(a, b);
+}
+// gather() of a part from 0, with `low` as above.
+template <class T>
+__device__ __forceinline__ RowStat gather_part(float m, const uint4 (&q)[kListPer], float k, uint32_t low) {
+    RowStat r{m, 0.f, 0.f};
+    if (sizeof(T) == 4 || low == 0u) {
+        gather<T>(r, q, k);
+        return r;
+    }
+    F2 s = 0ull, t = 0ull;
+    const F2 k2 = f2_dup(k), bias = f2_dup(kExpBias);
+#pragma unroll
+    for (int u = 0; u < kListPer; ++u) {
+        const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const F2 x = f2_fma3(word_less<T>(Elt<T>::max(w[i], low), m), k2, bias), e = f2_exp2(x);
+            s = f2_add(s, e);
+            f2_fma(t, e, x);
+        }
+    }
+    const float2 s2 = f2_split(s), t2 = f2_split(t);
+    r.s = s2.x + s2.y;
+    r.t = t2.x + t2.y;
+    return r;
+}
+
+// How a slice's statistics and maxima are held. kCoarse: words of maxima, and the bound from the
+// threads' own maxima, of which there are two for every entry of the list; kFine: finer
+// groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups.
+enum : int { kCoarse = 0, kFine = 1, kLong = 2 };
+template <int kMode>
+struct OwnStat {
+    using Type = RowStat;
+};
+template <>
+struct OwnStat<kLong> {
+    using Type = LongStat;
+};
+
+template <class T, int kOp, int kThreads, int kMode>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(ListArgs a, ListShape sh) {
+    using Own = typename OwnStat<kMode>::Type;
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;
     // keys [cap], sorted ones [room] (or groups to be read again), maxima; or segments' (m, S)
@@ -319,6 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
     uint64_t* sorted = keys + sh.cap;
     uint32_t* again = reinterpret_cast<uint32_t*>(sorted);
     uint16_t* maxima = reinterpret_cast<uint16_t*>(sorted + sh.room);
+    uint32_t* words = reinterpret_cast<uint32_t*>(sorted + sh.room);         // kCoarse: [batch][word][thread]
     float2* segment = reinterpret_cast<float2*>(keys);
     wait_for_previous();
     let_next_start();
@@ -334,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
     // The keys of a slice's entries that may be among the first K, those of the first K of the slice and
     // few more, to keys and their number to own.count (past the cap: not all are there). Every
     // thread of the block; r: the slice's statistics, maxima: those of its groups.
-    auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi) {
+    auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi, float thread_max) {
         if (tid == 0) own.count = n_again = pick.digit = 0;
         if (sh.group_log < 0) {
             __syncthreads();
@@ -345,7 +620,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
             __syncthreads();
             return;
         }
-        const int n_max = (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << sh.group_log) - 1) >> sh.group_log) * kThreads;
+        const int log = kMode == kCoarse ? 2 : sh.group_log;         // of a group's vectors
+        const int n_max = (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
         const uint32_t top_key = order_key(r.m) >> 16;
         uint32_t reach = 0;
         for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {       // bins of one value, then of 64
@@ -354,10 +630,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
 #pragma unroll
             for (int i = 0; i < kBins / 4; ++i) bins[i] = make_uint4(0, 0, 0, 0);
             __syncthreads();
-            for (int i = tid; i < n_max; i += kThreads) {
-                const uint32_t key = maxima[i], bin = (top_key - key) >> coarse;
+            const auto count = [&](uint32_t key) {
+                const uint32_t bin = (top_key - key) >> coarse;
                 if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
-            }
+            };
+            if (kMode == kCoarse) count(max_key(thread_max));
+            else
+                for (int i = tid; i < n_max; i += kThreads) count(maxima[i]);
             __syncthreads();
             uint32_t sum = 0;
 #pragma unroll
@@ -386,35 +665,63 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
         }
         // (0: fewer than K groups have entries; all entries may be wanted)
         const uint32_t least = max(reach, 1u);
-        for (int i = tid; i < n_max; i += kThreads)
-            if (maxima[i] >= least) {
-                const uint32_t at = atomicAdd(&n_again, 1u);
-                if (at < 2u * sh.room) again[at] = i;
+        const float smallest = reach > 0 ? order_value(reach << 16) : -FLT_MAX;
+        // (whole warps: n_max is a multiple of the block's threads)
+        const auto push = [&](bool hit, int id, uint32_t& to) {
+            const unsigned hits = __ballot_sync(0xffffffffu, hit);
+            const uint32_t at = to + __popc(hits & ((1u << lane) - 1u));
+            if (hit && at < 2u * sh.room) again[at] = id;
+            to += __popc(hits);
+        };
+        const auto room_for = [&](bool first, bool second) {
+            const int n = __popc(__ballot_sync(0xffffffffu, first)) + __popc(__ballot_sync(0xffffffffu, second));
+            uint32_t to = 0;
+            if (n > 0 && lane == 0) to = atomicAdd(&n_again, (uint32_t)n);
+            return n > 0 ? __shfl_sync(0xffffffffu, to, 0) : ~0u;
+        };
+        if constexpr (kMode == kCoarse) {
+            for (int i = tid; i < n_max; i += 2 * kThreads) {
+                const bool x = Elt<T>::largest(words[i]) >= smallest, y = Elt<T>::largest(words[i + kThreads]) >= smallest;
+                uint32_t to = room_for(x, y);
+                if (to == ~0u) continue;
+                push(x, i, to);
+                push(y, i + kThreads, to);
             }
+        } else {
+            for (int i = tid; i < n_max; i += kThreads) {
+                const bool x = maxima[i] >= least;
+                uint32_t to = room_for(x, false);
+                if (to != ~0u) push(x, i, to);
+            }
+        }
         __syncthreads();
         if (n_again > 2u * sh.room) {
             if (tid == 0) own.count = sh.cap + 1;
         } else {
-            const int items = (int)n_again << sh.group_log;
+            const int items = (int)n_again << log;
             for (int item = tid; item < items; item += kThreads) {
-                const int id = (int)again[item >> sh.group_log];
-                const int n = (id / kThreads << sh.group_log) + (item & ((1 << sh.group_log) - 1));
+                const int id = (int)again[item >> log], n = (id / kThreads << log) + (item & ((1 << log) - 1));
                 const int v = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
                 if (v >= v_hi) continue;
                 const uint4 q = view.vec(v);
+                if (!(vec_max<T>(reinterpret_cast<const uint4(&)[1]>(q)) >= smallest)) continue;
+                uint32_t hits = 0;
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const float e = entry_of<T>(q, i);
-                    const uint32_t key = order_key(e);
-                    if (key >> 16 >= least && e > -INFINITY) {
-                        const uint32_t at = atomicAdd(&own.count, 1u);
-                        if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, v * W - view.h + i);
-                    }
+                for (int i = 0; i < W; ++i) hits |= entry_of<T>(q, i) >= smallest ? 1u << i : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int i = __ffs(hits) - 1;
+                    float e = entry_of<T>(q, 0);
+#pragma unroll
+                    for (int o = 1; o < W; ++o)
+                        if (i == o) e = entry_of<T>(q, o);
+                    const uint32_t at = atomicAdd(&own.count, 1u);
+                    if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, v * W - view.h + i);
                 }
             }
         }
         __syncthreads();
     };
+    const float low_reach = 160.f / a.k;
     for (int64_t row = blockIdx.x / C; row < a.n; row += gridDim.x / C) {
         const int token = a.tokens ? a.tokens[row] : 0;
         const bool first = tid == 0 && rank == 0;
@@ -451,27 +758,29 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
         if (kOp == kListTop && a.tokens) zt = Elt<T>::get(z[token]);
 
         // ---- statistics; a warp's vectors of a batch follow one another
-        LongStat st{-INFINITY, {0.f, 0.f}, {0.f, 0.f}};
-        uint32_t before = 0;
+        Own st{};
+        st.m = -INFINITY;
+        uint32_t before = 0, low = 0;
         const bool ranked = kOp == kListTop && a.rank;
         Above<T> above;
         // entries count that are >= the token's before it, and larger ones behind it
         const uint32_t thr_before = ranked ? Above<T>::both(zt) : 0u, thr_behind = ranked ? Above<T>::both(Above<T>::next(zt)) : 0u;
-        int segments = 0, batch = 0;
-        float group_max = -INFINITY;
+        float thread_max = -INFINITY;                // of its vectors; kLong: of the present group's
         // the row's whole vectors; a partial first or last one is filled up
         const int full_lo = h > 0 ? 1 : 0, full_hi = (h + a.V) % W != 0 ? nv - 1 : nv;
         const uint4* src = reinterpret_cast<const uint4*>(z - h);
-        for (int b = v_lo; b < v_hi; b += kBatch, segments += kWarps, ++batch) {
+        const int batches = (v_hi - v_lo + kBatch - 1) / kBatch;
+        for (int batch = 0; batch < batches; ++batch) {
+            const int b = v_lo + batch * kBatch, v0 = b + warp * kWarpVecs + lane;
             uint4 x[kListPer];
-            const int v0 = b + warp * kWarpVecs + lane;
             if (b >= full_lo && b + kBatch <= min(v_hi, full_hi)) {
 #pragma unroll
                 for (int u = 0; u < kListPer; ++u) x[u] = src[v0 + u * 32];
             } else {
-                const int lo = full_lo, n = max(0, min(v_hi, full_hi) - lo);
+                const int n = max(0, min(v_hi, full_hi) - full_lo);
 #pragma unroll
-                for (int u = 0; u < kListPer; ++u) x[u] = (uint32_t)(v0 + u * 32 - lo) < (uint32_t)n ? src[v0 + u * 32] : Elt<T>::none();
+                for (int u = 0; u < kListPer; ++u)
+                    x[u] = (uint32_t)(v0 + u * 32 - full_lo) < (uint32_t)n ? src[v0 + u * 32] : Elt<T>::none();
                 if (v0 == 0 && full_lo > 0) x[0] = load_part(z, -h, a.V);
                 const int tail = full_hi < nv && nv <= v_hi ? nv - 1 - v0 : -1;
                 if (tail >= 0 && tail < kWarpVecs && tail % 32 == 0 && !(tail == 0 && v0 == 0 && full_lo > 0)) {
@@ -482,32 +791,49 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
                 }
             }
             float mx;
-            if (!kAll && sh.group_log >= 0) {
-                uint16_t* out = maxima + tid + (batch << 3 >> min(sh.group_log, 3)) * kThreads;
-                mx = group_maxima<T>(x, sh.group_log, out, kThreads);
-                if (sh.group_log >= 3) {
-                    group_max = fmaxf(group_max, mx);
-                    if ((batch + 1) % (1 << (sh.group_log - 3)) == 0 || b + kBatch >= v_hi) {
-                        maxima[(batch >> (sh.group_log - 3)) * kThreads + tid] =
-                            group_max > -INFINITY ? (uint16_t)(order_key(group_max) >> 16) : (uint16_t)0;
-                        group_max = -INFINITY;
+            if constexpr (kAll) {
+                mx = vec_max<T>(x);
+            } else if constexpr (kMode == kCoarse) {
+                const Words<T> m(x);
+                if (sh.group_log >= 0) {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) words[(batch * kWords + i) * kThreads + tid] = m.w[i];
+                }
+                mx = m.largest;
+                thread_max = fmaxf(thread_max, mx);
+            } else {
+                mx = group_maxima<T>(x, sh.group_log, maxima + tid + (batch << 3 >> min(sh.group_log, 3)) * kThreads, kThreads);
+                if (sh.group_log > 3) {
+                    thread_max = fmaxf(thread_max, mx);
+                    const int per = 1 << (sh.group_log - 3);
+                    if ((batch + 1) % per == 0 || batch + 1 == batches) {
+                        maxima[batch / per * kThreads + tid] = max_key(thread_max);
+                        thread_max = -INFINITY;
                     }
                 }
-            } else {
-                mx = vec_max<T>(x);
             }
-            raise(st, warp_max(mx), a.k);
+            mx = warp_max(mx);
+            if (!(mx <= st.m)) {
+                raise(st, mx, a.k);
+                low = low_of<T>(st.m, a.k, low_reach);
+            }
             RowStat part{st.m, 0.f, 0.f};
-            if (st.m != -INFINITY) gather<T>(part, x, a.k);
-            st.s.add(part.s);
-            st.t.add(part.t);
+            if (st.m != -INFINITY) part = gather_part<T>(st.m, x, a.k, low);
+            join(st, part);
             if (kAll) {
                 const float s = warp_add(part.s);
-                if (lane == 0) segment[segments + warp] = make_float2(st.m, s);
+                if (lane == 0) segment[batch * kWarps + warp] = make_float2(st.m, s);
             }
-            if (ranked) {
+            if (ranked && !(mx < zt)) {              // (a warp's entries are all before the token, behind it, or both)
+                const int j0 = (v0 - lane) * W - h;
+                if (j0 > token || j0 + kWarpVecs * W <= token) {
+                    const uint32_t thr = j0 > token ? thr_behind : thr_before;
 #pragma unroll
-                for (int u = 0; u < kListPer; ++u) above.add(x[u], (v0 + u * 32 + 1) * W - h <= token ? thr_before : thr_behind);
+                    for (int u = 0; u < kListPer; ++u) above.add(x[u], thr);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kListPer; ++u) above.add(x[u], (v0 + u * 32 + 1) * W - h <= token ? thr_before : thr_behind);
+                }
                 before += above.take();
             }
         }
@@ -535,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
         }
         // ---- the keys of the slice's first K entries, and what the peers take
         if constexpr (!kAll) {
-            if (r.m != -INFINITY && fabsf(r.s) < INFINITY) collect(r, view, v_lo, v_hi);
+            if (r.m != -INFINITY && fabsf(r.s) < INFINITY) collect(r, view, v_lo, v_hi, thread_max);
             else if (tid == 0) own.count = 0;
         }
         float4 peer = make_float4(r.m, r.s, r.t, 0.f);               // lane i: CTA i's
@@ -559,150 +885,30 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
             if (kOp != kListTop && first) write_draw(a, row, -1, live ? NAN : 0.f, live ? NAN : 0.f, live ? NAN : 0.f);
         } else if constexpr (kAll) {
             if (warp == 0) {
-                // the CTA, then the segment, that holds the target; then its entries. Sums of many
-                // are in 64 bits; where rounding leaves none, the last one that has a mass.
+                // the CTA that holds the target, the last one with a mass where rounding leaves none
                 const double target = (double)row_uniform(a, row) * (double)r.s;
-                auto mass_at = [&](float m, float s) { return s * exp2_fast(fmaxf((m - r.m) * a.k, kXMin) + kExpBias); };
                 double passed = 0.0;
                 int cta = 0;
                 if (C > 1) {
-                    const float w = lane < C ? mass_at(peer.x, peer.y) : 0.f, cum = warp_scan(w, lane);
+                    const float w = lane < C ? mass_at(a, peer.x, peer.y, r) : 0.f, cum = warp_scan(w, lane);
                     const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && (double)cum > target),
                                    some = __ballot_sync(0xffffffffu, w > 0.f);
                     cta = hit ? __ffs(hit) - 1 : 31 - __clz(some);
                     passed = (double)__shfl_sync(0xffffffffu, cum - w, cta);
                 }
-                if (cta == rank) {
-                    int at = -1, last = 0;
-                    double last_passed = passed;
-                    for (int s0 = 0; s0 < segments && at < 0; s0 += 32) {
-                        const float2 sg = s0 + lane < segments ? segment[s0 + lane] : make_float2(-INFINITY, 0.f);
-                        const float w = sg.y > 0.f ? mass_at(sg.x, sg.y) : 0.f, cum = warp_scan(w, lane);
-                        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && passed + (double)cum > target),
-                                       some = __ballot_sync(0xffffffffu, w > 0.f);
-                        if (some) {
-                            const int k = 31 - __clz(some);
-                            last = s0 + k;
-                            last_passed = passed + (double)__shfl_sync(0xffffffffu, cum - w, k);
-                        }
-                        if (hit) {
-                            const int k = __ffs(hit) - 1;
-                            at = s0 + k;
-                            passed += (double)__shfl_sync(0xffffffffu, cum - w, k);
-                        } else {
-                            passed += (double)__shfl_sync(0xffffffffu, cum, 31);
-                        }
-                    }
-                    if (at < 0) {
-                        at = last;
-                        passed = last_passed;
-                    }
-                    const float rest = (float)(target - passed);
-                    const int v0 = v_lo + at * kWarpVecs + lane;
-                    float sum = 0.f;
-                    int found = -1, behind = -1;
-                    float fz = 0.f, bz = 0.f;
-                    for (int u = 0; u < kListPer && !__any_sync(0xffffffffu, found >= 0); ++u) {
-                        const int v = v0 + u * 32;
-                        const uint4 q = v < v_hi ? view.vec(v) : Elt<T>::none();
-                        float e[W], mine = 0.f;
-#pragma unroll
-                        for (int i = 0; i < W; ++i) {
-                            e[i] = exp2_fast(x_of(entry_of<T>(q, i), r.m, a.k));
-                            mine += e[i];
-                        }
-                        const float incl = warp_scan(mine, lane);
-                        float cum = sum + (incl - mine);
-#pragma unroll
-                        for (int i = 0; i < W; ++i) {
-                            cum += e[i];
-                            if (e[i] > 0.f) {
-                                behind = v * W - h + i;
-                                bz = entry_of<T>(q, i);
-                                if (found < 0 && cum > rest) {
-                                    found = behind;
-                                    fz = bz;
-                                }
-                            }
-                        }
-                        sum += __shfl_sync(0xffffffffu, incl, 31);
-                    }
-                    const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
-                    int lane_at, j;
-                    if (hit) {
-                        lane_at = __ffs(hit) - 1;
-                        j = found;
-                    } else {
-                        const int most = __reduce_max_sync(0xffffffffu, behind);
-                        lane_at = __ffs(__ballot_sync(0xffffffffu, behind == most)) - 1;
-                        j = behind;
-                        fz = bz;
-                    }
-                    if (lane == lane_at) {
-                        const float logp = log_prob(a, r, fz);
-                        write_draw(a, row, j, logp, row_entropy(r), logp);
-                    }
-                }
+                if (cta == rank) draw_all(a, row, r, view, v_lo, v_hi, segment, batches * kWarps, target, passed, lane);
             }
         } else {
             if (n_keys > (uint32_t)sh.cap) {
                 // ---- too many (the same in all CTAs of the row): a bound from all keys
-                uint64_t bound = 0;
-                uint32_t above = 0;
-                int shift = 48;
-                for (int pass = 0;; ++pass, shift -= 8) {
-                    uint32_t* hist = own.hist + 256 * (pass & 1);
-                    for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
-                    __syncthreads();
-                    each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
-                        const uint64_t key = entry_key(e, j);
-                        if (pass == 0 || key >> (shift + 8) == bound) atomicAdd(hist + ((uint32_t)(key >> shift) & 255u), 1u);
+                const uint64_t bound = bound_of_all<T, kThreads>(
+                    view, v_lo, v_hi, (uint32_t)a.K, (uint32_t)sh.cap, own.hist, &pick, tid, [] { __syncthreads(); }, meet,
+                    [&](const uint32_t* bin) {
+                        if (C == 1) return *bin;
+                        uint32_t n = 0;
+                        for (int c = 0; c < C; ++c) n += peer_load(bin, c);
+                        return n;
                     });
-                    meet();
-                    if (warp == 0) {
-                        uint32_t n[8], sum = 0;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int bin = 255 - 8 * lane - i;
-                            n[i] = hist[bin];
-                            if (C > 1) {
-                                n[i] = 0;
-                                for (int c = 0; c < C; ++c) n[i] += peer_load(hist + bin, c);
-                            }
-                            sum += n[i];
-                        }
-                        uint32_t upto = sum;
-#pragma unroll
-                        for (int o = 1; o < 32; o *= 2) {
-                            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-                            if (lane >= o) upto += x;
-                        }
-                        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= (uint32_t)a.K);
-                        if (hit ? lane == __ffs(hit) - 1 : lane == 0) {
-                            ListPick p{0, 0, 0};
-                            uint32_t cum = above + upto - sum;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                if (hit && p.at == 0 && cum + n[i] >= (uint32_t)a.K)
-                                    p = ListPick{(uint32_t)(255 - 8 * lane - i), cum, n[i]};
-                                cum += n[i];
-                            }
-                            pick = p;
-                        }
-                    }
-                    __syncthreads();
-                    const ListPick p = pick;
-                    if (p.at == 0) {                                     // in the first pass only: all of them
-                        bound = 0;
-                        break;
-                    }
-                    bound = bound << 8 | p.digit;
-                    above = p.above;
-                    if (above + p.at <= (uint32_t)sh.cap) {
-                        bound <<= shift;
-                        break;
-                    }
-                }
                 meet();                                              // the counts that were read
                 if (tid == 0) own.count = 0;
                 __syncthreads();
@@ -721,7 +927,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
                     n += more;
                 }
                 __syncthreads();
-                const uint64_t* list = sort_keys<kThreads>(keys, sorted, n, a.K, tid);
+                const uint64_t* list = sort_keys<kThreads>(keys, sorted, n, a.K, std::is_same<T, __nv_bfloat16>::value && a.V <= 65536, tid, [] { __syncthreads(); });
                 if (kOp == kListDraw) {
                     if (warp == 0) draw_listed(a, row, r, list, min(n, a.K), lane);
                 } else {
@@ -737,9 +943,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
     }
 }
 
-template <class T, int kOp, int kThreads>
-cudaError_t launch_list_threads(const ListArgs& a, const ListShape& sh, size_t bytes, cudaStream_t s) {
-    const auto kernel = token_list_kernel<T, kOp, kThreads>;
+template <class T, int kOp, int kThreads, int kMode>
+cudaError_t launch_list_mode(const ListArgs& a, const ListShape& sh, size_t bytes, cudaStream_t s) {
+    const auto kernel = token_list_kernel<T, kOp, kThreads, kMode>;
     if (bytes > 32 << 10) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != cudaSuccess) return e;
@@ -764,43 +970,39 @@ cudaError_t launch_list_threads(const ListArgs& a, const ListShape& sh, size_t b
     return cudaLaunchKernelEx(&cfg, kernel, a, sh);
 }
 
-template <class T, int kOp>
-cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
-    const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
-    ListShape sh{1, (int)nv, -1, 0, 0};
-    // Clusters while the CTAs' lists can be sorted together.
-    const bool all = kOp == kListDrawAll;
-    for (int c = 2; c <= 8 && (nv + c - 1) / c >= 512; c *= 2)
-        if (a.n * c <= 4 * (int64_t)n_sm && (all || (int64_t)c * a.K <= kListCap / 2)) {
-            sh.cluster = c;
-            sh.slice = (int)((nv + c - 1) / c);
-        }
-    const bool small = sh.slice <= 256;
-    const int batch = small ? 256 : 2048;
-    const int64_t padded = (sh.slice + batch - 1) / batch * batch;
-    size_t bytes = (size_t)padded / 256 * sizeof(float2);
-    if (!all) {
+template <class T, int kOp, int kThreads>
+cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s) {
+    constexpr int kBatch = kThreads * kListPer;
+    const int64_t batches = (sh.slice + kBatch - 1) / kBatch;
+    int mode = batches > kManyBatches ? kLong : kCoarse;
+    size_t bytes = (size_t)batches * (kThreads / 32) * sizeof(float2);
+    if (kOp != kListDrawAll) {
         // Maxima of as large groups as leave four for every entry of the list; none where all
         // entries can be sorted as well, or where they are too few.
-        int64_t groups = 0;
+        size_t maxima = 0;
         if (a.V > 192 && sh.slice >= 2 * a.K) {
-            sh.group_log = 0;
-            while (sh.group_log < 3 && sh.slice >= (int64_t)a.K << (sh.group_log + 3)) ++sh.group_log;
-            while (padded >> sh.group_log > kListGroups) ++sh.group_log;
-            groups = ((padded / (batch / 8) + (1 << sh.group_log) - 1) >> sh.group_log) * (batch / 8);
+            if (mode == kCoarse && 2 * a.K <= kThreads && sh.slice >= kBatch / 2) {
+                sh.group_log = 3;
+                maxima = batches * kWords * kThreads * sizeof(uint32_t);
+            } else {
+                if (mode == kCoarse) mode = kFine;
+                sh.group_log = 0;
+                while (sh.group_log < 2 && sh.slice >= (int64_t)a.K << (sh.group_log + 3)) ++sh.group_log;
+                while (batches * kBatch >> sh.group_log > kListGroups) ++sh.group_log;
+                maxima = ((batches * kListPer + (1 << sh.group_log) - 1) >> sh.group_log) * kThreads * sizeof(uint16_t);
+            }
         }
-        sh.cap = a.K * sh.cluster <= 256 && sh.group_log >= 0 ? 1024 : kListCap;
-        sh.room = a.K <= 256 ? 256 : 1024;
-        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + groups * sizeof(uint16_t);
+        sh.cap = sh.group_log < 0 || a.K * sh.cluster > 256 ? kListCap : a.K * sh.cluster > 64 ? 1024 : 512;
+        sh.room = a.K <= 128 ? 128 : a.K <= 256 ? 256 : 1024;
+        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + maxima;
     }
-    return small ? launch_list_threads<T, kOp, 32>(a, sh, bytes, s) : launch_list_threads<T, kOp, 256>(a, sh, bytes, s);
-}
-
-template <class T>
-cudaError_t launch_list_type(const ListArgs& a, int op, int n_sm, cudaStream_t s) {
-    if (op == kListTop) return launch_list_op<T, kListTop>(a, n_sm, s);
-    if (op == kListDraw) return launch_list_op<T, kListDraw>(a, n_sm, s);
-    return launch_list_op<T, kListDrawAll>(a, n_sm, s);
+    if constexpr (kThreads > 128) {
+        if (mode == kLong) return launch_list_mode<T, kOp, kThreads, kLong>(a, sh, bytes, s);
+    }
+    if constexpr (kOp != kListDrawAll) {
+        if (mode == kFine) return launch_list_mode<T, kOp, kThreads, kFine>(a, sh, bytes, s);
+    }
+    return launch_list_mode<T, kOp, kThreads, kCoarse>(a, sh, bytes, s);
 }
 
 }  // namespace

@@ -1,5 +1,5 @@
 // The most likely entries and the draw of bf16 logits.
-#include "token_list.cuh"
+#include "token_list_rows.cuh"
 
 namespace malib {
 

@@ -35,6 +35,8 @@ struct ListShape {
     int group_log;                                   // log 2 of a maximum's vectors; < 0: no maxima
     int cap;                                         // most keys that are sorted
     int room;                                        // sorted keys, or twice as many groups to be read again
+    int maxima;                                      // bytes of the groups' maxima
+    int slice_K;                                     // entries that a CTA lists: K, or a share of it
 };
 
 namespace {
@@ -64,7 +66,8 @@ __device__ __forceinline__ float key_logit(uint64_t key) { return order_value((u
 struct __align__(16) ListShared {
     float4 stat;                                     // m, S, t, entries before the token (bits)
     uint32_t count;                                  // keys collected; past the cap: not all are there
-    uint32_t pad[3];
+    uint32_t reach;                                  // the top 16 bits from which on they are all; 0: all are
+    uint32_t pad[2];
     uint32_t hist[kListBins];                        // or two of 256 bins
 };
 struct ListPick {
@@ -205,9 +208,15 @@ struct Above<__half> {
 // Sorts the n keys at `key` (room for the next power of two, 512 at least), largest first; what comes back
 // has the first K in order. Few of them are counted: a key's place is how many are larger; several lanes
 // share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
+// buckets: what the sort of more keys by bins needs; null: they are sorted by exchanges.
+struct Buckets {
+    uint32_t top_key;                                // of the row's maximum, its top 16 bits
+    uint32_t *bins, *warp_total;                     // [kListBins], [warps]
+    uint16_t* order;                                 // [cap]
+};
 template <int kThreads, class Sync>
 __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, bool narrow, int tid,
-                                                     Sync sync) {
+                                                     Sync sync, const Buckets* buckets = nullptr) {
     if (n <= max(128, kThreads + kThreads / 2)) {
         const int lanes = n * 8 <= kThreads ? 8 : n * 4 <= kThreads ? 4 : n * 2 <= kThreads ? 2 : 1;
         const auto narrowed = [](uint64_t k) { return (uint32_t)(k >> 24) & 0xffff0000u | (uint32_t)k & 0xffffu; };
@@ -250,6 +259,65 @@ __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* so
         }
         sync();
         return sorted;
+    }
+    if (buckets) {
+        const uint32_t top_key = buckets->top_key;
+        uint32_t *bins = buckets->bins, *warp_total = buckets->warp_total;
+        uint16_t* order = buckets->order;
+        // More of them, by the distance of a key's top 16 bits from the row's maximum: a key comes after those of
+        // smaller distances, and is counted among its bin's. Bins of many keys are left to the sort below.
+        constexpr int kBins = kListBins / kThreads;
+        const int lane = tid & 31, warp = tid >> 5;
+        const auto bin_of = [&](uint64_t k) { return min(top_key - (uint32_t)(k >> 40), (uint32_t)kListBins - 1); };
+        for (int i = tid; i < kListBins; i += kThreads) bins[i] = 0;
+        sync();
+        for (int i = tid; i < n; i += kThreads) atomicAdd(bins + bin_of(key[i]), 1u);
+        sync();
+        uint32_t sum = 0, most = 0, size[kBins];
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) {
+            size[i] = bins[kBins * tid + i];
+            sum += size[i];
+            most = max(most, size[i]);
+        }
+        uint32_t upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += q;
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 31) warp_total[warp] = upto | (most > 256 ? 1u << 31 : 0u);
+        sync();
+        bool many = false;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const uint32_t q = warp_total[w];
+            many |= q >> 31;
+            if (w < warp) upto += q & 0x7fffffffu;
+        }
+        if (!many) {
+            // a bin's first place, then, when its keys have taken theirs, the next bin's
+            upto -= sum;
+#pragma unroll
+            for (int i = 0; i < kBins; ++i) {
+                bins[kBins * tid + i] = upto;
+                upto += size[i];
+            }
+            sync();
+            for (int i = tid; i < n; i += kThreads) order[atomicAdd(bins + bin_of(key[i]), 1u)] = (uint16_t)i;
+            sync();
+            for (int i = tid; i < n; i += kThreads) {
+                const uint64_t own = key[i];
+                const uint32_t bin = bin_of(own), first = bin > 0 ? bins[bin - 1] : 0u, end = bins[bin];
+                int place = (int)first;
+                if (place >= K) continue;
+                for (uint32_t o = first; o < end; ++o) place += key[order[o]] > own;
+                if (place < K) sorted[place] = own;
+            }
+            sync();
+            return sorted;
+        }
     }
     int P = 256;
     while (P < n) P *= 2;
@@ -578,7 +646,7 @@ struct OwnStat<kLong> {
 };
 
 template <class T, int kOp, int kThreads, int kMode>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(ListArgs a, ListShape sh) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 128 ? 7 : 24) token_list_kernel(ListArgs a, ListShape sh) {
     using Own = typename OwnStat<kMode>::Type;
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;
@@ -594,6 +662,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
     uint32_t* again = reinterpret_cast<uint32_t*>(sorted);
     uint16_t* maxima = reinterpret_cast<uint16_t*>(sorted + sh.room);
     uint32_t* words = reinterpret_cast<uint32_t*>(sorted + sh.room);         // kCoarse: [batch][word][thread]
+    uint16_t* order = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(maxima) + sh.maxima);
     float2* segment = reinterpret_cast<float2*>(keys);
     wait_for_previous();
     let_next_start();
@@ -610,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
     // few more, to keys and their number to own.count (past the cap: not all are there). Every
     // thread of the block; r: the slice's statistics, maxima: those of its groups.
     auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi, float thread_max) {
-        if (tid == 0) own.count = n_again = pick.digit = 0;
+        if (tid == 0) own.count = own.reach = n_again = pick.digit = 0;
         if (sh.group_log < 0) {
             __syncthreads();
             each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
@@ -653,9 +722,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
 #pragma unroll
                 for (int w = 0; w < kWarps - 1; ++w) upto += w < warp ? warp_total[w] : 0u;
             }
-            if (upto >= (uint32_t)a.K && upto - sum < (uint32_t)a.K) {
+            if (upto >= (uint32_t)sh.slice_K && upto - sum < (uint32_t)sh.slice_K) {
                 uint32_t cum = upto - sum, bin = kBins * tid;
-                while ((cum += own.hist[bin]) < (uint32_t)a.K) ++bin;
+                while ((cum += own.hist[bin]) < (uint32_t)sh.slice_K) ++bin;
                 // the bin's smallest value, at least 1 (0 has no entries)
                 const uint32_t below = ((bin + 1) << coarse) - 1;
                 pick.digit = below < top_key ? top_key - below : 1u;
@@ -665,6 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
         }
         // (0: fewer than K groups have entries; all entries may be wanted)
         const uint32_t least = max(reach, 1u);
+        if (tid == 0) own.reach = reach;
         const float smallest = reach > 0 ? order_value(reach << 16) : -FLT_MAX;
         // (whole warps: n_max is a multiple of the block's threads)
         const auto push = [&](bool hit, int id, uint32_t& to) {
@@ -699,23 +769,34 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
             if (tid == 0) own.count = sh.cap + 1;
         } else {
             const int items = (int)n_again << log;
-            for (int item = tid; item < items; item += kThreads) {
-                const int id = (int)again[item >> log], n = (id / kThreads << log) + (item & ((1 << log) - 1));
-                const int v = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
-                if (v >= v_hi) continue;
-                const uint4 q = view.vec(v);
-                if (!(vec_max<T>(reinterpret_cast<const uint4(&)[1]>(q)) >= smallest)) continue;
-                uint32_t hits = 0;
+            constexpr int kAt = 2;                                           // loads in flight
+            for (int i0 = tid; i0 < items; i0 += kAt * kThreads) {
+                uint4 x[kAt];
+                int v[kAt];
 #pragma unroll
-                for (int i = 0; i < W; ++i) hits |= entry_of<T>(q, i) >= smallest ? 1u << i : 0u;
-                for (; hits; hits &= hits - 1) {
-                    const int i = __ffs(hits) - 1;
-                    float e = entry_of<T>(q, 0);
+                for (int u = 0; u < kAt; ++u) {
+                    const int item = i0 + u * kThreads;
+                    x[u] = Elt<T>::none();
+                    if (item >= items) continue;
+                    const int id = (int)again[item >> log], n = (id / kThreads << log) + (item & ((1 << log) - 1));
+                    v[u] = v_lo + (n >> 3) * kBatch + (id % kThreads >> 5) * kWarpVecs + (n & 7) * 32 + (id & 31);
+                    if (v[u] < v_hi) x[u] = view.vec(v[u]);
+                }
 #pragma unroll
-                    for (int o = 1; o < W; ++o)
-                        if (i == o) e = entry_of<T>(q, o);
-                    const uint32_t at = atomicAdd(&own.count, 1u);
-                    if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, v * W - view.h + i);
+                for (int u = 0; u < kAt; ++u) {
+                    if (!(vec_max<T>(reinterpret_cast<const uint4(&)[1]>(x[u])) >= smallest)) continue;
+                    uint32_t hits = 0;
+#pragma unroll
+                    for (int i = 0; i < W; ++i) hits |= entry_of<T>(x[u], i) >= smallest ? 1u << i : 0u;
+                    uint32_t to = atomicAdd(&own.count, (uint32_t)__popc(hits));
+                    for (; hits; hits &= hits - 1, ++to) {
+                        const int i = __ffs(hits) - 1;
+                        float e = entry_of<T>(x[u], 0);
+#pragma unroll
+                        for (int o = 1; o < W; ++o)
+                            if (i == o) e = entry_of<T>(x[u], o);
+                        if (to < (uint32_t)sh.cap) keys[to] = entry_key(e, v[u] * W - view.h + i);
+                    }
                 }
             }
         }
@@ -862,17 +943,20 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
         // ---- the keys of the slice's first K entries, and what the peers take
         if constexpr (!kAll) {
             if (r.m != -INFINITY && fabsf(r.s) < INFINITY) collect(r, view, v_lo, v_hi, thread_max);
-            else if (tid == 0) own.count = 0;
+            else if (tid == 0) own.count = own.reach = 0;
         }
         float4 peer = make_float4(r.m, r.s, r.t, 0.f);               // lane i: CTA i's
-        uint32_t n_keys = kAll ? 0 : own.count;
+        uint32_t n_keys = kAll ? 0 : own.count, reach = 0;
         if (C > 1) {
             if (tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
             meet();
             peer = lane < C ? peer_load(&own.stat, lane) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
             before = __reduce_add_sync(0xffffffffu, __float_as_uint(peer.w));
             r = reduce_stat<32>(RowStat{peer.x, peer.y, peer.z}, a.k);
-            if (!kAll) n_keys = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
+            if (!kAll) {
+                n_keys = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
+                reach = __reduce_max_sync(0xffffffffu, lane < C ? peer_load(&own.reach, lane) : 0u);
+            }
         }
         live = r.m != -INFINITY;
         const bool good = live && fabsf(r.s) < INFINITY;             // no NaN, no +infinity
@@ -927,7 +1011,30 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_list_kernel(L
                     n += more;
                 }
                 __syncthreads();
-                const uint64_t* list = sort_keys<kThreads>(keys, sorted, n, a.K, std::is_same<T, __nv_bfloat16>::value && a.V <= 65536, tid, [] { __syncthreads(); });
+                const auto sort = [&] {
+                    const Buckets b{order_key(r.m) >> 16, own.hist, warp_total, order};
+                    return sort_keys<kThreads>(keys, sorted, n, a.K, std::is_same<T, __nv_bfloat16>::value && a.V <= 65536, tid,
+                                               [] { __syncthreads(); }, kThreads >= 128 ? &b : nullptr);
+                };
+                const uint64_t* list = sort();
+                // Slices that list a share of K each: all entries from `reach` on are there. Where the first K go
+                // further down, this CTA finds them in the whole row.
+                if (C > 1 && sh.slice_K < a.K && n_keys <= (uint32_t)sh.cap && reach > 0 &&
+                    (n < a.K || (uint32_t)(list[a.K - 1] >> 40) < reach)) {
+                    __syncthreads();
+                    const auto sync = [] { __syncthreads(); };
+                    const uint64_t bound = bound_of_all<T, kThreads>(view, 0, nv, (uint32_t)a.K, (uint32_t)sh.cap, own.hist, &pick, tid,
+                                                                     sync, sync, [](const uint32_t* bin) { return *bin; });
+                    if (tid == 0) n_again = 0;
+                    __syncthreads();
+                    each_entry(view, 0, nv, tid, kThreads, [&](int j, float e) {
+                        const uint64_t key = entry_key(e, j);
+                        if (key >= bound) keys[atomicAdd(&n_again, 1u)] = key;
+                    });
+                    __syncthreads();
+                    n = (int)n_again;
+                    list = sort();
+                }
                 if (kOp == kListDraw) {
                     if (warp == 0) draw_listed(a, row, r, list, min(n, a.K), lane);
                 } else {
@@ -980,21 +1087,23 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
         // Maxima of as large groups as leave four for every entry of the list; none where all
         // entries can be sorted as well, or where they are too few.
         size_t maxima = 0;
-        if (a.V > 192 && sh.slice >= 2 * a.K) {
-            if (mode == kCoarse && 2 * a.K <= kThreads && sh.slice >= kBatch / 2) {
+        if (a.V > 192 && sh.slice >= 2 * sh.slice_K) {
+            if (mode == kCoarse && 2 * sh.slice_K <= kThreads && sh.slice >= kBatch / 2) {
                 sh.group_log = 3;
                 maxima = batches * kWords * kThreads * sizeof(uint32_t);
             } else {
                 if (mode == kCoarse) mode = kFine;
                 sh.group_log = 0;
-                while (sh.group_log < 2 && sh.slice >= (int64_t)a.K << (sh.group_log + 3)) ++sh.group_log;
+                while (sh.group_log < 2 && sh.slice >= (int64_t)sh.slice_K << (sh.group_log + 3)) ++sh.group_log;
                 while (batches * kBatch >> sh.group_log > kListGroups) ++sh.group_log;
                 maxima = ((batches * kListPer + (1 << sh.group_log) - 1) >> sh.group_log) * kThreads * sizeof(uint16_t);
             }
         }
-        sh.cap = sh.group_log < 0 || a.K * sh.cluster > 256 ? kListCap : a.K * sh.cluster > 64 ? 1024 : 512;
+        const int most = sh.slice_K * sh.cluster;
+        sh.cap = sh.group_log < 0 || most > 256 ? kListCap : most > 64 ? 1024 : 512;
         sh.room = a.K <= 128 ? 128 : a.K <= 256 ? 256 : 1024;
-        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + maxima;
+        sh.maxima = (int)((maxima + 15) / 16 * 16);
+        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + sh.maxima + (kThreads >= 128 ? sh.cap * sizeof(uint16_t) : 0);
     }
     if constexpr (kThreads > 128) {
         if (mode == kLong) return launch_list_mode<T, kOp, kThreads, kLong>(a, sh, bytes, s);

@@ -1,6 +1,7 @@
 // Lists and draws: the kernel that takes rows of a length, number and list.
 #pragma once
 
+#include "token_draw_stream.cuh"
 #include "token_list.cuh"
 #include "token_list_tiny.cuh"
 
@@ -16,14 +17,29 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
         if (a.V <= 32) return launch_list_tiny<T, kOp, 32>(a, n_sm, s);
     }
     const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
-    ListShape sh{1, (int)nv, -1, 0, 0};
-    // Clusters while the CTAs' lists can be sorted together.
-    for (int c = 2; c <= 8 && (nv + c - 1) / c >= 512; c *= 2)
-        if (a.n * c <= 4 * (int64_t)n_sm && (int64_t)c * a.K <= kListCap / 2) {
+    ListShape sh{};
+    sh.cluster = 1;
+    sh.group_log = -1;
+    // CTAs a row: as many as there are SMs for twice, with slices of 24 KB or more; lists of rows of more than
+    // 288 KB, which have few CTAs on the device for long, also over several rounds, with slices of 144 KB or
+    // more. us, C = 1, 2, 4 and 8, lists of 64 from 131,072 bf16 entries: 1 row 18.8, 16.0, 13.7, 15.0, 100
+    // rows 20, 22, 33, 38, 600 rows 43, 61, 121, 160; of 5 from 61 x 50,001 fp16 14.8, 12.3, 12.8, 16.6;
+    // of 1,024 from 151,111 fp32, 20 rows 57, 36, 27, 28, 100 rows 69, 50, 50, 64, 333 rows 141, 123, 117,
+    // 162; draws from one row of a million 76, 35, 21, 15.
+    for (int c = 2; c <= 8; c *= 2) {
+        const int64_t slice = (nv + c - 1) / c;
+        if ((slice >= 1536 && a.n * c <= 2 * (int64_t)n_sm) ||
+            (kOp != kListDrawAll && slice >= 9216 && a.n * c <= 16 * (int64_t)n_sm))
             sh.cluster = c;
-            sh.slice = (int)((nv + c - 1) / c);
-        }
+    }
+    // What the CTAs list is sorted together: K entries each as long as that is little, else a share of K with
+    // a quarter more, which has them all unless a slice has more than its share.
+    sh.slice = (int)((nv + sh.cluster - 1) / sh.cluster);
+    sh.slice_K = sh.cluster * a.K <= kListCap / 2 ? a.K : a.K / sh.cluster * 5 / 4 + 32;
     if (sh.slice <= 256) return launch_list_threads<T, kOp, 32>(a, sh, s);
+    if constexpr (kOp == kListDrawAll) {
+        if (sh.cluster == 1 && nv <= kStreamMostBatches * kStreamBatch) return launch_draw_stream<T>(a, nv, n_sm, s);
+    }
     if (sh.cluster == 1 && sh.slice <= kManyBatches * 128 * kListPer) return launch_list_threads<T, kOp, 128>(a, sh, s);
     return launch_list_threads<T, kOp, 256>(a, sh, s);
 }

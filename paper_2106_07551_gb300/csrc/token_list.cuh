@@ -133,15 +133,17 @@ struct Above<float> {
     }
     __device__ static uint32_t both(float z) { return __float_as_uint(z); }
     __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
-        const float t = __uint_as_float(thr);
-        n += __uint_as_float(q.x) >= t;
-        n += __uint_as_float(q.y) >= t;
-        n += __uint_as_float(q.z) >= t;
-        n += __uint_as_float(q.w) >= t;
+        n += mask(q.x, thr) + mask(q.y, thr);
+        n += mask(q.z, thr) + mask(q.w, thr);
     }
     __device__ __forceinline__ uint32_t take() {
-        const uint32_t r = n;
+        const uint32_t r = 0u - n;
         n = 0;
+        return r;
+    }
+    __device__ static uint32_t mask(uint32_t z, uint32_t thr) {      // -1 or 0
+        uint32_t r;
+        asm("set.ge.u32.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(z)), "f"(__uint_as_float(thr)));
         return r;
     }
 };
@@ -210,7 +212,7 @@ struct Above<__half> {
 // share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
 // buckets: what the sort of more keys by bins needs; null: they are sorted by exchanges.
 struct Buckets {
-    uint32_t top_key;                                // of the row's maximum, its top 16 bits
+    uint32_t top_key;                                // of the row's maximum, 32 bits
     uint32_t *bins, *warp_total;                     // [kListBins], [warps]
     uint16_t* order;                                 // [cap]
 };
@@ -264,11 +266,20 @@ __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* so
         const uint32_t top_key = buckets->top_key;
         uint32_t *bins = buckets->bins, *warp_total = buckets->warp_total;
         uint16_t* order = buckets->order;
-        // More of them, by the distance of a key's top 16 bits from the row's maximum: a key comes after those of
-        // smaller distances, and is counted among its bin's. Bins of many keys are left to the sort below.
+        // More of them, by the distance of a key's logit from the row's maximum, in 1,024 equal steps of the
+        // logits' bits: a key comes after those of smaller distances, and is counted among its bin's.
+        // Bins of many keys are left to the sort below.
         constexpr int kBins = kListBins / kThreads;
         const int lane = tid & 31, warp = tid >> 5;
-        const auto bin_of = [&](uint64_t k) { return min(top_key - (uint32_t)(k >> 40), (uint32_t)kListBins - 1); };
+        uint32_t least = ~0u;
+        for (int i = tid; i < n; i += kThreads) least = min(least, (uint32_t)(key[i] >> 24));
+        least = __reduce_min_sync(0xffffffffu, least);
+        if (lane == 0) warp_total[warp] = least;
+        sync();
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) least = min(least, warp_total[w]);
+        const int shift = max(0, 22 - __clz(top_key - least));       // distances below 2^(10 + shift)
+        const auto bin_of = [&](uint64_t k) { return (top_key - (uint32_t)(k >> 24)) >> shift; };
         for (int i = tid; i < kListBins; i += kThreads) bins[i] = 0;
         sync();
         for (int i = tid; i < n; i += kThreads) atomicAdd(bins + bin_of(key[i]), 1u);
@@ -1003,16 +1014,18 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 meet();
             }
             // ---- sorted in the first CTA
+            int n = (int)own.count;
             if (rank == 0) {
-                int n = (int)own.count;
                 for (int c = 1; c < C; ++c) {
                     const int more = (int)peer_load(&own.count, c);
                     for (int i = tid; i < more; i += kThreads) keys[n + i] = peer_load(keys + i, c);
                     n += more;
                 }
-                __syncthreads();
+            }
+            meet();                                                  // the other CTAs are done
+            if (rank == 0) {
                 const auto sort = [&] {
-                    const Buckets b{order_key(r.m) >> 16, own.hist, warp_total, order};
+                    const Buckets b{order_key(r.m), own.hist, warp_total, order};
                     return sort_keys<kThreads>(keys, sorted, n, a.K, std::is_same<T, __nv_bfloat16>::value && a.V <= 65536, tid,
                                                [] { __syncthreads(); }, kThreads >= 128 ? &b : nullptr);
                 };
@@ -1046,7 +1059,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 }
             }
         }
-        meet();                                                      // nothing of this row is read any more
+        // nothing of this row is read any more; of a list, nothing from peers since they met last
+        if (kAll || !good) meet();
+        else __syncthreads();
     }
 }
 

@@ -667,8 +667,8 @@ int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_
  * Kept are all unmasked entries (top_k 0), or of the first top_k those before which less than
  * top_p of the top_k's probability lies (at least one). With a random number u in [0, 1) the
  * token is the first kept entry, in the order of the index (top_k 0) or of the list, whose running
- * probability exceeds u times the kept one; entries whose probability is below 2^-126 of the
- * largest are not drawn. u >= 1 draws the last.
+ * probability exceeds u times the kept one; of entries whose probability is below 2^-98 of the
+ * largest some, below 2^-126 all, are not drawn. u >= 1, or NaN, draws the last that can be.
  * u is uniform[row], or without it the top 24 bits of the first word of Philox4x32-10 at counter
  * (sequence lo32, sequence hi32, step, agent) under `seed` over 2^24, as in malib_rollout: a
  * sequence's draws do not depend on the batch that it is in. agent < 2^31 (the counters of

@@ -95,11 +95,11 @@ struct Call {
         return MALIB_OK;
     }
 
-    // Work space: counters, partial sums, and a row's statistics or share of them.
-    int work() {
+    // Work space: counters, partial sums, and the statistics, or shares of them, of n rows.
+    int work(int64_t n) {
         static_assert(sizeof(TokenRow) == sizeof(RowSum), "one work space for either");
         void *fixed = nullptr, *rows = nullptr;
-        const int r = ctx_token_work(ctx, a.n * (int64_t)sizeof(RowSum), &fixed, &rows);
+        const int r = ctx_token_work(ctx, n * (int64_t)sizeof(RowSum), &fixed, &rows);
         if (r != MALIB_OK) return r;
         a.ticket = static_cast<unsigned*>(fixed);
         a.claims = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(fixed) + 128);
@@ -133,7 +133,7 @@ int malib_token_logprob(malib_ctx* ctx, const malib_token_batch* batch, float* l
     if (c.a.n == 0) return MALIB_OK;
     if (!c.opt(logp_out, 4) || !c.opt(entropy_out, 4))
         return c.bad("outputs must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(c.a.n)) != MALIB_OK) return r;
     c.a.logp = logp_out;
     c.a.entropy = entropy_out;
     return c.done(launch_token_rows(c.a, kTokLogp, c.v.n_sm, c.v.stream), 1);
@@ -157,7 +157,7 @@ int malib_learn_token_ppo(malib_ctx* ctx, const malib_token_batch* batch, const 
                       !c.opt(logp_out, 4)))
         return c.bad("old_logp, advantage, ref_logp and logp_out must be device memory of the context's device");
     if (!c.opt(stats_out, 4)) return c.bad("stats must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(c.a.n)) != MALIB_OK) return r;
     c.a.old_logp = loss->old_logp;
     c.a.adv = loss->advantage;
     c.a.ref = loss->ref_logp;
@@ -185,7 +185,7 @@ int malib_learn_token_pref(malib_ctx* ctx, const malib_token_batch* batch, const
     if (!c.dev(loss->offsets, 8)) return c.bad("offsets must be aligned device memory of the context's device");
     if ((c.a.n > 0 && !c.opt(loss->ref_logp, 4)) || !c.opt(reward_out, 4) || !c.opt(stats_out, 4))
         return c.bad("ref_logp, reward_out and stats must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(c.a.n)) != MALIB_OK) return r;
     c.a.rows = reinterpret_cast<TokenRow*>(c.a.row_sums);
     c.a.offsets = loss->offsets;
     c.a.n_pairs = loss->n_pairs;
@@ -211,7 +211,7 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
     if (c.a.n > 0 && (!c.dev(loss->ids, 4) || !c.dev(loss->teacher, elt_size(loss->teacher_dtype)) || !c.opt(loss_out, 4)))
         return c.bad("ids, teacher and loss_out must be aligned device memory of the context's device");
     if (!c.opt(stats_out, 4)) return c.bad("stats must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(c.a.n)) != MALIB_OK) return r;
     c.a.ids = loss->ids;
     c.a.teacher = loss->teacher;
     c.a.tdtype = loss->teacher_dtype;
@@ -235,7 +235,6 @@ int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_
     if (!c.dev(out->ids, 4) || !c.dev(out->top_logp, 4) || !c.opt(out->logp, 4) || !c.opt(out->entropy, 4) ||
         !c.opt(out->rank, 4))
         return c.bad("outputs must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
     ListArgs a{c.a};
     a.K = out->top;
     a.top_ids = out->ids;
@@ -263,7 +262,7 @@ int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const mal
         return c.bad("uniform, or sequence and step, must be aligned device memory of the context's device");
     if (!c.opt(token_out, 4) || !c.opt(logp_out, 4) || !c.opt(entropy_out, 4) || !c.opt(draw_logp_out, 4))
         return c.bad("outputs must be device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(0)) != MALIB_OK) return r;
     ListArgs a{c.a};
     a.K = draw->top_k;
     a.drawn = token_out;
@@ -296,7 +295,7 @@ int malib_learn_token_scores(malib_ctx* ctx, const malib_token_batch* batch, con
     if (!c.opt(scores->logp_grad, 4) || !c.opt(scores->entropy_grad, 4) || !c.opt(scores->ids, 4) ||
         (scores->ids && !c.dev(scores->top_grad, 4)))
         return c.bad("slopes and ids must be aligned device memory of the context's device");
-    if ((r = c.work()) != MALIB_OK) return r;
+    if ((r = c.work(0)) != MALIB_OK) return r;
     c.a.logp_grad = scores->logp_grad;
     c.a.entropy_grad = scores->entropy_grad;
     c.a.ids = scores->ids;

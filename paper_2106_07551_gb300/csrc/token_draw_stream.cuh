@@ -220,7 +220,7 @@ template <class T, class Own>
 cudaError_t launch_draw_stream_as(const ListArgs& a, int batches, int n_sm, cudaStream_t s) {
     const auto kernel = token_draw_stream_kernel<T, Own>;
     const size_t bytes = (size_t)kStreamStages * kStreamBatch * 16 + (size_t)kPlaces * batches * kSweepers * sizeof(float2);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kListMost);
     if (e != cudaSuccess) return e;
     int held = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&held, kernel, kStreamThreads, bytes);

@@ -42,6 +42,7 @@ struct ListShape {
 namespace {
 
 constexpr int kListCap = 2048;                       // most keys that are sorted, for any list
+constexpr int kListMost = 160 << 10;                 // dynamic shared memory: segments of 2^24 fp32 entries take 131 KB
 constexpr int kListPer = 8;                          // vectors of a thread in a batch
 constexpr int kWordVecs = 4, kWords = kListPer / kWordVecs;          // of a word of maxima; words of a batch
 constexpr int kListBins = 1024;                      // of the maxima's distances
@@ -368,9 +369,12 @@ __device__ __forceinline__ float warp_max(float v) {
     return r;
 }
 
-// A row's random number in [0, 1).
+// A row's random number in [0, 1); infinity for what draws the last entry.
 __device__ __forceinline__ float row_uniform(const ListArgs& a, int64_t row) {
-    if (a.uniform) return a.uniform[row];
+    if (a.uniform) {
+        const float u = a.uniform[row];
+        return u < 1.f ? u : INFINITY;
+    }
     return u24(draw((uint64_t)a.sequence[row], (uint32_t)a.step[row], a.agent, a.seed).x);
 }
 
@@ -424,6 +428,10 @@ __device__ __forceinline__ void draw_listed(const ListArgs& a, int64_t row, cons
 // The draw from a whole slice that holds the target (one warp): the segment, then its entries. `passed`
 // is the mass before the slice; sums of many are in 64 bits; where rounding leaves no entry, the
 // last one that has a mass is drawn.
+// An entry's mass is 0 below 2^-126 of the largest, but a sum of such entries, relative to a smaller
+// maximum, need not be: a segment (2,048 entries at most) counts from 2^-112 on and a slice (2^13
+// segments) from 2^-98, so that each has an entry that does.
+constexpr float kSegmentLeast = 0x1p-112f, kSliceLeast = 0x1p-98f;
 __device__ __forceinline__ float mass_at(const ListArgs& a, float m, float s, const RowStat& r) {
     return s * exp2_fast(fmaxf((m - r.m) * a.k, kXMin) + kExpBias);
 }
@@ -436,7 +444,9 @@ __device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const R
     double last_passed = passed;
     for (int s0 = 0; s0 < segments && at < 0; s0 += 32) {
         const float2 sg = s0 + lane < segments ? segment[s0 + lane] : make_float2(-INFINITY, 0.f);
-        const float w = sg.y > 0.f ? mass_at(a, sg.x, sg.y, r) : 0.f, cum = warp_scan(w, lane);
+        float w = sg.y > 0.f ? mass_at(a, sg.x, sg.y, r) : 0.f;
+        if (w < kSegmentLeast) w = 0.f;
+        const float cum = warp_scan(w, lane);
         const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && passed + (double)cum > target),
                        some = __ballot_sync(0xffffffffu, w > 0.f);
         if (some) {
@@ -746,7 +756,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         // (0: fewer than K groups have entries; all entries may be wanted)
         const uint32_t least = max(reach, 1u);
         if (tid == 0) own.reach = reach;
-        const float smallest = reach > 0 ? order_value(reach << 16) : -FLT_MAX;
+        // (a key below those of all values is a NaN's)
+        const float smallest = reach > 0 ? fmaxf(order_value(reach << 16), -FLT_MAX) : -FLT_MAX;
         // (whole warps: n_max is a multiple of the block's threads)
         const auto push = [&](bool hit, int id, uint32_t& to) {
             const unsigned hits = __ballot_sync(0xffffffffu, hit);
@@ -985,7 +996,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 double passed = 0.0;
                 int cta = 0;
                 if (C > 1) {
-                    const float w = lane < C ? mass_at(a, peer.x, peer.y, r) : 0.f, cum = warp_scan(w, lane);
+                    float w = lane < C ? mass_at(a, peer.x, peer.y, r) : 0.f;
+                    if (w < kSliceLeast) w = 0.f;
+                    const float cum = warp_scan(w, lane);
                     const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && (double)cum > target),
                                    some = __ballot_sync(0xffffffffu, w > 0.f);
                     cta = hit ? __ffs(hit) - 1 : 31 - __clz(some);
@@ -1068,8 +1081,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
 template <class T, int kOp, int kThreads, int kMode>
 cudaError_t launch_list_mode(const ListArgs& a, const ListShape& sh, size_t bytes, cudaStream_t s) {
     const auto kernel = token_list_kernel<T, kOp, kThreads, kMode>;
-    if (bytes > 32 << 10) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (bytes > 32 << 10) {                          // (one limit for all calls: threads may set it at once)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kListMost);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};

@@ -6,14 +6,21 @@ Each policy answers a prompt with a few tokens of a vocabulary; its network is a
 one in PyTorch (any network that gives a row of logits for every position would do). The
 library takes the logits from there:
 
-  * the rollout records each token's log-probability, one row per live answer and step
-    (``token_logprob``); a frozen reference policy's log-probabilities come from the same call;
+  * the rollout draws each token and records its log-probability, one row per live answer and
+    step (``token_sample``); a frozen reference policy's log-probabilities of them come from
+    ``token_logprob``;
+  * the hidden layer has dropout (``dropout``) whose mask is that of an answer and a position, so
+    that the learner's pass over the whole batch, and its backward pass, see the rollout's;
   * two members are trained by the clipped policy loss (``learn_token_ppo``), whose
     gradient is written over the logits and carried back by the network; the parameters
     move by ``adam_step``;
   * the first member is trained further on pairs of its answers, the better one of two
     to the same prompt being the chosen one (``learn_token_pref``);
-  * a new policy learns from the better member's largest logits (``learn_token_distill``).
+  * the first member's likeliest tokens are made likelier by a loss of the caller's own, whose
+    slopes at the log-probabilities and entropies the library carries back to the logits
+    (``learn_token_scores``);
+  * a new policy learns from the better member's most likely tokens (``token_top``,
+    ``learn_token_distill``).
 
 An answer ends after a random number of tokens; the rows after its end carry token -1
 and are left out by every call. A token earns 1 where it agrees with the prompt modulo 8,
@@ -29,11 +36,50 @@ sys.path.insert(0, str(pathlib.Path(__file__).resolve().parents[1]))
 from paper_2106_07551_gb300 import Context  # noqa: E402
 
 PROMPTS, LENGTH, HIDDEN, CLASSES = 16, 6, 64, 8
+DROP, SEED = 0.05, 2 ** 40 + 1
+
+
+class Dropout(torch.autograd.Function):
+    """``dropout`` of a layer: the backward pass is the same call on the gradient."""
+
+    @staticmethod
+    def forward(fn, x, ctx, sequence, step):
+        out = torch.empty_like(x)
+        ctx.dropout(x, out, DROP, SEED, 0, sequence, step)
+        fn.args = ctx, sequence, step
+        return out
+
+    @staticmethod
+    def backward(fn, grad):
+        ctx, sequence, step = fn.args
+        grad = grad.contiguous()
+        out = torch.empty_like(grad)
+        ctx.dropout(grad, out, DROP, SEED, 0, sequence, step)
+        return out, None, None, None
+
+
+class Scores(torch.autograd.Function):
+    """Log-probabilities of the tokens and entropies of rows of logits, for a loss of the caller's own."""
+
+    @staticmethod
+    def forward(fn, z, ctx, tokens):
+        logp, entropy = (torch.empty(len(tokens), device=z.device) for _ in range(2))
+        ctx.token_logprob(z, tokens, logp, entropy)
+        fn.save_for_backward(z, tokens)
+        fn.ctx = ctx
+        return logp, entropy
+
+    @staticmethod
+    def backward(fn, logp_grad, entropy_grad):
+        z, tokens = fn.saved_tensors
+        g = torch.empty_like(z)
+        fn.ctx.learn_token_scores(z, tokens, g, logp_grad.contiguous(), entropy_grad.contiguous())
+        return g, None, None
 
 
 class Policy:
-    """logits = relu(E[prompt] + F[previous token's class] + G[position]) W + b, its fp32
-    parameters in one flat tensor that ``adam_step`` moves."""
+    """logits = dropout(relu(E[prompt] + F[previous token's class] + G[position])) W + b, its fp32
+    parameters in one flat tensor that ``adam_step`` moves. Without sequences: no dropout."""
 
     def __init__(self, vocab, seed):
         gen = torch.Generator().manual_seed(seed)
@@ -49,7 +95,7 @@ class Policy:
         other.flat.data.copy_(self.flat.data)
         return other
 
-    def logits(self, prompt, previous, position):
+    def logits(self, prompt, previous, position, ctx=None, sequence=None):
         """[rows][vocab] in bf16, as the losses and the sampling read them."""
         at, parts = 0, []
         for s in self.shapes:
@@ -58,6 +104,8 @@ class Policy:
             at += n
         e, f, g, w, b = parts
         h = torch.relu(e[prompt] + f[previous % CLASSES] + g[position])
+        if sequence is not None:
+            h = Dropout.apply(h, ctx, sequence, position.int())
         return (h @ w + b).bfloat16()
 
     def update(self, ctx, lr):
@@ -67,26 +115,30 @@ class Policy:
 
 
 class Answers:
-    """Sampled answers, one row per (answer, position), answers in a row."""
+    """Sampled answers, one row per (answer, position), answers in a row. Every answer has a number of its
+    own, which its draws and its dropout masks hang on."""
+    made = 0
 
-    def __init__(self, ctx, policy, prompts, gen):
+    def __init__(self, ctx, policy, prompts, gen, drop=False):
         n, dev = prompts.numel(), prompts.device
+        number = torch.arange(Answers.made, Answers.made + n, device=dev)
+        Answers.made += n
         length = torch.randint(2, LENGTH + 1, (n,), generator=gen, device=dev)
         tokens = torch.full((n, LENGTH), -1, dtype=torch.int32, device=dev)
         logp = torch.zeros((n, LENGTH), device=dev)
         previous = torch.zeros(n, dtype=torch.long, device=dev)
         with torch.no_grad():
             for t in range(LENGTH):
-                z = policy.logits(prompts, previous, torch.full_like(previous, t))
-                chosen = torch.multinomial(torch.softmax(z.float(), -1), 1, generator=gen).view(-1)
-                live = t < length
-                token = torch.where(live, chosen, -1).int()
+                at = torch.full_like(previous, t)
+                z = policy.logits(prompts, previous, at, ctx, number if drop else None)
+                token = torch.where(t < length, 0, -1).int()       # answers that ended are left out
                 step = torch.empty(n, device=dev)
-                ctx.token_logprob(z, token, step)                  # one row per answer; those that ended are left out
+                ctx.token_sample(z, token, step, tokens=token, sequence=number, step=at.int(), seed=gen.initial_seed())
                 tokens[:, t], logp[:, t] = token, step
-                previous = chosen
+                previous = token.clamp(min=0).long()
         self.length, self.tokens, self.logp = length, tokens.view(-1), logp.view(-1)
         self.prompt = prompts.repeat_interleave(LENGTH)
+        self.number = number.repeat_interleave(LENGTH) if drop else None
         self.position = torch.arange(LENGTH, device=dev).repeat(n)
         self.previous = torch.cat([torch.zeros((n, 1), dtype=torch.long, device=dev), tokens[:, :-1].clamp(min=0).long()], 1).view(-1)
         self.live = self.tokens >= 0
@@ -112,13 +164,13 @@ def train_ppo(ctx, policy, reference, steps, answers_per_step, gen, lr=0.02):
     rewards = []
     for _ in range(steps):
         prompts = torch.randint(PROMPTS, (answers_per_step,), generator=gen, device="cuda")
-        a = Answers(ctx, policy, prompts, gen)
+        a = Answers(ctx, policy, prompts, gen, drop=True)
         rewards.append(a.mean_reward())
         advantage = a.reward - a.mean_reward()
         ref = reference_logp(ctx, reference, a)
         weight = torch.full_like(advantage, 1.0 / float(a.live.sum()))
         for _ in range(2):
-            z = policy.logits(*a.inputs())
+            z = policy.logits(*a.inputs(), ctx, a.number)
             g = z.detach().clone()                                 # autograd keeps z; the loss writes over the copy
             ctx.learn_token_ppo(g, a.tokens, a.logp, advantage, g, stats, weight=weight, ref_logp=ref, kl_coef=0.01,
                                 entropy_coef=0.001)
@@ -155,16 +207,35 @@ def train_pref(ctx, policy, steps, pairs, gen, lr=0.005):
     return losses, stats.tolist()
 
 
+def train_scores(ctx, policy, steps, rows, gen, lr=0.002):
+    """The policy's likeliest tokens are made likelier: the loss is the mean of -ln p of the first entry plus a
+    tenth of the entropy, differentiated by autograd down to the log-probabilities."""
+    losses = []
+    for _ in range(steps):
+        inputs = [torch.randint(k, (rows,), generator=gen, device="cuda") for k in (PROMPTS, CLASSES, LENGTH)]
+        z = policy.logits(*inputs)
+        first, logp = torch.empty((rows, 1), dtype=torch.int32, device="cuda"), torch.empty((rows, 1), device="cuda")
+        ctx.token_top(z.detach(), first, logp)
+        logp, entropy = Scores.apply(z, ctx, first.view(-1))
+        loss = (0.1 * entropy - logp).mean()
+        loss.backward()
+        policy.update(ctx, lr)
+        losses.append(loss.item())
+    ctx.sync()
+    return losses
+
+
 def distill(ctx, teacher, student, steps, rows, gen, top=32, lr=0.02):
-    """The student learns the teacher's `top` largest logits at random positions."""
+    """The student learns the teacher's `top` most likely tokens, by their ln p, at random positions."""
     stats, losses = torch.empty(3, device="cuda"), []
     for _ in range(steps):
         inputs = [torch.randint(k, (rows,), generator=gen, device="cuda") for k in (PROMPTS, CLASSES, LENGTH)]
         with torch.no_grad():
-            values, ids = teacher.logits(*inputs).topk(top, 1)
+            ids, values = torch.empty((rows, top), dtype=torch.int32, device="cuda"), torch.empty((rows, top), device="cuda")
+            ctx.token_top(teacher.logits(*inputs), ids, values)
         z = student.logits(*inputs)
         g = torch.empty_like(z)
-        ctx.learn_token_distill(z.detach(), ids.int(), values, g, stats)
+        ctx.learn_token_distill(z.detach(), ids, values, g, stats)
         z.backward(g)
         student.update(ctx, lr)
         losses.append(stats[1].item())
@@ -194,6 +265,9 @@ def main(argv=None):
         losses, stats = train_pref(ctx, members[0], args.steps, args.answers, gen)
         report["pref"] = {"losses": losses, "stats": stats}
         print(f"pairs of member 0: loss {losses[0]:.4f} -> {losses[-1]:.4f}, in order {stats[2]:.3f}")
+        losses = train_scores(ctx, members[0], 5, args.answers, gen)
+        report["scores"] = {"losses": losses}
+        print(f"likeliest tokens of member 0: loss {losses[0]:.3f} -> {losses[-1]:.3f}")
         best = max(range(2), key=lambda k: report["members"][k]["reward_last"])
         student = Policy(args.vocab, args.seed + 1)
         losses = distill(ctx, members[best], student, 2 * args.steps, 2 * args.answers, gen)

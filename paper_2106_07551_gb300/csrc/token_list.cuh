@@ -168,14 +168,14 @@ struct Above<__nv_bfloat16> {
     __device__ static uint32_t both(float z) { return __bfloat16_as_ushort(__float2bfloat16_rn(z)) * 0x10001u; }
     __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-        __nv_bfloat162 t;
-        *reinterpret_cast<uint32_t*>(&t) = thr;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __nv_bfloat162 v;
-            *reinterpret_cast<uint32_t*>(&v) = w[i];
-            n += __hge2_mask(v, t);
-        }
+        for (int i = 0; i < 4; ++i) n += mask(w[i], thr);
+    }
+    __device__ static uint32_t mask(uint32_t z, uint32_t thr) {      // -1 or 0 in each half
+        __nv_bfloat162 v, t;
+        *reinterpret_cast<uint32_t*>(&v) = z;
+        *reinterpret_cast<uint32_t*>(&t) = thr;
+        return __hge2_mask(v, t);
     }
     __device__ __forceinline__ uint32_t take() {
         const uint32_t r = count_masks(n);
@@ -192,14 +192,14 @@ struct Above<__half> {
     __device__ static uint32_t both(float z) { return __half_as_ushort(__float2half_rn(z)) * 0x10001u; }
     __device__ __forceinline__ void add(const uint4& q, uint32_t thr) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-        __half2 t;
-        *reinterpret_cast<uint32_t*>(&t) = thr;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __half2 v;
-            *reinterpret_cast<uint32_t*>(&v) = w[i];
-            n += __hge2_mask(v, t);
-        }
+        for (int i = 0; i < 4; ++i) n += mask(w[i], thr);
+    }
+    __device__ static uint32_t mask(uint32_t z, uint32_t thr) {
+        __half2 v, t;
+        *reinterpret_cast<uint32_t*>(&v) = z;
+        *reinterpret_cast<uint32_t*>(&t) = thr;
+        return __hge2_mask(v, t);
     }
     __device__ __forceinline__ uint32_t take() {
         const uint32_t r = count_masks(n);

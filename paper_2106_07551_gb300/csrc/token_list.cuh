@@ -211,7 +211,7 @@ struct Above<__half> {
 // Sorts the n keys at `key` (room for the next power of two, 512 at least), largest first; what comes back
 // has the first K in order. Few of them are counted: a key's place is how many are larger; several lanes
 // share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
-// buckets: what the sort of more keys by bins needs; null: they are sorted by exchanges.
+// buckets: what the sort of more keys by bins needs.
 struct Buckets {
     uint32_t top_key;                                // of the row's maximum, 32 bits
     uint32_t *bins, *warp_total;                     // [kListBins], [warps]
@@ -219,7 +219,7 @@ struct Buckets {
 };
 template <int kThreads, class Sync>
 __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, bool narrow, int tid,
-                                                     Sync sync, const Buckets* buckets = nullptr) {
+                                                     Sync sync, const Buckets& buckets) {
     if (n <= max(128, kThreads + kThreads / 2)) {
         const int lanes = n * 8 <= kThreads ? 8 : n * 4 <= kThreads ? 4 : n * 2 <= kThreads ? 2 : 1;
         const auto narrowed = [](uint64_t k) { return (uint32_t)(k >> 24) & 0xffff0000u | (uint32_t)k & 0xffffu; };
@@ -263,73 +263,71 @@ __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* so
         sync();
         return sorted;
     }
-    if (buckets) {
-        const uint32_t top_key = buckets->top_key;
-        uint32_t *bins = buckets->bins, *warp_total = buckets->warp_total;
-        uint16_t* order = buckets->order;
-        // More of them, by the distance of a key's logit from the row's maximum, in 1,024 equal steps of the
-        // logits' bits: a key comes after those of smaller distances, and is counted among its bin's.
-        // Bins of many keys are left to the sort below.
-        constexpr int kBins = kListBins / kThreads;
-        const int lane = tid & 31, warp = tid >> 5;
-        uint32_t least = ~0u;
-        for (int i = tid; i < n; i += kThreads) least = min(least, (uint32_t)(key[i] >> 24));
-        least = __reduce_min_sync(0xffffffffu, least);
-        if (lane == 0) warp_total[warp] = least;
-        sync();
+    const uint32_t top_key = buckets.top_key;
+    uint32_t *bins = buckets.bins, *warp_total = buckets.warp_total;
+    uint16_t* order = buckets.order;
+    // More of them, by the distance of a key's logit from the row's maximum, in 1,024 equal steps of the
+    // logits' bits: a key comes after those of smaller distances, and is counted among its bin's.
+    // Bins of many keys are left to the sort below.
+    constexpr int kBins = kListBins / kThreads;
+    const int lane = tid & 31, warp = tid >> 5;
+    uint32_t least = ~0u;
+    for (int i = tid; i < n; i += kThreads) least = min(least, (uint32_t)(key[i] >> 24));
+    least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) warp_total[warp] = least;
+    sync();
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) least = min(least, warp_total[w]);
-        const int shift = max(0, 22 - __clz(top_key - least));       // distances below 2^(10 + shift)
-        const auto bin_of = [&](uint64_t k) { return (top_key - (uint32_t)(k >> 24)) >> shift; };
-        for (int i = tid; i < kListBins; i += kThreads) bins[i] = 0;
-        sync();
-        for (int i = tid; i < n; i += kThreads) atomicAdd(bins + bin_of(key[i]), 1u);
-        sync();
-        uint32_t sum = 0, most = 0, size[kBins];
+    for (int w = 0; w < kThreads / 32; ++w) least = min(least, warp_total[w]);
+    const int shift = max(0, 22 - __clz(top_key - least));       // distances below 2^(10 + shift)
+    const auto bin_of = [&](uint64_t k) { return (top_key - (uint32_t)(k >> 24)) >> shift; };
+    for (int i = tid; i < kListBins; i += kThreads) bins[i] = 0;
+    sync();
+    for (int i = tid; i < n; i += kThreads) atomicAdd(bins + bin_of(key[i]), 1u);
+    sync();
+    uint32_t sum = 0, most = 0, size[kBins];
+#pragma unroll
+    for (int i = 0; i < kBins; ++i) {
+        size[i] = bins[kBins * tid + i];
+        sum += size[i];
+        most = max(most, size[i]);
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += q;
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) warp_total[warp] = upto | (most > 256 ? 1u << 31 : 0u);
+    sync();
+    bool many = false;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        const uint32_t q = warp_total[w];
+        many |= q >> 31;
+        if (w < warp) upto += q & 0x7fffffffu;
+    }
+    if (!many) {
+        // a bin's first place, then, when its keys have taken theirs, the next bin's
+        upto -= sum;
 #pragma unroll
         for (int i = 0; i < kBins; ++i) {
-            size[i] = bins[kBins * tid + i];
-            sum += size[i];
-            most = max(most, size[i]);
+            bins[kBins * tid + i] = upto;
+            upto += size[i];
         }
-        uint32_t upto = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += q;
-        }
-        most = __reduce_max_sync(0xffffffffu, most);
-        if (lane == 31) warp_total[warp] = upto | (most > 256 ? 1u << 31 : 0u);
         sync();
-        bool many = false;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            const uint32_t q = warp_total[w];
-            many |= q >> 31;
-            if (w < warp) upto += q & 0x7fffffffu;
+        for (int i = tid; i < n; i += kThreads) order[atomicAdd(bins + bin_of(key[i]), 1u)] = (uint16_t)i;
+        sync();
+        for (int i = tid; i < n; i += kThreads) {
+            const uint64_t own = key[i];
+            const uint32_t bin = bin_of(own), first = bin > 0 ? bins[bin - 1] : 0u, end = bins[bin];
+            int place = (int)first;
+            if (place >= K) continue;
+            for (uint32_t o = first; o < end; ++o) place += key[order[o]] > own;
+            if (place < K) sorted[place] = own;
         }
-        if (!many) {
-            // a bin's first place, then, when its keys have taken theirs, the next bin's
-            upto -= sum;
-#pragma unroll
-            for (int i = 0; i < kBins; ++i) {
-                bins[kBins * tid + i] = upto;
-                upto += size[i];
-            }
-            sync();
-            for (int i = tid; i < n; i += kThreads) order[atomicAdd(bins + bin_of(key[i]), 1u)] = (uint16_t)i;
-            sync();
-            for (int i = tid; i < n; i += kThreads) {
-                const uint64_t own = key[i];
-                const uint32_t bin = bin_of(own), first = bin > 0 ? bins[bin - 1] : 0u, end = bins[bin];
-                int place = (int)first;
-                if (place >= K) continue;
-                for (uint32_t o = first; o < end; ++o) place += key[order[o]] > own;
-                if (place < K) sorted[place] = own;
-            }
-            sync();
-            return sorted;
-        }
+        sync();
+        return sorted;
     }
     int P = 256;
     while (P < n) P *= 2;
@@ -667,7 +665,7 @@ struct OwnStat<kLong> {
 };
 
 template <class T, int kOp, int kThreads, int kMode>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 128 ? 7 : 24) token_list_kernel(ListArgs a, ListShape sh) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 7) token_list_kernel(ListArgs a, ListShape sh) {
     using Own = typename OwnStat<kMode>::Type;
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;
@@ -737,12 +735,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 const uint32_t q = __shfl_up_sync(0xffffffffu, upto, o);
                 if (lane >= o) upto += q;
             }
-            if (kWarps > 1) {
-                if (lane == 31) warp_total[warp] = upto;
-                __syncthreads();
+            if (lane == 31) warp_total[warp] = upto;
+            __syncthreads();
 #pragma unroll
-                for (int w = 0; w < kWarps - 1; ++w) upto += w < warp ? warp_total[w] : 0u;
-            }
+            for (int w = 0; w < kWarps - 1; ++w) upto += w < warp ? warp_total[w] : 0u;
             if (upto >= (uint32_t)sh.slice_K && upto - sum < (uint32_t)sh.slice_K) {
                 uint32_t cum = upto - sum, bin = kBins * tid;
                 while ((cum += own.hist[bin]) < (uint32_t)sh.slice_K) ++bin;
@@ -1040,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 const auto sort = [&] {
                     const Buckets b{order_key(r.m), own.hist, warp_total, order};
                     return sort_keys<kThreads>(keys, sorted, n, a.K, std::is_same<T, __nv_bfloat16>::value && a.V <= 65536, tid,
-                                               [] { __syncthreads(); }, kThreads >= 128 ? &b : nullptr);
+                                               [] { __syncthreads(); }, b);
                 };
                 const uint64_t* list = sort();
                 // Slices that list a share of K each: all entries from `reach` on are there. Where the first K go
@@ -1131,7 +1127,7 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
         sh.cap = sh.group_log < 0 || most > 256 ? kListCap : most > 64 ? 1024 : 512;
         sh.room = a.K <= 128 ? 128 : a.K <= 256 ? 256 : 1024;
         sh.maxima = (int)((maxima + 15) / 16 * 16);
-        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + sh.maxima + (kThreads >= 128 ? sh.cap * sizeof(uint16_t) : 0);
+        bytes = (size_t)(sh.cap + sh.room) * sizeof(uint64_t) + sh.maxima + sh.cap * sizeof(uint16_t);
     }
     if constexpr (kThreads > 128) {
         if (mode == kLong) return launch_list_mode<T, kOp, kThreads, kLong>(a, sh, bytes, s);

@@ -18,7 +18,7 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
         if (a.V <= 32) return launch_list_tiny<T, kOp, 32>(a, n_sm, s);
     }
     const int64_t nv = (a.V + 2 * (int64_t)Elt<T>::W - 2) / Elt<T>::W;               // most vectors of a row
-    if (nv <= 256 && (kOp == kListDrawAll || a.K <= kShortTop)) return launch_list_short<T, kOp>(a, nv, n_sm, s);
+    if (nv <= 256) return launch_list_short<T, kOp>(a, nv, n_sm, s);
     ListShape sh{};
     sh.cluster = 1;
     sh.group_log = -1;
@@ -38,9 +38,7 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     // a quarter more, which has them all unless a slice has more than its share.
     sh.slice = (int)((nv + sh.cluster - 1) / sh.cluster);
     sh.slice_K = sh.cluster * a.K <= kListCap / 2 ? a.K : a.K / sh.cluster * 5 / 4 + 32;
-    if constexpr (kOp != kListDrawAll) {
-        if (sh.slice <= 256) return launch_list_threads<T, kOp, 32>(a, sh, s);
-    } else {
+    if constexpr (kOp == kListDrawAll) {
         if (sh.cluster == 1 && nv <= kStreamMostBatches * kStreamBatch) return launch_draw_stream<T>(a, nv, n_sm, s);
     }
     if (sh.cluster == 1 && sh.slice <= kManyBatches * 128 * kListPer) return launch_list_threads<T, kOp, 128>(a, sh, s);

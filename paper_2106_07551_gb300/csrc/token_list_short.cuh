@@ -1,7 +1,7 @@
 // Lists and draws of rows of up to 4 KB: a warp a row, its entries in registers.
-// Lists of up to kShortTop entries sort those from a bound on, which has at least K from it on and few more:
-// bisected among the values between the smallest of the lanes' maxima, from which on there are 32 entries
-// at least, and the row's maximum.
+// Lists sort the entries from a bound on, which has at least K from it on and few more: bisected among the
+// values between the smallest of the lanes' maxima, from which on there are 32 entries at least, and the
+// row's maximum.
 #pragma once
 
 #include "token_list.cuh"
@@ -10,7 +10,8 @@ namespace malib {
 
 namespace {
 
-constexpr int kRowWarps = 4, kShortTop = 64, kShortCap = 128;        // rows of a CTA; entries of a list; keys that are sorted
+constexpr int kRowWarps = 4;                         // rows of a CTA
+constexpr int kShortTop = 128;                       // entries of lists that are sorted in 8 registers or fewer
 
 // Larger for larger entries of a type, the same for -0 and 0; the entry of a key; the key of the lowest finite one.
 // With the index they are sorted as Sorted, largest first.
@@ -51,9 +52,12 @@ struct ShortKey<__half> : HalfKey<__half> {
     }
 };
 
+// kLong: lists of more than kShortTop entries.
+template <int kOp, bool kLong>
 struct ShortRow {
-    uint16_t index[kShortCap];
-    uint64_t list[kShortTop];                        // for draws
+    static constexpr int kCap = kLong ? kTokenMaxTop : 2 * kShortTop;                // keys that are sorted
+    uint16_t index[kCap];
+    uint64_t list[kOp != kListDraw ? 1 : kLong ? kTokenMaxTop : kShortTop];
 };
 
 template <class T, int N>
@@ -99,8 +103,8 @@ __device__ __forceinline__ int hit_index(int bit, int more) {
     const int w = (bit & 15) + more;
     return (w >> 2) * 256 + 2 * (w & 3) + (bit >> 4);
 }
-template <class T>
-__device__ __forceinline__ uint32_t push_hits(ShortRow& s, Hits hits, uint32_t base, int first, int lane) {
+template <class T, class Row>
+__device__ __forceinline__ uint32_t push_hits(Row& s, Hits hits, uint32_t base, int first, int lane) {
     const uint32_t own = __popc(hits.a) + __popc(hits.b);
     uint32_t upto = own;
 #pragma unroll
@@ -110,39 +114,44 @@ __device__ __forceinline__ uint32_t push_hits(ShortRow& s, Hits hits, uint32_t b
     }
     uint32_t to = base + upto - own;
     for (; hits.a; hits.a &= hits.a - 1, ++to)
-        if (to < (uint32_t)kShortCap) s.index[to] = (uint16_t)(first + hit_index<T>(__ffs(hits.a) - 1, 0));
+        if (to < (uint32_t)Row::kCap) s.index[to] = (uint16_t)(first + hit_index<T>(__ffs(hits.a) - 1, 0));
     for (; hits.b; hits.b &= hits.b - 1, ++to)
-        if (to < (uint32_t)kShortCap) s.index[to] = (uint16_t)(first + hit_index<T>(__ffs(hits.b) - 1, 16));
+        if (to < (uint32_t)Row::kCap) s.index[to] = (uint16_t)(first + hit_index<T>(__ffs(hits.b) - 1, 16));
     return base + __shfl_sync(0xffffffffu, upto, 31);
 }
 
 // Sorts 32 R keys of a warp, largest first; key i is in register i / 32 of lane i % 32.
 template <int R, class K>
 __device__ __forceinline__ void sort_warp(K (&key)[R], int lane) {
-#pragma unroll
+#pragma unroll(R <= 4 ? 7 : 1)
     for (int size = 2; size <= 32 * R; size *= 2) {
 #pragma unroll
-        for (int gap = size / 2; gap > 0; gap /= 2) {
+        for (int gap = 16 * R; gap >= 32; gap /= 2) {
+            if (gap >= size) continue;
 #pragma unroll
             for (int q = 0; q < R; ++q) {
-                if (gap < 32) {
-                    const K other = __shfl_xor_sync(0xffffffffu, key[q], gap);
-                    const bool falls = ((32 * q + lane) & size) == 0, first = (lane & gap) == 0;
-                    key[q] = falls == first ? max(key[q], other) : min(key[q], other);
-                } else if ((q & gap / 32) == 0) {
-                    const K x = key[q], y = key[q + gap / 32];
-                    const bool falls = (32 * q & size) == 0;
-                    key[q] = falls ? max(x, y) : min(x, y);
-                    key[q + gap / 32] = falls ? min(x, y) : max(x, y);
-                }
+                if ((q & gap / 32) != 0) continue;
+                const K x = key[q], y = key[q + gap / 32];
+                const bool falls = (32 * q & size) == 0;
+                key[q] = falls ? max(x, y) : min(x, y);
+                key[q + gap / 32] = falls ? min(x, y) : max(x, y);
+            }
+        }
+#pragma unroll(R <= 4 ? 5 : 1)
+        for (int gap = min(16, size / 2); gap > 0; gap /= 2) {
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const K other = __shfl_xor_sync(0xffffffffu, key[q], gap);
+                const bool falls = ((32 * q + lane) & size) == 0, first = (lane & gap) == 0;
+                key[q] = falls == first ? max(key[q], other) : min(key[q], other);
             }
         }
     }
 }
 
 // f(place, key) for the first K of the n entries whose indexes are in s.index.
-template <class T, int R, class F>
-__device__ __forceinline__ void each_listed(const ShortRow& s, const T* z, int n, int K, int lane, F f) {
+template <class T, int R, class Row, class F>
+__device__ __forceinline__ void each_listed(const Row& s, const T* z, int n, int K, int lane, F f) {
     using Key = ShortKey<T>;
     typename Key::Sorted key[R];
 #pragma unroll
@@ -158,8 +167,8 @@ __device__ __forceinline__ void each_listed(const ShortRow& s, const T* z, int n
 
 // The first K entries of a row z (a warp's): f(place, key) of each; how many there are. Its entries have no NaN
 // and no +infinity, and m, the largest, is finite. x: a lane's vectors, vmax: the largest of each.
-template <class T, int N, class F>
-__device__ __forceinline__ int list_row(ShortRow& s, const T* z, const uint4 (&x)[N], const float (&vmax)[N], float m, int h, int K,
+template <class T, int N, class Row, class F>
+__device__ __forceinline__ int list_row(Row& s, const T* z, const uint4 (&x)[N], const float (&vmax)[N], float m, int h, int K,
                                         int lane, F f) {
     using Key = ShortKey<T>;
     constexpr int W = Elt<T>::W;
@@ -173,9 +182,10 @@ __device__ __forceinline__ int list_row(ShortRow& s, const T* z, const uint4 (&x
     }
     uint32_t lo = Key::kLowest, hi = Key::of(m) + 1;
     const float from = warp_min(K <= 32 ? most : second);
-    if (from > -INFINITY) lo = Key::of(from);
+    if (K <= 64 && from > -INFINITY) lo = Key::of(from);
     uint32_t n = count_from<T>(x, Key::value(lo));
-    const uint32_t enough = K <= 24 ? 32 : K <= 52 ? 64 : kShortCap;  // what is sorted at a time
+    // what is sorted in 1, 2, 4, .. registers
+    const uint32_t enough = K <= 24 ? 32 : K <= 52 ? 64 : K <= 104 ? 128 : K <= 232 ? 256 : K <= 480 ? 512 : Row::kCap;
     while (n > enough && hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2, c = count_from<T>(x, Key::value(mid));
         if (c >= (uint32_t)K) {
@@ -186,7 +196,7 @@ __device__ __forceinline__ int list_row(ShortRow& s, const T* z, const uint4 (&x
         }
     }
     const int first = lane * W - h;
-    if (n <= (uint32_t)kShortCap) {
+    if (n <= (uint32_t)Row::kCap) {
         push_hits<T>(s, hits_from<T>(x, Key::value(lo)), 0, first, lane);
     } else {
         // many equal ones at the bound (hi is lo's next, and fewer than K are from it on): the first of them
@@ -205,31 +215,40 @@ __device__ __forceinline__ int list_row(ShortRow& s, const T* z, const uint4 (&x
             }
             uint32_t to = base + upto - __popc(equal);
             for (; equal; equal &= equal - 1, ++to)
-                if (to < (uint32_t)kShortCap) s.index[to] = (uint16_t)(first + u * 32 * W + __ffs(equal) - 1);
+                if (to < (uint32_t)Row::kCap) s.index[to] = (uint16_t)(first + u * 32 * W + __ffs(equal) - 1);
             base += __shfl_sync(0xffffffffu, upto, 31);
         }
-        n = kShortCap;
+        n = Row::kCap;
     }
     __syncwarp();
-    if (n <= 32) each_listed<T, 1>(s, z, (int)n, K, lane, f);
-    else if (n <= 64) each_listed<T, 2>(s, z, (int)n, K, lane, f);
-    else each_listed<T, 4>(s, z, (int)n, K, lane, f);
+    if constexpr (Row::kCap <= 256) {
+        if (n <= 32) each_listed<T, 1>(s, z, (int)n, K, lane, f);
+        else if (n <= 64) each_listed<T, 2>(s, z, (int)n, K, lane, f);
+        else if (n <= 128) each_listed<T, 4>(s, z, (int)n, K, lane, f);
+        else each_listed<T, 8>(s, z, (int)n, K, lane, f);
+    } else {
+        if (n <= 256) each_listed<T, 8>(s, z, (int)n, K, lane, f);
+        else if (n <= 512) each_listed<T, 16>(s, z, (int)n, K, lane, f);
+        else each_listed<T, 32>(s, z, (int)n, K, lane, f);
+    }
     __syncwarp();
     return min((int)n, K);
 }
 
 // CTAs an SM: as many as registers last for.
-template <class T, int kOp, int N>
+template <class T, int kOp, int N, bool kLong>
 constexpr int short_ctas() {
-    return sizeof(T) == 4 && kOp == kListTop ? (N == 1 ? 11 : N == 2 ? 9 : N == 4 ? 7 : 5) : N <= 2 ? 12 : N == 4 ? 9 : 7;
+    if (kLong) return sizeof(T) == 4 ? 3 : 4;
+    return sizeof(T) == 4 && kOp != kListDrawAll ? (N == 1 ? 9 : N == 2 ? 8 : N == 4 ? 6 : 4) : N <= 2 ? 12 : N == 4 ? 9 : 7;
 }
 
-template <class T, int kOp, int N>
-__global__ void __launch_bounds__(32 * kRowWarps, short_ctas<T, kOp, N>()) token_list_short_kernel(ListArgs a) {
+template <class T, int kOp, int N, bool kLong>
+__global__ void __launch_bounds__(32 * kRowWarps, short_ctas<T, kOp, N, kLong>()) token_list_short_kernel(ListArgs a) {
     constexpr int W = Elt<T>::W;
-    __shared__ ShortRow shared[kOp == kListDrawAll ? 1 : kRowWarps];
+    using Row = ShortRow<kOp, kLong>;
+    __shared__ Row shared[kOp == kListDrawAll ? 1 : kRowWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    ShortRow& s = shared[kOp == kListDrawAll ? 0 : warp];
+    Row& s = shared[kOp == kListDrawAll ? 0 : warp];
     wait_for_previous();
     let_next_start();
     const int64_t step = (int64_t)gridDim.x * kRowWarps;
@@ -388,18 +407,22 @@ __global__ void __launch_bounds__(32 * kRowWarps, short_ctas<T, kOp, N>()) token
     }
 }
 
-template <class T, int kOp, int N>
+template <class T, int kOp, int N, bool kLong>
 cudaError_t launch_list_short_as(const ListArgs& a, int n_sm, cudaStream_t s) {
-    const int64_t blocks = (a.n + kRowWarps - 1) / kRowWarps, most = short_ctas<T, kOp, N>() * (int64_t)n_sm;
-    return launch_after(token_list_short_kernel<T, kOp, N>, (unsigned)(blocks < most ? blocks : most), 32 * kRowWarps, 0, s, a);
+    const int64_t blocks = (a.n + kRowWarps - 1) / kRowWarps, most = short_ctas<T, kOp, N, kLong>() * (int64_t)n_sm;
+    return launch_after(token_list_short_kernel<T, kOp, N, kLong>, (unsigned)(blocks < most ? blocks : most), 32 * kRowWarps, 0, s, a);
 }
 // nv: most vectors of a row, 256 at most.
 template <class T, int kOp>
 cudaError_t launch_list_short(const ListArgs& a, int64_t nv, int n_sm, cudaStream_t s) {
-    if (nv <= 32) return launch_list_short_as<T, kOp, 1>(a, n_sm, s);
-    if (nv <= 64) return launch_list_short_as<T, kOp, 2>(a, n_sm, s);
-    if (nv <= 128) return launch_list_short_as<T, kOp, 4>(a, n_sm, s);
-    return launch_list_short_as<T, kOp, 8>(a, n_sm, s);
+    if constexpr (kOp != kListDrawAll) {
+        if (a.K > kShortTop && nv > 64) return launch_list_short_as<T, kOp, 8, true>(a, n_sm, s);
+        if (a.K > kShortTop) return launch_list_short_as<T, kOp, 2, true>(a, n_sm, s);
+    }
+    if (nv <= 32) return launch_list_short_as<T, kOp, 1, false>(a, n_sm, s);
+    if (nv <= 64) return launch_list_short_as<T, kOp, 2, false>(a, n_sm, s);
+    if (nv <= 128) return launch_list_short_as<T, kOp, 4, false>(a, n_sm, s);
+    return launch_list_short_as<T, kOp, 8, false>(a, n_sm, s);
 }
 
 }  // namespace

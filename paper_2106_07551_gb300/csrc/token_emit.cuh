@@ -22,13 +22,13 @@ __device__ __forceinline__ float as_float(__half z) { return __half2float(z); }
 // A row of the policy loss whose slope at ln p is infinite (a KL term or a ratio past fp32, a
 // masked token with a KL term): its entries are infinite, and 0 times infinity or the difference
 // of two infinities would make NaN of some. One entry of such a row, or of any other: 0 where p is
-// 0, the slope's sign at the token.
+// 0, the slope's sign at the token; NaN in a row whose slopes are.
 __device__ __forceinline__ bool is_steep(const RowGrad& c) { return fabsf(c.c0) == INFINITY; }
 template <class T>
 __device__ __forceinline__ float emit_steep(T z, const RowGrad& c, float k, bool token) {
     const float x = x_of(as_float(z), c.m, k), e = exp2_fast(x);
     const float v = e == 0.f && is_steep(c) ? 0.f : e * fmaf(c.c1, fmaxf(x, kXMin), c.c0);
-    return !token ? v : fabsf(c.at) == INFINITY ? c.at : v + c.at;
+    return !token ? v : fabsf(c.at) == INFINITY && c.c0 == c.c0 ? c.at : v + c.at;
 }
 // Sixteen bytes of such a row, the token entry `at` of them.
 template <class T>

@@ -667,12 +667,14 @@ int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_
  * Kept are all unmasked entries (top_k 0), or of the first top_k those before which less than
  * top_p of the top_k's probability lies (at least one). With a random number u in [0, 1) the
  * token is the first kept entry, in the order of the index (top_k 0) or of the list, whose running
- * probability exceeds u times the kept one; of entries whose probability is below 2^-98 of the
+ * probability exceeds u times the kept one; of entries whose probability is below 2^-112 of the
  * largest some, below 2^-126 all, are not drawn. u >= 1, or NaN, draws the last that can be.
  * u is uniform[row], or without it the top 24 bits of the first word of Philox4x32-10 at counter
- * (sequence lo32, sequence hi32, step, agent) under `seed` over 2^24, as in malib_rollout: a
- * sequence's draws do not depend on the batch that it is in. agent < 2^31 (the counters of
- * malib_dropout are from there on). 0 <= top_k <= 1024; 0 < top_p <= 1, 1 without top_k.
+ * (sequence lo32, sequence hi32, step, agent) under `seed` over 2^24, as in malib_rollout. The token
+ * is a function of the row's logits and u: a sequence's draws do not depend on the batch that it is in,
+ * nor on where its rows lie. Masses are summed in fp32: u within some 1e-6 of the border of two entries may
+ * draw either. And u has 2^24 values: an entry whose probability is below 2^-24 may have none of them, its
+ * share then being its neighbours'. agent < 2^31 (the counters of malib_dropout are from there on). 0 <= top_k <= 1024; 0 < top_p <= 1, 1 without top_k.
  * batch->tokens: rows with a negative one are left out (their answer has ended); other values are
  * not looked at. token_out may be batch->tokens. Outputs [n_rows], each may be NULL: the token; its
  * ln p and H by the whole row; draw_logp, ln of the probability that it was drawn with

@@ -16,9 +16,14 @@
 // few groups), the bound is found from all keys: a histogram of their top 8 bits says in which bin
 // the K-th lies, one of the next 8 bits looks into that bin, and so on.
 //
-// The draw from the whole row takes the entries in the order of their index: sums of consecutive
-// entries are kept from the statistics' pass, the one that holds u times the whole is found among
+// The draw from the whole row takes the entries in the order of their index: sums of segments of 256
+// vectors are kept from the statistics' pass, the one that holds u times the whole is found among
 // them, and its entries alone are read again. The draw from a list takes them in the list's order.
+// A row's token is the same whatever its batch: neither the CTAs that share the row nor its place in memory
+// change a sum that decides it. Segments and their vectors are counted from the row's first entry (a vector
+// that the memory does not have so is put together from two), a segment's sum is relative to its own maximum,
+// and the segments are added in their order by one warp. (Segments of the memory's vectors, relative to the
+// maximum so far, gave 14 of 3,000 draws from 131,072 bf16 entries another token by a cluster than by the stream.)
 //
 // Rows of more than 4 KB (shorter ones: token_list_short.cuh) are a block's of 64, 128 or 256 threads each, or a
 // cluster's. The floor is reading the row once; what bounds it is the instructions of the sums (some six
@@ -35,6 +40,7 @@
 #include "token_common.cuh"
 #include "token_peer.cuh"
 #include "token_rollout.h"
+#include "token_shift.cuh"
 
 namespace malib {
 
@@ -117,6 +123,58 @@ __device__ __forceinline__ float entry_of(const uint4& q, int i) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     return Elt<T>::get(Elt<T>::word(w, i));
 }
+// A row's vectors by the index of their entries, wherever it lies in memory: v holds entries v W .. v W + W - 1 and
+// is put together from the memory's vectors v and v + 1 where the row starts inside one.
+template <int kWord>
+struct Word {
+    static constexpr int at = kWord;
+};
+// f(Word<the word of a vector that the row's entries start in>).
+template <class F>
+__device__ __forceinline__ void by_word(int by, F f) {
+    if (by < 8) {                                    // (a switch would look its way up in memory)
+        if (by < 4) f(Word<0>{});
+        else f(Word<1>{});
+    } else {
+        if (by < 12) f(Word<2>{});
+        else f(Word<3>{});
+    }
+}
+// A warp's vectors of the memory, lane + 32 u of them in lane `lane`, to as many of the row that starts `by` bytes
+// inside a vector. after: in lane 0, the vector behind the last.
+template <class T, int N>
+__device__ __forceinline__ void realign(uint4 (&x)[N], const uint4& after, int by, int lane) {
+    const uint32_t bits = 8u * (by & 3);
+    by_word(by, [&](auto word) {
+        constexpr int k = decltype(word)::at;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const uint4 next = u + 1 < N ? x[u + 1 < N ? u + 1 : u] : after;
+            const uint32_t mine[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, his[4] = {next.x, next.y, next.z, next.w};
+            uint32_t b[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < (sizeof(T) == 4 ? k : k + 1); ++i)
+                b[i] = __shfl_sync(0xffffffffu, lane == 0 ? his[i] : mine[i], (lane + 1) & 31);
+            x[u] = shifted<k>(x[u], make_uint4(b[0], b[1], b[2], b[3]), bits);
+        }
+    });
+}
+template <class T>
+struct IndexView {
+    static constexpr int W = Elt<T>::W;
+    const T* z;
+    int V;
+    __device__ __forceinline__ int vectors() const { return (V + W - 1) / W; }
+    __device__ __forceinline__ uint4 vec(int v) const {
+        const int by = (int)((uintptr_t)z & 15u), h = by / (int)sizeof(T), j = v * W;
+        if (by == 0 ? j + W > V : j < h || j - h + 2 * W > V) return load_part(z, j, V);
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(z + j) - by);
+        if (by == 0) return *p;
+        uint4 r;
+        by_word(by, [&](auto word) { r = shifted<decltype(word)::at>(p[0], p[1], 8u * (by & 3)); });
+        return r;
+    }
+};
 // f(j, z) for the unmasked entries of vectors [v0, v1), by n threads.
 template <class T, class F>
 __device__ __forceinline__ void each_entry(const RowView<T>& r, int v0, int v1, int tid, int n, F f) {
@@ -411,7 +469,20 @@ __device__ __forceinline__ float warp_max(float v) {
     return r;
 }
 
-// A row's random number in [0, 1); infinity for what draws the last entry.
+// A row's random number in [0, 1), infinity for what draws the last entry: what is read for it, and the number.
+struct RowUniform {
+    float u;
+    uint32_t step;
+    uint64_t sequence;
+};
+__device__ __forceinline__ RowUniform load_uniform(const ListArgs& a, int64_t row) {
+    if (a.uniform) return RowUniform{a.uniform[row], 0u, 0ull};
+    return RowUniform{0.f, (uint32_t)a.step[row], (uint64_t)a.sequence[row]};
+}
+__device__ __forceinline__ float uniform_of(const ListArgs& a, const RowUniform& r) {
+    if (a.uniform) return r.u < 1.f ? r.u : INFINITY;
+    return u24(draw(r.sequence, r.step, a.agent, a.seed).x);
+}
 __device__ __forceinline__ float row_uniform(const ListArgs& a, int64_t row) {
     if (a.uniform) {
         const float u = a.uniform[row];
@@ -467,51 +538,87 @@ __device__ __forceinline__ void draw_listed(const ListArgs& a, int64_t row, cons
     }
 }
 
-// The draw from a whole slice that holds the target (one warp): the segment, then its entries. `passed`
-// is the mass before the slice; sums of many are in 64 bits; where rounding leaves no entry, the
-// last one that has a mass is drawn.
+// The draw from a whole row (one warp): the segment that holds the target, then its entries. A lane has a segment,
+// or of more than 32 an odd number of them that follow one another; of more than 256 the lanes' masses are added
+// in 64 bits. Where rounding leaves no entry, the last one that has a mass is drawn. (No product here may join an
+// addition: the compiler would be free to round one caller's differently. Loops, not unrolled ones: a warp goes
+// through this once a row, and what it takes is mostly the instructions' way to it.)
 // An entry's mass is 0 below 2^-126 of the largest, but a sum of such entries, relative to a smaller
-// maximum, need not be: a segment (2,048 entries at most) counts from 2^-112 on and a slice (2^13
-// segments) from 2^-98, so that each has an entry that does.
-constexpr float kSegmentLeast = 0x1p-112f, kSliceLeast = 0x1p-98f;
-__device__ __forceinline__ float mass_at(const ListArgs& a, float m, float s, const RowStat& r) {
-    return s * exp2_fast(fmaxf((m - r.m) * a.k, kXMin) + kExpBias);
+// maximum, need not be: a segment (2,048 entries at most) counts from 2^-112 on, so that it has an entry that does.
+constexpr int kSegmentVecs = 32 * kListPer;
+constexpr float kSegmentLeast = 0x1p-112f;
+__device__ __forceinline__ double warp_scan(double v, int lane) {
+#pragma unroll 1
+    for (int o = 1; o < 32; o *= 2) {
+        const double b = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += b;
+    }
+    return v;
 }
-template <class T>
-__device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const RowStat& r, const RowView<T>& view, int v_lo,
-                                         int v_hi, const float2* segment, int segments, double target, double passed,
-                                         int lane) {
-    constexpr int W = Elt<T>::W, kWarpVecs = 32 * kListPer;
-    int at = -1, last = 0;
-    double last_passed = passed;
-    for (int s0 = 0; s0 < segments && at < 0; s0 += 32) {
-        const float2 sg = s0 + lane < segments ? segment[s0 + lane] : make_float2(-INFINITY, 0.f);
-        float w = sg.y > 0.f ? mass_at(a, sg.x, sg.y, r) : 0.f;
-        if (w < kSegmentLeast) w = 0.f;
-        const float cum = warp_scan(w, lane);
-        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && passed + (double)cum > target),
-                       some = __ballot_sync(0xffffffffu, w > 0.f);
-        if (some) {
-            const int k = 31 - __clz(some);
-            last = s0 + k;
-            last_passed = passed + (double)__shfl_sync(0xffffffffu, cum - w, k);
-        }
-        if (hit) {
-            const int k = __ffs(hit) - 1;
-            at = s0 + k;
-            passed += (double)__shfl_sync(0xffffffffu, cum - w, k);
-        } else {
-            passed += (double)__shfl_sync(0xffffffffu, cum, 31);
-        }
+// The first of the lanes that passes the target, or the last that has a mass.
+__device__ __forceinline__ int pick_lane(bool over, bool some, bool& hit) {
+    const unsigned o = __ballot_sync(0xffffffffu, over), s = __ballot_sync(0xffffffffu, some);
+    hit = o != 0;
+    return o ? __ffs(o) - 1 : 31 - __clz(s | 1u);
+}
+// The segment that holds u times the whole; rest: that less the mass before it. mass(i, have): of segment i, 0 if not.
+template <class Sum, class Mass>
+__device__ __forceinline__ int find_segment(int segments, float u01, Mass mass, float& rest, int lane) {
+    const int of = segments <= 32 ? 1 : (segments + 31) / 32 | 1;    // of a lane
+    Sum w;
+    if constexpr (sizeof(Sum) == 4) {
+        w = mass(lane * of, true);
+#pragma unroll 1
+        for (int i = 1; i < of; ++i) w += mass(lane * of + i, true);
+    } else {
+        Sum2 sum{0.f, 0.f};
+#pragma unroll 4
+        for (int i = 0; i < of; ++i) sum.add(mass(lane * of + i, true));
+        w = (double)sum.s + (double)sum.e;
     }
-    if (at < 0) {
-        at = last;
-        passed = last_passed;
+    const Sum cum = warp_scan(w, lane), total = __shfl_sync(0xffffffffu, cum, 31);
+    Sum target;
+    if constexpr (sizeof(Sum) == 4) target = __fmul_rn(u01, total);
+    else target = __dmul_rn((double)u01, total);
+    bool hit;
+    const int group = pick_lane(w > 0 && cum > target, w > 0, hit);
+    rest = (float)(target - __shfl_sync(0xffffffffu, cum - w, group));
+    if (of == 1) return group;
+    float passed = 0.f, before = 0.f;
+    int at = 0;
+    hit = false;
+#pragma unroll 1
+    for (int i = 0; i < of && !hit; i += 32) {
+        const float v = mass(group * of + i + lane, i + lane < of), upto = warp_scan(v, lane);
+        const int k = pick_lane(v > 0.f && passed + upto > rest, v > 0.f, hit);
+        if (__shfl_sync(0xffffffffu, v, k) > 0.f) {
+            at = group * of + i + k;
+            before = passed + __shfl_sync(0xffffffffu, upto - v, k);
+        }
+        passed += __shfl_sync(0xffffffffu, upto, 31);
     }
-    const float rest = (float)(target - passed);
-    const int v0 = v_lo + at * kWarpVecs + lane;
+    rest -= before;
+    return at;
+}
+// here(i): whether this warp finds the entry of segment i (CTAs of a cluster have their own).
+template <class T, class Here>
+__device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const RowStat& r, const IndexView<T>& view,
+                                         const float2* segment, float u01, Here here, int lane) {
+    constexpr int W = Elt<T>::W;
+    const int segments = (view.vectors() + kSegmentVecs - 1) / kSegmentVecs;
+    const auto mass = [&](int i, bool have) {
+        const float2 sg = have && i < segments ? segment[i] : make_float2(-INFINITY, 0.f);
+        const float w = sg.y > 0.f ? __fmul_rn(sg.y, exp2_fast(fmaxf((sg.x - r.m) * a.k, kXMin) + kExpBias)) : 0.f;
+        return w < kSegmentLeast ? 0.f : w;
+    };
+    float rest;
+    const int at = segments <= 256 ? find_segment<float>(segments, u01, mass, rest, lane)
+                                   : find_segment<double>(segments, u01, mass, rest, lane);
+    if (!here(at)) return;
+    const int v0 = at * kSegmentVecs + lane, v_hi = view.vectors();
     float sum = 0.f, fz = 0.f, bz = 0.f;
     int found = -1, behind = -1;                     // the entry that passes the target; the last one with a mass
+#pragma unroll 1
     for (int u = 0; u < kListPer && !__any_sync(0xffffffffu, found >= 0); ++u) {
         const int v = v0 + u * 32;
         const uint4 q = v < v_hi ? view.vec(v) : Elt<T>::none();
@@ -526,10 +633,10 @@ __device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const R
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             cum += e[i];
-            if (e[i] > 0.f) {
-                behind = v * W - view.h + i;
+            if (e[i] > 0.f && found < 0) {
+                behind = v * W + i;
                 bz = entry_of<T>(q, i);
-                if (found < 0 && cum > rest) {
+                if (cum > rest) {
                     found = behind;
                     fz = bz;
                 }
@@ -537,9 +644,9 @@ __device__ __forceinline__ void draw_all(const ListArgs& a, int64_t row, const R
         }
         sum += __shfl_sync(0xffffffffu, incl, 31);
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
-    int lane_at = __ffs(hit) - 1;
-    if (!hit) {
+    const unsigned at_hit = __ballot_sync(0xffffffffu, found >= 0);
+    int lane_at = __ffs(at_hit) - 1;
+    if (!at_hit) {
         lane_at = __ffs(__ballot_sync(0xffffffffu, behind == __reduce_max_sync(0xffffffffu, behind))) - 1;
         found = behind;
         fz = bz;
@@ -695,6 +802,23 @@ __device__ __forceinline__ RowStat gather_part(float m, const uint4 (&q)[kListPe
     return r;
 }
 
+// A draw's segment: its sums are relative to its own maximum mx (a warp's lanes have the same), and join those
+// of the segments so far relative to theirs. What comes back is the warp's whole mass.
+template <class T, class Own>
+__device__ __forceinline__ float sum_segment(Own& st, const uint4 (&x)[kListPer], float mx, float k, float low_reach) {
+    if (!(mx <= st.m)) raise(st, mx, k);
+    RowStat part{mx, 0.f, 0.f};
+    if (mx != -INFINITY) part = gather_part<T>(mx, x, k, low_of<T>(mx, k, low_reach));
+    const float s = warp_add(part.s);
+    if (mx < st.m) {
+        const float d = fmaxf((mx - st.m) * k, kXMin), f = exp2_fast(d + kExpBias);
+        part.t = f * fmaf(part.s, d, part.t);
+        part.s *= f;
+    }
+    join(st, part);
+    return s;
+}
+
 // How a slice's statistics and maxima are held. kCoarse: words of maxima, and the bound from the
 // threads' own maxima, of which there are two for every entry of the list; kWide: from the words', of
 // which there are four; kFine: finer groups, and the bound from theirs. kLong: more than kManyBatches
@@ -711,14 +835,14 @@ struct OwnStat<kLong> {
 };
 
 template <class T, int kOp, int kThreads, int kMode>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 128 ? 7 : 14) token_list_kernel(ListArgs a, ListShape sh) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kOp == kListDrawAll ? 3 : 4) : kThreads == 128 ? 7 : 14) token_list_kernel(ListArgs a, ListShape sh) {
     using Own = typename OwnStat<kMode>::Type;
-    constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = 32 * kListPer, kBatch = kWarps * kWarpVecs;
+    constexpr int W = Elt<T>::W, kWarps = kThreads / 32, kWarpVecs = kSegmentVecs, kBatch = kWarps * kWarpVecs;
     constexpr bool kAll = kOp == kListDrawAll, kWordMaxima = kMode == kCoarse || kMode == kWide;
     // keys [cap], sorted ones [room] (or groups to be read again), maxima; or segments' (m, S)
     extern __shared__ __align__(16) uint64_t keys[];
     __shared__ ListShared own;
-    __shared__ float4 red[kWarps];
+    __shared__ float4 red[kWarps], peers[kAll ? 8 : 1];              // peers: the statistics of a draw's CTAs
     __shared__ ListPick pick;
     __shared__ uint32_t n_again, warp_total[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -729,6 +853,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
     uint32_t* words = reinterpret_cast<uint32_t*>(sorted + sh.room);         // kCoarse: [batch][word][thread]
     uint16_t* order = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(maxima) + sh.maxima);
     float2* segment = reinterpret_cast<float2*>(keys);
+    if (kAll && C > 1) cluster_arrive();
     wait_for_previous();
     let_next_start();
     // Every CTA of the row comes here; what each wrote before is seen by all after it.
@@ -880,6 +1005,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         __syncthreads();
     };
     const float low_reach = 160.f / a.k;
+    bool met = false;                                // the cluster's CTAs, at their start
     for (int64_t row = blockIdx.x / C; row < a.n; row += gridDim.x / C) {
         const int token = a.tokens ? a.tokens[row] : 0;
         const bool first = tid == 0 && rank == 0;
@@ -914,6 +1040,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         const int v_lo = min(nv, rank * sh.slice), v_hi = min(nv, v_lo + sh.slice);
         float zt = 0.f;
         if (kOp == kListTop && a.tokens) zt = Elt<T>::get(z[token]);
+        RowUniform random{};
+        if (kAll && warp == 0) random = load_uniform(a, row);
 
         // ---- statistics; a warp's vectors of a batch follow one another
         Own st{};
@@ -927,6 +1055,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         // the row's whole vectors; a partial first or last one is filled up
         const int full_lo = h > 0 ? 1 : 0, full_hi = (h + a.V) % W != 0 ? nv - 1 : nv;
         const uint4* src = reinterpret_cast<const uint4*>(z - h);
+        const int per = sh.slice / kSegmentVecs;     // draws: segments of a CTA
         const int batches = (v_hi - v_lo + kBatch - 1) / kBatch;
         for (int batch = 0; batch < batches; ++batch) {
             const int b = v_lo + batch * kBatch, v0 = b + warp * kWarpVecs + lane;
@@ -946,6 +1075,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
 #pragma unroll
                     for (int u = 0; u < kListPer; ++u)
                         if (tail == u * 32) x[u] = q;
+                }
+            }
+            if constexpr (kAll) {
+                if (h > 0) {                         // (a slice's end is a batch's, or the row's)
+                    const int next = v0 + kWarpVecs;
+                    realign<T>(x, lane == 0 && next < nv ? view.vec(next) : Elt<T>::none(), (int)((uintptr_t)z & 15u), lane);
                 }
             }
             float mx;
@@ -969,6 +1104,18 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 }
             }
             mx = warp_max(mx);
+            if constexpr (kAll) {
+                const float s = sum_segment<T>(st, x, mx, a.k, low_reach);
+                // every CTA of the row has all segments
+                float2* to = segment + (rank * per + batch * kWarps + warp);
+                if (C == 1 && lane == 0) *to = make_float2(mx, s);
+                if (C > 1) {
+                    if (!met) cluster_wait();        // peers' shared memory is there to be written
+                    met = true;
+                    if (lane < C) peer_put(to, lane, make_float2(mx, s));
+                }
+                continue;
+            }
             if (!(mx <= st.m)) {
                 raise(st, mx, a.k);
                 low = low_of<T>(st.m, a.k, low_reach);
@@ -976,10 +1123,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             RowStat part{st.m, 0.f, 0.f};
             if (st.m != -INFINITY) part = gather_part<T>(st.m, x, a.k, low);
             join(st, part);
-            if (kAll) {
-                const float s = warp_add(part.s);
-                if (lane == 0) segment[batch * kWarps + warp] = make_float2(st.m, s);
-            }
             if (ranked && !(mx < zt)) {              // (a warp's entries are all before the token, behind it, or both)
                 const int j0 = (v0 - lane) * W - h;
                 if (j0 > token || j0 + kWarpVecs * W <= token) {
@@ -993,6 +1136,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
                 before += above.take();
             }
         }
+        if (kAll && C > 1 && !met) cluster_wait();
+        met = true;
         if (ranked) {
             // the token's own vector counted as one behind it; a masked token comes after every
             // entry before it
@@ -1023,13 +1168,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         float4 peer = make_float4(r.m, r.s, r.t, 0.f);               // lane i: CTA i's
         uint32_t n_keys = kAll ? 0 : own.count, reach = 0;
         if (C > 1) {
-            if (tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
+            if (kAll && warp == 0 && lane < C) peer_put(peers + rank, lane, peer);
+            if (!kAll && tid == 0) own.stat = make_float4(r.m, r.s, r.t, __uint_as_float(before));
             meet();
             uint2 found = make_uint2(0u, 0u);        // (all loads before the first use)
             peer = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            if (lane < C) {
+            if (kAll && lane < C) peer = peers[lane];
+            if (!kAll && lane < C) {
                 peer = peer_load(&own.stat, lane);
-                if (!kAll) found = make_uint2(peer_load(&own.count, lane), peer_load(&own.reach, lane));
+                found = make_uint2(peer_load(&own.count, lane), peer_load(&own.reach, lane));
             }
             before = __reduce_add_sync(0xffffffffu, __float_as_uint(peer.w));
             r = reduce_stat<32>(RowStat{peer.x, peer.y, peer.z}, a.k);
@@ -1048,22 +1195,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
             no_list(live ? NAN : 0.f);
             if (kOp != kListTop && first) write_draw(a, row, -1, live ? NAN : 0.f, live ? NAN : 0.f, live ? NAN : 0.f);
         } else if constexpr (kAll) {
-            if (warp == 0) {
-                // the CTA that holds the target, the last one with a mass where rounding leaves none
-                const double target = (double)row_uniform(a, row) * (double)r.s;
-                double passed = 0.0;
-                int cta = 0;
-                if (C > 1) {
-                    float w = lane < C ? mass_at(a, peer.x, peer.y, r) : 0.f;
-                    if (w < kSliceLeast) w = 0.f;
-                    const float cum = warp_scan(w, lane);
-                    const unsigned hit = __ballot_sync(0xffffffffu, w > 0.f && (double)cum > target),
-                                   some = __ballot_sync(0xffffffffu, w > 0.f);
-                    cta = hit ? __ffs(hit) - 1 : 31 - __clz(some);
-                    passed = (double)__shfl_sync(0xffffffffu, cum - w, cta);
-                }
-                if (cta == rank) draw_all(a, row, r, view, v_lo, v_hi, segment, batches * kWarps, target, passed, lane);
-            }
+            if (warp == 0)
+                draw_all<T>(a, row, r, IndexView<T>{z, a.V}, segment, uniform_of(a, random),
+                            [&](int i) { return i >= rank * per && (C == 1 || i < (rank + 1) * per); }, lane);
         } else {
             if (n_keys > (uint32_t)sh.cap) {
                 // ---- too many (the same in all CTAs of the row): a bound from all keys
@@ -1141,6 +1275,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kThreads == 12
         if (kAll || !good) meet();
         else __syncthreads();
     }
+    if (kAll && C > 1 && !met) cluster_wait();       // (no row was read)
 }
 
 template <class T, int kOp, int kThreads, int kMode>
@@ -1175,7 +1310,7 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
     constexpr int kBatch = kThreads * kListPer;
     const int64_t batches = (sh.slice + kBatch - 1) / kBatch;
     int mode = batches > kManyBatches ? kLong : kCoarse;
-    size_t bytes = (size_t)batches * (kThreads / 32) * sizeof(float2);
+    size_t bytes = (size_t)sh.cluster * batches * (kThreads / 32) * sizeof(float2);
     if (kOp != kListDrawAll) {
         // Maxima of as large groups as leave four for every entry of the list; none where all
         // entries can be sorted as well, or where they are too few.

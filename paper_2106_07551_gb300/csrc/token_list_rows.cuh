@@ -34,7 +34,7 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     for (int c = 2; c <= 8; c += c == 2 ? 1 : c == 3 ? 1 : c) {
         const int64_t slice = (nv + c - 1) / c;
         if ((slice >= 1536 && c != 3 && a.n * c <= 2 * (int64_t)n_sm) ||
-            (slice >= 8192 && c <= 3 && a.n * c * 4 <= 13 * (int64_t)n_sm) ||
+            (slice >= 8192 && c <= 3 && a.n * c * 4 <= (kOp == kListDrawAll ? 12 : 13) * (int64_t)n_sm) ||
             (a.K > 0 && c == 3 && nv > kManyBatches * 256 * kListPer && a.n * c <= 7 * (int64_t)n_sm) ||
             (a.K > 128 && slice >= 9216 && c <= 3 && a.n * c <= 16 * (int64_t)n_sm))
             sh.cluster = c;
@@ -42,6 +42,7 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     // What the CTAs list is sorted together: K entries each as long as that is little, else a share of K with
     // a quarter more, which has them all unless a slice has more than its share.
     sh.slice = (int)((nv + sh.cluster - 1) / sh.cluster);
+    if (kOp == kListDrawAll) sh.slice = (sh.slice + 256 * kListPer - 1) / (256 * kListPer) * (256 * kListPer);    // whole batches
     sh.slice_K = sh.cluster * a.K <= kListCap / 2 ? a.K : a.K / sh.cluster * 5 / 4 + 32;
     if constexpr (kOp == kListDrawAll) {
         if (sh.cluster == 1 && nv <= kStreamMostBatches * kStreamBatch) return launch_draw_stream<T>(a, nv, n_sm, s);

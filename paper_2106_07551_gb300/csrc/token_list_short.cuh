@@ -289,6 +289,8 @@ __global__ void __launch_bounds__(32 * kRowWarps, short_ctas<T, kOp, N, kLong>()
                 for (int u = 0; u < N; ++u)
                     if (u == tail / 32) x[u] = q;
             }
+            // (draws from the whole row: the same sums wherever it lies)
+            if (kOp == kListDrawAll && h > 0) realign<T>(x, Elt<T>::none(), (int)((uintptr_t)z & 15u), lane);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 vmax[u] = Elt<T>::largest(Elt<T>::max(Elt<T>::max(x[u].x, x[u].y), Elt<T>::max(x[u].z, x[u].w)));
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, short_ctas<T, kOp, N, kLong>()
                         before += w;
                         if (w > 0.f && !done) {
                             found = e;
-                            j = (u * 32 + lane) * W - h + i;
+                            j = (u * 32 + lane) * W + i;
                             done = before > target;
                         }
                     }

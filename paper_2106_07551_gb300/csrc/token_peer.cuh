@@ -25,6 +25,21 @@ __device__ __forceinline__ void peer_store(void* dst, uint64_t* bar, uint32_t ra
         : "memory");
 }
 
+// Writes 8 or 16 bytes to the same place of CTA `rank` of the cluster, seen after the next cluster barrier.
+__device__ __forceinline__ void peer_put(float2* dst, uint32_t rank, float2 v) {
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.v2.f32 [a], {%2, %3};\n}" ::"r"(
+                     smem_u32(dst)),
+                 "r"(rank), "f"(v.x), "f"(v.y)
+                 : "memory");
+}
+
+__device__ __forceinline__ void peer_put(float4* dst, uint32_t rank, float4 v) {
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.v4.f32 [a], {%2, %3, %4, %5};\n}" ::"r"(
+                     smem_u32(dst)),
+                 "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
+}
+
 // Reads the same place of CTA `rank` of the cluster, after a cluster barrier that follows its writes.
 __device__ __forceinline__ uint64_t peer_load(const uint64_t* src, uint32_t rank) {
     uint64_t v;

@@ -620,9 +620,10 @@ int malib_learn_token_distill(malib_ctx* ctx, const malib_token_batch* batch, co
  *   dL / dz_j = (1 / T) [ g 1(j = a) + sum_k h_k 1(j = id_k) - p_j (g + sum_k h_k) - e p_j (ln p_j + H) ].
  * An id listed more than once, or the token, has the sum of its slopes. Each of logp_grad,
  * entropy_grad and (ids, top_grad) may be NULL (0), not all; 1 <= top <= 1024 with ids. Rows are
- * left out by their token or as all -infinity; grad as for the losses, required. A row
- * with an infinite slope has the entries' own slopes / T where p_j = 0, else the infinity of their sign,
- * as the losses have; with a NaN, or infinities of both signs or at H, NaN.
+ * left out by their token or as all -infinity; grad as for the losses, required, and apart from
+ * the tokens, ids and slopes. A row with an infinite slope has the entries' own slopes / T where
+ * p_j = 0, else the infinity of their sign, as the losses have; with a NaN, or infinities of both
+ * signs or at H, NaN.
  */
 typedef struct malib_token_scores {
     const float* logp_grad;
@@ -641,7 +642,7 @@ int malib_learn_token_scores(malib_ctx* ctx, const malib_token_batch* batch, con
  * 0). Masked entries (logit -infinity) are never listed and never drawn. batch->tokens
  * may be NULL: no row is left out by its token. A row with a NaN or +infinity among its
  * logits gives NaN, ids and tokens of -1 and rank 0; so does a row that is left out, with 0
- * for NaN. No output may overlap the logits or another one; sums are fp32 or more.
+ * for NaN. Outputs that overlap an input or one another are refused; sums are fp32 or more.
  */
 
 /*
@@ -703,8 +704,8 @@ int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const mal
  * The backward pass is the same call on the gradient without residual (whose gradient is out's).
  * x, residual (may be NULL), out [n_rows][ld] of the type dtype, ld >= dim (columns from dim on are
  * not written), 0 for x or residual: one row that all share. out may be x or residual with the
- * same ld; otherwise their ranges must be apart. 1 <= dim <= 524,288; 0 <= p <= 1 - 2^-16;
- * sequence int64 [n_rows], step int32 [n_rows]. A dropped element of x has no influence, also
+ * same ld; otherwise their ranges must be apart, as must out's from sequence's and step's.
+ * 1 <= dim <= 524,288; 0 <= p <= 1 - 2^-16; sequence int64 [n_rows], step int32 [n_rows]. A dropped element of x has no influence, also
  * where it is infinite or NaN. All device memory of the context's device, aligned to its element;
  * asynchronous on the context's stream; no work space. n_rows == 0 is valid. Errors: EINVAL, ECUDA.
  */

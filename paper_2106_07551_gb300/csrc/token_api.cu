@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "malib.h"
+#include "spans.h"
 #include "token_common.cuh"
 #include "token_rollout.h"
 
@@ -79,9 +80,7 @@ struct Call {
         if (!dev(g->grad, (int)es)) return bad("gradient must be aligned device memory of the context's device");
         if (g->ld < a.V || g->ld > INT64_MAX / es / a.n) return bad("gradient row stride below vocab");
         if (g->grad != a.z || (g->ld != a.ld && a.n > 1)) {
-            const uintptr_t z0 = (uintptr_t)a.z, z1 = z0 + (uintptr_t)(((a.n - 1) * a.ld + a.V) * es);
-            const uintptr_t g0 = (uintptr_t)g->grad, g1 = g0 + (uintptr_t)(((a.n - 1) * g->ld + a.V) * es);
-            if (g0 < z1 && z0 < g1) return bad("gradient overlaps the logits other than in place");
+            if (!apart(logits(), Span(g->grad, row_bytes(a.n, g->ld, a.V, es)))) return bad("gradient overlaps the logits other than in place");
         }
         a.g = g->grad;
         a.gld = g->ld;
@@ -94,6 +93,10 @@ struct Call {
         a.w0 = a.n > 0 ? (float)(1.0 / (double)a.n) : 0.0f;
         return MALIB_OK;
     }
+
+    // The logits, and n values of 4 bytes.
+    Span logits() const { return Span(a.z, row_bytes(a.n, a.ld, a.V, elt_size(a.dtype))); }
+    Span four(const void* p, int64_t each = 1) const { return Span(p, (uint64_t)a.n * (uint64_t)each * 4); }
 
     // Work space: counters, partial sums, and the statistics, or shares of them, of n rows.
     int work(int64_t n) {
@@ -235,6 +238,10 @@ int malib_token_top(malib_ctx* ctx, const malib_token_batch* batch, const malib_
     if (!c.dev(out->ids, 4) || !c.dev(out->top_logp, 4) || !c.opt(out->logp, 4) || !c.opt(out->entropy, 4) ||
         !c.opt(out->rank, 4))
         return c.bad("outputs must be device memory of the context's device");
+    const Span in[] = {c.logits(), c.four(batch->tokens)};
+    const Span outs[] = {c.four(out->ids, out->top), c.four(out->top_logp, out->top), c.four(out->logp), c.four(out->entropy),
+                         c.four(out->rank)};
+    if (!all_apart(outs, in)) return c.bad("an output overlaps an input or another output");
     ListArgs a{c.a};
     a.K = out->top;
     a.top_ids = out->ids;
@@ -262,6 +269,11 @@ int malib_token_sample(malib_ctx* ctx, const malib_token_batch* batch, const mal
         return c.bad("uniform, or sequence and step, must be aligned device memory of the context's device");
     if (!c.opt(token_out, 4) || !c.opt(logp_out, 4) || !c.opt(entropy_out, 4) || !c.opt(draw_logp_out, 4))
         return c.bad("outputs must be device memory of the context's device");
+    // (tokens may be drawn in place)
+    const Span in[] = {c.logits(), c.four(batch->tokens == token_out ? nullptr : batch->tokens), c.four(draw->uniform),
+                       c.four(draw->uniform ? nullptr : draw->sequence, 2), c.four(draw->uniform ? nullptr : draw->step)};
+    const Span outs[] = {c.four(token_out), c.four(logp_out), c.four(entropy_out), c.four(draw_logp_out)};
+    if (!all_apart(outs, in)) return c.bad("an output overlaps an input or another output");
     if ((r = c.work(0)) != MALIB_OK) return r;
     ListArgs a{c.a};
     a.K = draw->top_k;
@@ -295,6 +307,10 @@ int malib_learn_token_scores(malib_ctx* ctx, const malib_token_batch* batch, con
     if (!c.opt(scores->logp_grad, 4) || !c.opt(scores->entropy_grad, 4) || !c.opt(scores->ids, 4) ||
         (scores->ids && !c.dev(scores->top_grad, 4)))
         return c.bad("slopes and ids must be aligned device memory of the context's device");
+    const Span in[] = {c.four(batch->tokens), c.four(scores->logp_grad), c.four(scores->entropy_grad),
+                       c.four(scores->ids, scores->top), c.four(scores->ids ? scores->top_grad : nullptr, scores->top)};
+    const Span outs[] = {Span(c.a.g, row_bytes(c.a.n, c.a.gld, c.a.V, elt_size(c.a.dtype)))};
+    if (!all_apart(outs, in)) return c.bad("gradient overlaps tokens, ids or slopes");
     if ((r = c.work(0)) != MALIB_OK) return r;
     c.a.logp_grad = scores->logp_grad;
     c.a.entropy_grad = scores->entropy_grad;
@@ -323,13 +339,13 @@ int malib_dropout(malib_ctx* ctx, const malib_dropout_batch* b) {
         return c.bad("x, residual and out must be aligned device memory of the context's device");
     if (!c.dev(b->sequence, 8) || !c.dev(b->step, 4))
         return c.bad("sequence and step must be aligned device memory of the context's device");
-    const auto apart = [&](const void* in, int64_t ld) {
-        if (!in || (in == b->out && (ld == b->ld_out || n == 1))) return true;
-        const uintptr_t i0 = (uintptr_t)in, i1 = i0 + (uintptr_t)(((n - 1) * ld + b->dim) * es);
-        const uintptr_t o0 = (uintptr_t)b->out, o1 = o0 + (uintptr_t)(((n - 1) * b->ld_out + b->dim) * es);
-        return o1 <= i0 || i1 <= o0;
+    const Span out(b->out, row_bytes(n, b->ld_out, b->dim, es));
+    const auto beside = [&](const void* in, int64_t ld) {
+        return !in || (in == b->out && (ld == b->ld_out || n == 1)) || apart(Span(in, row_bytes(n, ld, b->dim, es)), out);
     };
-    if (!apart(b->x, b->ld_x) || !apart(b->residual, b->ld_residual)) return c.bad("out overlaps x or residual other than in place");
+    if (!beside(b->x, b->ld_x) || !beside(b->residual, b->ld_residual)) return c.bad("out overlaps x or residual other than in place");
+    if (!apart(out, Span(b->sequence, (uint64_t)n * 8)) || !apart(out, Span(b->step, (uint64_t)n * 4)))
+        return c.bad("out overlaps sequence or step");
     DropArgs a{};
     a.x = b->x;
     a.residual = b->residual;

@@ -94,3 +94,31 @@ def test_infinities_of_both_signs(ctx, V, dt):
         want[at] = sign * INF
         np.testing.assert_array_equal(got[i], want)
     assert np.isfinite(got[10:]).all()
+
+
+@pytest.mark.parametrize("top", [1, 31, 33, 200, 1024])
+@pytest.mark.parametrize("V", [20, 300, 2500, 9000, 70_000, 300_000])
+def test_slopes_of_one_id_are_added_in_their_order(ctx, V, top):
+    """At a masked entry the gradient is the sum of its slopes: of all that are listed, in the list's order, then the
+    token's. Equal to the bit: fp32 sums one after another."""
+    n = 6
+    b = Batch(n, V, "f32", V + top, out=0.0)
+    z = b.z.copy()
+    few = np.stack([b.rng.permutation(V)[:8] for _ in range(n)])
+    z[np.arange(n)[:, None], few] = -np.inf              # eight masked entries, the token one of them
+    z[np.arange(n), [next(j for j in range(V) if j not in set(f)) for f in few]] = 1.0
+    b.tok[:] = few[:, 3]
+    b.set(z)
+    ids = few[np.arange(n)[:, None], b.rng.integers(0, 8, (n, top))]
+    ids[0] = few[0, 3]                                   # the token alone
+    ids[1, 1:] = -1                                      # once, and nothing else
+    ids[2, ::2] = -1
+    g, h = b.rng.normal(size=n).astype(np.float32), b.rng.normal(size=(n, top)).astype(np.float32)
+    got = call(ctx, b, g, None, ids, h)
+    for i in range(n):
+        want = {}
+        for j, x in list(zip(ids[i], h[i])) + [(b.tok[i], g[i])]:
+            if j >= 0:
+                want[j] = np.float32(want[j] + x) if j in want else x
+        for j in few[i]:
+            assert got[i, j] == want.get(j, 0.0), (i, j)

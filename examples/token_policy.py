@@ -115,8 +115,8 @@ class Policy:
 
 
 class Answers:
-    """Sampled answers, one row per (answer, position), answers in a row. Every answer has a number of its
-    own, which its draws and its dropout masks hang on."""
+    """Sampled answers, one row per (answer, position), answers in a row. Every answer of a run has a number of
+    its own, which its draws and its dropout masks hang on."""
     made = 0
 
     def __init__(self, ctx, policy, prompts, gen, drop=False):
@@ -251,6 +251,7 @@ def main(argv=None):
     ap.add_argument("--seed", type=int, default=0)
     args = ap.parse_args(argv)
     gen = torch.Generator(device="cuda").manual_seed(args.seed)
+    Answers.made = 0                                               # a seed gives the same run, also a second time
     base = Policy(args.vocab, args.seed)
     report = {"members": []}
     with Context(0) as ctx:

@@ -1312,11 +1312,11 @@ cudaError_t launch_list_threads(const ListArgs& a, ListShape sh, cudaStream_t s)
     int mode = batches > kManyBatches ? kLong : kCoarse;
     size_t bytes = (size_t)sh.cluster * batches * (kThreads / 32) * sizeof(float2);
     if (kOp != kListDrawAll) {
-        // Maxima of as large groups as leave four for every entry of the list; none where all
-        // entries can be sorted as well, or where they are too few.
+        // Maxima of as large groups as leave four for every entry of the list; none where the list takes a large
+        // part of the slice.
         size_t maxima = 0;
         if (mode == kCoarse) mode = kEntries;
-        if (a.V > 192 && sh.slice >= 2 * sh.slice_K) {
+        if (sh.slice >= 2 * sh.slice_K) {
             if (mode == kEntries && 2 * sh.slice_K <= kThreads && sh.slice >= kBatch / 2) {
                 mode = kCoarse;
                 sh.group_log = 3;

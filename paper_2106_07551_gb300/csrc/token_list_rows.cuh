@@ -52,8 +52,8 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     // 71 and 54, of 10 from 12,000 69 and 56, of 64 from 16,384 84 and 87, of 256 from 3,000 133 and 178.
     if constexpr (kOp != kListDrawAll) {
         if (sh.cluster == 1 && sh.slice <= 1536 && a.K <= 128) return launch_list_threads<T, kOp, 64>(a, sh, s);
+        if (sh.cluster == 1 && sh.slice <= kManyBatches * 128 * kListPer) return launch_list_threads<T, kOp, 128>(a, sh, s);
     }
-    if (sh.cluster == 1 && sh.slice <= kManyBatches * 128 * kListPer) return launch_list_threads<T, kOp, 128>(a, sh, s);
     return launch_list_threads<T, kOp, 256>(a, sh, s);
 }
 

@@ -406,8 +406,9 @@ class Context:
         top_k, of which the likeliest are kept up to top_p of their probability: the
         token, its ln p and the entropy by the whole row, and ln of the probability that
         it was drawn with. The random numbers are uniform [rows], or those of (seed;
-        sequence int64 [rows], step int32 [rows], agent). Rows with a negative token in
-        tokens (may be token_out itself) are left out (-1)."""
+        sequence int64 [rows], step int32 [rows], agent). A row's token does not depend on
+        the batch that the row is in. Rows with a negative token in tokens (may be
+        token_out itself) are left out (-1)."""
         b = _token_batch(logits, tokens, temperature)
         n, f32, i32 = b.n_rows, _Types.f32, _Types.i32
         d = TokenDraw(_vector(uniform, n, f32, "uniform"), _vector(sequence, n, _Types.i64, "sequence"),

@@ -26,12 +26,13 @@
 // maximum so far, gave 14 of 3,000 draws from 131,072 bf16 entries another token by a cluster than by the stream.)
 //
 // Rows of more than 4 KB (shorter ones: token_list_short.cuh) are a block's of 64, 128 or 256 threads each, or a
-// cluster's. The floor is reading the row once; what bounds it is the instructions of the sums (some six
-// an entry), and a row's selection, a chain of a dozen short steps with barriers between them that takes half
-// as long again: the blocks of an SM are at different steps. 8,192 x 65,536 bf16, a quarter left out, 64 entries
-// 180 us (4.5 TB/s, issue slots 59 %), 4,096 draws from the first 50 of 32,768 61 us (4.0 TB/s, 53 %), 333 x 151,111
-// fp32 with 1,024 79 us; one row of 131,072 with 20 by eight CTAs 10. Prefetches of the next batches into
-// L2 cost 6 %: memory does not keep the sums waiting.
+// cluster's. The floor is reading the row once. What bounds it: a block's loads, none of which are in flight while
+// the batch before is summed (the sums alone run at 4.9 TB/s so, at 6.4 as a stream), the instructions of the sums (some
+// six an entry), and a row's selection, a chain of a dozen short steps with barriers between them that takes half as
+// long again: the blocks of an SM are at different steps. 8,192 x 65,536 bf16, a quarter left out, 64 entries
+// 180 us (4.5 TB/s, issue slots 60 %), 4,096 draws from the first 50 of 32,768 62 us (3.9 TB/s, 53 %), 333 x 151,111
+// fp32 with 1,024 80 us; one row of 131,072 with 20 by eight CTAs 10. Prefetches of the next batches into
+// L2 cost 6 %.
 #pragma once
 
 #include <cfloat>

@@ -25,12 +25,15 @@ cudaError_t launch_list_op(const ListArgs& a, int n_sm, cudaStream_t s) {
     // CTAs a row: as many as there are SMs for twice, with slices of 24 KB or more. us, C = 1, 2, 4 and 8:
     // lists of 20 from one row of 131,072 bf16 entries 18.5, 15.4, 13.6, 14.6, of 64 from 100 rows 20, 21,
     // 31, 36; of 5 from 61 x 50,001 fp16 12.9, 11.3, 12.8, 16.5; draws from one row of a million 76, 35,
-    // 21, 15. Slices of 128 KB or more, by 2 or 3 while what an SM holds at a time takes them: of 1 from 164 x
-    // 184,696 fp32, C = 1, 2 and 3, 60, 42, 35, of 10 from 200 x 250,000 bf16 56, 40, 50. Rows whose sums would need
-    // their roundings' errors, by 3 while they are few: of 64 from 333 x 151,111 fp32 C = 1 and 3 68 and 62, of 20
-    // from 500 rows 72 and 84. Long lists, whose selection takes as long as the sums, from rows of more than
-    // 288 KB, also over several rounds, by 2 or 3: of 1,024 from 333 x 151,111 fp32, C = 1, 2, 3 and 4, 131, 109, 86,
-    // 94, 1,000 rows 251, 238, 223, 225.
+    // 21, 15. Slices of 128 KB or more, by 2 or 3 up to 13 CTAs for 4 SMs (of the 16 that lists hold, and the 12
+    // of draws): of 1 from 184,696 fp32, C = 1, 2 and 3, 164 rows 60, 43, 35, 200 rows 62, 43, 51, 240 rows 62, 46, 57; of
+    // 10 from 250,000 bf16, 164 rows 52, 38, 32, 200 rows 54, 39, 48, 240 rows 54, 41, 54. (At 300 rows, which the next
+    // rule takes, 64, 50, 61 and 54, 42, 58: 2 would be best.) Rows whose sums would need their roundings' errors, by 3
+    // up to 7 CTAs an SM, which are 354 rows: of 64 from 140,001 fp32, C = 1, 2 and 3, 354 rows 65, 67, 58, 420 rows
+    // 67, 73, 76, from 200,001 87, 91, 77 and 88, 97, 100. Long lists, whose selection takes as long as the sums, from
+    // rows of more than 288 KB, also over several rounds, by 2 or 3: of 1,024 from 333 x 151,111 fp32, C = 1, 2, 3 and
+    // 4, 131, 109, 86, 94, 1,000 rows 251, 238, 223, 225; of 300 from 80,001, C = 1, 2 and 3, 333 rows 66, 53, 51, 811
+    // 108, 90, 106, 1,300 165, 137, 159, from 160,001 bf16 79, 66, 63, 129, 110, 136, 195, 171, 205.
     for (int c = 2; c <= 8; c += c == 2 ? 1 : c == 3 ? 1 : c) {
         const int64_t slice = (nv + c - 1) / c;
         if ((slice >= 1536 && c != 3 && a.n * c <= 2 * (int64_t)n_sm) ||

@@ -176,6 +176,13 @@ def _vector(x, n, dtype, what):
     return x.data_ptr()
 
 
+def _word(value, what):
+    """A number that fits 32 bits (ctypes would take it modulo 2^32)."""
+    if not -2 ** 31 <= value < 2 ** 32:
+        raise ValueError(f"{what} must fit 32 bits")
+    return value
+
+
 def _token_dtype(x, what):
     code = _Types.codes.get(x.dtype)
     if code is None:
@@ -412,7 +419,7 @@ class Context:
         b = _token_batch(logits, tokens, temperature)
         n, f32, i32 = b.n_rows, _Types.f32, _Types.i32
         d = TokenDraw(_vector(uniform, n, f32, "uniform"), _vector(sequence, n, _Types.i64, "sequence"),
-                      _vector(step, n, i32, "step"), seed, agent, top_k, top_p)
+                      _vector(step, n, i32, "step"), seed, _word(agent, "agent"), _word(top_k, "top_k"), top_p)
         _check(self.lib, self.handle,
                self.lib.malib_token_sample(self.handle, C.byref(b), C.byref(d), _vector(token_out, n, i32, "token_out"),
                                            _vector(logp_out, n, f32, "logp_out"),
@@ -514,7 +521,7 @@ class Context:
             raise ValueError("sequence and step are needed")
         b = DropoutBatch(x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), n, ld, ld_res,
                          _token_rows(out, "out")[2], _vector(sequence, n, _Types.i64, "sequence"),
-                         _vector(step, n, _Types.i32, "step"), seed, p, d, _token_dtype(x, "x"), site)
+                         _vector(step, n, _Types.i32, "step"), seed, p, d, _token_dtype(x, "x"), _word(site, "site"))
         _check(self.lib, self.handle, self.lib.malib_dropout(self.handle, C.byref(b)))
 
     def exploitability(self, ids0, x, ids1, y):
